@@ -435,6 +435,114 @@ int pwlq_search_noalloc(const float* x, int64_t C, int64_t n, int bits, const fl
                         float* sse_all, int32_t* status_out, void* stream);
 size_t pwlq_search_noalloc_max_bytes(void);
 
+/* ------------------------------------------------------------------ training on 8-bit checkpoints
+ * What training keeps between the forward and the backward pass are activations: bell-shaped
+ * tensors with long tails, as the weights are (Sec. 1, Sec. 3.1), so the 7-bit scheme with its
+ * region bit holds them in one byte each.
+ *
+ * Format.  x is [rows, cols]; every row is cut into groups of `group` consecutive values (the last
+ * one may be shorter).  For each group
+ *     m = max |x|;  m < 2^-100 is held as 0, a group with an Inf or a NaN in it as m = NaN;
+ *     p = m * ratio, d = m - p, L = 63, s1 = p * (1/L), s2 = d * (1/L), inv1 = (1/p) * L,
+ *     inv2 = (1/d) * L  (0 where p resp. d is not positive), one rounding per operation,
+ * and a, tail, q and v follow by the sequence at the top of this file (constants by products, since
+ * a group is short; a level can differ from pwlq_quantize's where (a - z) * inv is at a tie within
+ * the rounding of inv).  byte = sign << 7 | region << 6 | q.
+ * A group with m = 0 or NaN has bytes 0; it decodes to +0 resp. to NaN.
+ *   codes   [rows, ldc] bytes, ldc >= cols and a multiple of 16, 16-byte aligned.  Bytes between
+ *           cols and the next multiple of 16 are written as 0, the rest is not touched
+ *   ranges  [rows, ceil(cols / group)] binary32, rows back to back
+ *   group   32, 64, 128 or 256
+ *   ratio   p / m in [2^-20, 1] (e.g. the winner of pwlq_search on a sample; 0.5 is 8-bit uniform)
+ * Types of value tensors: PWLQ_F32, PWLQ_BF16, PWLQ_F16.  A row pitch (ld*) counts elements, is at
+ * least the row's length, and need not be aligned; rows whose start is a multiple of 16 bytes are
+ * the fast case.  rows may be 0: sums over rows are then 0 and nothing else is written. */
+enum { PWLQ_F32 = 0, PWLQ_BF16 = 1, PWLQ_F16 = 2 };
+
+int pwlq_act8_encode(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int group,
+                     float ratio, uint8_t* codes, int64_t ldc, float* ranges, void* stream);
+/* y (of type dtype) = the values that the bytes stand for, rounded once. */
+int pwlq_act8_decode(const uint8_t* codes, int64_t ldc, const float* ranges, int64_t rows,
+                     int64_t cols, int group, float ratio, void* y, int dtype, int64_t ldy,
+                     void* stream);
+
+/* The norms around a residual block: what leaves the block is normalised, gated and added to the
+ * scaled residual stream, and the sum is normalised again for the next block, in one pass:
+ *     N(v; w) = v * rstd(v) * (w + weight_offset),   rstd(v) = (mean(v^2) + eps)^(-1/2)
+ *     r = residual_scale * x + gate[row / gate_tokens] * N(f; post_weight),   h = N(r; pre_weight)
+ * Everything between the loads and the stores is binary32; r and h are rounded once each.
+ *   x, f, r, h     [rows, cols] of type dtype.  f NULL: r = residual_scale * x (gate, post_weight
+ *                  NULL too).  post_weight NULL: f enters unnormalised.  pre_weight NULL: no h (h
+ *                  NULL).  r NULL: r is not delivered.  r may be x and h may be f (same pitch)
+ *   weights, gate  of type wtype (PWLQ_F32 or dtype): [cols], and [gate_rows, cols] at pitch ldgate;
+ *                  gate NULL: 1.  gate_rows * gate_tokens >= rows
+ *   cols           1 .. PWLQ_BLOCK_NORM_MAX_COLS
+ * Checkpoints for pwlq_block_norm_backward, in the same pass: r_codes / r_ranges / r_rstd (needed
+ * with pre_weight) and f_codes / f_ranges (needed with gate or post_weight), f_rstd (with
+ * post_weight); all NULL where nothing is saved.  They hold the binary32 r and the given f;
+ * *_rstd are [rows]. */
+#define PWLQ_BLOCK_NORM_MAX_COLS 16384
+typedef struct {
+    int64_t rows, cols, dtype, wtype;
+    const void* x; int64_t ldx;
+    const void* f; int64_t ldf;
+    const void* post_weight;
+    const void* pre_weight;
+    const void* gate; int64_t ldgate, gate_rows, gate_tokens;
+    double residual_scale, eps, weight_offset;   /* used as binary32 */
+    void* r; int64_t ldr;
+    void* h; int64_t ldh;
+    int64_t group; double ratio;                 /* of both checkpoints; ratio used as binary32 */
+    int64_t ldc;                                 /* pitch of both code arrays */
+    uint8_t* r_codes; float* r_ranges; float* r_rstd;
+    uint8_t* f_codes; float* f_ranges; float* f_rstd;
+} pwlq_block_norm_args;
+int pwlq_block_norm(const pwlq_block_norm_args* args, void* stream);
+
+/* Gradients of the above, taken at the checkpoints' values R, F (with the saved rstd, n = R or F
+ * times its rstd):
+ *     u = dh * (pre_weight + offset),  e = dr + rstd_r * (u - n_r * mean(u * n_r)),  dx = scale * e
+ *     dpre = sum over rows of dh * n_r
+ *     v = e * gate * (post_weight + offset),  df = rstd_f * (v - n_f * mean(v * n_f))
+ *     dpost = sum over rows of e * gate * n_f,
+ *     dgate = sum over the gate's rows of e * n_f * (post_weight + offset)
+ * without pre_weight e = dr, without post_weight df = e * gate and n_f = F, without gate 1.
+ * `fwd` is the forward call's argument block: sizes, weights, gate, checkpoints are read from it
+ * (x, f, r, h are not; f NULL there means no df, dgate, dpost).
+ *   dh, dr      [rows, cols] of the forward's dtype; dh is needed with pre_weight; dr NULL: 0
+ *   dx, df      outputs, or NULL; dx may be dr, df may be dh (same pitch)
+ *   dpre, dpost, dgate   [cols], [cols], [gate_rows, cols] (rows back to back) of the forward's
+ *               wtype, or NULL.  Sums are binary32 in a fixed order: bit-reproducible
+ *   workspace   pwlq_block_norm_backward_workspace_bytes(rows, cols, gate_rows) bytes, 256-byte
+ *               aligned (gate_rows 0 without gate); 0 for invalid arguments */
+typedef struct {
+    const void* dh; int64_t lddh;
+    const void* dr; int64_t lddr;
+    void* dx; int64_t lddx;
+    void* df; int64_t lddf;
+    void* dpre;
+    void* dpost;
+    void* dgate;
+    void* workspace; int64_t workspace_bytes;
+} pwlq_block_norm_grads;
+size_t pwlq_block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows);
+int pwlq_block_norm_backward(const pwlq_block_norm_args* fwd, const pwlq_block_norm_grads* grads,
+                             void* stream);
+
+/* Weight gradient of a projection y = x W^T from the checkpoint of its input:
+ *     dw[n, k] = sum over rows t of dy[t, n] * xhat[t, k]      (+ dw[n, k] if accumulate)
+ * xhat is the checkpoint's value rounded to dy's type, the products are exact and the sums binary32
+ * in a fixed order (bit-reproducible).
+ *   dy          [rows, outputs], PWLQ_BF16 or PWLQ_F16 (else PWLQ_ERR_UNSUPPORTED)
+ *   codes, ranges, group, ratio   the checkpoint of x [rows, cols]
+ *   dw          [outputs, cols], type dw_dtype (dy's type or PWLQ_F32), pitch lddw
+ *   workspace   pwlq_act8_weight_grad_workspace_bytes(...) bytes, 256-byte aligned */
+size_t pwlq_act8_weight_grad_workspace_bytes(int64_t rows, int64_t outputs, int64_t cols);
+int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outputs, int64_t lddy,
+                          const uint8_t* codes, int64_t ldc, const float* ranges, int64_t cols,
+                          int group, float ratio, void* dw, int dw_dtype, int64_t lddw,
+                          int accumulate, void* workspace, size_t workspace_bytes, void* stream);
+
 /* The streaming kernels (abs-max, quantize, dequantize) hand their data over through shared-memory
  * barriers that they await with a bounded number of polls; a wait that runs out makes the kernel
  * stop early and sets a flag on the current device.  This call reads the flags (it synchronises

@@ -1,0 +1,56 @@
+// Host-side launchers of the training operators (internal to the library).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/pwlq.h"
+
+namespace pwlq {
+
+constexpr int kF32 = PWLQ_F32, kBf16 = PWLQ_BF16, kF16 = PWLQ_F16;
+
+// An 8-bit checkpoint (format: include/pwlq.h).
+struct Act8Tensor {
+    uint8_t* codes;
+    int64_t ldc;
+    float* ranges;
+    int64_t rows, cols;
+    int group;
+    float ratio;
+    __host__ __device__ int64_t groups() const { return (cols + group - 1) / group; }
+};
+
+inline int group_shift(int group) { return group == 32 ? 5 : group == 64 ? 6 : group == 128 ? 7 : 8; }
+inline size_t type_size(int dtype) { return dtype == kF32 ? 4 : 2; }
+
+// Whether every row starts on a 16-byte boundary.
+inline bool rows_aligned(const void* p, int64_t ld, size_t size) {
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)size)) & 15) == 0;
+}
+
+cudaError_t launch_act8_encode(const void* x, int dtype, int64_t ldx, const Act8Tensor& a,
+                               cudaStream_t stream);
+cudaError_t launch_act8_decode(const Act8Tensor& a, void* y, int dtype, int64_t ldy,
+                               cudaStream_t stream);
+
+cudaError_t launch_block_norm(const pwlq_block_norm_args& a, cudaStream_t stream);
+size_t block_norm_backward_workspace(int64_t rows, int64_t cols, int64_t gate_rows);
+cudaError_t launch_block_norm_backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads& g,
+                                       cudaStream_t stream);
+
+struct WeightGrad {
+    const void* dy;
+    int dtype;
+    int64_t rows, outputs, lddy;
+    Act8Tensor x;
+    void* dw;
+    int dw_dtype;
+    int64_t lddw;
+    bool accumulate;
+};
+size_t weight_grad_workspace(int64_t rows, int64_t outputs, int64_t cols);
+cudaError_t launch_weight_grad(const WeightGrad& w, void* workspace, cudaStream_t stream);
+
+}  // namespace pwlq

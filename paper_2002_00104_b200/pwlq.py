@@ -10,7 +10,8 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+import struct
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -24,8 +25,11 @@ CODES_U8, CODES_PACKED = 0, 1
 MODEL_GAUSS_APPROX, MODEL_GAUSS_ROOT, MODEL_LAPLACE = 0, 1, 2
 MAX_K = 4096
 MAX_K2 = 64
+F32, BF16, F16 = range(3)
+BLOCK_NORM_MAX_COLS = 16384
 
 _P, _I64, _INT, _SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
+_F32, _STRUCT = ctypes.c_float, ctypes.c_char_p     # _STRUCT: an argument block packed into bytes
 _SIGNATURES = {
     "pwlq_absmax": (_INT, [_P, _I64, _I64, _P, _P]),
     "pwlq_absmax_ragged": (_INT, [_P, _P, _I64, _I64, _P, _P]),
@@ -92,6 +96,14 @@ _SIGNATURES = {
     "pwlq_select_workspace_bytes": (_SZ, [_I64, _I64]),
     "pwlq_select_analytic": (_INT, [_P, _I64, _I64, _P, _INT, _P, _P, _P, _SZ, _P]),
     "pwlq_select_analytic_ragged": (_INT, [_P, _P, _I64, _I64, _I64, _P, _INT, _P, _P, _P, _SZ, _P]),
+    "pwlq_act8_encode": (_INT, [_P, _INT, _I64, _I64, _I64, _INT, _F32, _P, _I64, _P, _P]),
+    "pwlq_act8_decode": (_INT, [_P, _I64, _P, _I64, _I64, _INT, _F32, _P, _INT, _I64, _P]),
+    "pwlq_block_norm": (_INT, [_STRUCT, _P]),
+    "pwlq_block_norm_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
+    "pwlq_block_norm_backward": (_INT, [_STRUCT, _STRUCT, _P]),
+    "pwlq_act8_weight_grad_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
+    "pwlq_act8_weight_grad": (_INT, [_P, _INT, _I64, _I64, _I64, _P, _I64, _P, _I64, _INT, _F32, _P,
+                                     _INT, _I64, _INT, _P, _SZ, _P]),
     "pwlq_device_status": (_INT, []),
     "pwlq_status_string": (ctypes.c_char_p, [_INT]),
     "pwlq_version": (ctypes.c_char_p, []),
@@ -797,3 +809,265 @@ def encode_host_unsigned(x_host, row_offsets_host, C, max_n, bits, ratios_host, 
         int(layout), _dev(dev_scratch, torch.uint8, "dev_scratch"), dev_scratch.numel(), None,
         _stream(stream))
     _check(rc, "pwlq_encode_host_unsigned")
+
+
+# ---------------------------------------------------------------- training on 8-bit checkpoints
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+class Act8(NamedTuple):
+    """An 8-bit checkpoint of a [rows, cols] tensor: one byte per value in ``codes`` [rows, pitch]
+    (pitch a multiple of 16), one range per group of a row in ``ranges`` [rows, groups]."""
+    codes: torch.Tensor
+    ranges: torch.Tensor
+    cols: int
+    group: int
+    ratio: float
+
+
+def _matrix(t: torch.Tensor, what: str, rows=None, cols=None, dtype=None):
+    """(data pointer, row pitch) of a [rows, cols] CUDA tensor whose rows are contiguous."""
+    if t.dim() != 2 or not t.is_cuda or t.dtype not in _DTYPES:
+        raise ValueError(f"{what} must be a [rows, cols] CUDA tensor of float32, bfloat16 or float16")
+    if (rows is not None and t.shape != (rows, cols)) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what} must be [{rows}, {cols}] of {dtype}, "
+                         f"got {list(t.shape)} of {t.dtype}")
+    r, c = t.shape
+    pitch, step = t.stride()
+    if c > 1 and step != 1:
+        raise ValueError(f"{what}: the values of a row must be adjacent")
+    if r < 2 or pitch < 0:
+        pitch = c
+    elif pitch < c:
+        raise ValueError(f"{what}: rows overlap (a broadcast tensor must be made whole first)")
+    return t.data_ptr(), pitch
+
+
+def _vector(t: Optional[torch.Tensor], what: str, cols: int):
+    if t is None:
+        return 0
+    if t.shape != (cols,) or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous CUDA tensor of {cols} values")
+    return t.data_ptr()
+
+
+def _launch_stream(t: torch.Tensor) -> int:
+    """Handle of PyTorch's current stream; the library launches on the current device."""
+    device = t.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError(f"tensors are on cuda:{device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _on(stream):
+    """What a call does on a stream other than the current one: its outputs and workspaces then
+    belong to that stream too, so that their memory is not handed on before it has run."""
+    return torch.cuda.stream(stream)
+
+
+def _act8(a: Act8, rows=None, cols=None):
+    """(codes pointer, pitch, ranges pointer) of a checkpoint, checked against its own layout."""
+    codes, ranges = a.codes, a.ranges
+    if (codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_cuda or
+            ranges.dtype != torch.float32 or not ranges.is_cuda or not ranges.is_contiguous() or
+            ranges.shape != (codes.shape[0], -(-a.cols // a.group)) or codes.shape[1] < a.cols or
+            codes.shape[1] % 16 or not codes.is_contiguous()):
+        raise ValueError("not a checkpoint: codes must be contiguous uint8 [rows, pitch] with a "
+                         "pitch that is a multiple of 16, ranges float32 [rows, groups]")
+    if rows is not None and (codes.shape[0] != rows or (cols is not None and a.cols != cols)):
+        raise ValueError(f"the checkpoint is of [{codes.shape[0]}, {a.cols}], not [{rows}, {cols}]")
+    return codes.data_ptr(), codes.shape[1], ranges.data_ptr()
+
+
+def act8_empty(rows: int, cols: int, group: int = 128, ratio: float = 0.5, device=None) -> Act8:
+    """An uninitialised checkpoint of a [rows, cols] tensor."""
+    return Act8(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device),
+                torch.empty((rows, -(-cols // group)), dtype=torch.float32, device=device),
+                cols, group, ratio)
+
+
+def act8_encode(x, group=128, ratio=0.5, out: Optional[Act8] = None, stream=None) -> Act8:
+    """``pwlq_act8_encode``: the 8-bit checkpoint of x [rows, cols] (fp32, bf16 or fp16)."""
+    if stream is not None:
+        with _on(stream):
+            return act8_encode(x, group, ratio, out)
+    ptr, pitch = _matrix(x, "x")
+    rows, cols = x.shape
+    a = out if out is not None else act8_empty(rows, cols, group, ratio, x.device)
+    codes, ldc, ranges = _act8(a, rows, cols)
+    _check(load_library().pwlq_act8_encode(ptr, _DTYPES[x.dtype], rows, cols, pitch, a.group,
+                                           a.ratio, codes, ldc, ranges, _launch_stream(x)),
+           "pwlq_act8_encode")
+    return a
+
+
+def act8_decode(saved: Act8, dtype=torch.float32, out=None, stream=None):
+    """``pwlq_act8_decode``: the [rows, cols] values of a checkpoint."""
+    if stream is not None:
+        with _on(stream):
+            return act8_decode(saved, dtype, out)
+    codes, ldc, ranges = _act8(saved)
+    rows, cols = saved.codes.shape[0], saved.cols
+    if out is None:
+        out = torch.empty((rows, cols), dtype=dtype, device=saved.codes.device)
+    ptr, pitch = _matrix(out, "out", rows, cols, out.dtype)
+    _check(load_library().pwlq_act8_decode(codes, ldc, ranges, rows, cols, saved.group, saved.ratio,
+                                           ptr, _DTYPES[out.dtype], pitch, _launch_stream(out)),
+           "pwlq_act8_decode")
+    return out
+
+
+class BlockNormSaved(NamedTuple):
+    """What ``block_norm`` keeps for ``block_norm_backward``: the checkpoints, the norms' factors,
+    the weights and gate it was given, and its settings."""
+    r: Optional[Act8]
+    f: Optional[Act8]
+    r_rstd: Optional[torch.Tensor]
+    f_rstd: Optional[torch.Tensor]
+    pre_weight: Optional[torch.Tensor]
+    post_weight: Optional[torch.Tensor]
+    gate: Optional[torch.Tensor]
+    dtype: torch.dtype
+    has_f: bool
+    block: bytes                     # pwlq_block_norm_args of the forward call
+
+
+# pwlq_block_norm_args and pwlq_block_norm_grads of include/pwlq.h
+_BLOCK_ARGS = struct.Struct("4q QqQqQQQqqq 3d QqQq qdq QQQQQQ")
+_BLOCK_GRADS = struct.Struct("QqQqQqQq QQQ Qq")
+
+
+def block_norm(x, f=None, pre_weight=None, post_weight=None, gate=None, gate_tokens=None,
+               residual_scale=1.0, eps=1e-6, weight_offset=0.0, save=None, out=None, stream=None):
+    """``pwlq_block_norm``: r = residual_scale * x + gate * N(f; post_weight), h = N(r; pre_weight).
+
+    x and f are [rows, cols]; weights are [cols]; ``gate`` is [gate_rows, cols], row i for the rows
+    i * gate_tokens ... of x (default: the rows shared out evenly).  ``save`` = (group, ratio) keeps
+    8-bit checkpoints for ``block_norm_backward``.  ``out`` = (r, h) tensors to write into.  Returns
+    (r, h, saved); h is None without ``pre_weight``, saved without ``save``."""
+    if stream is not None:
+        with _on(stream):
+            return block_norm(x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps,
+                              weight_offset, save, out)
+    xp, ldx = _matrix(x, "x")
+    rows, cols = x.shape
+    dtype, device = x.dtype, x.device
+    fp, ldf = _matrix(f, "f", rows, cols, dtype) if f is not None else (0, 0)
+    wtype = dtype
+    for w in (pre_weight, post_weight, gate):
+        if w is not None:
+            wtype = w.dtype
+            break
+    for w in (pre_weight, post_weight, gate):
+        if w is not None and (w.dtype != wtype or wtype not in (dtype, torch.float32)):
+            raise ValueError("weights and gate must share one type: float32 or that of x")
+    pre, post = _vector(pre_weight, "pre_weight", cols), _vector(post_weight, "post_weight", cols)
+    gp, ldg, gate_rows, every = 0, 0, 0, 0
+    if gate is not None:
+        gate_rows = gate.shape[0]
+        gp, ldg = _matrix(gate, "gate", gate_rows, cols, wtype)
+        every = int(gate_tokens) if gate_tokens else -(-rows // max(gate_rows, 1))
+        every = max(every, 1)
+    r, h = out if out is not None else (None, None)
+    if r is None:
+        r = torch.empty((rows, cols), dtype=dtype, device=device)
+    rp, ldr = _matrix(r, "r", rows, cols, dtype)
+    hp, ldh = 0, 0
+    if pre_weight is not None:
+        if h is None:
+            h = torch.empty((rows, cols), dtype=dtype, device=device)
+        hp, ldh = _matrix(h, "h", rows, cols, dtype)
+    else:
+        h = None
+    group, ratio, ldc = 0, 0.0, 0
+    r8 = f8 = rs = fs = None
+    rc = rr = fc = fr = rsp = fsp = 0
+    if save is not None:
+        group, ratio = int(save[0]), float(save[1])
+        if pre_weight is not None:
+            r8 = act8_empty(rows, cols, group, ratio, device)
+            rs = torch.empty(rows, dtype=torch.float32, device=device)
+            (rc, ldc, rr), rsp = _act8(r8), rs.data_ptr()
+        if gate is not None or post_weight is not None:
+            f8 = act8_empty(rows, cols, group, ratio, device)
+            fc, ldc, fr = _act8(f8)
+        if post_weight is not None:
+            fs = torch.empty(rows, dtype=torch.float32, device=device)
+            fsp = fs.data_ptr()
+    block = _BLOCK_ARGS.pack(rows, cols, _DTYPES[dtype], _DTYPES[wtype], xp, ldx, fp, ldf, post, pre,
+                             gp, ldg, gate_rows, every, residual_scale, eps, weight_offset, rp, ldr,
+                             hp, ldh, group, ratio, ldc, rc, rr, rsp, fc, fr, fsp)
+    _check(load_library().pwlq_block_norm(block, _launch_stream(x)), "pwlq_block_norm")
+    if save is None:
+        return r, h, None
+    return r, h, BlockNormSaved(r8, f8, rs, fs, pre_weight, post_weight, gate, dtype, f is not None,
+                                block)
+
+
+def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None, stream=None):
+    """``pwlq_block_norm_backward``: dict(dx, df, dpre, dpost, dgate) from the gradients of h and r
+    (dr None: 0); entries whose operand the forward call did not have are None."""
+    if stream is not None:
+        with _on(stream):
+            return block_norm_backward(saved, dh, dr, workspace)
+    some = dh if dh is not None else dr
+    if some is None or (dh is None) != (saved.pre_weight is None):
+        raise ValueError("dh is needed exactly where the forward call had a pre_weight, dr where it "
+                         "had none")
+    rows, cols = _BLOCK_ARGS.unpack_from(saved.block)[:2]
+    dtype, device = saved.dtype, some.device
+    dhp, lddh = _matrix(dh, "dh", rows, cols, dtype) if dh is not None else (0, 0)
+    drp, lddr = _matrix(dr, "dr", rows, cols, dtype) if dr is not None else (0, 0)
+    pre, post, gate = saved.pre_weight, saved.post_weight, saved.gate
+    dx = torch.empty((rows, cols), dtype=dtype, device=device)
+    df = torch.empty((rows, cols), dtype=dtype, device=device) if saved.has_f else None
+    dpre = torch.empty_like(pre) if pre is not None else None
+    dpost = torch.empty_like(post) if post is not None else None
+    dgate = torch.empty(gate.shape, dtype=gate.dtype, device=device) if gate is not None else None
+    lib = load_library()
+    need = 0
+    if pre is not None or post is not None or gate is not None:
+        need = lib.pwlq_block_norm_backward_workspace_bytes(
+            rows, cols, gate.shape[0] if gate is not None else 0)
+        if workspace is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+    grads = _BLOCK_GRADS.pack(
+        dhp, lddh, drp, lddr, dx.data_ptr(), cols, df.data_ptr() if df is not None else 0, cols,
+        dpre.data_ptr() if pre is not None else 0, dpost.data_ptr() if post is not None else 0,
+        dgate.data_ptr() if gate is not None else 0,
+        workspace.data_ptr() if need else 0, workspace.numel() if need else 0)
+    _check(lib.pwlq_block_norm_backward(saved.block, grads, _launch_stream(some)),
+           "pwlq_block_norm_backward")
+    return {"dx": dx, "df": df, "dpre": dpre, "dpost": dpost, "dgate": dgate}
+
+
+def act8_weight_grad_workspace_bytes(rows: int, outputs: int, cols: int) -> int:
+    return int(load_library().pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols))
+
+
+def act8_weight_grad(dy, saved: Act8, dtype=None, out=None, accumulate=False, workspace=None,
+                     stream=None):
+    """``pwlq_act8_weight_grad``: dw [outputs, cols] = dy^T xhat of a projection y = x W^T, from
+    dy [rows, outputs] (bf16 or fp16) and the checkpoint of x.  dw is of dy's type or float32
+    (``dtype`` or ``out``); ``accumulate`` adds to ``out``."""
+    if stream is not None:
+        with _on(stream):
+            return act8_weight_grad(dy, saved, dtype, out, accumulate, workspace)
+    dyp, lddy = _matrix(dy, "dy")
+    rows, outputs = dy.shape
+    codes, ldc, ranges = _act8(saved, rows)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        out = torch.empty((outputs, saved.cols), dtype=dtype or dy.dtype, device=dy.device)
+    dwp, lddw = _matrix(out, "out", outputs, saved.cols, out.dtype)
+    lib = load_library()
+    if workspace is None:
+        need = lib.pwlq_act8_weight_grad_workspace_bytes(rows, outputs, saved.cols)
+        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+    _check(lib.pwlq_act8_weight_grad(dyp, _DTYPES[dy.dtype], rows, outputs, lddy, codes, ldc, ranges,
+                                     saved.cols, saved.group, saved.ratio, dwp, _DTYPES[out.dtype],
+                                     lddw, int(accumulate), _dev(workspace, torch.uint8, "workspace"),
+                                     workspace.numel(), _launch_stream(dy)), "pwlq_act8_weight_grad")
+    return out
