@@ -536,8 +536,12 @@ int pwlq_block_norm_backward(const pwlq_block_norm_args* fwd, const pwlq_block_n
  *   dy          [rows, outputs], PWLQ_BF16 or PWLQ_F16 (else PWLQ_ERR_UNSUPPORTED)
  *   codes, ranges, group, ratio   the checkpoint of x [rows, cols]
  *   dw          [outputs, cols], type dw_dtype (dy's type or PWLQ_F32), pitch lddw
- *   workspace   pwlq_act8_weight_grad_workspace_bytes(...) bytes, 256-byte aligned */
-size_t pwlq_act8_weight_grad_workspace_bytes(int64_t rows, int64_t outputs, int64_t cols);
+ *   workspace   pwlq_act8_weight_grad_workspace_bytes(...) bytes, 256-byte aligned: xhat in 16 bits,
+ *               binary32 pieces of the last tiles, and a copy of dy unless its rows start on 16-byte
+ *               boundaries (dy_aligned).  The size depends on the current device's SM count
+ * pwlq_device_status reports a bounded wait of this call that ran out. */
+size_t pwlq_act8_weight_grad_workspace_bytes(int64_t rows, int64_t outputs, int64_t cols,
+                                             int dy_aligned);
 int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outputs, int64_t lddy,
                           const uint8_t* codes, int64_t ldc, const float* ranges, int64_t cols,
                           int group, float ratio, void* dw, int dw_dtype, int64_t lddw,

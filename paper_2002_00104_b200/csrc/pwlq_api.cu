@@ -4,6 +4,7 @@
 
 #include "../../include/pwlq.h"
 #include "pwlq_kernels.h"
+#include "pwlq_train.h"
 
 namespace {
 
@@ -874,9 +875,10 @@ int pwlq_select_analytic_ragged(const float* x, const int64_t* row_offsets, int6
 }
 
 int pwlq_device_status(void) {
-    const int a = pwlq::take_absmax_timeout_flag(), q = pwlq::take_quantize_timeout_flag();
-    if (a < 0 || q < 0) return 1 << PWLQ_ERR_CUDA;
-    return (((a | q) & 1) ? (1 << PWLQ_ERR_TIMEOUT) : 0) |
+    const int a = pwlq::take_absmax_timeout_flag(), q = pwlq::take_quantize_timeout_flag(),
+              w = pwlq::take_weight_grad_timeout_flag();
+    if (a < 0 || q < 0 || w < 0) return 1 << PWLQ_ERR_CUDA;
+    return (((a | q | w) & 1) ? (1 << PWLQ_ERR_TIMEOUT) : 0) |
            (((a | q) & 2) ? (1 << PWLQ_ERR_INVALID_ARG) : 0);
 }
 

@@ -50,7 +50,11 @@ struct WeightGrad {
     int64_t lddw;
     bool accumulate;
 };
-size_t weight_grad_workspace(int64_t rows, int64_t outputs, int64_t cols);
+// aligned: dy's rows start on 16-byte boundaries (else the workspace holds a copy whose rows do).
+size_t weight_grad_workspace(int64_t rows, int64_t outputs, int64_t cols, bool aligned);
 cudaError_t launch_weight_grad(const WeightGrad& w, void* workspace, cudaStream_t stream);
+// 1 if a bounded wait of the weight gradient has expired on the current device since the last call,
+// -1 if the flag could not be read.
+int take_weight_grad_timeout_flag();
 
 }  // namespace pwlq

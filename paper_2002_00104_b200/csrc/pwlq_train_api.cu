@@ -154,9 +154,10 @@ int pwlq_block_norm_backward(const pwlq_block_norm_args* fwd, const pwlq_block_n
     return from_cuda(pwlq::launch_block_norm_backward(a, g, as_stream(stream)));
 }
 
-size_t pwlq_act8_weight_grad_workspace_bytes(int64_t rows, int64_t outputs, int64_t cols) {
+size_t pwlq_act8_weight_grad_workspace_bytes(int64_t rows, int64_t outputs, int64_t cols,
+                                             int dy_aligned) {
     if (check_size(rows, cols) || check_size(rows, outputs)) return 0;
-    return pwlq::weight_grad_workspace(rows, outputs, cols);
+    return pwlq::weight_grad_workspace(rows, outputs, cols, dy_aligned != 0);
 }
 
 int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outputs, int64_t lddy,
@@ -167,11 +168,12 @@ int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outpu
     if (int rc = check_size(rows, cols)) return rc;
     if (!is_dtype(dtype) || !is_dtype(dw_dtype) || (dw_dtype != PWLQ_F32 && dw_dtype != dtype))
         return PWLQ_ERR_INVALID_ARG;
-    if (dtype == PWLQ_F32) return PWLQ_ERR_UNSUPPORTED;
+    if (dtype == PWLQ_F32 || rows * ((cols + 4095) / 4096) > kMaxRows) return PWLQ_ERR_UNSUPPORTED;
     if (bad_tensor(dy, dtype, lddy, rows, outputs) || bad_format(group, ratio) ||
         bad_codes(codes, ldc, ranges, rows, cols) || bad_tensor(dw, dw_dtype, lddw, outputs, cols))
         return PWLQ_ERR_INVALID_ARG;
-    const size_t need = pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols);
+    const size_t need = pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols,
+                                                              pwlq::rows_aligned(dy, lddy, 2));
     if (need && (!workspace || workspace_bytes < need)) return PWLQ_ERR_WORKSPACE;
     if (misaligned(workspace, 256)) return PWLQ_ERR_INVALID_ARG;
     pwlq::WeightGrad w = {dy, dtype, rows, outputs, lddy,

@@ -1,69 +1,458 @@
 // Weight gradient of a projection from the 8-bit checkpoint of its input:
 // dw[n, k] = sum over t of dy[t, n] * xhat[t, k], xhat rounded to dy's type.
+//
+// The checkpoint is decoded to 16 bits in the workspace first (one pass, bound by HBM); then a pair
+// of CTAs owns 256 x 256 of dw (n x k) and walks the rows t in steps of 64: each CTA brings 128
+// columns of either operand in with TMA, and the pair's tensor cores multiply what both hold
+// (tcgen05, cta_group::2, M = N = 256).  Both operands lie with their columns innermost, as in
+// memory: nothing is transposed.  The sums stay in tensor memory, two tiles of 256 columns, so that
+// a tile's results leave while the next one is summed.
+//
+// The pairs are persistent.  Whole tiles go round the pairs first; the tiles of the last, partial
+// round are cut along t so that they fill it, their binary32 pieces go to the workspace, and a
+// second kernel adds them in the order of t.
+#include <mutex>
+#include <type_traits>
+
 #include "pwlq_act8.cuh"
+#include "pwlq_tcgen05.cuh"
 #include "pwlq_train.h"
 
 namespace pwlq {
+
+static __device__ int g_weight_grad_timeout;    // a bounded wait expired
+
 namespace {
 
-constexpr int kTile = 64, kStep = 16;
+constexpr int kTile = 256;                      // of dw, both ways, per pair of CTAs
+constexpr int kHalf = 128;                      // a CTA's share of either operand
+constexpr int kStep = 64;                       // rows t per stage
+constexpr int kStages = 6;
+constexpr int kBlockBytes = kStep * 128;        // 64 columns x 64 rows of 16-bit values
+constexpr int kOperandBytes = 2 * kBlockBytes;
+constexpr int kStageBytes = 2 * kOperandBytes;
+constexpr int kEpilogueWarps = 4, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
+constexpr int kThreads = 32 * (kMmaWarp + 1);
+constexpr int kMinSteps = 4;                    // of a piece of a cut tile
 
-// One 64 x 64 tile of dw per CTA, 4 x 4 sums per thread, kStep rows staged at a time.
-template <typename T, typename W>
-__global__ void __launch_bounds__(256) weight_grad_kernel(WeightGrad w, int group_shift) {
-    __shared__ float sy[kStep][kTile], sx[kStep][kTile];
-    const T* dy = static_cast<const T*>(w.dy);
-    const int64_t n0 = (int64_t)blockIdx.y * kTile, k0 = (int64_t)blockIdx.x * kTile;
-    const int tn = threadIdx.x / 16, tk = threadIdx.x % 16;
-    const int64_t groups = w.x.groups();
-    float acc[4][4] = {};
-    for (int64_t t0 = 0; t0 < w.rows; t0 += kStep) {
-        for (int i = threadIdx.x; i < kStep * kTile; i += 256) {
-            const int64_t t = t0 + i / kTile, n = n0 + i % kTile, k = k0 + i % kTile;
-            sy[i / kTile][i % kTile] =
-                t < w.rows && n < w.outputs ? to_f32(dy[t * w.lddy + n]) : 0.0f;
-            float v = 0.0f;
-            if (t < w.rows && k < w.x.cols)
-                v = act8_value(w.x.codes[t * w.x.ldc + k],
-                               act8_params(w.x.ranges[t * groups + (k >> group_shift)], w.x.ratio));
-            sx[i / kTile][i % kTile] = to_f32(from_f32<T>(v));
-        }
-        __syncthreads();
-#pragma unroll
-        for (int t = 0; t < kStep; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    acc[i][j] = fmaf(sy[t][tn * 4 + i], sx[t][tk + 16 * j], acc[i][j]);
-        __syncthreads();
+struct Shared {
+    uint64_t full[kStages];        // in the leading CTA: both halves of both operands are there
+    uint64_t empty[kStages];       // in each CTA: the stage has been multiplied
+    uint64_t sum_full[2], sum_empty[2];
+    uint32_t tmem;
+    float turn[kEpilogueWarps][32][33];    // a warp's 32 x 32 results on their way to dw
+};
+constexpr size_t kSmemBytes = kStages * kStageBytes + 1024 + sizeof(Shared);
+
+// The work: units 0 .. whole - 1 are whole tiles, the rest are pieces of the last tiles.
+struct Schedule {
+    int tiles_n, tiles_k;
+    int64_t whole;                 // uncut tiles
+    int64_t pieces;                // per cut tile
+    int64_t units;
+    int64_t steps;                 // of a whole tile
+};
+struct Unit {
+    int64_t n0, k0, step0, step1;
+    int64_t slot;                  // of its piece in the workspace, -1: a whole tile
+};
+__device__ __forceinline__ Unit unit_of(const Schedule& s, int64_t u) {
+    Unit w;
+    int64_t tile = u;
+    w.step0 = 0;
+    w.step1 = s.steps;
+    w.slot = -1;
+    if (u >= s.whole) {
+        w.slot = u - s.whole;
+        tile = s.whole + w.slot / s.pieces;
+        const int64_t piece = w.slot % s.pieces;
+        w.step0 = s.steps * piece / s.pieces;
+        w.step1 = s.steps * (piece + 1) / s.pieces;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t n = n0 + tn * 4 + i, k = k0 + tk + 16 * j;
-            if (n >= w.outputs || k >= w.x.cols) continue;
-            W* at = static_cast<W*>(w.dw) + n * w.lddw + k;
-            *at = from_f32<W>(w.accumulate ? acc[i][j] + to_f32(*at) : acc[i][j]);
+    w.n0 = tile % s.tiles_n * kTile;
+    w.k0 = tile / s.tiles_n * kTile;
+    return w;
+}
+
+struct Params {
+    WeightGrad w;
+    Schedule s;
+    float* pieces;                 // workspace: [slot][256][256]
+    int64_t groups;
+    int group_shift;
+    bool vec_out;                  // rows of dw start on 16-byte boundaries
+};
+
+// A wait of a whole warp, by its first lane; the same answer in every lane.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, unsigned parity) {
+    bool ok = true;
+    if ((threadIdx.x & 31) == 0) ok = mbar_wait_cluster(bar, parity);
+    return __all_sync(0xffffffffu, ok);
+}
+
+// One lane: this CTA's columns of both operands, two boxes of 64 each per stage.
+__device__ void tma_loop(const Params& p, const CUtensorMap* map, const CUtensorMap* xmap, Shared& sh,
+                         unsigned char* stages, uint32_t rank) {
+    const uint32_t full = peer_addr(sh.full, 0);
+    int stage = 0;
+    unsigned phase = 0;
+    bool ok = true;
+    for (int64_t u = blockIdx.x >> 1; u < p.s.units && ok; u += gridDim.x >> 1) {
+        const Unit unit = unit_of(p.s, u);
+        const int n = (int)(unit.n0 + rank * kHalf), k = (int)(unit.k0 + rank * kHalf);
+        for (int64_t step = unit.step0; step < unit.step1; ++step) {
+            if (!mbar_wait_cluster(&sh.empty[stage], phase ^ 1)) { ok = false; break; }
+            if (rank == 0) mbar_expect_tx(&sh.full[stage], 4 * kOperandBytes);
+            unsigned char* to = stages + stage * kStageBytes;
+            const uint32_t bar = full + stage * (uint32_t)sizeof(uint64_t);
+            tma_load_pair(to, map, n, (int)(step * kStep), bar);
+            tma_load_pair(to + kBlockBytes, map, n + 64, (int)(step * kStep), bar);
+            tma_load_pair(to + kOperandBytes, xmap, k, (int)(step * kStep), bar);
+            tma_load_pair(to + kOperandBytes + kBlockBytes, xmap, k + 64, (int)(step * kStep), bar);
+            if (++stage == kStages) { stage = 0; phase ^= 1; }
         }
+    }
+    if (!ok) g_weight_grad_timeout = 1;
+    // copies in flight end before the CTA does: every stage comes back empty (at once if unused)
+    for (int i = 0; i < kStages; ++i) {
+        if (!mbar_wait_cluster(&sh.empty[stage], phase ^ 1)) { g_weight_grad_timeout = 1; break; }
+        if (++stage == kStages) { stage = 0; phase ^= 1; }
+    }
+}
+
+// One lane of the leading CTA: the products of both.
+template <typename T>
+__device__ void mma_loop(const Params& p, Shared& sh, unsigned char* stages, uint32_t tmem) {
+    constexpr uint32_t idesc = mma_f16_idesc(std::is_same<T, __nv_bfloat16>::value, kTile, kTile);
+    int stage = 0, sum = 0;
+    unsigned phase = 0, sum_phase = 0;
+    for (int64_t u = blockIdx.x >> 1; u < p.s.units; u += gridDim.x >> 1) {
+        const Unit unit = unit_of(p.s, u);
+        if (!mbar_wait_cluster(&sh.sum_empty[sum], sum_phase ^ 1)) { g_weight_grad_timeout = 1; return; }
+        tcgen05_after_sync();
+        const uint32_t d = tmem + sum * kTile;
+        for (int64_t step = unit.step0; step < unit.step1; ++step) {
+            if (!mbar_wait_cluster(&sh.full[stage], phase)) { g_weight_grad_timeout = 1; return; }
+            tcgen05_after_sync();
+            const uint32_t at = smem_addr(stages + stage * kStageBytes);
+            const uint64_t a = outer_major_desc(at, kBlockBytes);
+            const uint64_t b = outer_major_desc(at + kOperandBytes, kBlockBytes);
+#pragma unroll
+            for (int i = 0; i < kStep / 16; ++i)      // 16 rows t are 2048 bytes of either operand
+                mma_f16_pair(d, a + i * (2048 >> 4), b + i * (2048 >> 4), idesc,
+                             step > unit.step0 || i > 0);
+            mma_commit_pair(&sh.empty[stage]);
+            if (++stage == kStages) { stage = 0; phase ^= 1; }
+        }
+        mma_commit_pair(&sh.sum_full[sum]);
+        if (++sum == 2) { sum = 0; sum_phase ^= 1; }
+    }
+}
+
+// A warp's 32 x 32 results (one row per lane) to rows of dw that start at `to`, `ld` apart; `rows`
+// and `cols` of them exist.
+template <typename W>
+__device__ __forceinline__ void put_block(float* v, float (*turn)[33], W* to, int64_t ld, int rows, int cols,
+                                          bool vec, bool accumulate) {
+    const int lane = threadIdx.x & 31;
+    if (vec && cols >= 32) {
+        if (lane >= rows) return;
+        to += lane * ld;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            Raw8<W> raw;
+            if (accumulate) {
+                float old[8];
+                raw.load(to + 8 * i);
+                raw.get(old);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[8 * i + k] += old[k];
+            }
+            raw.set(v + 8 * i);
+            raw.store(to + 8 * i);
+        }
+        return;
+    }
+    // rows off their alignment, or the last columns: turned in shared memory, so that a warp writes
+    // 32 neighbours of a row (one value per lane and row took 42 us for 515 x 1283 results)
+#pragma unroll
+    for (int i = 0; i < 32; ++i) turn[lane][i] = v[i];
+    __syncwarp();
+    for (int i = 0; i < 32; ++i) {
+        const float r = turn[i][lane];
+        if (i < rows && lane < cols) {
+            W* at = to + i * ld + lane;
+            *at = from_f32<W>(accumulate ? r + to_f32(*at) : r);
+        }
+    }
+    __syncwarp();
 }
 
 template <typename T>
-cudaError_t launch(const WeightGrad& w, cudaStream_t stream) {
-    const dim3 grid((unsigned)((w.x.cols + kTile - 1) / kTile),
-                    (unsigned)((w.outputs + kTile - 1) / kTile));
-    auto* kernel = w.dw_dtype == kF32 ? weight_grad_kernel<T, float> : weight_grad_kernel<T, T>;
-    kernel<<<grid, 256, 0, stream>>>(w, group_shift(w.x.group));
+__device__ void epilogue_loop(const Params& p, Shared& sh, uint32_t tmem, uint32_t rank) {
+    const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+    const uint32_t empty = peer_addr(sh.sum_empty, 0);
+    int sum = 0;
+    unsigned phase = 0;
+    for (int64_t u = blockIdx.x >> 1; u < p.s.units; u += gridDim.x >> 1) {
+        const Unit unit = unit_of(p.s, u);
+        if (!warp_wait(&sh.sum_full[sum], phase)) { g_weight_grad_timeout = 1; return; }
+        tcgen05_after_sync();
+        const int64_t row = rank * kHalf + quarter * 32, n = unit.n0 + row;      // of the warp's first lane
+        for (int c = 0; c < kTile; c += 32) {
+            float v[32];
+            __syncwarp();
+            tmem_load32(tmem + ((uint32_t)(quarter * 32) << 16) + sum * kTile + c, v);
+            const int64_t k = unit.k0 + c;
+            if (unit.slot >= 0) {
+                float4* to = reinterpret_cast<float4*>(p.pieces + (unit.slot * kTile + row + lane) * kTile + c);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            } else if (n < p.w.outputs && k < p.w.x.cols) {
+                const int rows = (int)min((int64_t)32, p.w.outputs - n), cols = (int)min((int64_t)32, p.w.x.cols - k);
+                const int64_t at = n * p.w.lddw + k;
+                if (p.w.dw_dtype == kF32)
+                    put_block(v, sh.turn[quarter], static_cast<float*>(p.w.dw) + at, p.w.lddw, rows, cols,
+                              p.vec_out, p.w.accumulate);
+                else
+                    put_block(v, sh.turn[quarter], static_cast<T*>(p.w.dw) + at, p.w.lddw, rows, cols,
+                              p.vec_out, p.w.accumulate);
+            }
+        }
+        tcgen05_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(empty + sum * (uint32_t)sizeof(uint64_t));
+        if (++sum == 2) { sum = 0; phase ^= 1; }
+    }
+}
+
+template <typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+weight_grad_kernel(const __grid_constant__ CUtensorMap dy, const __grid_constant__ CUtensorMap xhat,
+                   const __grid_constant__ Params p) {
+    extern __shared__ unsigned char raw[];
+    // the swizzle counts from 1024-byte boundaries
+    unsigned char* stages = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+    Shared& sh = *reinterpret_cast<Shared*>(stages + kStages * kStageBytes);
+    const int warp = threadIdx.x >> 5;
+    const uint32_t rank = cluster_rank();
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(&sh.full[i], 1);
+            mbar_init(&sh.empty[i], 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sh.sum_full[i], 1);
+            mbar_init(&sh.sum_empty[i], 2 * kEpilogueWarps);
+        }
+        fence_barrier_init();
+    }
+    if (warp == kMmaWarp) tmem_alloc_pair(&sh.tmem);
+    tcgen05_before_sync();
+    __syncthreads();
+    cluster_sync();
+    tcgen05_after_sync();
+    const uint32_t tmem = sh.tmem;
+
+    if (warp < kEpilogueWarps) {
+        epilogue_loop<T>(p, sh, tmem, rank);
+    } else if (warp == kTmaWarp) {
+        if ((threadIdx.x & 31) == 0) tma_loop(p, &dy, &xhat, sh, stages, rank);
+    } else if (rank == 0) {
+        if ((threadIdx.x & 31) == 0) mma_loop<T>(p, sh, stages, tmem);
+    }
+    __syncwarp();
+    tcgen05_before_sync();
+    cluster_sync();
+    tcgen05_after_sync();
+    if (warp == kMmaWarp) tmem_free_pair(tmem);
+}
+
+// Adds the pieces of the cut tiles in the order of t: eight columns of one row per thread.
+template <typename T>
+__global__ void __launch_bounds__(256) weight_grad_pieces_kernel(const __grid_constant__ Params p) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t cut = i / (kTile * (kTile / 8));
+    const int row = (int)(i / (kTile / 8) % kTile), c = (int)(i % (kTile / 8)) * 8;
+    const int64_t tile = p.s.whole + cut;
+    const int64_t n = tile % p.s.tiles_n * kTile + row, k = tile / p.s.tiles_n * kTile + c;
+    if (n >= p.w.outputs || k >= p.w.x.cols) return;
+    float v[8] = {};
+    for (int64_t s = 0; s < p.s.pieces; ++s) {
+        const float* from = p.pieces + ((cut * p.s.pieces + s) * kTile + row) * kTile + c;
+        const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
+        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
+        v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+    }
+    const int valid = (int)min((int64_t)8, p.w.x.cols - k);
+    auto put = [&](auto* to) {
+        using W = typename std::remove_pointer<decltype(to)>::type;
+        Raw8<W> raw;
+        if (p.w.accumulate) {
+            float old[8];
+            if (p.vec_out) load8<true>(raw, to, valid);
+            else load8<false>(raw, to, valid);
+            raw.get(old);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += old[j];
+        }
+        if (p.vec_out) store8<true>(v, to, valid);
+        else store8<false>(v, to, valid);
+    };
+    if (p.w.dw_dtype == kF32) put(static_cast<float*>(p.w.dw) + n * p.w.lddw + k);
+    else put(static_cast<T*>(p.w.dw) + n * p.w.lddw + k);
+}
+
+// dy with rows that start on 16-byte boundaries, for a dy whose rows do not (TMA's condition).
+__global__ void __launch_bounds__(256)
+realign_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t pitch, int64_t cols) {
+    const int64_t row = blockIdx.x;
+    for (int64_t c = threadIdx.x; c < pitch; c += 256)
+        to[row * pitch + c] = c < cols ? from[row * ld + c] : (uint16_t)0;
+}
+
+// dw without rows: zeros, or left as it is.
+template <typename W>
+__global__ void clear_kernel(W* dw, int64_t ld, int64_t cols) {
+    for (int64_t c = threadIdx.x; c < cols; c += blockDim.x) dw[blockIdx.x * ld + c] = from_f32<W>(0.0f);
+}
+
+// Pairs of CTAs that run side by side on the current device (looked up once per device).
+int resident_pairs() {
+    static std::mutex mutex;
+    static int known[64] = {};
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 74;
+    std::lock_guard<std::mutex> lock(mutex);
+    if (!known[dev]) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 74;
+        known[dev] = sms / 2 > 0 ? sms / 2 : 1;
+    }
+    return known[dev];
+}
+
+Schedule schedule(int64_t rows, int64_t outputs, int64_t cols, int64_t pairs) {
+    Schedule s;
+    s.tiles_n = (int)((outputs + kTile - 1) / kTile);
+    s.tiles_k = (int)((cols + kTile - 1) / kTile);
+    s.steps = (rows + kStep - 1) / kStep;
+    const int64_t tiles = (int64_t)s.tiles_n * s.tiles_k;
+    const int64_t left = tiles % pairs;
+    s.pieces = left ? pairs / left : 1;
+    if (s.pieces > s.steps / kMinSteps) s.pieces = s.steps / kMinSteps > 0 ? s.steps / kMinSteps : 1;
+    s.whole = s.pieces > 1 ? tiles - left : tiles;
+    s.units = s.whole + (tiles - s.whole) * s.pieces;
+    return s;
+}
+
+// The workspace: the pieces' sums, then dy's copy, then the decoded checkpoint.
+inline size_t piece_bytes(int64_t rows, int64_t outputs, int64_t cols) {
+    const Schedule s = schedule(rows, outputs, cols, resident_pairs());
+    return (size_t)(s.units - s.whole) * kTile * kTile * sizeof(float);
+}
+
+// cuTensorMapEncodeTiled, through the runtime: the library does not link the driver.
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                 const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                                 CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
+                                 CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled() {
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// Map of a [rows, cols] matrix of 16-bit values in boxes of 64 columns x kStep rows.
+template <typename T>
+cudaError_t map_columns(CUtensorMap& map, const void* p, int64_t cols, int64_t rows, int64_t pitch) {
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)pitch * sizeof(T)};
+    const cuuint32_t box[2] = {64, kStep}, unit[2] = {1, 1};
+    const CUresult rc = encode(
+        &map, std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+        2, const_cast<void*>(p), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return rc == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+inline int64_t realigned_pitch(int64_t cols) { return (cols + 7) / 8 * 8; }
+
+inline size_t copy_bytes(int64_t rows, int64_t cols) {
+    return ((size_t)rows * realigned_pitch(cols) * 2 + 255) / 256 * 256;
+}
+
+template <typename T>
+cudaError_t launch(const WeightGrad& w, void* workspace, cudaStream_t stream) {
+    if (w.rows == 0) {
+        if (w.accumulate) return cudaSuccess;
+        if (w.dw_dtype == kF32)
+            clear_kernel<<<(unsigned)w.outputs, 256, 0, stream>>>(static_cast<float*>(w.dw), w.lddw, w.x.cols);
+        else
+            clear_kernel<<<(unsigned)w.outputs, 256, 0, stream>>>(static_cast<T*>(w.dw), w.lddw, w.x.cols);
+        return cudaGetLastError();
+    }
+    const int64_t pairs = resident_pairs();
+    Params p;
+    p.w = w;
+    p.s = schedule(w.rows, w.outputs, w.x.cols, pairs);
+    p.groups = w.x.groups();
+    p.group_shift = group_shift(w.x.group);
+    p.vec_out = rows_aligned(w.dw, w.lddw, type_size(w.dw_dtype));
+    p.pieces = static_cast<float*>(workspace);
+
+    unsigned char* at = static_cast<unsigned char*>(workspace) + piece_bytes(w.rows, w.outputs, w.x.cols);
+    const void* dy = w.dy;
+    int64_t pitch = w.lddy;
+    if (!rows_aligned(w.dy, w.lddy, sizeof(T))) {
+        pitch = realigned_pitch(w.outputs);
+        realign_kernel<<<(unsigned)w.rows, 256, 0, stream>>>(static_cast<const uint16_t*>(w.dy), w.lddy,
+                                                             reinterpret_cast<uint16_t*>(at), pitch, w.outputs);
+        if (cudaError_t e = cudaGetLastError()) return e;
+        dy = at;
+        at += copy_bytes(w.rows, w.outputs);
+    }
+    CUtensorMap map, xmap;
+    if (cudaError_t e = map_columns<T>(map, dy, w.outputs, w.rows, pitch)) return e;
+    const int64_t xpitch = realigned_pitch(w.x.cols);
+    if (cudaError_t e = launch_act8_decode(w.x, at, w.dtype, xpitch, stream)) return e;
+    if (cudaError_t e = map_columns<T>(xmap, at, w.x.cols, w.rows, xpitch)) return e;
+    auto* kernel = weight_grad_kernel<T>;
+    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes))
+        return e;
+    const int64_t ctas = 2 * (p.s.units < pairs ? p.s.units : pairs);
+    kernel<<<(unsigned)ctas, kThreads, kSmemBytes, stream>>>(map, xmap, p);
+    if (cudaError_t e = cudaGetLastError()) return e;
+    const int64_t cut = (int64_t)p.s.tiles_n * p.s.tiles_k - p.s.whole;
+    if (!cut) return cudaSuccess;
+    weight_grad_pieces_kernel<T><<<(unsigned)(cut * kTile * (kTile / 8) / 256), 256, 0, stream>>>(p);
     return cudaGetLastError();
 }
 
 }  // namespace
 
-size_t weight_grad_workspace(int64_t, int64_t, int64_t) { return 256; }
+size_t weight_grad_workspace(int64_t rows, int64_t outputs, int64_t cols, bool aligned) {
+    return piece_bytes(rows, outputs, cols) + (aligned ? 0 : copy_bytes(rows, outputs)) +
+           copy_bytes(rows, cols);
+}
 
-cudaError_t launch_weight_grad(const WeightGrad& w, void*, cudaStream_t stream) {
-    return w.dtype == kBf16 ? launch<__nv_bfloat16>(w, stream) : launch<__half>(w, stream);
+cudaError_t launch_weight_grad(const WeightGrad& w, void* workspace, cudaStream_t stream) {
+    return w.dtype == kBf16 ? launch<__nv_bfloat16>(w, workspace, stream) : launch<__half>(w, workspace, stream);
+}
+
+int take_weight_grad_timeout_flag() {
+    int v = 0;
+    const int zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_weight_grad_timeout, sizeof(v)) != cudaSuccess) return -1;
+    if (v && cudaMemcpyToSymbol(g_weight_grad_timeout, &zero, sizeof(zero)) != cudaSuccess) return -1;
+    return v;
 }
 
 }  // namespace pwlq

@@ -101,7 +101,7 @@ _SIGNATURES = {
     "pwlq_block_norm": (_INT, [_STRUCT, _P]),
     "pwlq_block_norm_backward_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
     "pwlq_block_norm_backward": (_INT, [_STRUCT, _STRUCT, _P]),
-    "pwlq_act8_weight_grad_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
+    "pwlq_act8_weight_grad_workspace_bytes": (_SZ, [_I64, _I64, _I64, _INT]),
     "pwlq_act8_weight_grad": (_INT, [_P, _INT, _I64, _I64, _I64, _P, _I64, _P, _I64, _INT, _F32, _P,
                                      _INT, _I64, _INT, _P, _SZ, _P]),
     "pwlq_device_status": (_INT, []),
@@ -1042,8 +1042,9 @@ def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None,
     return {"dx": dx, "df": df, "dpre": dpre, "dpost": dpost, "dgate": dgate}
 
 
-def act8_weight_grad_workspace_bytes(rows: int, outputs: int, cols: int) -> int:
-    return int(load_library().pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols))
+def act8_weight_grad_workspace_bytes(rows: int, outputs: int, cols: int, dy_aligned=True) -> int:
+    return int(load_library().pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols,
+                                                                    int(dy_aligned)))
 
 
 def act8_weight_grad(dy, saved: Act8, dtype=None, out=None, accumulate=False, workspace=None,
@@ -1064,7 +1065,8 @@ def act8_weight_grad(dy, saved: Act8, dtype=None, out=None, accumulate=False, wo
     dwp, lddw = _matrix(out, "out", outputs, saved.cols, out.dtype)
     lib = load_library()
     if workspace is None:
-        need = lib.pwlq_act8_weight_grad_workspace_bytes(rows, outputs, saved.cols)
+        need = lib.pwlq_act8_weight_grad_workspace_bytes(rows, outputs, saved.cols,
+                                                         int((dyp | lddy * 2) % 16 == 0))
         workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
     _check(lib.pwlq_act8_weight_grad(dyp, _DTYPES[dy.dtype], rows, outputs, lddy, codes, ldc, ranges,
                                      saved.cols, saved.group, saved.ratio, dwp, _DTYPES[out.dtype],

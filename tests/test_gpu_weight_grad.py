@@ -137,6 +137,7 @@ def test_refusals():
         pwlq.act8_weight_grad(dy, saved, accumulate=True)
     with pytest.raises(ValueError):
         pwlq.act8_weight_grad(dy, saved, out=torch.empty(32, 47, device="cuda"))
+    odd = torch.zeros(16, 33, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(pwlq.PwlqError) as e:
-        pwlq.act8_weight_grad(dy, saved, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
+        pwlq.act8_weight_grad(odd, saved, workspace=torch.empty(0, dtype=torch.uint8, device="cuda"))
     assert e.value.status == pwlq.ERR_WORKSPACE

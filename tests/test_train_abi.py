@@ -88,9 +88,9 @@ def test_block_norm_backward(lib):
 
 def test_weight_grad(lib):
     from paper_2002_00104_b200 import pwlq
-    need = lib.pwlq_act8_weight_grad_workspace_bytes(8, 32, 100)
-    assert need > 0 and lib.pwlq_act8_weight_grad_workspace_bytes(8, 0, 100) == 0
-    good = [A, pwlq.BF16, 8, 32, 32, B, 112, C, 100, 64, 0.5, A, pwlq.F32, 100, 0, A, need, None]
+    need = lib.pwlq_act8_weight_grad_workspace_bytes(8, 32, 100, 0)
+    assert need > 0 and lib.pwlq_act8_weight_grad_workspace_bytes(8, 0, 100, 0) == 0
+    good = [A, pwlq.BF16, 8, 32, 33, B, 112, C, 100, 64, 0.5, A, pwlq.F32, 100, 0, A, need, None]
 
     def rc(i, v):
         args = list(good)
