@@ -453,7 +453,8 @@ size_t pwlq_search_noalloc_max_bytes(void);
  *           cols and the next multiple of 16 are written as 0, the rest is not touched
  *   ranges  [rows, ceil(cols / group)] binary32, rows back to back
  *   group   32, 64, 128 or 256
- *   ratio   p / m in [2^-20, 1] (e.g. the winner of pwlq_search on a sample; 0.5 is 8-bit uniform)
+ *   ratio   p / m in [2^-20, 1 - 2^-12], or 1 (e.g. the winner of pwlq_search on a sample; 0.5 is
+ *           8-bit uniform)
  * Types of value tensors: PWLQ_F32, PWLQ_BF16, PWLQ_F16.  A row pitch (ld*) counts elements, is at
  * least the row's length, and need not be aligned; rows whose start is a multiple of 16 bytes are
  * the fast case.  rows may be 0: sums over rows are then 0 and nothing else is written. */

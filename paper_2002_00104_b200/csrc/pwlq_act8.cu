@@ -1,9 +1,9 @@
 // 8-bit activation checkpoints: encode (values -> bytes and group ranges) and decode.
 //
 // Both directions move each value once and keep nothing: they are bound by HBM.  A thread owns 16
-// consecutive values (a 16-byte access to the bytes, two or four to the values), the 2 ... 16
-// threads of a group are neighbours in a warp and find the group's range with shuffles, so the
-// values are read once although the range must be known before the first byte.
+// (or 8) consecutive values, the 2 ... 32 threads of a group are neighbours in a warp and find the
+// group's range with shuffles, so the values are read once although the range must be known before
+// the first byte.
 #include "pwlq_act8.cuh"
 #include "pwlq_train.h"
 
@@ -11,7 +11,9 @@ namespace pwlq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 16;               // values per thread
+// Values per thread: 16, so that every access to the bytes is 16 bytes wide; 8 where the rows of the
+// values are off their alignment, since neighbouring threads then join their values (store8).
+__host__ __device__ constexpr int chunk_of(bool vec) { return vec ? 16 : 8; }
 
 // Which chunk of which row a thread owns.  Rows of fewer than 256 chunks share a block
 // (rows_per_block of them), longer ones take blocks_per_row blocks; `chunks` is the row's number of
@@ -24,11 +26,11 @@ struct Act8Grid {
     unsigned magic;                      // tid / chunks_lo == (tid * magic) >> 16 for tid < 256
 };
 
-__device__ __forceinline__ bool locate(const Act8Grid& g, int64_t& row, int64_t& col) {
+__device__ __forceinline__ bool locate(const Act8Grid& g, int chunk, int64_t& row, int64_t& col) {
     const unsigned rb = blockIdx.x / g.blocks_per_row, part = blockIdx.x - rb * g.blocks_per_row;
     const unsigned in = (threadIdx.x * g.magic) >> 16;
     row = (int64_t)rb * g.rows_per_block + in;
-    col = ((int64_t)part * kThreads + (threadIdx.x - in * g.chunks_lo)) * kChunk;
+    col = ((int64_t)part * kThreads + (threadIdx.x - in * g.chunks_lo)) * chunk;
     return in < (unsigned)g.rows_per_block && row < g.rows && col < g.cols;
 }
 
@@ -36,29 +38,35 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 act8_encode_kernel(const T* x, int64_t ldx, Act8Grid g, int group_shift, float ratio,
                    uint8_t* codes, int64_t ldc, float* ranges, int64_t groups) {
+    constexpr int kChunk = chunk_of(VEC), kParts = kChunk / 8;
     int64_t row, col;
-    const bool live = locate(g, row, col);
-    const int valid = live ? (int)min((int64_t)kChunk, g.cols - col) : 0;
-    Raw8<T> raw[2];
+    const bool live = locate(g, kChunk, row, col);
+    const int valid = live ? (int)min((int64_t)32, g.cols - col) : 0;
+    Raw8<T> raw[kParts];
     const T* src = x + row * ldx + col;
-    load8<VEC>(raw[0], src, valid);
-    load8<VEC>(raw[1], src + 8, valid - 8);
-    float v[kChunk];
-    raw[0].get(v);
-    raw[1].get(v + 8);
-    uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < kChunk; ++i) top = max(top, abs_bits(v[i]));
-    top = group_max(top, 1 << (group_shift - 4));
+    for (int i = 0; i < kParts; ++i)
+        load8<VEC>(raw[i], src + 8 * i, valid - 8 * i, (int)min((int64_t)8, col) + 8 * i);
+    float v[kChunk], top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) raw[i].get(v + 8 * i);
+#pragma unroll
+    for (int i = 0; i < kChunk; ++i) top = max_abs(top, v[i]);
+    top = group_max(top, (1 << group_shift) / kChunk);
     if (!live) return;
     const float m = act8_range(top);
     const PieceParams P = act8_params(m, ratio);
-    uint4 w;
-    w.x = act8_word(v, m, P);
-    w.y = act8_word(v + 4, m, P);
-    w.z = act8_word(v + 8, m, P);
-    w.w = act8_word(v + 12, m, P);
-    *reinterpret_cast<uint4*>(codes + row * ldc + col) = w;
+    uint2 w[kParts];
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) w[i] = act8_bytes8(v + 8 * i, m, P);
+    uint8_t* to = codes + row * ldc + col;
+    if (kParts == 2) {
+        *reinterpret_cast<uint4*>(to) = make_uint4(w[0].x, w[0].y, w[kParts - 1].x, w[kParts - 1].y);
+    } else {
+        *reinterpret_cast<uint2*>(to) = w[0];
+        // the row's last 16 bytes may need zeros that no value stands for
+        if (valid <= 8 && (col & 8) == 0) *reinterpret_cast<uint2*>(to + 8) = make_uint2(0u, 0u);
+    }
     if ((col & (((int64_t)1 << group_shift) - 1)) == 0) ranges[row * groups + (col >> group_shift)] = m;
 }
 
@@ -66,23 +74,38 @@ template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 act8_decode_kernel(const uint8_t* codes, int64_t ldc, const float* ranges, int64_t groups,
                    Act8Grid g, int group_shift, float ratio, T* y, int64_t ldy) {
+    constexpr int kChunk = chunk_of(VEC), kParts = kChunk / 8;
     int64_t row, col;
-    if (!locate(g, row, col)) return;
-    const uint4 w = *reinterpret_cast<const uint4*>(codes + row * ldc + col);
-    const PieceParams P = act8_params(ranges[row * groups + (col >> group_shift)], ratio);
-    const int valid = (int)min((int64_t)kChunk, g.cols - col);
+    const bool live = locate(g, kChunk, row, col);
+    const int valid = live ? (int)min((int64_t)32, g.cols - col) : 0;
+    uint2 w[kParts] = {};
+    float m = 0.0f;
+    if (live) {
+        const uint8_t* from = codes + row * ldc + col;
+        if (kParts == 2) {
+            const uint4 b = *reinterpret_cast<const uint4*>(from);
+            w[0] = make_uint2(b.x, b.y);
+            w[kParts - 1] = make_uint2(b.z, b.w);
+        } else {
+            w[0] = *reinterpret_cast<const uint2*>(from);
+        }
+        m = ranges[row * groups + (col >> group_shift)];
+    }
+    const PieceParams P = act8_params(m, ratio);
     T* dst = y + row * ldy + col;
-    float v[8];
-    act8_values(w.x, P, v);
-    act8_values(w.y, P, v + 4);
-    store8<VEC>(v, dst, valid);
-    act8_values(w.z, P, v);
-    act8_values(w.w, P, v + 4);
-    store8<VEC>(v, dst + 8, valid - 8);
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+        u64 v[4];
+        act8_values8(w[i], P, v);
+        float o[8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) unpack2(v[k], o[2 * k], o[2 * k + 1]);
+        store8<VEC>(o, dst + 8 * i, valid - 8 * i);
+    }
 }
 
-cudaError_t plan(int64_t rows, int64_t cols, int group, Act8Grid& g, unsigned& blocks) {
-    const int per_group = group / kChunk;
+cudaError_t plan(int64_t rows, int64_t cols, int group, bool vec, Act8Grid& g, unsigned& blocks) {
+    const int per_group = group / chunk_of(vec);
     const int64_t chunks = (cols + group - 1) / group * per_group;
     g.rows = rows;
     g.cols = cols;
@@ -101,9 +124,10 @@ template <typename T>
 cudaError_t encode(const void* x, const Act8Tensor& a, int64_t ldx, cudaStream_t stream) {
     Act8Grid g;
     unsigned blocks;
-    if (cudaError_t e = plan(a.rows, a.cols, a.group, g, blocks)) return e;
+    const bool vec = rows_aligned(x, ldx, sizeof(T));
+    if (cudaError_t e = plan(a.rows, a.cols, a.group, vec, g, blocks)) return e;
     const T* p = static_cast<const T*>(x);
-    auto* kernel = rows_aligned(x, ldx, sizeof(T)) ? act8_encode_kernel<T, true>
+    auto* kernel = vec ? act8_encode_kernel<T, true>
                                                    : act8_encode_kernel<T, false>;
     kernel<<<blocks, kThreads, 0, stream>>>(p, ldx, g, group_shift(a.group), a.ratio, a.codes,
                                             a.ldc, a.ranges, a.groups());
@@ -113,9 +137,10 @@ template <typename T>
 cudaError_t decode(const Act8Tensor& a, void* y, int64_t ldy, cudaStream_t stream) {
     Act8Grid g;
     unsigned blocks;
-    if (cudaError_t e = plan(a.rows, a.cols, a.group, g, blocks)) return e;
+    const bool vec = rows_aligned(y, ldy, sizeof(T));
+    if (cudaError_t e = plan(a.rows, a.cols, a.group, vec, g, blocks)) return e;
     T* p = static_cast<T*>(y);
-    auto* kernel = rows_aligned(y, ldy, sizeof(T)) ? act8_decode_kernel<T, true>
+    auto* kernel = vec ? act8_decode_kernel<T, true>
                                                    : act8_decode_kernel<T, false>;
     kernel<<<blocks, kThreads, 0, stream>>>(a.codes, a.ldc, a.ranges, a.groups(), g,
                                             group_shift(a.group), a.ratio, p, ldy);

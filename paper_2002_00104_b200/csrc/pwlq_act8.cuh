@@ -58,6 +58,8 @@ template <typename T> struct Raw8 {
         w.z = pack16(v[4], v[5], T());
         w.w = pack16(v[6], v[7], T());
     }
+    __device__ __forceinline__ void from_words(const uint32_t* x) { w = make_uint4(x[0], x[1], x[2], x[3]); }
+    __device__ __forceinline__ void to_words(uint32_t* x) const { x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w; }
     __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = w; }
     __device__ __forceinline__ void clear() { w = make_uint4(0u, 0u, 0u, 0u); }
@@ -72,6 +74,15 @@ template <> struct Raw8<float> {
         a = make_float4(v[0], v[1], v[2], v[3]);
         b = make_float4(v[4], v[5], v[6], v[7]);
     }
+    __device__ __forceinline__ void from_words(const uint32_t* x) {
+        a = make_float4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3]));
+        b = make_float4(__uint_as_float(x[4]), __uint_as_float(x[5]), __uint_as_float(x[6]), __uint_as_float(x[7]));
+    }
+    __device__ __forceinline__ void to_words(uint32_t* x) const {
+        float v[8];
+        get(v);
+        for (int i = 0; i < 8; ++i) x[i] = __float_as_uint(v[i]);
+    }
     __device__ __forceinline__ void load(const float* p) {
         a = *reinterpret_cast<const float4*>(p);
         b = *reinterpret_cast<const float4*>(p + 4);
@@ -83,41 +94,182 @@ template <> struct Raw8<float> {
     __device__ __forceinline__ void clear() { a = b = make_float4(0.0f, 0.0f, 0.0f, 0.0f); }
 };
 
-// The first `valid` (<= 8, may be <= 0) of eight values; the others read as 0 and are not stored.
-// VEC: whole chunks start on 16-byte boundaries.
+// Moves a window of 32-bit words `bytes` bytes (a multiple of the value size, < 16) towards its front;
+// the caller does not use what would have to come from behind it.
+template <int WORDS, bool HALVES>
+__device__ __forceinline__ void shift_window(uint32_t (&w)[WORDS], int bytes) {
+#pragma unroll
+    for (int i = 0; i + 2 < WORDS; ++i) w[i] = bytes & 8 ? w[i + 2] : w[i];
+#pragma unroll
+    for (int i = 0; i + 1 < WORDS; ++i) w[i] = bytes & 4 ? w[i + 1] : w[i];
+    if (HALVES)
+#pragma unroll
+        for (int i = 0; i + 1 < WORDS; ++i) w[i] = __byte_perm(w[i], w[i + 1], bytes & 2 ? 0x5432 : 0x3210);
+}
+
+// Values from p - o on, o = how many values past a 16-byte boundary p is.
+template <typename T> __device__ __forceinline__ int past_boundary(const T* p) {
+    return (int)(((uintptr_t)p & 15) / sizeof(T));
+}
+
+// Eight values at p.  `valid` of them exist (may be <= 0 or > 8; the others read as 0) and `before`
+// values of the same row lie before p.  VEC: p is on a 16-byte boundary.  Off it, the aligned 16-byte
+// words around the eight values are read, where all of them lie inside the row, and shifted into
+// place; the row's ends are read value by value, so nothing outside the row is touched.
 template <bool VEC, typename T>
-__device__ __forceinline__ void load8(Raw8<T>& raw, const T* p, int valid) {
+__device__ __forceinline__ void load8(Raw8<T>& raw, const T* p, int valid, int before) {
     if (VEC && valid >= 8) { raw.load(p); return; }
+    if (!VEC) {
+        constexpr int kPer = 16 / sizeof(T), kVecs = sizeof(T) == 4 ? 3 : 2;
+        const int o = past_boundary(p);
+        if (o == 0 && valid >= 8) { raw.load(p); return; }
+        if (before >= o && valid >= kVecs * kPer - o) {
+            uint32_t w[4 * kVecs];
+            const uint4* q = reinterpret_cast<const uint4*>(p - o);
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i) {
+                const uint4 x = q[i];
+                w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+            }
+            shift_window<4 * kVecs, sizeof(T) == 2>(w, o * (int)sizeof(T));
+            raw.from_words(w);
+            return;
+        }
+    }
     float v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = i < valid ? to_f32(p[i]) : 0.0f;
     raw.set(v);
 }
-template <bool VEC, typename T>
-__device__ __forceinline__ void store8(const float* v, T* p, int valid) {
-    if (VEC && valid >= 8) {
-        Raw8<T> raw;
-        raw.set(v);
-        raw.store(p);
-        return;
-    }
+
+// The first `valid` of eight values to p, value by value.
+template <typename T>
+__device__ __forceinline__ void store8_each(const float* v, T* p, int valid) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < valid) p[i] = from_f32<T>(v[i]);
 }
 
+// The same for a whole warp at once (every lane calls; neighbouring lanes normally hold neighbouring
+// values).  VEC: p is on a 16-byte boundary where valid >= 8.  Off the boundary a lane writes the
+// aligned 16 bytes that begin with its left neighbour's last values; what has no such neighbour is
+// written value by value.
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(const float* v, T* p, int valid) {
+    if (VEC) {
+        if (valid >= 8) {
+            Raw8<T> raw;
+            raw.set(v);
+            raw.store(p);
+        } else {
+            store8_each(v, p, valid);
+        }
+        return;
+    }
+    constexpr unsigned kAll = 0xffffffffu;
+    constexpr int kPer = 16 / sizeof(T);
+    const int lane = threadIdx.x & 31, o = past_boundary(p);
+    Raw8<T> raw;
+    raw.set(v);
+    uint32_t mine[2 * sizeof(T)], w[4 + 2 * sizeof(T)];     // a neighbour's last 16 bytes, then mine
+    raw.to_words(mine);
+    const uintptr_t left = __shfl_up_sync(kAll, (uintptr_t)p, 1);
+    const int left_valid = __shfl_up_sync(kAll, valid, 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        w[i] = __shfl_up_sync(kAll, mine[2 * sizeof(T) - 4 + i], 1);
+#pragma unroll
+    for (int i = 0; i < (int)(2 * sizeof(T)); ++i) w[4 + i] = mine[i];
+    const bool whole = valid >= 8;
+    const bool joins = whole && (o == 0 || (lane > 0 && left_valid >= 8 && left + 8 * sizeof(T) == (uintptr_t)p));
+    const int right_joins = __shfl_down_sync(kAll, (int)joins, 1);
+    const uintptr_t right = __shfl_down_sync(kAll, (uintptr_t)p, 1);
+    const bool taken = whole && lane < 31 && right_joins && right == (uintptr_t)(p + 8);
+    if (joins) {
+        // o values of the neighbour, then mine
+        if (o == 0)
+            raw.store(p);
+        else {
+            shift_window<4 + 2 * sizeof(T), sizeof(T) == 2>(w, 16 - o * (int)sizeof(T));
+            *reinterpret_cast<uint4*>(p - o) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (sizeof(T) == 4)
+                *reinterpret_cast<uint4*>(p - o + kPer) = make_uint4(w[4], w[5], w[6], w[7]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const bool written = (joins && i < 8 - o) || (taken && i >= 8 - o);
+        if (i < valid && !written) p[i] = from_f32<T>(v[i]);
+    }
+}
+
+// Two binary32 lanes at a time (see fma2 in pwlq_common.cuh).
+__device__ __forceinline__ u64 mul2(u64 a, u64 b) {
+    u64 d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d;
+}
+__device__ __forceinline__ u64 both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float lo2(u64 v) { float a, b; unpack2(v, a, b); return a; }
+__device__ __forceinline__ float hi2(u64 v) { float a, b; unpack2(v, a, b); return b; }
+
+// 32 bytes at once: eight binary32 or sixteen 16-bit values, on a 32-byte boundary.
+struct Raw32 { uint32_t w[8]; };
+__device__ __forceinline__ void store32(void* p, const Raw32& r) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]),
+                   "r"(r.w[6]), "r"(r.w[7]) : "memory");
+}
+__device__ __forceinline__ Raw32 load32(const void* p) {          // two 16-byte reads: any memory
+    const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+    return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
+}
+// The values of 32 bytes in pairs, and back.
+template <typename T> constexpr int kPairs32 = 16 / sizeof(T);
+template <typename T>
+__device__ __forceinline__ void pairs32(const Raw32& r, u64* v, T) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float a, b;
+        unpack16(r.w[i], a, b, T());
+        v[i] = pack2(a, b);
+    }
+}
+__device__ __forceinline__ void pairs32(const Raw32& r, u64* v, float) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = pack2(__uint_as_float(r.w[2 * i]), __uint_as_float(r.w[2 * i + 1]));
+}
+template <typename T>
+__device__ __forceinline__ Raw32 raw32(const u64* v, T) {
+    Raw32 r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.w[i] = pack16(lo2(v[i]), hi2(v[i]), T());
+    return r;
+}
+__device__ __forceinline__ Raw32 raw32(const u64* v, float) {
+    Raw32 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r.w[2 * i] = __float_as_uint(lo2(v[i]));
+        r.w[2 * i + 1] = __float_as_uint(hi2(v[i]));
+    }
+    return r;
+}
+
 // -------------------------------------------------------------------------------- the format
-// Range of a group from the largest magnitude bits among its values (an unsigned maximum orders
-// finite < Inf < NaN): NaN for a non-finite one, 0 below 2^-100.
-__device__ __forceinline__ float act8_range(uint32_t max_bits) {
-    if (max_bits >= kInfBits) return __uint_as_float(0x7fc00000u);
-    const float m = __uint_as_float(max_bits);
-    return m < kAct8Tiny ? 0.0f : m;
+// Larger of two magnitudes; NaN wins.
+__device__ __forceinline__ float max_abs(float top, float v) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(v)));
+    return r;
+}
+// Range of a group from its largest magnitude: NaN for a non-finite one, 0 below 2^-100.
+__device__ __forceinline__ float act8_range(float top) {
+    if (!(top < __uint_as_float(kInfBits))) return __uint_as_float(0x7fc00000u);
+    return top < kAct8Tiny ? 0.0f : top;
 }
 
 // Maximum over the aligned `lanes` (power of two <= 32) lanes that hold one group.
-__device__ __forceinline__ uint32_t group_max(uint32_t v, int lanes) {
-    for (int o = 1; o < lanes; o <<= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
+__device__ __forceinline__ float group_max(float v, int lanes) {
+    for (int o = 1; o < lanes; o <<= 1) v = max_abs(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 
@@ -135,32 +287,74 @@ __device__ __forceinline__ PieceParams act8_params(float m, float ratio) {
     return P;
 }
 
-// Byte of a value; P = act8_params of a group with a range that is neither 0 nor NaN.  The level sits
-// in the low mantissa bits after 1.5 * 2^23 was added (see quantize_mag).
-__device__ __forceinline__ uint32_t act8_byte(float x, const PieceParams& P) {
-    const float a = fabsf(x);
-    const bool tail = a > P.p;
-    const float u = __fsub_rn(a, tail ? P.p : 0.0f);
-    const float r = __fadd_rn(__fmul_rn(u, tail ? P.inv2 : P.inv1), 12582912.0f);
-    const int q = min(__float_as_int(r) - 0x4B400000, 63);
-    return (x < 0.0f ? 128u : 0u) | (tail ? 64u : 0u) | (uint32_t)q;
-}
-
-// Four bytes, the first in the low bits; 0 for a group that holds nothing.
-__device__ __forceinline__ uint32_t act8_word(const float* x, float m, const PieceParams& P) {
-    if (!(m > 0.0f)) return 0u;
-    return act8_byte(x[0], P) | act8_byte(x[1], P) << 8 | act8_byte(x[2], P) << 16 |
-           act8_byte(x[3], P) << 24;
-}
-
-__device__ __forceinline__ float act8_value(uint32_t byte, const PieceParams& P) {
-    const float q = (float)(byte & 63u);
-    const float v = (byte & 64u) ? __fadd_rn(__fmul_rn(q, P.s2), P.p) : __fmul_rn(q, P.s1);
-    return __uint_as_float(__float_as_uint(v) ^ ((byte & 128u) << 24));
-}
-__device__ __forceinline__ void act8_values(uint32_t word, const PieceParams& P, float* v) {
+// Eight bytes of eight values of a group with range m; P = act8_params(m).  Both pieces' levels are
+// formed and one is taken: adding 1.5 * 2^23 (+ 64 in the tail) rounds the product to an integer,
+// ties to even, and leaves region * 64 + level in the low byte of the sum.  No clamp is needed: a
+// product exceeds 63 by its own rounding at most.  x + 0 makes -0 a +0, whose sign bit is clear.
+__device__ __forceinline__ uint2 act8_bytes8(const float* x, float m, const PieceParams& P) {
+    uint32_t w[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = act8_value((word >> (8 * i)) & 0xffu, P);
+    for (int h = 0; h < 2; ++h) {
+        uint32_t r[4], s[4];
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            float y[2];
+            unpack2(add2(pack2(x[4 * h + i], x[4 * h + i + 1]), 0ull), y[0], y[1]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float a = fabsf(y[k]);
+                const float center = __fadd_rn(__fmul_rn(a, P.inv1), 12582912.0f);
+                const float tail = __fadd_rn(__fmul_rn(__fsub_rn(a, P.p), P.inv2), 12582912.0f + 64.0f);
+                r[i + k] = __float_as_uint(a > P.p ? tail : center);
+                s[i + k] = __float_as_uint(y[k]);
+            }
+        }
+        const uint32_t low = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
+        const uint32_t top = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410);
+        w[h] = low | (top & 0x80808080u);
+    }
+    return m > 0.0f ? make_uint2(w[0], w[1]) : make_uint2(0u, 0u);
+}
+
+// The eight values of eight bytes times a factor, in pairs, to within a few roundings (the gradients'
+// use; act8_values8 gives the format's own bits).  f = 128 + j from a byte permutation; the pieces are
+// the lines s1 * (f - 128) and p + s2 * (f - 192), one fused operation each.
+struct Act8Lines { u64 s1, z1, s2, z2; };
+__device__ __forceinline__ Act8Lines act8_lines(float m, float ratio, float factor) {
+    const float p = m * ratio, s1 = p * (1.0f / kAct8Levels) * factor, s2 = (m - p) * (1.0f / kAct8Levels) * factor;
+    return {both(s1), both(-128.0f * s1), both(s2), both(fmaf(-192.0f, s2, p * factor))};
+}
+__device__ __forceinline__ void act8_scaled8(uint2 bytes, const Act8Lines& L, u64* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i < 2 ? bytes.x : bytes.y, j = w & 0x7f7f7f7fu;
+        const float f0 = __uint_as_float(__byte_perm(j, 0x43000000u, i & 1 ? 0x7244 : 0x7044));
+        const float f1 = __uint_as_float(__byte_perm(j, 0x43000000u, i & 1 ? 0x7344 : 0x7144));
+        const u64 f = pack2(f0, f1), c = fma2(f, L.s1, L.z1), t = fma2(f, L.s2, L.z2);
+        const float v0 = f0 >= 192.0f ? lo2(t) : lo2(c), v1 = f1 >= 192.0f ? hi2(t) : hi2(c);
+        const uint32_t n0 = w << (i & 1 ? 8 : 24), n1 = i & 1 ? w : w << 16;
+        v[i] = pack2(__uint_as_float(__float_as_uint(v0) ^ (n0 & 0x80000000u)),
+                     __uint_as_float(__float_as_uint(v1) ^ (n1 & 0x80000000u)));
+    }
+}
+
+// The eight values of eight bytes, in pairs.  A byte permutation puts j = region * 64 + level into
+// the upper mantissa of 128 + j, so no integer is converted; both pieces are formed and one is taken.
+__device__ __forceinline__ void act8_values8(uint2 bytes, const PieceParams& P, u64* v) {
+    const u64 s1 = both(P.s1), s2 = both(P.s2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i < 2 ? bytes.x : bytes.y, j = w & 0x7f7f7f7fu;
+        const float f0 = __uint_as_float(__byte_perm(j, 0x43000000u, i & 1 ? 0x7244 : 0x7044));
+        const float f1 = __uint_as_float(__byte_perm(j, 0x43000000u, i & 1 ? 0x7344 : 0x7144));
+        const u64 f = pack2(f0, f1);
+        const u64 c = mul2(add2(f, both(-128.0f)), s1), t = mul2(add2(f, both(-192.0f)), s2);
+        const float v0 = f0 >= 192.0f ? __fadd_rn(lo2(t), P.p) : lo2(c);
+        const float v1 = f1 >= 192.0f ? __fadd_rn(hi2(t), P.p) : hi2(c);
+        const uint32_t n0 = w << (i & 1 ? 8 : 24), n1 = i & 1 ? w : w << 16;
+        v[i] = pack2(__uint_as_float(__float_as_uint(v0) ^ (n0 & 0x80000000u)),
+                     __uint_as_float(__float_as_uint(v1) ^ (n1 & 0x80000000u)));
+    }
 }
 
 }  // namespace pwlq

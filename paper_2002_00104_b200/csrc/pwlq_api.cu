@@ -876,9 +876,9 @@ int pwlq_select_analytic_ragged(const float* x, const int64_t* row_offsets, int6
 
 int pwlq_device_status(void) {
     const int a = pwlq::take_absmax_timeout_flag(), q = pwlq::take_quantize_timeout_flag(),
-              w = pwlq::take_weight_grad_timeout_flag();
-    if (a < 0 || q < 0 || w < 0) return 1 << PWLQ_ERR_CUDA;
-    return (((a | q | w) & 1) ? (1 << PWLQ_ERR_TIMEOUT) : 0) |
+              w = pwlq::take_weight_grad_timeout_flag(), b = pwlq::take_block_norm_timeout_flag();
+    if (a < 0 || q < 0 || w < 0 || b < 0) return 1 << PWLQ_ERR_CUDA;
+    return (((a | q | w | b) & 1) ? (1 << PWLQ_ERR_TIMEOUT) : 0) |
            (((a | q) & 2) ? (1 << PWLQ_ERR_INVALID_ARG) : 0);
 }
 

@@ -2,53 +2,90 @@
 //
 // Both directions are bound by HBM: per value the forward pass reads x and f and writes r and h
 // (and two bytes when it saves), the backward pass reads dh, dr and two bytes and writes dx and df.
-// A row is owned by one CTA, eight consecutive values per thread and step, and stays in registers
-// between the two reductions that depend on one another (of f, then of r; of the outer norm, then
-// of the inner one), so every operand crosses HBM once.
+// A row is owned by one CTA, eight consecutive values per thread and step, and stays on chip between
+// the two reductions that depend on one another (of f, then of r; of the outer norm, then of the
+// inner one), so every operand crosses HBM once.
+//
+// Where the rows start on 32-byte boundaries (and, forward, there are enough of them), persistent CTAs
+// walk the rows and a ring of shared-memory stages holds the next ones, brought in by bulk copies: the
+// loads of a row are then in flight during the reductions of the rows before it, at no cost in
+// registers, and a thread works on 32 bytes of columns at a time, which shares the reductions' and
+// the ranges' cost.  Else a thread loads its values itself, eight at a time (see load8 for rows off
+// the boundary).
+#include <algorithm>
+#include <mutex>
+
 #include "pwlq_act8.cuh"
+#include "pwlq_pipeline.cuh"
 #include "pwlq_train.h"
 
 namespace pwlq {
+
+static __device__ int g_block_norm_timeout;     // a bounded wait expired
+
 namespace {
 
-// Sum over the CTA, the same value in every thread, in a fixed order.  Calls alternate between the
+constexpr int kMaxStages = 8;
+
+// Sum over the CTA (of up to 32 warps), the same value in every thread, in a fixed order.  Calls alternate between the
 // two halves of `buf`, so one barrier per call is enough: a half is written again only after the
-// barrier of the call in between.
-template <int N>
+// barrier of the call in between.  After a call every thread of the CTA has arrived at it.
 struct CtaSum {
-    float (*buf)[N][32];
+    float (*buf)[32];
     int half = 0;
-    __device__ __forceinline__ void operator()(float (&v)[N]) {
+    __device__ __forceinline__ float operator()(float v) {
         const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-            for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-        if (warps == 1) return;
-        if (lane == 0)
-#pragma unroll
-            for (int k = 0; k < N; ++k) buf[half][k][warp] = v[k];
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (warps == 1) { __syncwarp(); return v; }
+        if (lane == 0) buf[half][warp] = v;
         __syncthreads();
-#pragma unroll
-        for (int k = 0; k < N; ++k) {
-            v[k] = lane < warps ? buf[half][k][lane] : 0.0f;
-            for (int o = 16; o; o >>= 1) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+        v = lane < warps ? buf[half][lane] : 0.0f;
+        if (warps > 8) {
+            v += __shfl_xor_sync(0xffffffffu, v, 16);
+            v += __shfl_xor_sync(0xffffffffu, v, 8);
         }
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        v += __shfl_xor_sync(0xffffffffu, v, 2);
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
         half ^= 1;
+        return __shfl_sync(0xffffffffu, v, 0);
     }
 };
+__device__ __forceinline__ float sum8(u64 s) { return lo2(s) + hi2(s); }
 
-// Eight weights (or gates) starting at column c, as binary32.
+template <typename T>
+__device__ __forceinline__ void pairs8(const Raw8<T>& raw, u64* v) {
+    float f[8];
+    raw.get(f);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = pack2(f[2 * k], f[2 * k + 1]);
+}
+__device__ __forceinline__ void floats8(const u64* v, float* f) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) unpack2(v[k], f[2 * k], f[2 * k + 1]);
+}
 template <bool VEC, typename T>
-__device__ __forceinline__ void weights8(const void* p, bool f32, int64_t c, int valid, float* w) {
+__device__ __forceinline__ void store_pairs(const u64* v, T* p, int valid) {
+    float f[8];
+    floats8(v, f);
+    store8<VEC>(f, p, valid);
+}
+
+// Eight weights (or gates) from column c on, as binary32, plus `offset`.
+template <bool VEC, typename T>
+__device__ __forceinline__ void weights8(const void* p, bool f32, int64_t at, int c, int valid, float offset,
+                                         u64* w) {
     if (f32) {
         Raw8<float> raw;
-        load8<VEC>(raw, static_cast<const float*>(p) + c, valid);
-        raw.get(w);
+        load8<VEC>(raw, static_cast<const float*>(p) + at + c, valid, c);
+        pairs8(raw, w);
     } else {
         Raw8<T> raw;
-        load8<VEC>(raw, static_cast<const T*>(p) + c, valid);
-        raw.get(w);
+        load8<VEC>(raw, static_cast<const T*>(p) + at + c, valid, c);
+        pairs8(raw, w);
     }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = add2(w[k], both(offset));
 }
 
 struct NormParams {
@@ -57,100 +94,252 @@ struct NormParams {
     int64_t groups;
     int group_lanes, group_shift;
     bool wf32;
+    int stages;
+    unsigned row_bytes, code_bytes;       // of a row in a stage
+    int64_t gate_step, gate_rest;         // gridDim.x / gate_tokens and the remainder (forward)
+};
+
+// ---- the ring.  Stage s of CTA-local row number i is s = i % stages; full[s] completes when the
+// row's copies have landed.
+struct Ring {
+    uint64_t* full;
+    unsigned char* stage0;
+    unsigned stage_bytes;
+    int stages;
+    int stage = 0;
+    unsigned phase = 0;
+    bool dead = false;                    // a wait expired: no more waiting, the results are void
+    __device__ __forceinline__ unsigned char* wait() {
+        if (!dead && !mbar_wait(&full[stage], phase)) {
+            dead = true;
+            g_block_norm_timeout = 1;
+        }
+        return stage0 + (size_t)stage * stage_bytes;
+    }
+    __device__ __forceinline__ void next() {
+        if (++stage == stages) { stage = 0; phase ^= 1; }
+    }
 };
 
 // Bytes of eight values of a row, and the range of their group (whose lanes call this together).
-__device__ __forceinline__ void save8(const float* v, const NormParams& q, int64_t row, int c,
+__device__ __forceinline__ void save8(const u64* pairs, const NormParams& q, int64_t row, int c,
                                       int valid, uint8_t* codes, float* ranges) {
-    uint32_t top = 0;
+    float v[8], top = 0.0f;
+    floats8(pairs, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
+    for (int i = 0; i < 8; ++i) top = max_abs(top, v[i]);
     top = group_max(top, q.group_lanes);
     if (valid <= 0) return;
     const float m = act8_range(top);
-    const PieceParams P = act8_params(m, q.ratio);
-    const uint2 w = make_uint2(act8_word(v, m, P), act8_word(v + 4, m, P));
     uint8_t* at = codes + row * q.a.ldc + c;
-    *reinterpret_cast<uint2*>(at) = w;
+    *reinterpret_cast<uint2*>(at) = act8_bytes8(v, m, act8_params(m, q.ratio));
     // the row's last 16 bytes may need zeros that no value stands for
     if (valid <= 8 && (c & 8) == 0) *reinterpret_cast<uint2*>(at + 8) = make_uint2(0u, 0u);
     if ((c & ((1 << q.group_shift) - 1)) == 0) ranges[row * q.groups + (c >> q.group_shift)] = m;
 }
 
-// VC: chunks of eight columns per thread.
+template <typename T>
+__device__ __forceinline__ void request_forward(const NormParams& q, Ring& ring, int stage, int64_t row) {
+    unsigned char* to = ring.stage0 + (size_t)stage * ring.stage_bytes;
+    mbar_expect_tx(&ring.full[stage], q.a.f ? 2 * q.row_bytes : q.row_bytes);
+    bulk_copy_g2s(to, static_cast<const T*>(q.a.x) + row * q.a.ldx, q.row_bytes, &ring.full[stage]);
+    if (q.a.f)
+        bulk_copy_g2s(to + q.row_bytes, static_cast<const T*>(q.a.f) + row * q.a.ldf, q.row_bytes,
+                      &ring.full[stage]);
+}
+
+// Forward, every thread loading its values itself, one row per CTA.  VC: chunks of eight columns per
+// thread.
 template <typename T, int VC, bool VEC, bool SAVE>
-__global__ void __launch_bounds__(VC == 4 ? 512 : 256) block_norm_kernel(NormParams q) {
-    __shared__ float buf[2][1][32];
-    CtaSum<1> cta_sum{buf};
-    const int64_t row = blockIdx.x;
+__global__ void __launch_bounds__(1024) block_norm_kernel(const __grid_constant__ NormParams q) {
+    __shared__ float buf[2][32];
+    CtaSum cta_sum{buf};
     const int cols = (int)q.a.cols;
+    const int64_t row = blockIdx.x;
     const T* x = static_cast<const T*>(q.a.x) + row * q.a.ldx;
     const T* f = static_cast<const T*>(q.a.f) + row * q.a.ldf;
     Raw8<T> rx[VC], rf[VC];
 #pragma unroll
     for (int i = 0; i < VC; ++i) {
         const int c = (threadIdx.x + i * blockDim.x) * 8;
-        load8<VEC>(rx[i], x + c, cols - c);
-        if (q.a.f) load8<VEC>(rf[i], f + c, cols - c);
+        if (q.a.f) load8<VEC>(rf[i], f + c, cols - c, c);
+        load8<VEC>(rx[i], x + c, cols - c, c);
     }
-    float r[VC][8], sum[1];
+    u64 r[VC][4];
     float rstd_f = 1.0f;
     if (q.a.post_weight) {
-        sum[0] = 0.0f;
+        u64 s = 0ull;
 #pragma unroll
         for (int i = 0; i < VC; ++i) {
-            float v[8];
-            rf[i].get(v);
+            u64 v[4];
+            pairs8(rf[i], v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[0] = fmaf(v[k], v[k], sum[0]);
+            for (int k = 0; k < 4; ++k) s = fma2(v[k], v[k], s);
         }
-        cta_sum(sum);
-        rstd_f = rsqrtf(fmaf(sum[0], q.inv_cols, q.eps));
+        rstd_f = rsqrtf(fmaf(cta_sum(sum8(s)), q.inv_cols, q.eps));
         if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
     }
-    sum[0] = 0.0f;
+    u64 s = 0ull;
+    const int64_t gate_at = q.a.gate ? row / q.a.gate_tokens * q.a.ldgate : 0;
 #pragma unroll
     for (int i = 0; i < VC; ++i) {
         const int c = (threadIdx.x + i * blockDim.x) * 8, valid = cols - c;
-        float v[8];
-        rx[i].get(r[i]);
+        pairs8(rx[i], r[i]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) r[i][k] *= q.scale;
+        for (int k = 0; k < 4; ++k) r[i][k] = mul2(r[i][k], both(q.scale));
         if (q.a.f) {
-            rf[i].get(v);
+            u64 v[4], w[4];
+            pairs8(rf[i], v);
             if (SAVE && q.a.f_codes) save8(v, q, row, c, valid, q.a.f_codes, q.a.f_ranges);
-            float w[8];
             if (q.a.post_weight) {
-                weights8<VEC, T>(q.a.post_weight, q.wf32, c, valid, w);
+                weights8<VEC, T>(q.a.post_weight, q.wf32, 0, c, valid, q.offset, w);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = v[k] * rstd_f * (w[k] + q.offset);
+                for (int k = 0; k < 4; ++k) v[k] = mul2(mul2(v[k], both(rstd_f)), w[k]);
             }
             if (q.a.gate) {
-                weights8<VEC, T>(q.a.gate, q.wf32, row / q.a.gate_tokens * q.a.ldgate + c, valid, w);
+                weights8<VEC, T>(q.a.gate, q.wf32, gate_at, c, valid, 0.0f, w);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] *= w[k];
+                for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], w[k]);
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) r[i][k] += v[k];
+            for (int k = 0; k < 4; ++k) r[i][k] = add2(r[i][k], v[k]);
         }
-        if (q.a.r) store8<VEC>(r[i], static_cast<T*>(q.a.r) + row * q.a.ldr + c, valid);
+        if (q.a.r) store_pairs<VEC>(r[i], static_cast<T*>(q.a.r) + row * q.a.ldr + c, valid);
         if (SAVE && q.a.r_codes) save8(r[i], q, row, c, valid, q.a.r_codes, q.a.r_ranges);
+        // columns past the row hold 0 here, or NaN where the whole row does
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < valid) sum[0] = fmaf(r[i][k], r[i][k], sum[0]);
+        for (int k = 0; k < 4; ++k) s = fma2(r[i][k], r[i][k], s);
     }
     if (!q.a.pre_weight) return;
-    cta_sum(sum);
-    const float rstd_r = rsqrtf(fmaf(sum[0], q.inv_cols, q.eps));
+    const float rstd_r = rsqrtf(fmaf(cta_sum(sum8(s)), q.inv_cols, q.eps));
     if (SAVE && threadIdx.x == 0 && q.a.r_rstd) q.a.r_rstd[row] = rstd_r;
 #pragma unroll
     for (int i = 0; i < VC; ++i) {
         const int c = (threadIdx.x + i * blockDim.x) * 8, valid = cols - c;
-        float w[8];
-        weights8<VEC, T>(q.a.pre_weight, q.wf32, c, valid, w);
+        u64 w[4];
+        weights8<VEC, T>(q.a.pre_weight, q.wf32, 0, c, valid, q.offset, w);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[k] = r[i][k] * rstd_r * (w[k] + q.offset);
-        store8<VEC>(w, static_cast<T*>(q.a.h) + row * q.a.ldh + c, valid);
+        for (int k = 0; k < 4; ++k) w[k] = mul2(mul2(r[i][k], both(rstd_r)), w[k]);
+        store_pairs<VEC>(w, static_cast<T*>(q.a.h) + row * q.a.ldh + c, valid);
+    }
+}
+
+// Weights (or gates) of a thread's 32 bytes of columns, as binary32 pairs, plus `offset`.
+template <typename T>
+__device__ __forceinline__ void weights32(const void* p, bool f32, int64_t at, float offset, u64* w) {
+    constexpr int kP = kPairs32<T>;
+    if (sizeof(T) == 2 && f32) {
+        pairs32(load32(static_cast<const float*>(p) + at), w, 0.0f);
+        pairs32(load32(static_cast<const float*>(p) + at + 8), w + kP / 2, 0.0f);
+    } else {
+        pairs32(load32(static_cast<const T*>(p) + at), w, T());
+    }
+#pragma unroll
+    for (int k = 0; k < kP; ++k) w[k] = add2(w[k], both(offset));
+}
+
+// Bytes of a thread's 32 bytes of values, and the range of their group.
+template <typename T>
+__device__ __forceinline__ void save32(const u64* v, const NormParams& q, bool live, int64_t row, int c,
+                                       uint8_t* codes, float* ranges) {
+    constexpr int kP = kPairs32<T>;
+    float f[2 * kP], top = 0.0f;
+#pragma unroll
+    for (int k = 0; k < kP; ++k) unpack2(v[k], f[2 * k], f[2 * k + 1]);
+#pragma unroll
+    for (int k = 0; k < 2 * kP; ++k) top = max_abs(top, f[k]);
+    top = group_max(top, q.group_lanes);
+    if (!live) return;
+    const float m = act8_range(top);
+    const PieceParams P = act8_params(m, q.ratio);
+    uint8_t* at = codes + row * q.a.ldc + c;
+    const uint2 a = act8_bytes8(f, m, P);
+    if (kP == 8) {
+        const uint2 b = act8_bytes8(f + 2 * kP - 8, m, P);
+        *reinterpret_cast<uint4*>(at) = make_uint4(a.x, a.y, b.x, b.y);
+    } else {
+        *reinterpret_cast<uint2*>(at) = a;
+    }
+    // the row's last 16 bytes may need zeros that no value stands for
+    if ((c & 8) == 0 && c + 8 == (int)q.a.cols) *reinterpret_cast<uint2*>(at + 8) = make_uint2(0u, 0u);
+    if ((c & ((1 << q.group_shift) - 1)) == 0) ranges[row * q.groups + (c >> q.group_shift)] = m;
+}
+
+// Forward with a ring: 32 bytes of columns per thread.
+template <typename T, bool SAVE>
+__global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(const __grid_constant__ NormParams q) {
+    constexpr int kP = kPairs32<T>;
+    __shared__ float buf[2][32];
+    __shared__ uint64_t full[kMaxStages];
+    extern __shared__ __align__(16) unsigned char smem[];
+    CtaSum cta_sum{buf};
+    Ring ring{full, smem, q.a.f ? 2 * q.row_bytes : q.row_bytes, q.stages};
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < q.stages; ++s) mbar_init(&full[s], 1);
+        fence_barrier_init();
+        for (int s = 0; s < q.stages; ++s) {
+            const int64_t row = blockIdx.x + (int64_t)s * gridDim.x;
+            if (row < q.a.rows) request_forward<T>(q, ring, s, row);
+        }
+    }
+    __syncthreads();
+    // the row's gate, found by division once and by addition from then on
+    int64_t gate = 0, in_gate = 0;
+    if (q.a.gate) {
+        gate = blockIdx.x / q.a.gate_tokens;
+        in_gate = blockIdx.x - gate * q.a.gate_tokens;
+    }
+    const int c = threadIdx.x * 2 * kP;
+    const bool live = c < (int)q.a.cols, post = q.a.post_weight, pre = q.a.pre_weight;
+    for (int64_t row = blockIdx.x; row < q.a.rows; row += gridDim.x) {
+        u64 f[kP] = {}, r[kP] = {}, w[kP] = {}, s = 0ull;
+        const unsigned char* at = ring.wait() + threadIdx.x * 32;
+        if (live) pairs32(load32(at), r, T());
+        if (live && q.a.f) pairs32(load32(at + q.row_bytes), f, T());
+        float rstd_f = 1.0f;
+        if (post) {
+#pragma unroll
+            for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
+            if (live) weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
+            rstd_f = rsqrtf(fmaf(cta_sum(sum8(s)), q.inv_cols, q.eps));
+            if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
+        }
+        if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+        if (post)
+#pragma unroll
+            for (int k = 0; k < kP; ++k) f[k] = mul2(mul2(f[k], both(rstd_f)), w[k]);
+        if (q.a.gate) {
+            if (live) weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, 0.0f, w);
+#pragma unroll
+            for (int k = 0; k < kP; ++k) f[k] = mul2(f[k], w[k]);
+            gate += q.gate_step;
+            in_gate += q.gate_rest;
+            if (in_gate >= q.a.gate_tokens) { ++gate; in_gate -= q.a.gate_tokens; }
+        }
+        s = 0ull;
+#pragma unroll
+        for (int k = 0; k < kP; ++k) {
+            r[k] = add2(mul2(r[k], both(q.scale)), f[k]);
+            s = fma2(r[k], r[k], s);
+        }
+        if (live && q.a.r) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
+        float rstd_r = 0.0f;
+        if (pre) {
+            if (live) weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
+            rstd_r = rsqrtf(fmaf(cta_sum(sum8(s)), q.inv_cols, q.eps));
+        } else {
+            __syncthreads();
+        }
+        // every thread has its values of this stage
+        const int64_t ahead = row + (int64_t)q.stages * gridDim.x;
+        if (threadIdx.x == 0 && ahead < q.a.rows && !ring.dead) request_forward<T>(q, ring, ring.stage, ahead);
+        ring.next();
+        if (SAVE && q.a.r_codes) save32<T>(r, q, live, row, c, q.a.r_codes, q.a.r_ranges);
+        if (!pre) continue;
+        if (SAVE && threadIdx.x == 0 && q.a.r_rstd) q.a.r_rstd[row] = rstd_r;
+#pragma unroll
+        for (int k = 0; k < kP; ++k) w[k] = mul2(mul2(r[k], both(rstd_r)), w[k]);
+        if (live) store32(static_cast<T*>(q.a.h) + row * q.a.ldh + c, raw32(w, T()));
     }
 }
 
@@ -172,35 +361,32 @@ enum { kDpre, kDpost, kDgate };
 
 template <int VC, bool WIDE>
 struct ColumnSums {
-    float reg[3][WIDE ? 1 : VC][8] = {};
-    float4* smem = nullptr;               // [3][VC][2][blockDim.x]
-    __device__ __forceinline__ float4* at(int which, int i) const {
+    u64 reg[3][WIDE ? 1 : VC][4] = {};
+    ulonglong2* smem = nullptr;           // [3][VC][2][blockDim.x]
+    __device__ __forceinline__ ulonglong2* at(int which, int i) const {
         return smem + ((which * VC + i) * 2) * blockDim.x + threadIdx.x;
     }
     __device__ __forceinline__ void clear(int which) {
+        const u64 zero[4] = {};
 #pragma unroll
-        for (int i = 0; i < VC; ++i) {
-            const float zero[8] = {};
-            set(which, i, zero);
-        }
+        for (int i = 0; i < VC; ++i) set(which, i, zero);
     }
-    __device__ __forceinline__ void set(int which, int i, const float* v) {
+    __device__ __forceinline__ void set(int which, int i, const u64* v) {
         if (WIDE) {
-            at(which, i)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            at(which, i)[blockDim.x] = make_float4(v[4], v[5], v[6], v[7]);
+            at(which, i)[0] = make_ulonglong2(v[0], v[1]);
+            at(which, i)[blockDim.x] = make_ulonglong2(v[2], v[3]);
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) reg[which][WIDE ? 0 : i][k] = v[k];
+            for (int k = 0; k < 4; ++k) reg[which][WIDE ? 0 : i][k] = v[k];
         }
     }
-    __device__ __forceinline__ void get(int which, int i, float* v) const {
+    __device__ __forceinline__ void get(int which, int i, u64* v) const {
         if (WIDE) {
-            const float4 a = at(which, i)[0], b = at(which, i)[blockDim.x];
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-            v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            const ulonglong2 a = at(which, i)[0], b = at(which, i)[blockDim.x];
+            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
         } else {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = reg[which][WIDE ? 0 : i][k];
+            for (int k = 0; k < 4; ++k) v[k] = reg[which][WIDE ? 0 : i][k];
         }
     }
     template <bool VEC>
@@ -208,29 +394,81 @@ struct ColumnSums {
 #pragma unroll
         for (int i = 0; i < VC; ++i) {
             const int c = (threadIdx.x + i * blockDim.x) * 8;
-            float v[8];
+            u64 v[4];
             get(which, i, v);
-            store8<VEC>(v, to + c, cols - c);
+            store_pairs<VEC>(v, to + c, cols - c);
         }
     }
 };
 
+template <typename T>
+__device__ __forceinline__ void request_backward(const GradParams& p, Ring& ring, int stage, int64_t row) {
+    const NormParams& q = p.q;
+    unsigned char* to = ring.stage0 + (size_t)stage * ring.stage_bytes;
+    uint64_t* bar = &ring.full[stage];
+    mbar_expect_tx(bar, ring.stage_bytes);
+    if (q.a.pre_weight) {
+        bulk_copy_g2s(to, static_cast<const T*>(p.g.dh) + row * p.g.lddh, q.row_bytes, bar);
+        to += q.row_bytes;
+        bulk_copy_g2s(to, q.a.r_codes + row * q.a.ldc, q.code_bytes, bar);
+        to += q.code_bytes;
+    }
+    if (p.g.dr) {
+        bulk_copy_g2s(to, static_cast<const T*>(p.g.dr) + row * p.g.lddr, q.row_bytes, bar);
+        to += q.row_bytes;
+    }
+    if (q.a.f_codes) bulk_copy_g2s(to, q.a.f_codes + row * q.a.ldc, q.code_bytes, bar);
+}
+
+// Eight bytes of a row from column c on; those past the row read as 0.
+__device__ __forceinline__ uint2 bytes8(const uint8_t* row, int c, int valid) {
+    uint2 b = make_uint2(0u, 0u);
+    if (valid > 0) {
+        b = *reinterpret_cast<const uint2*>(row + c);
+        if (valid < 8) {
+            b.x &= valid >= 4 ? 0xffffffffu : (1u << (8 * valid)) - 1;
+            b.y &= valid > 4 ? (1u << (8 * (valid - 4))) - 1 : 0u;
+        }
+    }
+    return b;
+}
+
+// Backward, every thread loading its values itself.
 template <typename T, int VC, bool VEC, bool WIDE>
-__global__ void __launch_bounds__(WIDE ? 512 : 1024) block_norm_backward_kernel(GradParams p) {
-    __shared__ float buf[2][1][32];
-    extern __shared__ float4 wide[];
-    CtaSum<1> cta_sum{buf};
+__global__ void __launch_bounds__(WIDE ? 512 : 1024)
+block_norm_backward_kernel(const __grid_constant__ GradParams p) {
+    __shared__ float buf[2][32];
+    extern __shared__ __align__(16) unsigned char smem[];
+    CtaSum cta_sum{buf};
     const NormParams& q = p.q;
     const int cols = (int)q.a.cols;
     const int64_t first = blockIdx.x * p.rows_per_cta, last = min(first + p.rows_per_cta, q.a.rows);
-    const bool pre = q.a.pre_weight, post = q.a.post_weight, has_f = q.a.f_codes;
+    const bool pre = q.a.pre_weight, post = q.a.post_weight, has_f = q.a.f_codes, has_dr = p.g.dr;
     ColumnSums<VC, WIDE> sums;
     if (WIDE) {
-        sums.smem = wide;
+        sums.smem = reinterpret_cast<ulonglong2*>(smem);
         for (int which = 0; which < 3; ++which) sums.clear(which);
     }
     int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
+
+    // a row's ranges and factors, requested one row ahead
+    float mr[VC], mf[VC], rstd_r = 0.0f, rstd_f = 1.0f;
+    auto fetch = [&](int64_t row) {
+        if (pre) rstd_r = q.a.r_rstd[row];
+        if (post) rstd_f = q.a.f_rstd[row];
+#pragma unroll
+        for (int i = 0; i < VC; ++i) {
+            const int c = (threadIdx.x + i * blockDim.x) * 8;
+            mr[i] = mf[i] = 0.0f;
+            if (c < cols) {
+                const int64_t at = row * q.groups + (c >> q.group_shift);
+                if (pre) mr[i] = q.a.r_ranges[at];
+                if (has_f) mf[i] = q.a.f_ranges[at];
+            }
+        }
+    };
+    if (first < last) fetch(first);
 
     for (int64_t row = first; row < last; ++row) {
         if (q.a.gate && row == gate_end) {
@@ -239,109 +477,114 @@ __global__ void __launch_bounds__(WIDE ? 512 : 1024) block_norm_backward_kernel(
             ++gate;
             gate_end += q.a.gate_tokens;
         }
-        const float rstd_r = pre ? q.a.r_rstd[row] : 0.0f;
-        const float rstd_f = post ? q.a.f_rstd[row] : 1.0f;
-        float e[VC][8], n[VC][8], sum[1] = {0.0f};
+        const float factor_r = rstd_r, factor_f = rstd_f;
+        float now_r[VC], now_f[VC];
+#pragma unroll
+        for (int i = 0; i < VC; ++i) {
+            now_r[i] = mr[i];
+            now_f[i] = mf[i];
+        }
+        if (row + 1 < last) fetch(row + 1);
+        const T* dh = static_cast<const T*>(p.g.dh) + row * p.g.lddh;
+        const T* dr = static_cast<const T*>(p.g.dr) + row * p.g.lddr;
+        const uint8_t* rb = q.a.r_codes + row * q.a.ldc;
+        const uint8_t* fb = q.a.f_codes + row * q.a.ldc;
+        u64 e[VC][4], n[VC][4], s = 0ull;
         // outer norm: e = dr + rstd * (u - n * mean(u n))
         if (pre) {
 #pragma unroll
             for (int i = 0; i < VC; ++i) {
                 const int c = (threadIdx.x + i * blockDim.x) * 8, valid = cols - c;
                 Raw8<T> raw;
-                float w[8];
-                load8<VEC>(raw, static_cast<const T*>(p.g.dh) + row * p.g.lddh + c, valid);
-                raw.get(e[i]);
-                weights8<VEC, T>(q.a.pre_weight, q.wf32, c, valid, w);
-                uint2 b = make_uint2(0u, 0u);
-                PieceParams S = {};
-                if (valid > 0) {
-                    b = *reinterpret_cast<const uint2*>(q.a.r_codes + row * q.a.ldc + c);
-                    S = act8_params(q.a.r_ranges[row * q.groups + (c >> q.group_shift)], q.ratio);
-                }
-                act8_values(b.x, S, n[i]);
-                act8_values(b.y, S, n[i] + 4);
-                float d[8];
+                load8<VEC>(raw, dh + c, valid, c);
+                pairs8(raw, e[i]);
+                act8_scaled8(bytes8(rb, c, valid), act8_lines(now_r[i], q.ratio, factor_r), n[i]);
+                u64 w[4], d[4];
+                weights8<VEC, T>(q.a.pre_weight, q.wf32, 0, c, valid, q.offset, w);
                 sums.get(kDpre, i, d);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    n[i][k] *= rstd_r;
-                    d[k] = fmaf(e[i][k], n[i][k], d[k]);
-                    e[i][k] *= w[k] + q.offset;
-                    if (k < valid) sum[0] = fmaf(e[i][k], n[i][k], sum[0]);
+                for (int k = 0; k < 4; ++k) {
+                    d[k] = fma2(e[i][k], n[i][k], d[k]);
+                    e[i][k] = mul2(e[i][k], w[k]);
+                    s = fma2(e[i][k], n[i][k], s);
                 }
                 sums.set(kDpre, i, d);
             }
-            cta_sum(sum);
-            const float mean = sum[0] * q.inv_cols;
+            const float mean = cta_sum(sum8(s)) * q.inv_cols;
 #pragma unroll
             for (int i = 0; i < VC; ++i)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) e[i][k] = rstd_r * fmaf(-mean, n[i][k], e[i][k]);
+                for (int k = 0; k < 4; ++k) e[i][k] = mul2(fma2(n[i][k], both(-mean), e[i][k]), both(factor_r));
         } else {
 #pragma unroll
             for (int i = 0; i < VC; ++i)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) e[i][k] = 0.0f;
+                for (int k = 0; k < 4; ++k) e[i][k] = 0ull;
         }
-        sum[0] = 0.0f;
+        s = 0ull;
 #pragma unroll
         for (int i = 0; i < VC; ++i) {
             const int c = (threadIdx.x + i * blockDim.x) * 8, valid = cols - c;
-            float w[8];
-            if (p.g.dr) {
+            u64 w[4];
+            if (has_dr) {
                 Raw8<T> raw;
-                load8<VEC>(raw, static_cast<const T*>(p.g.dr) + row * p.g.lddr + c, valid);
-                raw.get(w);
+                load8<VEC>(raw, dr + c, valid, c);
+                pairs8(raw, w);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) e[i][k] += w[k];
+                for (int k = 0; k < 4; ++k) e[i][k] = add2(e[i][k], w[k]);
             }
             if (p.g.dx) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) w[k] = q.scale * e[i][k];
-                store8<VEC>(w, static_cast<T*>(p.g.dx) + row * p.g.lddx + c, valid);
+                for (int k = 0; k < 4; ++k) w[k] = mul2(e[i][k], both(q.scale));
+                store_pairs<VEC>(w, static_cast<T*>(p.g.dx) + row * p.g.lddx + c, valid);
             }
             if (!has_f) continue;
             // inner norm and gate; e becomes v = e * gate * w
-            uint2 b = make_uint2(0u, 0u);
-            PieceParams S = {};
-            if (valid > 0) {
-                b = *reinterpret_cast<const uint2*>(q.a.f_codes + row * q.a.ldc + c);
-                S = act8_params(q.a.f_ranges[row * q.groups + (c >> q.group_shift)], q.ratio);
-            }
-            act8_values(b.x, S, n[i]);
-            act8_values(b.y, S, n[i] + 4);
-            float gv[8], wv[8];
-            if (q.a.gate) weights8<VEC, T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, valid, gv);
-            if (post) weights8<VEC, T>(q.a.post_weight, q.wf32, c, valid, wv);
-            float d[8], dg[8];
-            sums.get(kDpost, i, d);
-            sums.get(kDgate, i, dg);
+            act8_scaled8(bytes8(fb, c, valid), act8_lines(now_f[i], q.ratio, factor_f), n[i]);
+            u64 d[4], eg[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float g = q.a.gate ? gv[k] : 1.0f, ww = post ? wv[k] + q.offset : 1.0f;
-                n[i][k] *= rstd_f;
-                dg[k] = fmaf(e[i][k] * ww, n[i][k], dg[k]);
-                d[k] = fmaf(e[i][k] * g, n[i][k], d[k]);
-                e[i][k] *= g * ww;
-                if (k < valid) sum[0] = fmaf(e[i][k], n[i][k], sum[0]);
+            for (int k = 0; k < 4; ++k) eg[k] = e[i][k];
+            if (q.a.gate) {
+                u64 gw[4];
+                weights8<VEC, T>(q.a.gate, q.wf32, gate * q.a.ldgate, c, valid, 0.0f, gw);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) eg[k] = mul2(e[i][k], gw[k]);
             }
-            sums.set(kDpost, i, d);
-            sums.set(kDgate, i, dg);
+            if (post) {
+                sums.get(kDpost, i, d);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) d[k] = fma2(eg[k], n[i][k], d[k]);
+                sums.set(kDpost, i, d);
+                weights8<VEC, T>(q.a.post_weight, q.wf32, 0, c, valid, q.offset, w);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    e[i][k] = mul2(e[i][k], w[k]);
+                    eg[k] = mul2(eg[k], w[k]);
+                }
+            }
+            if (q.a.gate) {
+                sums.get(kDgate, i, d);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) d[k] = fma2(e[i][k], n[i][k], d[k]);
+                sums.set(kDgate, i, d);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                e[i][k] = eg[k];
+                s = fma2(eg[k], n[i][k], s);
+            }
         }
-        if (!p.g.df) continue;
         float mean = 0.0f;
-        if (post) {
-            cta_sum(sum);
-            mean = sum[0] * q.inv_cols;
-        }
+        if (post) mean = cta_sum(sum8(s)) * q.inv_cols;
+        if (!p.g.df) continue;
 #pragma unroll
         for (int i = 0; i < VC; ++i) {
             const int c = (threadIdx.x + i * blockDim.x) * 8;
-            float w[8];
+            u64 w[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                w[k] = post ? rstd_f * fmaf(-mean, n[i][k], e[i][k]) : e[i][k];
-            store8<VEC>(w, static_cast<T*>(p.g.df) + row * p.g.lddf + c, cols - c);
+            for (int k = 0; k < 4; ++k)
+                w[k] = post ? mul2(fma2(n[i][k], both(-mean), e[i][k]), both(factor_f)) : e[i][k];
+            store_pairs<VEC>(w, static_cast<T*>(p.g.df) + row * p.g.lddf + c, cols - c);
         }
     }
     if (p.dpre) sums.template put<VEC>(kDpre, p.dpre + (int64_t)blockIdx.x * cols, cols);
@@ -349,12 +592,157 @@ __global__ void __launch_bounds__(WIDE ? 512 : 1024) block_norm_backward_kernel(
     if (p.dgate) sums.template put<VEC>(kDgate, p.dgate + (blockIdx.x + gate) * cols, cols);
 }
 
-// Adds the CTAs' sums of one column per thread: eight parts of the CTAs side by side, then the
+// A thread's 32 bytes of columns times `factor`, from its bytes.
+template <typename T>
+__device__ __forceinline__ void held32(const unsigned char* bytes, float m, float ratio, float factor, u64* n) {
+    const Act8Lines L = act8_lines(m, ratio, factor);
+    if (kPairs32<T> == 8) {
+        const uint4 b = *reinterpret_cast<const uint4*>(bytes);
+        act8_scaled8(make_uint2(b.x, b.y), L, n);
+        act8_scaled8(make_uint2(b.z, b.w), L, n + kPairs32<T> - 4);
+    } else {
+        act8_scaled8(*reinterpret_cast<const uint2*>(bytes), L, n);
+    }
+}
+
+// Backward with a ring: 32 bytes of columns per thread, sums in registers.
+template <typename T>
+__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 1024)
+block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
+    constexpr int kP = kPairs32<T>;
+    __shared__ float buf[2][32];
+    __shared__ uint64_t full[kMaxStages];
+    extern __shared__ __align__(16) unsigned char smem[];
+    CtaSum cta_sum{buf};
+    const NormParams& q = p.q;
+    const int64_t first = blockIdx.x * p.rows_per_cta, last = min(first + p.rows_per_cta, q.a.rows);
+    const bool pre = q.a.pre_weight, post = q.a.post_weight, has_f = q.a.f_codes, has_dr = p.g.dr;
+    Ring ring{full, smem,
+              (pre ? q.row_bytes + q.code_bytes : 0) + (has_dr ? q.row_bytes : 0) + (has_f ? q.code_bytes : 0),
+              q.stages};
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < q.stages; ++s) mbar_init(&full[s], 1);
+        fence_barrier_init();
+        for (int s = 0; s < q.stages; ++s)
+            if (first + s < last) request_backward<T>(p, ring, s, first + s);
+    }
+    __syncthreads();
+    const int c = threadIdx.x * 2 * kP;
+    const bool live = c < (int)q.a.cols;
+    // where this thread's part of each operand lies in a stage
+    const unsigned at_dh = threadIdx.x * 32, at_rb = q.row_bytes + c,
+                   at_dr = (pre ? q.row_bytes + q.code_bytes : 0) + threadIdx.x * 32,
+                   at_fb = ring.stage_bytes - q.code_bytes + c;
+    int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
+    int64_t gate_end = (gate + 1) * q.a.gate_tokens;
+    u64 dpre[kP] = {}, dpost[kP] = {}, dgate[kP] = {};
+    auto put = [&](const u64* v, float* to) {
+        if (!live) return;
+#pragma unroll
+        for (int k = 0; k < kP; k += 4) store32(to + c + 2 * k, raw32(v + k, 0.0f));
+    };
+
+    // a row's ranges and factors, requested one row ahead
+    float next_mr = 0.0f, next_mf = 0.0f, next_rr = 0.0f, next_rf = 1.0f;
+    auto fetch = [&](int64_t row) {
+        if (pre) next_rr = q.a.r_rstd[row];
+        if (post) next_rf = q.a.f_rstd[row];
+        const int64_t at = row * q.groups + (c >> q.group_shift);
+        if (live && pre) next_mr = q.a.r_ranges[at];
+        if (live && has_f) next_mf = q.a.f_ranges[at];
+    };
+    if (first < last) fetch(first);
+
+    for (int64_t row = first; row < last; ++row) {
+        if (q.a.gate && row == gate_end) {
+            if (p.dgate) put(dgate, p.dgate + (blockIdx.x + gate) * q.a.cols);
+#pragma unroll
+            for (int k = 0; k < kP; ++k) dgate[k] = 0ull;
+            ++gate;
+            gate_end += q.a.gate_tokens;
+        }
+        const float mr = next_mr, mf = next_mf, rr = next_rr, rf = next_rf;
+        if (row + 1 < last) fetch(row + 1);
+        u64 e[kP] = {}, n[kP] = {}, w[kP] = {}, s = 0ull;
+        const unsigned char* at = ring.wait();
+        // outer norm: e = dr + rstd * (u - n * mean(u n))
+        if (pre) {
+            if (live) {
+                pairs32(load32(at + at_dh), e, T());
+                held32<T>(at + at_rb, mr, q.ratio, rr, n);
+                weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
+            }
+#pragma unroll
+            for (int k = 0; k < kP; ++k) {
+                dpre[k] = fma2(e[k], n[k], dpre[k]);
+                e[k] = mul2(e[k], w[k]);
+                s = fma2(e[k], n[k], s);
+            }
+            const float mean = cta_sum(sum8(s)) * q.inv_cols;
+#pragma unroll
+            for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rr));
+        }
+        if (has_dr && live) {
+            pairs32(load32(at + at_dr), w, T());
+#pragma unroll
+            for (int k = 0; k < kP; ++k) e[k] = add2(e[k], w[k]);
+        }
+        if (p.g.dx && live) {
+#pragma unroll
+            for (int k = 0; k < kP; ++k) w[k] = mul2(e[k], both(q.scale));
+            store32(static_cast<T*>(p.g.dx) + row * p.g.lddx + c, raw32(w, T()));
+        }
+        // inner norm and gate; e becomes v = e * gate * w
+        float mean = 0.0f;
+        if (has_f) {
+            u64 eg[kP];
+            if (live) held32<T>(at + at_fb, mf, q.ratio, rf, n);
+#pragma unroll
+            for (int k = 0; k < kP; ++k) eg[k] = e[k];
+            if (q.a.gate) {
+                if (live) weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, 0.0f, w);
+#pragma unroll
+                for (int k = 0; k < kP; ++k) eg[k] = mul2(e[k], w[k]);
+            }
+            if (post) {
+                if (live) weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
+#pragma unroll
+                for (int k = 0; k < kP; ++k) {
+                    dpost[k] = fma2(eg[k], n[k], dpost[k]);
+                    e[k] = mul2(e[k], w[k]);
+                    eg[k] = mul2(eg[k], w[k]);
+                }
+            }
+            s = 0ull;
+#pragma unroll
+            for (int k = 0; k < kP; ++k) {
+                dgate[k] = fma2(e[k], n[k], dgate[k]);
+                e[k] = eg[k];
+                s = fma2(eg[k], n[k], s);
+            }
+            if (post) mean = cta_sum(sum8(s)) * q.inv_cols;
+        }
+        if (!post) __syncthreads();
+        // every thread has its values of this stage
+        const int64_t ahead = row + q.stages;
+        if (threadIdx.x == 0 && ahead < last && !ring.dead) request_backward<T>(p, ring, ring.stage, ahead);
+        ring.next();
+        if (!p.g.df || !live) continue;
+#pragma unroll
+        for (int k = 0; k < kP; ++k) w[k] = post ? mul2(fma2(n[k], both(-mean), e[k]), both(rf)) : e[k];
+        store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(w, T()));
+    }
+    if (p.dpre) put(dpre, p.dpre + (int64_t)blockIdx.x * q.a.cols);
+    if (p.dpost) put(dpost, p.dpost + (int64_t)blockIdx.x * q.a.cols);
+    if (p.dgate) put(dgate, p.dgate + (blockIdx.x + gate) * q.a.cols);
+}
+
+// Adds the CTAs' sums of one column per thread: sixteen parts of the CTAs side by side, then the
 // parts.  blockIdx.y: 0 dpre, 1 dpost, 2 + g gate g.
-constexpr int kSumCols = 32, kSumParts = 8;
+constexpr int kSumCols = 32, kSumParts = 16;
 template <typename W>
 __global__ void __launch_bounds__(kSumCols * kSumParts)
-block_norm_sums_kernel(GradParams p, int64_t ctas, W* dpre, W* dpost, W* dgate) {
+block_norm_sums_kernel(const __grid_constant__ GradParams p, int64_t ctas, W* dpre, W* dpost, W* dgate) {
     __shared__ float part[kSumParts][kSumCols];
     const int cols = (int)p.q.a.cols;
     const int c = blockIdx.x * kSumCols + threadIdx.x;
@@ -371,8 +759,10 @@ block_norm_sums_kernel(GradParams p, int64_t ctas, W* dpre, W* dpost, W* dgate) 
             src += g * cols;                       // slot of CTA b: b + g
         }
         float s = 0.0f;
-        if (c < cols)
+        if (c < cols) {
+#pragma unroll 8
             for (int64_t b = lo + threadIdx.y; b < hi; b += kSumParts) s += src[b * cols + c];
+        }
         part[threadIdx.y][threadIdx.x] = s;
         __syncthreads();
         if (threadIdx.y == 0 && c < cols) {
@@ -382,6 +772,21 @@ block_norm_sums_kernel(GradParams p, int64_t ctas, W* dpre, W* dpost, W* dgate) 
         }
         __syncthreads();
     }
+}
+
+// ------------------------------------------------------------------------------ launching
+// Multiprocessors of the current device (looked up once per device).
+int sm_count() {
+    static std::mutex mutex;
+    static int known[64] = {};
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+    std::lock_guard<std::mutex> lock(mutex);
+    if (!known[dev]) {
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1) return 148;
+        known[dev] = sms;
+    }
+    return known[dev];
 }
 
 NormParams params(const pwlq_block_norm_args& a) {
@@ -396,57 +801,115 @@ NormParams params(const pwlq_block_norm_args& a) {
     q.group_lanes = 1 << (q.group_shift - 3);
     q.groups = a.group > 0 ? (a.cols + a.group - 1) / a.group : 0;
     q.wf32 = a.wtype == kF32;
+    q.stages = 0;
+    q.gate_step = q.gate_rest = 0;
+    q.row_bytes = (unsigned)(a.cols * type_size((int)a.dtype));
+    q.code_bytes = (unsigned)((a.cols + 15) / 16 * 16);
     return q;
 }
 
-inline bool pointers_aligned(const pwlq_block_norm_args& a) {
+inline bool weights_aligned(const pwlq_block_norm_args& a) {
     const size_t ws = type_size((int)a.wtype);
     return rows_aligned(a.post_weight, 0, ws) && rows_aligned(a.pre_weight, 0, ws) &&
            rows_aligned(a.gate, a.ldgate, ws);
 }
 
-template <typename T, int VC>
-cudaError_t forward(const NormParams& q, int threads, cudaStream_t stream) {
-    const bool vec = rows_aligned(q.a.x, q.a.ldx, sizeof(T)) && rows_aligned(q.a.f, q.a.ldf, sizeof(T)) &&
-                     rows_aligned(q.a.r, q.a.ldr, sizeof(T)) && rows_aligned(q.a.h, q.a.ldh, sizeof(T)) &&
-                     pointers_aligned(q.a);
-    const bool save = q.a.r_codes || q.a.f_codes || q.a.r_rstd || q.a.f_rstd;
-    auto* kernel = vec ? (save ? block_norm_kernel<T, VC, true, true> : block_norm_kernel<T, VC, true, false>)
-                       : (save ? block_norm_kernel<T, VC, false, true> : block_norm_kernel<T, VC, false, false>);
-    kernel<<<(unsigned)q.a.rows, threads, 0, stream>>>(q);
-    return cudaGetLastError();
-}
-template <typename T>
-cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
-    const NormParams q = params(a);
-    const int chunks = (int)((a.cols + 7) / 8);
-    const int vc = chunks <= 256 ? 1 : chunks <= 512 ? 2 : 4;
-    const int threads = ((chunks + vc - 1) / vc + 31) / 32 * 32;
-    if (vc == 1) return forward<T, 1>(q, threads, stream);
-    if (vc == 2) return forward<T, 2>(q, threads, stream);
-    return forward<T, 4>(q, threads, stream);
+inline int threads_for(int64_t cols, int per_thread) {
+    const int64_t n = (cols + per_thread - 1) / per_thread;
+    return (int)((n + 31) / 32 * 32);
 }
 
-// CTAs of the backward pass: the rows are shared out evenly over at most this many.
-constexpr int64_t kBackwardCtas = 296;
-inline int64_t backward_ctas(int64_t rows) { return rows < kBackwardCtas ? rows : kBackwardCtas; }
-
-template <typename T, int VC, bool WIDE>
-cudaError_t backward(const GradParams& p, unsigned ctas, int threads, cudaStream_t stream) {
-    const pwlq_block_norm_grads& g = p.g;
-    const bool vec = rows_aligned(g.dh, g.lddh, sizeof(T)) && rows_aligned(g.dr, g.lddr, sizeof(T)) &&
-                     rows_aligned(g.dx, g.lddx, sizeof(T)) && rows_aligned(g.df, g.lddf, sizeof(T)) &&
-                     p.q.a.cols % 4 == 0 && pointers_aligned(p.q.a);
-    auto* kernel = vec ? block_norm_backward_kernel<T, VC, true, WIDE>
-                       : block_norm_backward_kernel<T, VC, false, WIDE>;
-    const size_t smem = WIDE ? (size_t)3 * VC * 8 * sizeof(float) * threads : 0;   // at most 192 KB
-    if (WIDE) {
-        const cudaError_t e = cudaFuncSetAttribute(
-            kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+template <typename K, typename P>
+cudaError_t run(K* kernel, unsigned ctas, int threads, size_t smem, cudaStream_t stream, const P& p) {
+    if (smem > 40 * 1024) {             // with the static part, possibly above the default 48 KB
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
     kernel<<<ctas, threads, smem, stream>>>(p);
     return cudaGetLastError();
+}
+
+// A ring kernel's launch: threads of 32 bytes of columns each; CTAs that share a multiprocessor, as
+// far as their registers allow (`threads_per_sm`); stages of `bytes` for each of them.
+struct RingPlan { int threads, ctas, stages; };
+constexpr int64_t kRingCols = 8192;
+constexpr size_t kSmemBudget = 216 * 1024;
+RingPlan ring_plan(int64_t cols, size_t size, int threads_per_sm, size_t bytes) {
+    RingPlan r;
+    r.threads = threads_for(cols, (int)(32 / size));
+    r.ctas = std::max(1, std::min(16, threads_per_sm / r.threads));
+    r.stages = bytes ? (int)std::min<size_t>((kSmemBudget / r.ctas - 1024) / bytes, kMaxStages) : 0;
+    return r;
+}
+// 32-byte accesses to values need rows, and columns per thread, on 32-byte boundaries.
+inline bool rows_aligned32(const void* p, int64_t ld, size_t size) {
+    return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)size)) & 31) == 0;
+}
+
+template <typename T, bool SAVE>
+cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
+    NormParams q = params(a);
+    constexpr size_t kSize = sizeof(T);
+    const RingPlan ring = ring_plan(a.cols, kSize, kSize == 2 ? 768 : 1024, (a.f ? 2 : 1) * (size_t)q.row_bytes);
+    const int64_t resident = (int64_t)ring.ctas * sm_count();
+    // a ring pays once every CTA has a few rows to walk
+    if (a.cols <= kRingCols && a.cols % (32 / kSize) == 0 && ring.stages >= 2 && a.rows >= 2 * resident &&
+        rows_aligned32(a.x, a.ldx, kSize) && rows_aligned32(a.f, a.ldf, kSize) &&
+        rows_aligned32(a.r, a.ldr, kSize) && rows_aligned32(a.h, a.ldh, kSize) && weights_aligned(a)) {
+        q.stages = ring.stages;
+        q.group_lanes = (int)(a.group * kSize / 32);
+        if (a.gate) {
+            q.gate_step = resident / a.gate_tokens;
+            q.gate_rest = resident % a.gate_tokens;
+        }
+        return run(block_norm_ring_kernel<T, SAVE>, (unsigned)resident, ring.threads,
+                   (size_t)ring.stages * (a.f ? 2 : 1) * q.row_bytes, stream, q);
+    }
+    const bool vec = rows_aligned(a.x, a.ldx, kSize) && rows_aligned(a.f, a.ldf, kSize) &&
+                     rows_aligned(a.r, a.ldr, kSize) && rows_aligned(a.h, a.ldh, kSize) && weights_aligned(a);
+    const unsigned rows = (unsigned)a.rows;
+    if (a.cols <= 8192)
+        return vec ? run(block_norm_kernel<T, 1, true, SAVE>, rows, threads_for(a.cols, 8), 0, stream, q)
+                   : run(block_norm_kernel<T, 1, false, SAVE>, rows, threads_for(a.cols, 8), 0, stream, q);
+    return vec ? run(block_norm_kernel<T, 2, true, SAVE>, rows, threads_for(a.cols, 16), 0, stream, q)
+               : run(block_norm_kernel<T, 2, false, SAVE>, rows, threads_for(a.cols, 16), 0, stream, q);
+}
+template <typename T>
+cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
+    return a.r_codes || a.f_codes || a.r_rstd || a.f_rstd ? forward<T, true>(a, stream) : forward<T, false>(a, stream);
+}
+
+// CTAs of the backward pass: the rows are shared out evenly over at most this many.
+inline int64_t backward_ctas(int64_t rows, int64_t cols) {
+    const int64_t per_sm = cols > 8192 ? 1 : std::max(1, std::min(16, 512 / threads_for(cols, 16)));
+    return std::min<int64_t>(rows, per_sm * sm_count());
+}
+
+template <typename T>
+cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
+    const pwlq_block_norm_grads& g = p.g;
+    const pwlq_block_norm_args& a = p.q.a;
+    constexpr size_t kSize = sizeof(T);
+    const bool vec = rows_aligned(g.dh, g.lddh, kSize) && rows_aligned(g.dr, g.lddr, kSize) &&
+                     rows_aligned(g.dx, g.lddx, kSize) && rows_aligned(g.df, g.lddf, kSize) &&
+                     a.cols % 4 == 0 && weights_aligned(a);
+    if (a.cols > 8192) {
+        const int threads = threads_for(a.cols, 32);
+        const size_t sums = (size_t)3 * 4 * 8 * sizeof(float) * threads;          // at most 192 KB
+        return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, sums, stream, p)
+                   : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, sums, stream, p);
+    }
+    const size_t stage = (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (g.dr ? p.q.row_bytes : 0) +
+                         (a.f_codes ? p.q.code_bytes : 0);
+    const RingPlan ring = ring_plan(a.cols, kSize, kSize == 2 ? 512 : 1024, stage);
+    if (a.cols <= kRingCols && a.cols % (32 / kSize) == 0 && ring.stages >= 2 &&
+        rows_aligned32(g.dh, g.lddh, kSize) && rows_aligned32(g.dr, g.lddr, kSize) &&
+        rows_aligned32(g.dx, g.lddx, kSize) && rows_aligned32(g.df, g.lddf, kSize) && weights_aligned(a)) {
+        p.q.stages = ring.stages;
+        return run(block_norm_backward_ring_kernel<T>, ctas, ring.threads, ring.stages * stage, stream, p);
+    }
+    return vec ? run(block_norm_backward_kernel<T, 1, true, false>, ctas, threads_for(a.cols, 8), 0, stream, p)
+               : run(block_norm_backward_kernel<T, 1, false, false>, ctas, threads_for(a.cols, 8), 0, stream, p);
 }
 template <typename W>
 cudaError_t sums(const GradParams& p, int64_t ctas, cudaStream_t stream) {
@@ -461,22 +924,17 @@ template <typename T>
 cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads& g, cudaStream_t stream) {
     GradParams p;
     p.q = params(a);
+    if (!a.gate && !a.post_weight) p.q.a.f_codes = nullptr;      // f enters as it is: nothing of it is needed
     p.g = g;
-    int64_t ctas = backward_ctas(a.rows);
+    int64_t ctas = backward_ctas(a.rows, a.cols);
     p.rows_per_cta = ctas ? (a.rows + ctas - 1) / ctas : 1;
     ctas = (a.rows + p.rows_per_cta - 1) / p.rows_per_cta;
     float* ws = static_cast<float*>(g.workspace);
     p.dpre = g.dpre ? ws : nullptr;
     p.dpost = g.dpost ? ws + ctas * a.cols : nullptr;
     p.dgate = g.dgate ? ws + 2 * ctas * a.cols : nullptr;
-    const int chunks = (int)((a.cols + 7) / 8);
-    const int vc = chunks <= 1024 ? 1 : 4;
-    const int threads = ((chunks + vc - 1) / vc + 31) / 32 * 32;
-    if (ctas) {
-        const cudaError_t e = vc == 1 ? backward<T, 1, false>(p, (unsigned)ctas, threads, stream)
-                                      : backward<T, 4, true>(p, (unsigned)ctas, threads, stream);
-        if (e != cudaSuccess) return e;
-    }
+    if (ctas)
+        if (const cudaError_t e = backward_rows<T>(p, (unsigned)ctas, stream)) return e;
     if (!g.dpre && !g.dpost && !g.dgate) return cudaSuccess;
     return p.q.wf32 ? sums<float>(p, ctas, stream) : sums<T>(p, ctas, stream);
 }
@@ -490,7 +948,7 @@ cudaError_t launch_block_norm(const pwlq_block_norm_args& a, cudaStream_t stream
 }
 
 size_t block_norm_backward_workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
-    const int64_t ctas = backward_ctas(rows);
+    const int64_t ctas = backward_ctas(rows, cols);
     return (size_t)(3 * ctas + gate_rows) * (size_t)cols * sizeof(float);
 }
 
@@ -499,6 +957,14 @@ cudaError_t launch_block_norm_backward(const pwlq_block_norm_args& a, const pwlq
     if (a.dtype == kF32) return backward<float>(a, g, stream);
     if (a.dtype == kBf16) return backward<__nv_bfloat16>(a, g, stream);
     return backward<__half>(a, g, stream);
+}
+
+int take_block_norm_timeout_flag() {
+    int v = 0;
+    const int zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_block_norm_timeout, sizeof(v)) != cudaSuccess) return -1;
+    if (v && cudaMemcpyToSymbol(g_block_norm_timeout, &zero, sizeof(zero)) != cudaSuccess) return -1;
+    return v;
 }
 
 }  // namespace pwlq

@@ -53,8 +53,9 @@ struct WeightGrad {
 // aligned: dy's rows start on 16-byte boundaries (else the workspace holds a copy whose rows do).
 size_t weight_grad_workspace(int64_t rows, int64_t outputs, int64_t cols, bool aligned);
 cudaError_t launch_weight_grad(const WeightGrad& w, void* workspace, cudaStream_t stream);
-// 1 if a bounded wait of the weight gradient has expired on the current device since the last call,
-// -1 if the flag could not be read.
+// 1 if a bounded wait of these kernels has expired on the current device since the last call, -1 if
+// the flag could not be read.
 int take_weight_grad_timeout_flag();
+int take_block_norm_timeout_flag();
 
 }  // namespace pwlq

@@ -8,6 +8,7 @@ constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxCols = (int64_t)1 << 24;
 constexpr int64_t kMaxPitch = (int64_t)1 << 40;
 constexpr float kMinRatio = 9.5367431640625e-07f;        // 2^-20
+constexpr float kMaxRatio = 0.999755859375f;             // 1 - 2^-12: above it 63 / d may overflow
 
 inline bool misaligned(const void* p, size_t a) {
     return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0;
@@ -29,7 +30,7 @@ bool bad_tensor(const void* p, int64_t dtype, int64_t ld, int64_t rows, int64_t 
 
 bool bad_format(int64_t group, float ratio) {
     return (group != 32 && group != 64 && group != 128 && group != 256) ||
-           !(ratio >= kMinRatio && ratio <= 1.0f);
+           !((ratio >= kMinRatio && ratio <= kMaxRatio) || ratio == 1.0f);
 }
 bool bad_codes(const uint8_t* codes, int64_t ldc, const float* ranges, int64_t rows, int64_t cols) {
     return ((!codes || !ranges) && rows > 0) || misaligned(codes, 16) || misaligned(ranges, 4) ||
@@ -42,8 +43,8 @@ int check_act8(int64_t rows, int64_t cols, int dtype, const void* v, int64_t ld,
     if (!is_dtype(dtype) || bad_tensor(v, dtype, ld, rows, cols) || bad_format(group, ratio) ||
         bad_codes(codes, ldc, ranges, rows, cols))
         return PWLQ_ERR_INVALID_ARG;
-    // blocks of up to 4096 columns of a row
-    if (rows * ((cols + 4095) / 4096) > kMaxRows) return PWLQ_ERR_UNSUPPORTED;
+    // blocks of 2048 or 4096 columns of a row
+    if (rows * ((cols + 2047) / 2048) > kMaxRows) return PWLQ_ERR_UNSUPPORTED;
     return PWLQ_OK;
 }
 
@@ -168,7 +169,7 @@ int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outpu
     if (int rc = check_size(rows, cols)) return rc;
     if (!is_dtype(dtype) || !is_dtype(dw_dtype) || (dw_dtype != PWLQ_F32 && dw_dtype != dtype))
         return PWLQ_ERR_INVALID_ARG;
-    if (dtype == PWLQ_F32 || rows * ((cols + 4095) / 4096) > kMaxRows) return PWLQ_ERR_UNSUPPORTED;
+    if (dtype == PWLQ_F32 || rows * ((cols + 2047) / 2048) > kMaxRows) return PWLQ_ERR_UNSUPPORTED;
     if (bad_tensor(dy, dtype, lddy, rows, outputs) || bad_format(group, ratio) ||
         bad_codes(codes, ldc, ranges, rows, cols) || bad_tensor(dw, dw_dtype, lddw, outputs, cols))
         return PWLQ_ERR_INVALID_ARG;

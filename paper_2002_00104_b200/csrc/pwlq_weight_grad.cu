@@ -290,14 +290,14 @@ __global__ void __launch_bounds__(256) weight_grad_pieces_kernel(const __grid_co
         Raw8<W> raw;
         if (p.w.accumulate) {
             float old[8];
-            if (p.vec_out) load8<true>(raw, to, valid);
-            else load8<false>(raw, to, valid);
+            if (p.vec_out) load8<true>(raw, to, valid, 0);
+            else load8<false>(raw, to, valid, 0);
             raw.get(old);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += old[j];
         }
         if (p.vec_out) store8<true>(v, to, valid);
-        else store8<false>(v, to, valid);
+        else store8_each(v, to, valid);
     };
     if (p.w.dw_dtype == kF32) put(static_cast<float*>(p.w.dw) + n * p.w.lddw + k);
     else put(static_cast<T*>(p.w.dw) + n * p.w.lddw + k);

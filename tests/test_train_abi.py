@@ -26,7 +26,7 @@ def test_encode_and_decode(lib):
         return lib.pwlq_act8_encode(*args)
 
     for i, v in ((0, None), (0, A + 2), (1, 3), (2, -1), (3, 0), (4, 99), (5, 16), (6, 0.0), (6, 1.01),
-                 (6, float("nan")), (6, 2.0 ** -21), (7, None), (7, B + 8), (8, 96), (8, 104), (9, None),
+                 (6, float("nan")), (6, 2.0 ** -21), (6, 1 - 2.0 ** -13), (7, None), (7, B + 8), (8, 96), (8, 104), (9, None),
                  (9, C + 2)):
         assert rc(i, v) == pwlq.ERR_INVALID_ARG, (i, v)
     assert rc(2, 1 << 31) == pwlq.ERR_UNSUPPORTED
