@@ -269,7 +269,9 @@ __device__ __forceinline__ float act8_range(float top) {
 
 // Maximum over the aligned `lanes` (power of two <= 32) lanes that hold one group.
 __device__ __forceinline__ float group_max(float v, int lanes) {
-    for (int o = 1; o < lanes; o <<= 1) v = max_abs(v, __shfl_xor_sync(0xffffffffu, v, o));
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1)
+        if (o < lanes) v = max_abs(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
 

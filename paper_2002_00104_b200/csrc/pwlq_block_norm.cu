@@ -224,9 +224,9 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const __grid_constant_
     }
 }
 
-// Weights (or gates) of a thread's 32 bytes of columns, as binary32 pairs, plus `offset`.
+// Weights (or gates) of a thread's 32 bytes of columns, as binary32 pairs (plus `offset`).
 template <typename T>
-__device__ __forceinline__ void weights32(const void* p, bool f32, int64_t at, float offset, u64* w) {
+__device__ __forceinline__ void weights32(const void* p, bool f32, int64_t at, u64* w) {
     constexpr int kP = kPairs32<T>;
     if (sizeof(T) == 2 && f32) {
         pairs32(load32(static_cast<const float*>(p) + at), w, 0.0f);
@@ -234,8 +234,12 @@ __device__ __forceinline__ void weights32(const void* p, bool f32, int64_t at, f
     } else {
         pairs32(load32(static_cast<const T*>(p) + at), w, T());
     }
+}
+template <typename T>
+__device__ __forceinline__ void weights32(const void* p, bool f32, int64_t at, float offset, u64* w) {
+    weights32<T>(p, f32, at, w);
 #pragma unroll
-    for (int k = 0; k < kP; ++k) w[k] = add2(w[k], both(offset));
+    for (int k = 0; k < kPairs32<T>; ++k) w[k] = add2(w[k], both(offset));
 }
 
 // Bytes of a thread's 32 bytes of values, and the range of their group.
@@ -289,44 +293,51 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
         gate = blockIdx.x / q.a.gate_tokens;
         in_gate = blockIdx.x - gate * q.a.gate_tokens;
     }
-    const int c = threadIdx.x * 2 * kP;
-    const bool live = c < (int)q.a.cols, post = q.a.post_weight, pre = q.a.pre_weight;
+    // threads past the row repeat its last columns (so that a group's range stays its own) and
+    // neither store nor count
+    const bool live = (int)threadIdx.x * 2 * kP < (int)q.a.cols, post = q.a.post_weight, pre = q.a.pre_weight;
+    const int c = live ? (int)threadIdx.x * 2 * kP : (int)q.a.cols - 2 * kP;
     for (int64_t row = blockIdx.x; row < q.a.rows; row += gridDim.x) {
-        u64 f[kP] = {}, r[kP] = {}, w[kP] = {}, s = 0ull;
-        const unsigned char* at = ring.wait() + threadIdx.x * 32;
-        if (live) pairs32(load32(at), r, T());
-        if (live && q.a.f) pairs32(load32(at + q.row_bytes), f, T());
-        float rstd_f = 1.0f;
-        if (post) {
+        u64 r[kP], w[kP], s = 0ull;
+        const unsigned char* at = ring.wait() + c * (int)sizeof(T);
+        pairs32(load32(at), r, T());
 #pragma unroll
-            for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
-            if (live) weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
-            rstd_f = rsqrtf(fmaf(cta_sum(sum8(s)), q.inv_cols, q.eps));
-            if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
-        }
-        if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
-        if (post)
+        for (int k = 0; k < kP; ++k) r[k] = mul2(r[k], both(q.scale));
+        if (q.a.f) {
+            u64 f[kP];
+            pairs32(load32(at + q.row_bytes), f, T());
+            if (post) {
 #pragma unroll
-            for (int k = 0; k < kP; ++k) f[k] = mul2(mul2(f[k], both(rstd_f)), w[k]);
-        if (q.a.gate) {
-            if (live) weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, 0.0f, w);
+                for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
+                weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
+                const float rstd_f = rsqrtf(fmaf(cta_sum(live ? sum8(s) : 0.0f), q.inv_cols, q.eps));
+                if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
+                if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
 #pragma unroll
-            for (int k = 0; k < kP; ++k) f[k] = mul2(f[k], w[k]);
-            gate += q.gate_step;
-            in_gate += q.gate_rest;
-            if (in_gate >= q.a.gate_tokens) { ++gate; in_gate -= q.a.gate_tokens; }
+                for (int k = 0; k < kP; ++k) f[k] = mul2(mul2(f[k], both(rstd_f)), w[k]);
+            } else if (SAVE && q.a.f_codes) {
+                save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+            }
+            if (q.a.gate) {
+                weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, w);
+#pragma unroll
+                for (int k = 0; k < kP; ++k) r[k] = fma2(f[k], w[k], r[k]);
+                gate += q.gate_step;
+                in_gate += q.gate_rest;
+                if (in_gate >= q.a.gate_tokens) { ++gate; in_gate -= q.a.gate_tokens; }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kP; ++k) r[k] = add2(r[k], f[k]);
+            }
         }
         s = 0ull;
 #pragma unroll
-        for (int k = 0; k < kP; ++k) {
-            r[k] = add2(mul2(r[k], both(q.scale)), f[k]);
-            s = fma2(r[k], r[k], s);
-        }
+        for (int k = 0; k < kP; ++k) s = fma2(r[k], r[k], s);
         if (live && q.a.r) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
         float rstd_r = 0.0f;
         if (pre) {
-            if (live) weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
-            rstd_r = rsqrtf(fmaf(cta_sum(sum8(s)), q.inv_cols, q.eps));
+            weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
+            rstd_r = rsqrtf(fmaf(cta_sum(live ? sum8(s) : 0.0f), q.inv_cols, q.eps));
         } else {
             __syncthreads();
         }
@@ -627,11 +638,12 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
             if (first + s < last) request_backward<T>(p, ring, s, first + s);
     }
     __syncthreads();
-    const int c = threadIdx.x * 2 * kP;
-    const bool live = c < (int)q.a.cols;
+    // threads past the row repeat its last columns and neither store nor count
+    const bool live = (int)threadIdx.x * 2 * kP < (int)q.a.cols;
+    const int c = live ? (int)threadIdx.x * 2 * kP : (int)q.a.cols - 2 * kP;
     // where this thread's part of each operand lies in a stage
-    const unsigned at_dh = threadIdx.x * 32, at_rb = q.row_bytes + c,
-                   at_dr = (pre ? q.row_bytes + q.code_bytes : 0) + threadIdx.x * 32,
+    const unsigned at_dh = c * (int)sizeof(T), at_rb = q.row_bytes + c,
+                   at_dr = (pre ? q.row_bytes + q.code_bytes : 0) + c * (int)sizeof(T),
                    at_fb = ring.stage_bytes - q.code_bytes + c;
     int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
@@ -648,8 +660,8 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         if (pre) next_rr = q.a.r_rstd[row];
         if (post) next_rf = q.a.f_rstd[row];
         const int64_t at = row * q.groups + (c >> q.group_shift);
-        if (live && pre) next_mr = q.a.r_ranges[at];
-        if (live && has_f) next_mf = q.a.f_ranges[at];
+        if (pre) next_mr = q.a.r_ranges[at];
+        if (has_f) next_mf = q.a.f_ranges[at];
     };
     if (first < last) fetch(first);
 
@@ -663,29 +675,30 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         }
         const float mr = next_mr, mf = next_mf, rr = next_rr, rf = next_rf;
         if (row + 1 < last) fetch(row + 1);
-        u64 e[kP] = {}, n[kP] = {}, w[kP] = {}, s = 0ull;
+        u64 e[kP], n[kP], w[kP];
         const unsigned char* at = ring.wait();
         // outer norm: e = dr + rstd * (u - n * mean(u n))
         if (pre) {
-            if (live) {
-                pairs32(load32(at + at_dh), e, T());
-                held32<T>(at + at_rb, mr, q.ratio, rr, n);
-                weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
-            }
+            pairs32(load32(at + at_dh), e, T());
+            held32<T>(at + at_rb, mr, q.ratio, rr, n);
+            weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
+            u64 s = 0ull;
 #pragma unroll
             for (int k = 0; k < kP; ++k) {
                 dpre[k] = fma2(e[k], n[k], dpre[k]);
                 e[k] = mul2(e[k], w[k]);
                 s = fma2(e[k], n[k], s);
             }
-            const float mean = cta_sum(sum8(s)) * q.inv_cols;
+            const float mean = cta_sum(live ? sum8(s) : 0.0f) * q.inv_cols;
 #pragma unroll
             for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rr));
-        }
-        if (has_dr && live) {
-            pairs32(load32(at + at_dr), w, T());
+            if (has_dr) {
+                pairs32(load32(at + at_dr), w, T());
 #pragma unroll
-            for (int k = 0; k < kP; ++k) e[k] = add2(e[k], w[k]);
+                for (int k = 0; k < kP; ++k) e[k] = add2(e[k], w[k]);
+            }
+        } else {                          // without the outer norm dr is all there is
+            pairs32(load32(at + at_dr), e, T());
         }
         if (p.g.dx && live) {
 #pragma unroll
@@ -695,32 +708,38 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         // inner norm and gate; e becomes v = e * gate * w
         float mean = 0.0f;
         if (has_f) {
-            u64 eg[kP];
-            if (live) held32<T>(at + at_fb, mf, q.ratio, rf, n);
-#pragma unroll
-            for (int k = 0; k < kP; ++k) eg[k] = e[k];
+            held32<T>(at + at_fb, mf, q.ratio, rf, n);
+            u64 s = 0ull;
             if (q.a.gate) {
-                if (live) weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, 0.0f, w);
+                u64 g[kP];
+                weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, g);
+                if (post) {
+                    weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
 #pragma unroll
-                for (int k = 0; k < kP; ++k) eg[k] = mul2(e[k], w[k]);
-            }
-            if (post) {
-                if (live) weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
+                    for (int k = 0; k < kP; ++k) {
+                        const u64 en = mul2(e[k], n[k]);
+                        dpost[k] = fma2(en, g[k], dpost[k]);
+                        dgate[k] = fma2(en, w[k], dgate[k]);
+                        e[k] = mul2(e[k], mul2(g[k], w[k]));
+                        s = fma2(e[k], n[k], s);
+                    }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kP; ++k) {
+                        dgate[k] = fma2(e[k], n[k], dgate[k]);
+                        e[k] = mul2(e[k], g[k]);
+                    }
+                }
+            } else {                      // f was kept for its norm
+                weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) {
-                    dpost[k] = fma2(eg[k], n[k], dpost[k]);
+                    dpost[k] = fma2(e[k], n[k], dpost[k]);
                     e[k] = mul2(e[k], w[k]);
-                    eg[k] = mul2(eg[k], w[k]);
+                    s = fma2(e[k], n[k], s);
                 }
             }
-            s = 0ull;
-#pragma unroll
-            for (int k = 0; k < kP; ++k) {
-                dgate[k] = fma2(e[k], n[k], dgate[k]);
-                e[k] = eg[k];
-                s = fma2(eg[k], n[k], s);
-            }
-            if (post) mean = cta_sum(sum8(s)) * q.inv_cols;
+            if (post) mean = cta_sum(live ? sum8(s) : 0.0f) * q.inv_cols;
         }
         if (!post) __syncthreads();
         // every thread has its values of this stage
@@ -728,9 +747,10 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         if (threadIdx.x == 0 && ahead < last && !ring.dead) request_backward<T>(p, ring, ring.stage, ahead);
         ring.next();
         if (!p.g.df || !live) continue;
+        if (post)
 #pragma unroll
-        for (int k = 0; k < kP; ++k) w[k] = post ? mul2(fma2(n[k], both(-mean), e[k]), both(rf)) : e[k];
-        store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(w, T()));
+            for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rf));
+        store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(e, T()));
     }
     if (p.dpre) put(dpre, p.dpre + (int64_t)blockIdx.x * q.a.cols);
     if (p.dpost) put(dpost, p.dpost + (int64_t)blockIdx.x * q.a.cols);
@@ -833,7 +853,8 @@ cudaError_t run(K* kernel, unsigned ctas, int threads, size_t smem, cudaStream_t
 // far as their registers allow (`threads_per_sm`); stages of `bytes` for each of them.
 struct RingPlan { int threads, ctas, stages; };
 constexpr int64_t kRingCols = 8192;
-constexpr size_t kSmemBudget = 216 * 1024;
+// what is left of the 228 KB is cache for the weights, which every row reads again
+constexpr size_t kSmemBudget = 160 * 1024;
 RingPlan ring_plan(int64_t cols, size_t size, int threads_per_sm, size_t bytes) {
     RingPlan r;
     r.threads = threads_for(cols, (int)(32 / size));
@@ -902,7 +923,7 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
     const size_t stage = (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (g.dr ? p.q.row_bytes : 0) +
                          (a.f_codes ? p.q.code_bytes : 0);
     const RingPlan ring = ring_plan(a.cols, kSize, kSize == 2 ? 512 : 1024, stage);
-    if (a.cols <= kRingCols && a.cols % (32 / kSize) == 0 && ring.stages >= 2 &&
+    if (a.cols <= kRingCols && a.cols % (32 / kSize) == 0 && ring.stages >= 2 && (a.pre_weight || g.dr) &&
         rows_aligned32(g.dh, g.lddh, kSize) && rows_aligned32(g.dr, g.lddr, kSize) &&
         rows_aligned32(g.dx, g.lddx, kSize) && rows_aligned32(g.df, g.lddf, kSize) && weights_aligned(a)) {
         p.q.stages = ring.stages;
