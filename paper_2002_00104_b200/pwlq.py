@@ -812,7 +812,12 @@ def encode_host_unsigned(x_host, row_offsets_host, C, max_n, bits, ratios_host, 
 
 
 # ---------------------------------------------------------------- training on 8-bit checkpoints
+# These calls are made once per layer and step, often on few rows, so what they do on the host is
+# kept short: one look at each tensor's attributes, and argument blocks packed in one go.
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
 class Act8(NamedTuple):
@@ -825,39 +830,50 @@ class Act8(NamedTuple):
     ratio: float
 
 
-def _matrix(t: torch.Tensor, what: str, rows=None, cols=None, dtype=None):
-    """(data pointer, row pitch) of a [rows, cols] CUDA tensor whose rows are contiguous."""
-    if t.dim() != 2 or not t.is_cuda or t.dtype not in _DTYPES:
-        raise ValueError(f"{what} must be a [rows, cols] CUDA tensor of float32, bfloat16 or float16")
-    if (rows is not None and t.shape != (rows, cols)) or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{what} must be [{rows}, {cols}] of {dtype}, "
-                         f"got {list(t.shape)} of {t.dtype}")
-    r, c = t.shape
+def _home(t: torch.Tensor, what: str) -> int:
+    """Device index of a call's first tensor, which has to be the current device: the library
+    launches there."""
+    device = t.get_device()
+    if device < 0 or device != _device():
+        raise ValueError(f"{what} must be on the current CUDA device (cuda:{_device()}), "
+                         f"it is on {t.device}")
+    return device
+
+
+def _matrix(t: torch.Tensor, what: str, shape, dtype, device):
+    """(data pointer, row pitch) of a tensor of this shape, type and device with adjacent values in
+    its rows."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device:
+        raise ValueError(f"{what} must be {list(shape)} of {dtype} on cuda:{device}, "
+                         f"got {list(t.shape)} of {t.dtype} on {t.device}")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
     pitch, step = t.stride()
-    if c > 1 and step != 1:
+    if shape[1] > 1 and step != 1:
         raise ValueError(f"{what}: the values of a row must be adjacent")
-    if r < 2 or pitch < 0:
-        pitch = c
-    elif pitch < c:
+    if shape[0] < 2:
+        pitch = shape[1]
+    elif pitch < shape[1]:
         raise ValueError(f"{what}: rows overlap (a broadcast tensor must be made whole first)")
     return t.data_ptr(), pitch
 
 
-def _vector(t: Optional[torch.Tensor], what: str, cols: int):
-    if t is None:
-        return 0
-    if t.shape != (cols,) or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous CUDA tensor of {cols} values")
+def _shape2(t: torch.Tensor, what: str):
+    if t.dim() != 2 or t.dtype not in _DTYPES:
+        raise ValueError(f"{what} must be a [rows, cols] tensor of float32, bfloat16 or float16")
+    return t.shape
+
+
+def _vector(t: torch.Tensor, what: str, shape, dtype, device):
+    if t.shape != shape or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous {list(shape)} of {dtype} on cuda:{device}, "
+                         f"got {list(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
-def _launch_stream(t: torch.Tensor) -> int:
-    """Handle of PyTorch's current stream; the library launches on the current device."""
-    device = t.get_device()
-    if device != torch.cuda.current_device():
-        raise ValueError(f"tensors are on cuda:{device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
-    return torch._C._cuda_getCurrentRawStream(device)
+def _like(t: torch.Tensor):
+    """Uninitialised contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
 def _on(stream):
@@ -866,15 +882,16 @@ def _on(stream):
     return torch.cuda.stream(stream)
 
 
-def _act8(a: Act8, rows=None, cols=None):
+def _act8(a: Act8, device, rows=None, cols=None):
     """(codes pointer, pitch, ranges pointer) of a checkpoint, checked against its own layout."""
     codes, ranges = a.codes, a.ranges
-    if (codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_cuda or
-            ranges.dtype != torch.float32 or not ranges.is_cuda or not ranges.is_contiguous() or
-            ranges.shape != (codes.shape[0], -(-a.cols // a.group)) or codes.shape[1] < a.cols or
-            codes.shape[1] % 16 or not codes.is_contiguous()):
-        raise ValueError("not a checkpoint: codes must be contiguous uint8 [rows, pitch] with a "
-                         "pitch that is a multiple of 16, ranges float32 [rows, groups]")
+    if (codes.dtype != torch.uint8 or codes.dim() != 2 or codes.get_device() != device or
+            not codes.is_contiguous() or codes.shape[1] < a.cols or codes.shape[1] % 16 or
+            ranges.dtype != torch.float32 or ranges.get_device() != device or
+            not ranges.is_contiguous() or ranges.shape != (codes.shape[0], -(-a.cols // a.group))):
+        raise ValueError(f"not a checkpoint on cuda:{device}: codes must be contiguous uint8 "
+                         "[rows, pitch] with a pitch that is a multiple of 16, ranges float32 "
+                         "[rows, groups]")
     if rows is not None and (codes.shape[0] != rows or (cols is not None and a.cols != cols)):
         raise ValueError(f"the checkpoint is of [{codes.shape[0]}, {a.cols}], not [{rows}, {cols}]")
     return codes.data_ptr(), codes.shape[1], ranges.data_ptr()
@@ -892,14 +909,18 @@ def act8_encode(x, group=128, ratio=0.5, out: Optional[Act8] = None, stream=None
     if stream is not None:
         with _on(stream):
             return act8_encode(x, group, ratio, out)
-    ptr, pitch = _matrix(x, "x")
-    rows, cols = x.shape
-    a = out if out is not None else act8_empty(rows, cols, group, ratio, x.device)
-    codes, ldc, ranges = _act8(a, rows, cols)
-    _check(load_library().pwlq_act8_encode(ptr, _DTYPES[x.dtype], rows, cols, pitch, a.group,
-                                           a.ratio, codes, ldc, ranges, _launch_stream(x)),
+    device = _home(x, "x")
+    shape = rows, cols = _shape2(x, "x")
+    ptr, pitch = _matrix(x, "x", shape, x.dtype, device)
+    if out is None:
+        out = act8_empty(rows, cols, group, ratio, x.device)
+        codes, ldc, ranges = out.codes.data_ptr(), -(-cols // 16) * 16, out.ranges.data_ptr()
+    else:
+        codes, ldc, ranges = _act8(out, device, rows, cols)
+    _check(load_library().pwlq_act8_encode(ptr, _DTYPES[x.dtype], rows, cols, pitch, out.group,
+                                           out.ratio, codes, ldc, ranges, _raw_stream(device)),
            "pwlq_act8_encode")
-    return a
+    return out
 
 
 def act8_decode(saved: Act8, dtype=torch.float32, out=None, stream=None):
@@ -907,13 +928,19 @@ def act8_decode(saved: Act8, dtype=torch.float32, out=None, stream=None):
     if stream is not None:
         with _on(stream):
             return act8_decode(saved, dtype, out)
-    codes, ldc, ranges = _act8(saved)
-    rows, cols = saved.codes.shape[0], saved.cols
+    device = _home(saved.codes, "the checkpoint")
+    codes, ldc, ranges = _act8(saved, device)
+    shape = rows, cols = saved.codes.shape[0], saved.cols
     if out is None:
-        out = torch.empty((rows, cols), dtype=dtype, device=saved.codes.device)
-    ptr, pitch = _matrix(out, "out", rows, cols, out.dtype)
+        out = torch.empty(shape, dtype=dtype, device=saved.codes.device)
+        ptr, pitch = out.data_ptr(), cols
+    else:
+        dtype = out.dtype
+        ptr, pitch = _matrix(out, "out", shape, dtype, device)
+    if dtype not in _DTYPES:
+        raise ValueError("values are float32, bfloat16 or float16")
     _check(load_library().pwlq_act8_decode(codes, ldc, ranges, rows, cols, saved.group, saved.ratio,
-                                           ptr, _DTYPES[out.dtype], pitch, _launch_stream(out)),
+                                           ptr, _DTYPES[dtype], pitch, _raw_stream(device)),
            "pwlq_act8_decode")
     return out
 
@@ -928,6 +955,7 @@ class BlockNormSaved(NamedTuple):
     pre_weight: Optional[torch.Tensor]
     post_weight: Optional[torch.Tensor]
     gate: Optional[torch.Tensor]
+    shape: tuple
     dtype: torch.dtype
     has_f: bool
     block: bytes                     # pwlq_block_norm_args of the forward call
@@ -950,59 +978,70 @@ def block_norm(x, f=None, pre_weight=None, post_weight=None, gate=None, gate_tok
         with _on(stream):
             return block_norm(x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps,
                               weight_offset, save, out)
-    xp, ldx = _matrix(x, "x")
-    rows, cols = x.shape
-    dtype, device = x.dtype, x.device
-    fp, ldf = _matrix(f, "f", rows, cols, dtype) if f is not None else (0, 0)
+    device = _home(x, "x")
+    shape = rows, cols = _shape2(x, "x")
+    dtype = x.dtype
+    xp, ldx = _matrix(x, "x", shape, dtype, device)
+    fp = ldf = pre = post = gp = ldg = gate_rows = every = hp = ldh = 0
+    if f is not None:
+        fp, ldf = _matrix(f, "f", shape, dtype, device)
+    some = pre_weight if pre_weight is not None else post_weight if post_weight is not None else gate
     wtype = dtype
-    for w in (pre_weight, post_weight, gate):
-        if w is not None:
-            wtype = w.dtype
-            break
-    for w in (pre_weight, post_weight, gate):
-        if w is not None and (w.dtype != wtype or wtype not in (dtype, torch.float32)):
-            raise ValueError("weights and gate must share one type: float32 or that of x")
-    pre, post = _vector(pre_weight, "pre_weight", cols), _vector(post_weight, "post_weight", cols)
-    gp, ldg, gate_rows, every = 0, 0, 0, 0
-    if gate is not None:
-        gate_rows = gate.shape[0]
-        gp, ldg = _matrix(gate, "gate", gate_rows, cols, wtype)
-        every = int(gate_tokens) if gate_tokens else -(-rows // max(gate_rows, 1))
-        every = max(every, 1)
+    if some is not None:
+        wtype = some.dtype
+        if wtype != dtype and wtype != torch.float32:
+            raise ValueError("weights and gate must be of x's type or float32")
+        wshape = (cols,)
+        if pre_weight is not None:
+            pre = _vector(pre_weight, "pre_weight", wshape, wtype, device)
+        if post_weight is not None:
+            post = _vector(post_weight, "post_weight", wshape, wtype, device)
+        if gate is not None:
+            gate_rows = gate.shape[0]
+            gp, ldg = _matrix(gate, "gate", (gate_rows, cols), wtype, device)
+            every = int(gate_tokens) if gate_tokens else max(-(-rows // max(gate_rows, 1)), 1)
     r, h = out if out is not None else (None, None)
     if r is None:
-        r = torch.empty((rows, cols), dtype=dtype, device=device)
-    rp, ldr = _matrix(r, "r", rows, cols, dtype)
-    hp, ldh = 0, 0
-    if pre_weight is not None:
-        if h is None:
-            h = torch.empty((rows, cols), dtype=dtype, device=device)
-        hp, ldh = _matrix(h, "h", rows, cols, dtype)
+        r = _like(x)
+        rp, ldr = r.data_ptr(), cols
     else:
+        rp, ldr = _matrix(r, "r", shape, dtype, device)
+    if pre_weight is None:
         h = None
-    group, ratio, ldc = 0, 0.0, 0
+    elif h is None:
+        h = _like(x)
+        hp, ldh = h.data_ptr(), cols
+    else:
+        hp, ldh = _matrix(h, "h", shape, dtype, device)
+    if save is None:
+        block = _BLOCK_ARGS.pack(rows, cols, _DTYPES[dtype], _DTYPES[wtype], xp, ldx, fp, ldf, post,
+                                 pre, gp, ldg, gate_rows, every, residual_scale, eps, weight_offset,
+                                 rp, ldr, hp, ldh, 0, 0.0, 0, 0, 0, 0, 0, 0, 0)
+        _check(load_library().pwlq_block_norm(block, _raw_stream(device)), "pwlq_block_norm")
+        return r, h, None
+    group, ratio = int(save[0]), float(save[1])
+    ldc = -(-cols // 16) * 16
     r8 = f8 = rs = fs = None
     rc = rr = fc = fr = rsp = fsp = 0
-    if save is not None:
-        group, ratio = int(save[0]), float(save[1])
-        if pre_weight is not None:
-            r8 = act8_empty(rows, cols, group, ratio, device)
-            rs = torch.empty(rows, dtype=torch.float32, device=device)
-            (rc, ldc, rr), rsp = _act8(r8), rs.data_ptr()
-        if gate is not None or post_weight is not None:
-            f8 = act8_empty(rows, cols, group, ratio, device)
-            fc, ldc, fr = _act8(f8)
+    if pre_weight is not None:
+        r8 = act8_empty(rows, cols, group, ratio, x.device)
+        rs = r8.ranges.new_empty(rows)
+        rc, rr, rsp = r8.codes.data_ptr(), r8.ranges.data_ptr(), rs.data_ptr()
+    if gate is not None or post_weight is not None:
+        if r8 is None:
+            f8 = act8_empty(rows, cols, group, ratio, x.device)
+        else:
+            f8 = Act8(torch.empty_like(r8.codes), torch.empty_like(r8.ranges), cols, group, ratio)
+        fc, fr = f8.codes.data_ptr(), f8.ranges.data_ptr()
         if post_weight is not None:
-            fs = torch.empty(rows, dtype=torch.float32, device=device)
+            fs = f8.ranges.new_empty(rows)
             fsp = fs.data_ptr()
     block = _BLOCK_ARGS.pack(rows, cols, _DTYPES[dtype], _DTYPES[wtype], xp, ldx, fp, ldf, post, pre,
                              gp, ldg, gate_rows, every, residual_scale, eps, weight_offset, rp, ldr,
                              hp, ldh, group, ratio, ldc, rc, rr, rsp, fc, fr, fsp)
-    _check(load_library().pwlq_block_norm(block, _launch_stream(x)), "pwlq_block_norm")
-    if save is None:
-        return r, h, None
-    return r, h, BlockNormSaved(r8, f8, rs, fs, pre_weight, post_weight, gate, dtype, f is not None,
-                                block)
+    _check(load_library().pwlq_block_norm(block, _raw_stream(device)), "pwlq_block_norm")
+    return r, h, BlockNormSaved(r8, f8, rs, fs, pre_weight, post_weight, gate, shape, dtype,
+                                f is not None, block)
 
 
 def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None, stream=None):
@@ -1012,32 +1051,45 @@ def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None,
         with _on(stream):
             return block_norm_backward(saved, dh, dr, workspace)
     some = dh if dh is not None else dr
-    if some is None or (dh is None) != (saved.pre_weight is None):
+    pre, post, gate = saved.pre_weight, saved.post_weight, saved.gate
+    if some is None or (dh is None) != (pre is None):
         raise ValueError("dh is needed exactly where the forward call had a pre_weight, dr where it "
                          "had none")
-    rows, cols = _BLOCK_ARGS.unpack_from(saved.block)[:2]
-    dtype, device = saved.dtype, some.device
-    dhp, lddh = _matrix(dh, "dh", rows, cols, dtype) if dh is not None else (0, 0)
-    drp, lddr = _matrix(dr, "dr", rows, cols, dtype) if dr is not None else (0, 0)
-    pre, post, gate = saved.pre_weight, saved.post_weight, saved.gate
-    dx = torch.empty((rows, cols), dtype=dtype, device=device)
-    df = torch.empty((rows, cols), dtype=dtype, device=device) if saved.has_f else None
-    dpre = torch.empty_like(pre) if pre is not None else None
-    dpost = torch.empty_like(post) if post is not None else None
-    dgate = torch.empty(gate.shape, dtype=gate.dtype, device=device) if gate is not None else None
+    shape, dtype = saved.shape, saved.dtype
+    cols = shape[1]
+    device = _home(some, "the gradient")
+    kept = saved.r.codes if pre is not None else saved.f.codes if saved.f is not None else some
+    if kept.get_device() != device:
+        raise ValueError(f"the forward call ran on {kept.device}, the gradient is on {some.device}")
+    dhp = lddh = drp = lddr = dfp = dprep = dpostp = dgatep = wsp = need = gate_rows = 0
+    if dh is not None:
+        dhp, lddh = _matrix(dh, "dh", shape, dtype, device)
+    if dr is not None:
+        drp, lddr = _matrix(dr, "dr", shape, dtype, device)
+    df = dpre = dpost = dgate = None
+    dx = _like(some)
+    if saved.has_f:
+        df = _like(some)
+        dfp = df.data_ptr()
+    if pre is not None:
+        dpre = _like(pre)
+        dprep = dpre.data_ptr()
+    if post is not None:
+        dpost = _like(post)
+        dpostp = dpost.data_ptr()
+    if gate is not None:
+        dgate = _like(gate)
+        dgatep, gate_rows = dgate.data_ptr(), gate.shape[0]
     lib = load_library()
-    need = 0
-    if pre is not None or post is not None or gate is not None:
-        need = lib.pwlq_block_norm_backward_workspace_bytes(
-            rows, cols, gate.shape[0] if gate is not None else 0)
+    if dprep or dpostp or dgatep:
         if workspace is None:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
-    grads = _BLOCK_GRADS.pack(
-        dhp, lddh, drp, lddr, dx.data_ptr(), cols, df.data_ptr() if df is not None else 0, cols,
-        dpre.data_ptr() if pre is not None else 0, dpost.data_ptr() if post is not None else 0,
-        dgate.data_ptr() if gate is not None else 0,
-        workspace.data_ptr() if need else 0, workspace.numel() if need else 0)
-    _check(lib.pwlq_block_norm_backward(saved.block, grads, _launch_stream(some)),
+            workspace = torch.empty(
+                lib.pwlq_block_norm_backward_workspace_bytes(shape[0], cols, gate_rows),
+                dtype=torch.uint8, device=some.device)
+        wsp, need = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
+    grads = _BLOCK_GRADS.pack(dhp, lddh, drp, lddr, dx.data_ptr(), cols, dfp, cols, dprep, dpostp,
+                              dgatep, wsp, need)
+    _check(lib.pwlq_block_norm_backward(saved.block, grads, _raw_stream(device)),
            "pwlq_block_norm_backward")
     return {"dx": dx, "df": df, "dpre": dpre, "dpost": dpost, "dgate": dgate}
 
@@ -1055,21 +1107,30 @@ def act8_weight_grad(dy, saved: Act8, dtype=None, out=None, accumulate=False, wo
     if stream is not None:
         with _on(stream):
             return act8_weight_grad(dy, saved, dtype, out, accumulate, workspace)
-    dyp, lddy = _matrix(dy, "dy")
-    rows, outputs = dy.shape
-    codes, ldc, ranges = _act8(saved, rows)
+    device = _home(dy, "dy")
+    shape = rows, outputs = _shape2(dy, "dy")
+    dyp, lddy = _matrix(dy, "dy", shape, dy.dtype, device)
+    codes, ldc, ranges = _act8(saved, device, rows)
+    cols = saved.cols
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
-        out = torch.empty((outputs, saved.cols), dtype=dtype or dy.dtype, device=dy.device)
-    dwp, lddw = _matrix(out, "out", outputs, saved.cols, out.dtype)
+        dtype = dtype or dy.dtype
+        out = torch.empty((outputs, cols), dtype=dtype, device=dy.device)
+        dwp, lddw = out.data_ptr(), cols
+    else:
+        dtype = out.dtype
+        dwp, lddw = _matrix(out, "out", (outputs, cols), dtype, device)
+    if dtype not in _DTYPES:
+        raise ValueError("dw is float32, bfloat16 or float16")
     lib = load_library()
     if workspace is None:
-        need = lib.pwlq_act8_weight_grad_workspace_bytes(rows, outputs, saved.cols,
+        need = lib.pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols,
                                                          int((dyp | lddy * 2) % 16 == 0))
         workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
     _check(lib.pwlq_act8_weight_grad(dyp, _DTYPES[dy.dtype], rows, outputs, lddy, codes, ldc, ranges,
-                                     saved.cols, saved.group, saved.ratio, dwp, _DTYPES[out.dtype],
-                                     lddw, int(accumulate), _dev(workspace, torch.uint8, "workspace"),
-                                     workspace.numel(), _launch_stream(dy)), "pwlq_act8_weight_grad")
+                                     cols, saved.group, saved.ratio, dwp, _DTYPES[dtype], lddw,
+                                     int(accumulate), _dev(workspace, torch.uint8, "workspace"),
+                                     workspace.numel(), _raw_stream(device)),
+           "pwlq_act8_weight_grad")
     return out
