@@ -53,9 +53,9 @@ act8_encode_kernel(const T* x, int64_t ldx, Act8Grid g, int group_shift, float r
 #pragma unroll
     for (int i = 0; i < kChunk; ++i) top = max_abs(top, v[i]);
     top = group_max(top, (1 << group_shift) / kChunk);
-    if (!live) return;
     const float m = act8_range(top);
-    const PieceParams P = act8_params(m, ratio);
+    const PieceParams P = act8_params_paired(m, ratio);
+    if (!live) return;
     uint2 w[kParts];
 #pragma unroll
     for (int i = 0; i < kParts; ++i) w[i] = act8_bytes8(v + 8 * i, m, P);
@@ -91,17 +91,81 @@ act8_decode_kernel(const uint8_t* codes, int64_t ldc, const float* ranges, int64
         }
         m = ranges[row * groups + (col >> group_shift)];
     }
-    const PieceParams P = act8_params(m, ratio);
+    u64 v[4 * kParts];
+    act8_decode<kParts>(w, m, ratio, v);
     T* dst = y + row * ldy + col;
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
-        u64 v[4];
-        act8_values8(w[i], P, v);
         float o[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) unpack2(v[k], o[2 * k], o[2 * k + 1]);
+        for (int k = 0; k < 4; ++k) unpack2(v[4 * i + k], o[2 * k], o[2 * k + 1]);
         store8<VEC>(o, dst + 8 * i, valid - 8 * i);
     }
+}
+
+// Without gaps between the rows, and with whole groups, there are no rows to find: chunk i is the 16
+// values, and the 16 bytes, from 16 i on.  kFlatChunks of them per thread, a block's width apart, are
+// requested together.
+constexpr int kFlatChunks = 2;
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+act8_encode_flat_kernel(const T* x, int64_t chunks, int group_shift, float ratio, uint8_t* codes, float* ranges) {
+    const int64_t first = (int64_t)blockIdx.x * (kThreads * kFlatChunks) + threadIdx.x;
+    Raw8<T> raw[kFlatChunks][2];
+#pragma unroll
+    for (int j = 0; j < kFlatChunks; ++j) {
+        const int64_t i = min(first + j * kThreads, chunks - 1);      // lanes past the end repeat it
+        raw[j][0].load(x + 16 * i);
+        raw[j][1].load(x + 16 * i + 8);
+    }
+#pragma unroll
+    for (int j = 0; j < kFlatChunks; ++j) {
+        const int64_t i = first + j * kThreads;
+        float v[16], top = 0.0f;
+        raw[j][0].get(v);
+        raw[j][1].get(v + 8);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) top = max_abs(top, v[k]);
+        const float m = act8_range(group_max(top, 1 << (group_shift - 4)));
+        const PieceParams P = act8_params_paired(m, ratio);
+        if (i >= chunks) continue;           // the whole warp goes on: it shuffles
+        const uint2 a = act8_bytes8(v, m, P), b = act8_bytes8(v + 8, m, P);
+        *reinterpret_cast<uint4*>(codes + 16 * i) = make_uint4(a.x, a.y, b.x, b.y);
+        if ((i & ((1 << (group_shift - 4)) - 1)) == 0) ranges[i >> (group_shift - 4)] = m;
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(kThreads)
+act8_decode_flat_kernel(const uint8_t* codes, const float* ranges, int64_t chunks, int group_shift, float ratio,
+                        T* y) {
+    const int64_t first = (int64_t)blockIdx.x * (kThreads * kFlatChunks) + threadIdx.x;
+    uint4 w[kFlatChunks];
+    float m[kFlatChunks];
+#pragma unroll
+    for (int j = 0; j < kFlatChunks; ++j) {
+        const int64_t i = min(first + j * kThreads, chunks - 1);
+        w[j] = *reinterpret_cast<const uint4*>(codes + 16 * i);
+        m[j] = ranges[i >> (group_shift - 4)];
+    }
+#pragma unroll
+    for (int j = 0; j < kFlatChunks; ++j) {
+        const int64_t i = first + j * kThreads;
+        if (i >= chunks) return;
+        const uint2 bytes[2] = {make_uint2(w[j].x, w[j].y), make_uint2(w[j].z, w[j].w)};
+        u64 v[8];
+        act8_decode<2>(bytes, m[j], ratio, v);
+        T* to = y + 16 * i;
+        store32(to, raw32(v, T()));
+        if (sizeof(T) == 4) store32(to + 8, raw32(v + 4, T()));
+    }
+}
+// Whether the flat kernels do: 32-byte boundaries, no gaps, whole groups.
+inline bool is_flat(const void* values, int64_t ld, const Act8Tensor& a) {
+    return (reinterpret_cast<uintptr_t>(values) & 31) == 0 && ld == a.cols && a.ldc == a.cols && a.cols % a.group == 0;
+}
+inline unsigned flat_blocks(const Act8Tensor& a) {
+    const int64_t per_block = kThreads * kFlatChunks * 16;
+    return (unsigned)((a.rows * a.cols + per_block - 1) / per_block);
 }
 
 cudaError_t plan(int64_t rows, int64_t cols, int group, bool vec, Act8Grid& g, unsigned& blocks) {
@@ -124,6 +188,11 @@ template <typename T>
 cudaError_t encode(const void* x, const Act8Tensor& a, int64_t ldx, cudaStream_t stream) {
     Act8Grid g;
     unsigned blocks;
+    if (is_flat(x, ldx, a)) {
+        act8_encode_flat_kernel<T><<<flat_blocks(a), kThreads, 0, stream>>>(
+            static_cast<const T*>(x), a.rows * a.cols / 16, group_shift(a.group), a.ratio, a.codes, a.ranges);
+        return cudaGetLastError();
+    }
     const bool vec = rows_aligned(x, ldx, sizeof(T));
     if (cudaError_t e = plan(a.rows, a.cols, a.group, vec, g, blocks)) return e;
     const T* p = static_cast<const T*>(x);
@@ -137,6 +206,11 @@ template <typename T>
 cudaError_t decode(const Act8Tensor& a, void* y, int64_t ldy, cudaStream_t stream) {
     Act8Grid g;
     unsigned blocks;
+    if (is_flat(y, ldy, a)) {
+        act8_decode_flat_kernel<T><<<flat_blocks(a), kThreads, 0, stream>>>(
+            a.codes, a.ranges, a.rows * a.cols / 16, group_shift(a.group), a.ratio, static_cast<T*>(y));
+        return cudaGetLastError();
+    }
     const bool vec = rows_aligned(y, ldy, sizeof(T));
     if (cudaError_t e = plan(a.rows, a.cols, a.group, vec, g, blocks)) return e;
     T* p = static_cast<T*>(y);

@@ -289,6 +289,21 @@ __device__ __forceinline__ PieceParams act8_params(float m, float ratio) {
     return P;
 }
 
+// The same for a group that is spread over an even number of lanes from an even lane on, all of which
+// call together: a pair of lanes shares the two reciprocals, the encoder's most expensive part.
+__device__ __forceinline__ PieceParams act8_params_paired(float m, float ratio) {
+    PieceParams P;
+    P.p = __fmul_rn(m, ratio);
+    const float d = __fsub_rn(m, P.p);
+    const bool odd = threadIdx.x & 1;
+    const float of = odd ? d : P.p;
+    const float mine = of > 0.0f ? __fmul_rn(__frcp_rn(of), kAct8Levels) : 0.0f;
+    const float other = __shfl_xor_sync(0xffffffffu, mine, 1);
+    P.inv1 = odd ? other : mine;
+    P.inv2 = odd ? mine : other;
+    return P;
+}
+
 // Eight bytes of eight values of a group with range m; P = act8_params(m).  Both pieces' levels are
 // formed and one is taken: adding 1.5 * 2^23 (+ 64 in the tail) rounds the product to an integer,
 // ties to even, and leaves region * 64 + level in the low byte of the sum.  No clamp is needed: a
@@ -300,16 +315,19 @@ __device__ __forceinline__ uint2 act8_bytes8(const float* x, float m, const Piec
         uint32_t r[4], s[4];
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
-            float y[2];
+            float y[2], c[2], t[2];
             unpack2(add2(pack2(x[4 * h + i], x[4 * h + i + 1]), 0ull), y[0], y[1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float a = fabsf(y[k]);
-                const float center = __fadd_rn(__fmul_rn(a, P.inv1), 12582912.0f);
-                const float tail = __fadd_rn(__fmul_rn(__fsub_rn(a, P.p), P.inv2), 12582912.0f + 64.0f);
-                r[i + k] = __float_as_uint(a > P.p ? tail : center);
-                s[i + k] = __float_as_uint(y[k]);
+                c[k] = __fmul_rn(fabsf(y[k]), P.inv1);
+                t[k] = __fmul_rn(__fsub_rn(fabsf(y[k]), P.p), P.inv2);
             }
+            const u64 center = add2(pack2(c[0], c[1]), both(12582912.0f));
+            const u64 tail = add2(pack2(t[0], t[1]), both(12582912.0f + 64.0f));
+            r[i] = __float_as_uint(fabsf(y[0]) > P.p ? lo2(tail) : lo2(center));
+            r[i + 1] = __float_as_uint(fabsf(y[1]) > P.p ? hi2(tail) : hi2(center));
+            s[i] = __float_as_uint(y[0]);
+            s[i + 1] = __float_as_uint(y[1]);
         }
         const uint32_t low = __byte_perm(__byte_perm(r[0], r[1], 0x0040), __byte_perm(r[2], r[3], 0x0040), 0x5410);
         const uint32_t top = __byte_perm(__byte_perm(s[0], s[1], 0x0073), __byte_perm(s[2], s[3], 0x0073), 0x5410);
@@ -341,22 +359,37 @@ __device__ __forceinline__ void act8_scaled8(uint2 bytes, const Act8Lines& L, u6
 }
 
 // The eight values of eight bytes, in pairs.  A byte permutation puts j = region * 64 + level into
-// the upper mantissa of 128 + j, so no integer is converted; both pieces are formed and one is taken.
+// the upper mantissa of f = 128 + j, so no integer is converted; f * s - 128 * s in one fused operation
+// is exact before its one rounding (128 * s is exact, 192 * s would not be), so the products are the
+// format's.  Both pieces are formed and one is taken.  Not for ranges above kAct8Big, where 128 * s may
+// overflow.
+constexpr float kAct8Big = 1.0e38f;
 __device__ __forceinline__ void act8_values8(uint2 bytes, const PieceParams& P, u64* v) {
-    const u64 s1 = both(P.s1), s2 = both(P.s2);
+    const u64 s1 = both(P.s1), z1 = both(-128.0f * P.s1), s2 = both(P.s2), z2 = both(-128.0f * P.s2), p = both(P.p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t w = i < 2 ? bytes.x : bytes.y, j = w & 0x7f7f7f7fu;
         const float f0 = __uint_as_float(__byte_perm(j, 0x43000000u, i & 1 ? 0x7244 : 0x7044));
         const float f1 = __uint_as_float(__byte_perm(j, 0x43000000u, i & 1 ? 0x7344 : 0x7144));
-        const u64 f = pack2(f0, f1);
-        const u64 c = mul2(add2(f, both(-128.0f)), s1), t = mul2(add2(f, both(-192.0f)), s2);
-        const float v0 = f0 >= 192.0f ? __fadd_rn(lo2(t), P.p) : lo2(c);
-        const float v1 = f1 >= 192.0f ? __fadd_rn(hi2(t), P.p) : hi2(c);
+        const u64 f = pack2(f0, f1), c = fma2(f, s1, z1);
+        const u64 t = add2(fma2(add2(f, both(-64.0f)), s2, z2), p);
+        const float v0 = f0 >= 192.0f ? lo2(t) : lo2(c), v1 = f1 >= 192.0f ? hi2(t) : hi2(c);
         const uint32_t n0 = w << (i & 1 ? 8 : 24), n1 = i & 1 ? w : w << 16;
         v[i] = pack2(__uint_as_float(__float_as_uint(v0) ^ (n0 & 0x80000000u)),
                      __uint_as_float(__float_as_uint(v1) ^ (n1 & 0x80000000u)));
     }
+}
+// The 8 * N values of 8 * N bytes of a group with any range: above kAct8Big the constants are those of
+// m / 256 and the values are scaled back, exactly.
+template <int N>
+__device__ __forceinline__ void act8_decode(const uint2* bytes, float m, float ratio, u64* v) {
+    const bool big = m > kAct8Big;
+    const PieceParams P = act8_params(big ? m * 0.00390625f : m, ratio);
+#pragma unroll
+    for (int i = 0; i < N; ++i) act8_values8(bytes[i], P, v + 4 * i);
+    if (big)
+#pragma unroll
+        for (int k = 0; k < 4 * N; ++k) v[k] = mul2(v[k], both(256.0f));
 }
 
 }  // namespace pwlq

@@ -129,10 +129,11 @@ __device__ __forceinline__ void save8(const u64* pairs, const NormParams& q, int
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max_abs(top, v[i]);
     top = group_max(top, q.group_lanes);
-    if (valid <= 0) return;
     const float m = act8_range(top);
+    const PieceParams P = act8_params_paired(m, q.ratio);
+    if (valid <= 0) return;
     uint8_t* at = codes + row * q.a.ldc + c;
-    *reinterpret_cast<uint2*>(at) = act8_bytes8(v, m, act8_params(m, q.ratio));
+    *reinterpret_cast<uint2*>(at) = act8_bytes8(v, m, P);
     // the row's last 16 bytes may need zeros that no value stands for
     if (valid <= 8 && (c & 8) == 0) *reinterpret_cast<uint2*>(at + 8) = make_uint2(0u, 0u);
     if ((c & ((1 << q.group_shift) - 1)) == 0) ranges[row * q.groups + (c >> q.group_shift)] = m;
@@ -253,9 +254,9 @@ __device__ __forceinline__ void save32(const u64* v, const NormParams& q, bool l
 #pragma unroll
     for (int k = 0; k < 2 * kP; ++k) top = max_abs(top, f[k]);
     top = group_max(top, q.group_lanes);
-    if (!live) return;
     const float m = act8_range(top);
-    const PieceParams P = act8_params(m, q.ratio);
+    const PieceParams P = act8_params_paired(m, q.ratio);
+    if (!live) return;
     uint8_t* at = codes + row * q.a.ldc + c;
     const uint2 a = act8_bytes8(f, m, P);
     if (kP == 8) {
