@@ -15,23 +15,27 @@ constexpr int kThreads = 256;
 // values are off their alignment, since neighbouring threads then join their values (store8).
 __host__ __device__ constexpr int chunk_of(bool vec) { return vec ? 16 : 8; }
 
-// Which chunk of which row a thread owns.  Rows of fewer than 256 chunks share a block
-// (rows_per_block of them), longer ones take blocks_per_row blocks; `chunks` is the row's number of
-// chunks rounded up to whole groups, so that a group's threads are an aligned part of a warp.
+// Which chunk of which row a thread owns.  Rows of up to 256 chunks share a block (rows_per_block of
+// them), longer ones take blocks_per_row equal blocks; a row's chunks are counted in whole groups, so
+// that a group's threads are an aligned part of a warp.  A block has as many warps as that takes, so
+// that a row of 172 chunks does not leave a third of 256 threads idle.
 struct Act8Grid {
     int64_t rows, cols;
+    int threads;
     int chunks_lo;                       // chunks per row inside one block
     int rows_per_block;
     unsigned blocks_per_row;
     unsigned magic;                      // tid / chunks_lo == (tid * magic) >> 16 for tid < 256
 };
 
-__device__ __forceinline__ bool locate(const Act8Grid& g, int chunk, int64_t& row, int64_t& col) {
+// valid: how many values the row has from the chunk's first on (<= 0: the thread has nothing to do).
+__device__ __forceinline__ bool locate(const Act8Grid& g, int chunk, int64_t& row, int64_t& col, int& valid) {
     const unsigned rb = blockIdx.x / g.blocks_per_row, part = blockIdx.x - rb * g.blocks_per_row;
     const unsigned in = (threadIdx.x * g.magic) >> 16;
     row = (int64_t)rb * g.rows_per_block + in;
-    col = ((int64_t)part * kThreads + (threadIdx.x - in * g.chunks_lo)) * chunk;
-    return in < (unsigned)g.rows_per_block && row < g.rows && col < g.cols;
+    col = ((int64_t)part * g.chunks_lo + (threadIdx.x - in * g.chunks_lo)) * chunk;
+    valid = in < (unsigned)g.rows_per_block && row < g.rows ? (int)(g.cols - col) : 0;
+    return valid > 0;
 }
 
 template <typename T, bool VEC>
@@ -40,8 +44,8 @@ act8_encode_kernel(const T* x, int64_t ldx, Act8Grid g, int group_shift, float r
                    uint8_t* codes, int64_t ldc, float* ranges, int64_t groups) {
     constexpr int kChunk = chunk_of(VEC), kParts = kChunk / 8;
     int64_t row, col;
-    const bool live = locate(g, kChunk, row, col);
-    const int valid = live ? (int)min((int64_t)32, g.cols - col) : 0;
+    int valid;
+    const bool live = locate(g, kChunk, row, col, valid);
     Raw8<T> raw[kParts];
     const T* src = x + row * ldx + col;
 #pragma unroll
@@ -76,8 +80,10 @@ act8_decode_kernel(const uint8_t* codes, int64_t ldc, const float* ranges, int64
                    Act8Grid g, int group_shift, float ratio, T* y, int64_t ldy) {
     constexpr int kChunk = chunk_of(VEC), kParts = kChunk / 8;
     int64_t row, col;
-    const bool live = locate(g, kChunk, row, col);
-    const int valid = live ? (int)min((int64_t)32, g.cols - col) : 0;
+    int valid;
+    const bool live = locate(g, kChunk, row, col, valid);
+    allow_dependents();
+    if (!__any_sync(0xffffffffu, live)) return;
     uint2 w[kParts] = {};
     float m = 0.0f;
     if (live) {
@@ -138,6 +144,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads)
 act8_decode_flat_kernel(const uint8_t* codes, const float* ranges, int64_t chunks, int group_shift, float ratio,
                         T* y) {
+    allow_dependents();
     const int64_t first = (int64_t)blockIdx.x * (kThreads * kFlatChunks) + threadIdx.x;
     uint4 w[kFlatChunks];
     float m[kFlatChunks];
@@ -173,9 +180,15 @@ cudaError_t plan(int64_t rows, int64_t cols, int group, bool vec, Act8Grid& g, u
     const int64_t chunks = (cols + group - 1) / group * per_group;
     g.rows = rows;
     g.cols = cols;
-    g.chunks_lo = (int)(chunks < kThreads ? chunks : kThreads);
-    g.rows_per_block = kThreads / g.chunks_lo;
     const int64_t per_row = (chunks + kThreads - 1) / kThreads;
+    if (per_row == 1) {
+        g.chunks_lo = (int)chunks;
+        g.rows_per_block = kThreads / g.chunks_lo;
+        g.threads = (g.chunks_lo * g.rows_per_block + 31) / 32 * 32;
+    } else {
+        g.rows_per_block = 1;
+        g.threads = g.chunks_lo = (int)((chunks + per_row - 1) / per_row + 31) / 32 * 32;
+    }
     g.magic = (unsigned)(65536 / g.chunks_lo + 1);
     const int64_t n = (rows + g.rows_per_block - 1) / g.rows_per_block * per_row;
     if (n > ((int64_t)1 << 31) - 1) return cudaErrorInvalidConfiguration;
@@ -198,7 +211,7 @@ cudaError_t encode(const void* x, const Act8Tensor& a, int64_t ldx, cudaStream_t
     const T* p = static_cast<const T*>(x);
     auto* kernel = vec ? act8_encode_kernel<T, true>
                                                    : act8_encode_kernel<T, false>;
-    kernel<<<blocks, kThreads, 0, stream>>>(p, ldx, g, group_shift(a.group), a.ratio, a.codes,
+    kernel<<<blocks, g.threads, 0, stream>>>(p, ldx, g, group_shift(a.group), a.ratio, a.codes,
                                             a.ldc, a.ranges, a.groups());
     return cudaGetLastError();
 }
@@ -216,7 +229,7 @@ cudaError_t decode(const Act8Tensor& a, void* y, int64_t ldy, cudaStream_t strea
     T* p = static_cast<T*>(y);
     auto* kernel = vec ? act8_decode_kernel<T, true>
                                                    : act8_decode_kernel<T, false>;
-    kernel<<<blocks, kThreads, 0, stream>>>(a.codes, a.ldc, a.ranges, a.groups(), g,
+    kernel<<<blocks, g.threads, 0, stream>>>(a.codes, a.ldc, a.ranges, a.groups(), g,
                                             group_shift(a.group), a.ratio, p, ldy);
     return cudaGetLastError();
 }

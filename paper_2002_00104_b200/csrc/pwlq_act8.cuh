@@ -13,6 +13,12 @@ constexpr float kAct8Levels = 63.0f;            // L of the 7-bit scheme
 constexpr float kAct8Tiny = 7.8886090522101181e-31f;   // 2^-100: a smaller range is held as 0
 constexpr uint32_t kInfBits = 0x7f800000u;
 
+// A kernel that was launched as the dependent of the one before it may start once all blocks of that
+// one have called allow_dependents (or have ended), and must call await_previous before it touches
+// anything that the earlier kernel writes or reads.
+__device__ __forceinline__ void allow_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ------------------------------------------------------------------------------ typed access
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -59,7 +65,6 @@ template <typename T> struct Raw8 {
         w.w = pack16(v[6], v[7], T());
     }
     __device__ __forceinline__ void from_words(const uint32_t* x) { w = make_uint4(x[0], x[1], x[2], x[3]); }
-    __device__ __forceinline__ void to_words(uint32_t* x) const { x[0] = w.x; x[1] = w.y; x[2] = w.z; x[3] = w.w; }
     __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<uint4*>(p) = w; }
     __device__ __forceinline__ void clear() { w = make_uint4(0u, 0u, 0u, 0u); }
@@ -77,11 +82,6 @@ template <> struct Raw8<float> {
     __device__ __forceinline__ void from_words(const uint32_t* x) {
         a = make_float4(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]), __uint_as_float(x[3]));
         b = make_float4(__uint_as_float(x[4]), __uint_as_float(x[5]), __uint_as_float(x[6]), __uint_as_float(x[7]));
-    }
-    __device__ __forceinline__ void to_words(uint32_t* x) const {
-        float v[8];
-        get(v);
-        for (int i = 0; i < 8; ++i) x[i] = __float_as_uint(v[i]);
     }
     __device__ __forceinline__ void load(const float* p) {
         a = *reinterpret_cast<const float4*>(p);
@@ -150,10 +150,10 @@ __device__ __forceinline__ void store8_each(const float* v, T* p, int valid) {
         if (i < valid) p[i] = from_f32<T>(v[i]);
 }
 
-// The same for a whole warp at once (every lane calls; neighbouring lanes normally hold neighbouring
-// values).  VEC: p is on a 16-byte boundary where valid >= 8.  Off the boundary a lane writes the
-// aligned 16 bytes that begin with its left neighbour's last values; what has no such neighbour is
-// written value by value.
+// The same for a whole warp at once: every lane calls.  VEC: p is on a 16-byte boundary where
+// valid >= 8.  Off the boundary, lanes that hold consecutive parts of one row (valid counts to the
+// row's end in all of them) turn their values in shared memory, so that a warp writes 32 neighbours at
+// a time; parts of several rows are written value by value.
 template <bool VEC, typename T>
 __device__ __forceinline__ void store8(const float* v, T* p, int valid) {
     if (VEC) {
@@ -167,40 +167,24 @@ __device__ __forceinline__ void store8(const float* v, T* p, int valid) {
         return;
     }
     constexpr unsigned kAll = 0xffffffffu;
-    constexpr int kPer = 16 / sizeof(T);
-    const int lane = threadIdx.x & 31, o = past_boundary(p);
+    __shared__ Raw8<T> turn[32][32];
+    const int lane = threadIdx.x & 31;
+    Raw8<T>* const mine = turn[threadIdx.x >> 5];
+    T* const p0 = reinterpret_cast<T*>(__shfl_sync(kAll, (uintptr_t)p, 0));
+    const int valid0 = __shfl_sync(kAll, valid, 0);
+    if (!__all_sync(kAll, p == p0 + 8 * lane && (valid == valid0 - 8 * lane || (valid <= 0 && valid0 <= 8 * lane)))) {
+        store8_each(v, p, valid);
+        return;
+    }
     Raw8<T> raw;
     raw.set(v);
-    uint32_t mine[2 * sizeof(T)], w[4 + 2 * sizeof(T)];     // a neighbour's last 16 bytes, then mine
-    raw.to_words(mine);
-    const uintptr_t left = __shfl_up_sync(kAll, (uintptr_t)p, 1);
-    const int left_valid = __shfl_up_sync(kAll, valid, 1);
+    __syncwarp();
+    mine[lane] = raw;
+    __syncwarp();
+    const T* from = reinterpret_cast<const T*>(mine);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        w[i] = __shfl_up_sync(kAll, mine[2 * sizeof(T) - 4 + i], 1);
-#pragma unroll
-    for (int i = 0; i < (int)(2 * sizeof(T)); ++i) w[4 + i] = mine[i];
-    const bool whole = valid >= 8;
-    const bool joins = whole && (o == 0 || (lane > 0 && left_valid >= 8 && left + 8 * sizeof(T) == (uintptr_t)p));
-    const int right_joins = __shfl_down_sync(kAll, (int)joins, 1);
-    const uintptr_t right = __shfl_down_sync(kAll, (uintptr_t)p, 1);
-    const bool taken = whole && lane < 31 && right_joins && right == (uintptr_t)(p + 8);
-    if (joins) {
-        // o values of the neighbour, then mine
-        if (o == 0)
-            raw.store(p);
-        else {
-            shift_window<4 + 2 * sizeof(T), sizeof(T) == 2>(w, 16 - o * (int)sizeof(T));
-            *reinterpret_cast<uint4*>(p - o) = make_uint4(w[0], w[1], w[2], w[3]);
-            if (sizeof(T) == 4)
-                *reinterpret_cast<uint4*>(p - o + kPer) = make_uint4(w[4], w[5], w[6], w[7]);
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const bool written = (joins && i < 8 - o) || (taken && i >= 8 - o);
-        if (i < valid && !written) p[i] = from_f32<T>(v[i]);
-    }
+    for (int i = 0; i < 8; ++i)
+        if (32 * i + lane < valid0) p0[32 * i + lane] = from[32 * i + lane];
 }
 
 // Two binary32 lanes at a time (see fma2 in pwlq_common.cuh).

@@ -408,7 +408,10 @@ struct ColumnSums {
             const int c = (threadIdx.x + i * blockDim.x) * 8;
             u64 v[4];
             get(which, i, v);
-            store_pairs<VEC>(v, to + c, cols - c);
+            float f[8];
+            floats8(v, f);
+            if (VEC) store8<true>(f, to + c, cols - c);
+            else store8_each(f, to + c, cols - c);       // once per CTA or gate
         }
     }
 };

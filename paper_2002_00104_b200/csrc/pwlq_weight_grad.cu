@@ -31,7 +31,7 @@ constexpr int kStages = 6;
 constexpr int kBlockBytes = kStep * 128;        // 64 columns x 64 rows of 16-bit values
 constexpr int kOperandBytes = 2 * kBlockBytes;
 constexpr int kStageBytes = 2 * kOperandBytes;
-constexpr int kEpilogueWarps = 4, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
+constexpr int kEpilogueWarps = 8, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
 constexpr int kThreads = 32 * (kMmaWarp + 1);
 constexpr int kMinSteps = 4;                    // of a piece of a cut tile
 
@@ -77,7 +77,7 @@ __device__ __forceinline__ Unit unit_of(const Schedule& s, int64_t u) {
 struct Params {
     WeightGrad w;
     Schedule s;
-    float* pieces;                 // workspace: [slot][256][256]
+    float* pieces;                 // workspace: [slot][block of 32 x 32][four columns][row][4]
     int64_t groups;
     int group_shift;
     bool vec_out;                  // rows of dw start on 16-byte boundaries
@@ -149,6 +149,11 @@ __device__ void mma_loop(const Params& p, Shared& sh, unsigned char* stages, uin
     }
 }
 
+// Where the block of 32 x 32 values at (row, column) of a piece begins.
+__device__ __forceinline__ int64_t piece_block(int64_t slot, int64_t row, int64_t c) {
+    return slot * (kTile * kTile) + (row / 32 * (kTile / 32) + c / 32) * 1024;
+}
+
 // A warp's 32 x 32 results (one row per lane) to rows of dw that start at `to`, `ld` apart; `rows`
 // and `cols` of them exist.
 template <typename W>
@@ -190,7 +195,9 @@ __device__ __forceinline__ void put_block(float* v, float (*turn)[33], W* to, in
 
 template <typename T>
 __device__ void epilogue_loop(const Params& p, Shared& sh, uint32_t tmem, uint32_t rank) {
-    const int lane = threadIdx.x & 31, quarter = (threadIdx.x >> 5) & 3;
+    // a warp reads the quarter of the lanes that its number selects; two share it, half the columns each
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quarter = warp & 3;
+    const int first = (warp >> 2) * (kTile / 2);
     const uint32_t empty = peer_addr(sh.sum_empty, 0);
     int sum = 0;
     unsigned phase = 0;
@@ -199,23 +206,24 @@ __device__ void epilogue_loop(const Params& p, Shared& sh, uint32_t tmem, uint32
         if (!warp_wait(&sh.sum_full[sum], phase)) { g_weight_grad_timeout = 1; return; }
         tcgen05_after_sync();
         const int64_t row = rank * kHalf + quarter * 32, n = unit.n0 + row;      // of the warp's first lane
-        for (int c = 0; c < kTile; c += 32) {
+        for (int c = first; c < first + kTile / 2; c += 32) {
             float v[32];
             __syncwarp();
             tmem_load32(tmem + ((uint32_t)(quarter * 32) << 16) + sum * kTile + c, v);
             const int64_t k = unit.k0 + c;
             if (unit.slot >= 0) {
-                float4* to = reinterpret_cast<float4*>(p.pieces + (unit.slot * kTile + row + lane) * kTile + c);
+                float4* to = reinterpret_cast<float4*>(p.pieces + piece_block(unit.slot, row, c)) + lane;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) to[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                for (int i = 0; i < 8; ++i)
+                    to[32 * i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
             } else if (n < p.w.outputs && k < p.w.x.cols) {
                 const int rows = (int)min((int64_t)32, p.w.outputs - n), cols = (int)min((int64_t)32, p.w.x.cols - k);
                 const int64_t at = n * p.w.lddw + k;
                 if (p.w.dw_dtype == kF32)
-                    put_block(v, sh.turn[quarter], static_cast<float*>(p.w.dw) + at, p.w.lddw, rows, cols,
+                    put_block(v, sh.turn[warp], static_cast<float*>(p.w.dw) + at, p.w.lddw, rows, cols,
                               p.vec_out, p.w.accumulate);
                 else
-                    put_block(v, sh.turn[quarter], static_cast<T*>(p.w.dw) + at, p.w.lddw, rows, cols,
+                    put_block(v, sh.turn[warp], static_cast<T*>(p.w.dw) + at, p.w.lddw, rows, cols,
                               p.vec_out, p.w.accumulate);
             }
         }
@@ -253,6 +261,8 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy, const __grid_constant
     cluster_sync();
     tcgen05_after_sync();
     const uint32_t tmem = sh.tmem;
+    allow_dependents();
+    await_previous();                      // the operands' kernels, and the last reader of the workspace
 
     if (warp < kEpilogueWarps) {
         epilogue_loop<T>(p, sh, tmem, rank);
@@ -268,39 +278,34 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy, const __grid_constant
     if (warp == kMmaWarp) tmem_free_pair(tmem);
 }
 
-// Adds the pieces of the cut tiles in the order of t: eight columns of one row per thread.
+// Adds the pieces of the cut tiles in the order of t: a warp per block of 32 x 32 values.
+constexpr int kPieceWarps = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) weight_grad_pieces_kernel(const __grid_constant__ Params p) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t cut = i / (kTile * (kTile / 8));
-    const int row = (int)(i / (kTile / 8) % kTile), c = (int)(i % (kTile / 8)) * 8;
+__global__ void __launch_bounds__(32 * kPieceWarps) weight_grad_pieces_kernel(const __grid_constant__ Params p) {
+    __shared__ float turn[kPieceWarps][32][33];
+    await_previous();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr int kBlocks = (kTile / 32) * (kTile / 32);
+    const int64_t block = (int64_t)blockIdx.x * kPieceWarps + warp, cut = block / kBlocks;
+    const int row = (int)(block % kBlocks) / (kTile / 32) * 32, c = (int)(block % (kTile / 32)) * 32;
     const int64_t tile = p.s.whole + cut;
     const int64_t n = tile % p.s.tiles_n * kTile + row, k = tile / p.s.tiles_n * kTile + c;
     if (n >= p.w.outputs || k >= p.w.x.cols) return;
-    float v[8] = {};
+    float v[32] = {};
     for (int64_t s = 0; s < p.s.pieces; ++s) {
-        const float* from = p.pieces + ((cut * p.s.pieces + s) * kTile + row) * kTile + c;
-        const float4 a = *reinterpret_cast<const float4*>(from), b = *reinterpret_cast<const float4*>(from + 4);
-        v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w;
-        v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
-    }
-    const int valid = (int)min((int64_t)8, p.w.x.cols - k);
-    auto put = [&](auto* to) {
-        using W = typename std::remove_pointer<decltype(to)>::type;
-        Raw8<W> raw;
-        if (p.w.accumulate) {
-            float old[8];
-            if (p.vec_out) load8<true>(raw, to, valid, 0);
-            else load8<false>(raw, to, valid, 0);
-            raw.get(old);
+        const float4* from = reinterpret_cast<const float4*>(p.pieces + piece_block(cut * p.s.pieces + s, row, c)) + lane;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += old[j];
+        for (int i = 0; i < 8; ++i) {
+            const float4 a = from[32 * i];
+            v[4 * i] += a.x; v[4 * i + 1] += a.y; v[4 * i + 2] += a.z; v[4 * i + 3] += a.w;
         }
-        if (p.vec_out) store8<true>(v, to, valid);
-        else store8_each(v, to, valid);
-    };
-    if (p.w.dw_dtype == kF32) put(static_cast<float*>(p.w.dw) + n * p.w.lddw + k);
-    else put(static_cast<T*>(p.w.dw) + n * p.w.lddw + k);
+    }
+    const int rows = (int)min((int64_t)32, p.w.outputs - n), cols = (int)min((int64_t)32, p.w.x.cols - k);
+    const int64_t at = n * p.w.lddw + k;
+    if (p.w.dw_dtype == kF32)
+        put_block(v, turn[warp], static_cast<float*>(p.w.dw) + at, p.w.lddw, rows, cols, p.vec_out, p.w.accumulate);
+    else
+        put_block(v, turn[warp], static_cast<T*>(p.w.dw) + at, p.w.lddw, rows, cols, p.vec_out, p.w.accumulate);
 }
 
 // dy with rows that start on 16-byte boundaries, for a dy whose rows do not (TMA's condition).
@@ -349,6 +354,24 @@ Schedule schedule(int64_t rows, int64_t outputs, int64_t cols, int64_t pairs) {
 inline size_t piece_bytes(int64_t rows, int64_t outputs, int64_t cols) {
     const Schedule s = schedule(rows, outputs, cols, resident_pairs());
     return (size_t)(s.units - s.whole) * kTile * kTile * sizeof(float);
+}
+
+// Launches a kernel that may begin while the one before it in the stream still runs (it waits for that
+// one's end itself).
+template <typename... P, typename... A>
+cudaError_t launch_dependent(void (*kernel)(P...), unsigned blocks, int threads, size_t smem, cudaStream_t stream,
+                             const A&... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(blocks);
+    config.blockDim = dim3((unsigned)threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = &attr;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
 }
 
 // cuTensorMapEncodeTiled, through the runtime: the library does not link the driver.
@@ -424,16 +447,18 @@ cudaError_t launch(const WeightGrad& w, void* workspace, cudaStream_t stream) {
     const int64_t xpitch = realigned_pitch(w.x.cols);
     if (cudaError_t e = launch_act8_decode(w.x, at, w.dtype, xpitch, stream)) return e;
     if (cudaError_t e = map_columns<T>(xmap, at, w.x.cols, w.rows, xpitch)) return e;
-    auto* kernel = weight_grad_kernel<T>;
-    if (cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBytes))
+    if (cudaError_t e = cudaFuncSetAttribute(weight_grad_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)kSmemBytes))
         return e;
     const int64_t ctas = 2 * (p.s.units < pairs ? p.s.units : pairs);
-    kernel<<<(unsigned)ctas, kThreads, kSmemBytes, stream>>>(map, xmap, p);
-    if (cudaError_t e = cudaGetLastError()) return e;
+    if (cudaError_t e = launch_dependent(weight_grad_kernel<T>, (unsigned)ctas, kThreads, kSmemBytes, stream, map,
+                                         xmap, p))
+        return e;
     const int64_t cut = (int64_t)p.s.tiles_n * p.s.tiles_k - p.s.whole;
     if (!cut) return cudaSuccess;
-    weight_grad_pieces_kernel<T><<<(unsigned)(cut * kTile * (kTile / 8) / 256), 256, 0, stream>>>(p);
-    return cudaGetLastError();
+    const int64_t blocks = cut * (kTile / 32) * (kTile / 32);
+    return launch_dependent(weight_grad_pieces_kernel<T>, (unsigned)(blocks / kPieceWarps), 32 * kPieceWarps, 0,
+                            stream, p);
 }
 
 }  // namespace
