@@ -44,6 +44,10 @@ __device__ __forceinline__ void fence_proxy_async_all() {
     asm volatile("fence.proxy.async;" ::: "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
 // Box at (x, y) of a two-dimensional tensor map into this CTA's shared memory; the bytes count on
 // an mbarrier of either CTA of the pair (bar: a shared::cluster address).  x * element size must be
 // a multiple of 16 bytes.

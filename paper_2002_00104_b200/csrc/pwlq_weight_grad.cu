@@ -33,7 +33,9 @@ constexpr int kOperandBytes = 2 * kBlockBytes;
 constexpr int kStageBytes = 2 * kOperandBytes;
 constexpr int kEpilogueWarps = 8, kTmaWarp = kEpilogueWarps, kMmaWarp = kTmaWarp + 1;
 constexpr int kThreads = 32 * (kMmaWarp + 1);
-constexpr int kMinSteps = 4;                    // of a piece of a cut tile
+// A cut costs about 4 us (the pieces' way through memory, and a second kernel), a step 0.36 us: tiles
+// of fewer than kCutSteps steps stay whole, and a piece has at least kMinSteps.
+constexpr int kCutSteps = 24, kMinSteps = 6;
 
 struct Shared {
     uint64_t full[kStages];        // in the leading CTA: both halves of both operands are there
@@ -193,6 +195,22 @@ __device__ __forceinline__ void put_block(float* v, float (*turn)[33], W* to, in
     __syncwarp();
 }
 
+// Four results of one row to dw, the first `valid` of which exist.
+template <typename W>
+__device__ __forceinline__ void put4(const float* r, W* to, int valid, bool vec, bool accumulate) {
+    struct alignas(4 * sizeof(W)) Four { W v[4]; } out;
+    if (vec && valid == 4) {
+        if (accumulate) out = *reinterpret_cast<const Four*>(to);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out.v[i] = from_f32<W>(accumulate ? r[i] + to_f32(out.v[i]) : r[i]);
+        *reinterpret_cast<Four*>(to) = out;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < valid) to[i] = from_f32<W>(accumulate ? r[i] + to_f32(to[i]) : r[i]);
+}
+
 template <typename T>
 __device__ void epilogue_loop(const Params& p, Shared& sh, uint32_t tmem, uint32_t rank) {
     // a warp reads the quarter of the lanes that its number selects; two share it, half the columns each
@@ -256,6 +274,10 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy, const __grid_constant
         fence_barrier_init();
     }
     if (warp == kMmaWarp) tmem_alloc_pair(&sh.tmem);
+    if (threadIdx.x == kTmaWarp * 32) {
+        prefetch_map(&dy);
+        prefetch_map(&xhat);
+    }
     tcgen05_before_sync();
     __syncthreads();
     cluster_sync();
@@ -278,34 +300,41 @@ weight_grad_kernel(const __grid_constant__ CUtensorMap dy, const __grid_constant
     if (warp == kMmaWarp) tmem_free_pair(tmem);
 }
 
-// Adds the pieces of the cut tiles in the order of t: a warp per block of 32 x 32 values.
-constexpr int kPieceWarps = 4;
+// Adds the pieces of the cut tiles in the order of t: a CTA per block of 32 x 32 values, four columns of
+// one row per thread, eight pieces requested at a time (one after the other, 32 pieces of a 256 x 256
+// tile took 40 us).
 template <typename T>
-__global__ void __launch_bounds__(32 * kPieceWarps) weight_grad_pieces_kernel(const __grid_constant__ Params p) {
-    __shared__ float turn[kPieceWarps][32][33];
-    await_previous();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__global__ void __launch_bounds__(256) weight_grad_pieces_kernel(const __grid_constant__ Params p) {
+    __shared__ float turn[32][36];
     constexpr int kBlocks = (kTile / 32) * (kTile / 32);
-    const int64_t block = (int64_t)blockIdx.x * kPieceWarps + warp, cut = block / kBlocks;
-    const int row = (int)(block % kBlocks) / (kTile / 32) * 32, c = (int)(block % (kTile / 32)) * 32;
+    const int64_t cut = blockIdx.x / kBlocks;
+    const int block = (int)(blockIdx.x % kBlocks);
     const int64_t tile = p.s.whole + cut;
-    const int64_t n = tile % p.s.tiles_n * kTile + row, k = tile / p.s.tiles_n * kTile + c;
-    if (n >= p.w.outputs || k >= p.w.x.cols) return;
-    float v[32] = {};
-    for (int64_t s = 0; s < p.s.pieces; ++s) {
-        const float4* from = reinterpret_cast<const float4*>(p.pieces + piece_block(cut * p.s.pieces + s, row, c)) + lane;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float4 a = from[32 * i];
-            v[4 * i] += a.x; v[4 * i + 1] += a.y; v[4 * i + 2] += a.z; v[4 * i + 3] += a.w;
-        }
+    const int64_t n0 = tile % p.s.tiles_n * kTile + block / (kTile / 32) * 32;
+    const int64_t k0 = tile / p.s.tiles_n * kTile + block % (kTile / 32) * 32;
+    if (n0 >= p.w.outputs || k0 >= p.w.x.cols) return;
+    const float4* from = reinterpret_cast<const float4*>(p.pieces) +
+                         (cut * p.s.pieces * kBlocks + block) * 256 + threadIdx.x;
+    await_previous();
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
+    for (int s = 0; s < (int)p.s.pieces; ++s) {
+        const float4 a = __ldcg(from + (int64_t)s * (kTile * kTile / 4));
+        v.x += a.x; v.y += a.y; v.z += a.z; v.w += a.w;
     }
-    const int rows = (int)min((int64_t)32, p.w.outputs - n), cols = (int)min((int64_t)32, p.w.x.cols - k);
-    const int64_t at = n * p.w.lddw + k;
+    // as it was written: threads of a warp hold the 32 rows of four columns
+    *reinterpret_cast<float4*>(&turn[threadIdx.x & 31][threadIdx.x / 32 * 4]) = v;
+    __syncthreads();
+    const int row = threadIdx.x / 8, c = threadIdx.x % 8 * 4;
+    v = *reinterpret_cast<const float4*>(&turn[row][c]);
+    const int64_t n = n0 + row, k = k0 + c;
+    if (n >= p.w.outputs || k >= p.w.x.cols) return;
+    const int valid = (int)min((int64_t)4, p.w.x.cols - k);
+    const float r[4] = {v.x, v.y, v.z, v.w};
     if (p.w.dw_dtype == kF32)
-        put_block(v, turn[warp], static_cast<float*>(p.w.dw) + at, p.w.lddw, rows, cols, p.vec_out, p.w.accumulate);
+        put4(r, static_cast<float*>(p.w.dw) + n * p.w.lddw + k, valid, p.vec_out, p.w.accumulate);
     else
-        put_block(v, turn[warp], static_cast<T*>(p.w.dw) + at, p.w.lddw, rows, cols, p.vec_out, p.w.accumulate);
+        put4(r, static_cast<T*>(p.w.dw) + n * p.w.lddw + k, valid, p.vec_out, p.w.accumulate);
 }
 
 // dy with rows that start on 16-byte boundaries, for a dy whose rows do not (TMA's condition).
@@ -343,8 +372,8 @@ Schedule schedule(int64_t rows, int64_t outputs, int64_t cols, int64_t pairs) {
     s.steps = (rows + kStep - 1) / kStep;
     const int64_t tiles = (int64_t)s.tiles_n * s.tiles_k;
     const int64_t left = tiles % pairs;
-    s.pieces = left ? pairs / left : 1;
-    if (s.pieces > s.steps / kMinSteps) s.pieces = s.steps / kMinSteps > 0 ? s.steps / kMinSteps : 1;
+    s.pieces = left && s.steps >= kCutSteps ? pairs / left : 1;
+    if (s.pieces > 1 && s.pieces > s.steps / kMinSteps) s.pieces = s.steps / kMinSteps;
     s.whole = s.pieces > 1 ? tiles - left : tiles;
     s.units = s.whole + (tiles - s.whole) * s.pieces;
     return s;
@@ -456,8 +485,7 @@ cudaError_t launch(const WeightGrad& w, void* workspace, cudaStream_t stream) {
         return e;
     const int64_t cut = (int64_t)p.s.tiles_n * p.s.tiles_k - p.s.whole;
     if (!cut) return cudaSuccess;
-    const int64_t blocks = cut * (kTile / 32) * (kTile / 32);
-    return launch_dependent(weight_grad_pieces_kernel<T>, (unsigned)(blocks / kPieceWarps), 32 * kPieceWarps, 0,
+    return launch_dependent(weight_grad_pieces_kernel<T>, (unsigned)(cut * (kTile / 32) * (kTile / 32)), 256, 0,
                             stream, p);
 }
 
