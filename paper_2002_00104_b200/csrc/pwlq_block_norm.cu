@@ -225,23 +225,34 @@ __global__ void __launch_bounds__(1024) block_norm_kernel(const __grid_constant_
     }
 }
 
-// Weights (or gates) of a thread's 32 bytes of columns, as binary32 pairs (plus `offset`).
-template <typename T>
-__device__ __forceinline__ void weights32(const void* p, bool f32, int64_t at, u64* w) {
-    constexpr int kP = kPairs32<T>;
-    if (sizeof(T) == 2 && f32) {
-        pairs32(load32(static_cast<const float*>(p) + at), w, 0.0f);
-        pairs32(load32(static_cast<const float*>(p) + at + 8), w + kP / 2, 0.0f);
-    } else {
-        pairs32(load32(static_cast<const T*>(p) + at), w, T());
+// Weights (or gates) of a thread's 32 bytes of columns: requested early, unpacked where they are used.
+// WF32: binary32 beside 16-bit values.
+template <typename T, bool WF32>
+struct Weights {
+    static constexpr bool kWide = WF32 && sizeof(T) == 2;
+    Raw32 raw[kWide ? 2 : 1];
+    __device__ __forceinline__ void load(const void* p, int64_t at) {
+        if (kWide) {
+            raw[0] = load32(static_cast<const float*>(p) + at);
+            raw[kWide ? 1 : 0] = load32(static_cast<const float*>(p) + at + 8);
+        } else {
+            raw[0] = load32(static_cast<const T*>(p) + at);
+        }
     }
-}
-template <typename T>
-__device__ __forceinline__ void weights32(const void* p, bool f32, int64_t at, float offset, u64* w) {
-    weights32<T>(p, f32, at, w);
+    __device__ __forceinline__ void get(u64* w) const {
+        if (kWide) {
+            pairs32(raw[0], w, 0.0f);
+            pairs32(raw[kWide ? 1 : 0], w + kPairs32<T> / 2, 0.0f);
+        } else {
+            pairs32(raw[0], w, T());
+        }
+    }
+    __device__ __forceinline__ void get(u64* w, float offset) const {
+        get(w);
 #pragma unroll
-    for (int k = 0; k < kPairs32<T>; ++k) w[k] = add2(w[k], both(offset));
-}
+        for (int k = 0; k < kPairs32<T>; ++k) w[k] = add2(w[k], both(offset));
+    }
+};
 
 // Bytes of a thread's 32 bytes of values, and the range of their group.
 template <typename T>
@@ -271,7 +282,7 @@ __device__ __forceinline__ void save32(const u64* v, const NormParams& q, bool l
 }
 
 // Forward with a ring: 32 bytes of columns per thread.
-template <typename T, bool SAVE>
+template <typename T, bool SAVE, bool WF32>
 __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(const __grid_constant__ NormParams q) {
     constexpr int kP = kPairs32<T>;
     __shared__ float buf[2][32];
@@ -300,6 +311,8 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
     const int c = live ? (int)threadIdx.x * 2 * kP : (int)q.a.cols - 2 * kP;
     for (int64_t row = blockIdx.x; row < q.a.rows; row += gridDim.x) {
         u64 r[kP], w[kP], s = 0ull;
+        Weights<T, WF32> wt;
+        if (post) wt.load(q.a.post_weight, c);
         const unsigned char* at = ring.wait() + c * (int)sizeof(T);
         pairs32(load32(at), r, T());
 #pragma unroll
@@ -310,17 +323,19 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
             if (post) {
 #pragma unroll
                 for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
-                weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
                 const float rstd_f = rsqrtf(fmaf(cta_sum(live ? sum8(s) : 0.0f), q.inv_cols, q.eps));
                 if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
                 if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+                wt.get(w, q.offset);
+                if (q.a.gate) wt.load(q.a.gate, gate * q.a.ldgate + c);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) f[k] = mul2(mul2(f[k], both(rstd_f)), w[k]);
-            } else if (SAVE && q.a.f_codes) {
-                save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+            } else {
+                if (q.a.gate) wt.load(q.a.gate, gate * q.a.ldgate + c);
+                if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
             }
             if (q.a.gate) {
-                weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, w);
+                wt.get(w);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) r[k] = fma2(f[k], w[k], r[k]);
                 gate += q.gate_step;
@@ -337,7 +352,7 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
         if (live && q.a.r) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
         float rstd_r = 0.0f;
         if (pre) {
-            weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
+            wt.load(q.a.pre_weight, c);
             rstd_r = rsqrtf(fmaf(cta_sum(live ? sum8(s) : 0.0f), q.inv_cols, q.eps));
         } else {
             __syncthreads();
@@ -349,6 +364,7 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
         if (SAVE && q.a.r_codes) save32<T>(r, q, live, row, c, q.a.r_codes, q.a.r_ranges);
         if (!pre) continue;
         if (SAVE && threadIdx.x == 0 && q.a.r_rstd) q.a.r_rstd[row] = rstd_r;
+        wt.get(w, q.offset);
 #pragma unroll
         for (int k = 0; k < kP; ++k) w[k] = mul2(mul2(r[k], both(rstd_r)), w[k]);
         if (live) store32(static_cast<T*>(q.a.h) + row * q.a.ldh + c, raw32(w, T()));
@@ -621,7 +637,7 @@ __device__ __forceinline__ void held32(const unsigned char* bytes, float m, floa
 }
 
 // Backward with a ring: 32 bytes of columns per thread, sums in registers.
-template <typename T>
+template <typename T, bool WF32>
 __global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 1024)
 block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     constexpr int kP = kPairs32<T>;
@@ -680,12 +696,16 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         const float mr = next_mr, mf = next_mf, rr = next_rr, rf = next_rf;
         if (row + 1 < last) fetch(row + 1);
         u64 e[kP], n[kP], w[kP];
+        Weights<T, WF32> wt, gt;
+        if (pre) wt.load(q.a.pre_weight, c);
         const unsigned char* at = ring.wait();
         // outer norm: e = dr + rstd * (u - n * mean(u n))
         if (pre) {
             pairs32(load32(at + at_dh), e, T());
             held32<T>(at + at_rb, mr, q.ratio, rr, n);
-            weights32<T>(q.a.pre_weight, q.wf32, c, q.offset, w);
+            wt.get(w, q.offset);
+            if (post) wt.load(q.a.post_weight, c);
+            if (q.a.gate) gt.load(q.a.gate, gate * q.a.ldgate + c);
             u64 s = 0ull;
 #pragma unroll
             for (int k = 0; k < kP; ++k) {
@@ -702,6 +722,8 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
                 for (int k = 0; k < kP; ++k) e[k] = add2(e[k], w[k]);
             }
         } else {                          // without the outer norm dr is all there is
+            if (post) wt.load(q.a.post_weight, c);
+            if (q.a.gate) gt.load(q.a.gate, gate * q.a.ldgate + c);
             pairs32(load32(at + at_dr), e, T());
         }
         if (p.g.dx && live) {
@@ -716,9 +738,9 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
             u64 s = 0ull;
             if (q.a.gate) {
                 u64 g[kP];
-                weights32<T>(q.a.gate, q.wf32, gate * q.a.ldgate + c, g);
+                gt.get(g);
                 if (post) {
-                    weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
+                    wt.get(w, q.offset);
 #pragma unroll
                     for (int k = 0; k < kP; ++k) {
                         const u64 en = mul2(e[k], n[k]);
@@ -735,7 +757,7 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
                     }
                 }
             } else {                      // f was kept for its norm
-                weights32<T>(q.a.post_weight, q.wf32, c, q.offset, w);
+                wt.get(w, q.offset);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) {
                     dpost[k] = fma2(e[k], n[k], dpost[k]);
@@ -887,8 +909,8 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
             q.gate_step = resident / a.gate_tokens;
             q.gate_rest = resident % a.gate_tokens;
         }
-        return run(block_norm_ring_kernel<T, SAVE>, (unsigned)resident, ring.threads,
-                   (size_t)ring.stages * (a.f ? 2 : 1) * q.row_bytes, stream, q);
+        return run(q.wf32 ? block_norm_ring_kernel<T, SAVE, true> : block_norm_ring_kernel<T, SAVE, kSize == 4>,
+                   (unsigned)resident, ring.threads, (size_t)ring.stages * (a.f ? 2 : 1) * q.row_bytes, stream, q);
     }
     const bool vec = rows_aligned(a.x, a.ldx, kSize) && rows_aligned(a.f, a.ldf, kSize) &&
                      rows_aligned(a.r, a.ldr, kSize) && rows_aligned(a.h, a.ldh, kSize) && weights_aligned(a);
@@ -931,7 +953,8 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
         rows_aligned32(g.dh, g.lddh, kSize) && rows_aligned32(g.dr, g.lddr, kSize) &&
         rows_aligned32(g.dx, g.lddx, kSize) && rows_aligned32(g.df, g.lddf, kSize) && weights_aligned(a)) {
         p.q.stages = ring.stages;
-        return run(block_norm_backward_ring_kernel<T>, ctas, ring.threads, ring.stages * stage, stream, p);
+        return run(p.q.wf32 ? block_norm_backward_ring_kernel<T, true> : block_norm_backward_ring_kernel<T, kSize == 4>,
+                   ctas, ring.threads, ring.stages * stage, stream, p);
     }
     return vec ? run(block_norm_backward_kernel<T, 1, true, false>, ctas, threads_for(a.cols, 8), 0, stream, p)
                : run(block_norm_backward_kernel<T, 1, false, false>, ctas, threads_for(a.cols, 8), 0, stream, p);
