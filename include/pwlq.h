@@ -447,7 +447,7 @@ size_t pwlq_search_noalloc_max_bytes(void);
  *     inv2 = (1/d) * L  (0 where p resp. d is not positive), one rounding per operation,
  * and a, tail, q and v follow by the sequence at the top of this file (constants by products, since
  * a group is short; a level can differ from pwlq_quantize's where (a - z) * inv is at a tie within
- * the rounding of inv).  byte = sign << 7 | region << 6 | q.
+ * the rounding of inv).  byte = sign << 7 | region << 6 | q, sign = x's sign bit.
  * A group with m = 0 or NaN has bytes 0; it decodes to +0 resp. to NaN.
  *   codes   [rows, ldc] bytes, ldc >= cols and a multiple of 16, 16-byte aligned.  Bytes between
  *           cols and the next multiple of 16 are written as 0, the rest is not touched

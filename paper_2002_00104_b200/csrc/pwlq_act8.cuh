@@ -291,7 +291,7 @@ __device__ __forceinline__ PieceParams act8_params_paired(float m, float ratio) 
 // Eight bytes of eight values of a group with range m; P = act8_params(m).  Both pieces' levels are
 // formed and one is taken: adding 1.5 * 2^23 (+ 64 in the tail) rounds the product to an integer,
 // ties to even, and leaves region * 64 + level in the low byte of the sum.  No clamp is needed: a
-// product exceeds 63 by its own rounding at most.  x + 0 makes -0 a +0, whose sign bit is clear.
+// product exceeds 63 by its own rounding at most.
 __device__ __forceinline__ uint2 act8_bytes8(const float* x, float m, const PieceParams& P) {
     uint32_t w[2];
 #pragma unroll
@@ -299,8 +299,8 @@ __device__ __forceinline__ uint2 act8_bytes8(const float* x, float m, const Piec
         uint32_t r[4], s[4];
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
-            float y[2], c[2], t[2];
-            unpack2(add2(pack2(x[4 * h + i], x[4 * h + i + 1]), 0ull), y[0], y[1]);
+            const float* y = x + 4 * h + i;
+            float c[2], t[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 c[k] = __fmul_rn(fabsf(y[k]), P.inv1);

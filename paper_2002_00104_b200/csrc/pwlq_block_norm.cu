@@ -33,13 +33,16 @@ constexpr int kMaxStages = 8;
 struct CtaSum {
     float (*buf)[32];
     int half = 0;
-    __device__ __forceinline__ float operator()(float v) {
-        const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    // post() hands a thread's part in, total() waits for the others'; what does not need the sum goes
+    // in between.
+    __device__ __forceinline__ void post(float v) {
         for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (warps == 1) { __syncwarp(); return v; }
-        if (lane == 0) buf[half][warp] = v;
+        if ((threadIdx.x & 31) == 0) buf[half][threadIdx.x >> 5] = v;
+    }
+    __device__ __forceinline__ float total() {
+        const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
         __syncthreads();
-        v = lane < warps ? buf[half][lane] : 0.0f;
+        float v = lane < warps ? buf[half][lane] : 0.0f;
         if (warps > 8) {
             v += __shfl_xor_sync(0xffffffffu, v, 16);
             v += __shfl_xor_sync(0xffffffffu, v, 8);
@@ -49,6 +52,10 @@ struct CtaSum {
         v += __shfl_xor_sync(0xffffffffu, v, 1);
         half ^= 1;
         return __shfl_sync(0xffffffffu, v, 0);
+    }
+    __device__ __forceinline__ float operator()(float v) {
+        post(v);
+        return total();
     }
 };
 __device__ __forceinline__ float sum8(u64 s) { return lo2(s) + hi2(s); }
@@ -323,9 +330,10 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
             if (post) {
 #pragma unroll
                 for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
-                const float rstd_f = rsqrtf(fmaf(cta_sum(live ? sum8(s) : 0.0f), q.inv_cols, q.eps));
-                if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
+                cta_sum.post(live ? sum8(s) : 0.0f);
                 if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+                const float rstd_f = rsqrtf(fmaf(cta_sum.total(), q.inv_cols, q.eps));
+                if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
                 wt.get(w, q.offset);
                 if (q.a.gate) wt.load(q.a.gate, gate * q.a.ldgate + c);
 #pragma unroll
@@ -349,19 +357,19 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
         s = 0ull;
 #pragma unroll
         for (int k = 0; k < kP; ++k) s = fma2(r[k], r[k], s);
-        if (live && q.a.r) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
-        float rstd_r = 0.0f;
         if (pre) {
+            cta_sum.post(live ? sum8(s) : 0.0f);
             wt.load(q.a.pre_weight, c);
-            rstd_r = rsqrtf(fmaf(cta_sum(live ? sum8(s) : 0.0f), q.inv_cols, q.eps));
-        } else {
-            __syncthreads();
         }
+        if (live && q.a.r) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
+        if (SAVE && q.a.r_codes) save32<T>(r, q, live, row, c, q.a.r_codes, q.a.r_ranges);
+        float rstd_r = 0.0f;
+        if (pre) rstd_r = rsqrtf(fmaf(cta_sum.total(), q.inv_cols, q.eps));
+        else __syncthreads();
         // every thread has its values of this stage
         const int64_t ahead = row + (int64_t)q.stages * gridDim.x;
         if (threadIdx.x == 0 && ahead < q.a.rows && !ring.dead) request_forward<T>(q, ring, ring.stage, ahead);
         ring.next();
-        if (SAVE && q.a.r_codes) save32<T>(r, q, live, row, c, q.a.r_codes, q.a.r_ranges);
         if (!pre) continue;
         if (SAVE && threadIdx.x == 0 && q.a.r_rstd) q.a.r_rstd[row] = rstd_r;
         wt.get(w, q.offset);
@@ -372,25 +380,27 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
 }
 
 // Backward.  CTA b owns the rows [b * rows_per_cta, ...) and its columns' sums over them; the sums
-// go to the workspace once per CTA (those of the gate also where the gate changes) and a second
-// kernel adds them in a fixed order.  The sums live in registers up to 8192 columns (24 per
-// thread); wider rows, whose sums alone would take three quarters of the register file, keep them
-// in shared memory (WIDE), where every thread touches its own columns only.
-// Workspace: [ctas][cols] of dpre, [ctas][cols] of dpost, [ctas + gate_rows][cols] of dgate, whose
-// slot b + g holds CTA b's share of gate g (every CTA and every gate moves on by at least one).
+// go to the workspace and a second kernel adds them in a fixed order.  Within the rows of one gate g,
+// the gate and the weight w are the same in every row, so one sum A = sum of e * n serves both
+// gradients: dgate_g = w * A_g and dpost = sum over the gates of g * A_g.  A goes out where the gate
+// changes and at the CTA's end.  The sums live in registers up to 8192 columns (16 per thread and
+// chunk); wider rows keep them in shared memory (WIDE), where every thread touches its own columns
+// only.
+// Workspace: [ctas][cols] of dpre, [ctas + gate_rows][cols] of A, whose slot b + g holds CTA b's share
+// of gate g (every CTA and every gate moves on by at least one).
 struct GradParams {
     NormParams q;
     pwlq_block_norm_grads g;
     int64_t rows_per_cta;
-    float *dpre, *dpost, *dgate;          // workspace; nullptr: not wanted
+    float *dpre, *inner;                  // workspace; nullptr: not wanted
 };
 
-enum { kDpre, kDpost, kDgate };
+enum { kDpre, kInner };
 
 template <int VC, bool WIDE>
 struct ColumnSums {
-    u64 reg[3][WIDE ? 1 : VC][4] = {};
-    ulonglong2* smem = nullptr;           // [3][VC][2][blockDim.x]
+    u64 reg[2][WIDE ? 1 : VC][4] = {};
+    ulonglong2* smem = nullptr;           // [2][VC][2][blockDim.x]
     __device__ __forceinline__ ulonglong2* at(int which, int i) const {
         return smem + ((which * VC + i) * 2) * blockDim.x + threadIdx.x;
     }
@@ -478,7 +488,7 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
     ColumnSums<VC, WIDE> sums;
     if (WIDE) {
         sums.smem = reinterpret_cast<ulonglong2*>(smem);
-        for (int which = 0; which < 3; ++which) sums.clear(which);
+        for (int which = 0; which < 2; ++which) sums.clear(which);
     }
     int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
@@ -503,8 +513,8 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
 
     for (int64_t row = first; row < last; ++row) {
         if (q.a.gate && row == gate_end) {
-            if (p.dgate) sums.template put<VEC>(kDgate, p.dgate + (blockIdx.x + gate) * cols, cols);
-            sums.clear(kDgate);
+            if (p.inner) sums.template put<VEC>(kInner, p.inner + (blockIdx.x + gate) * cols, cols);
+            sums.clear(kInner);
             ++gate;
             gate_end += q.a.gate_tokens;
         }
@@ -572,37 +582,23 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
             if (!has_f) continue;
             // inner norm and gate; e becomes v = e * gate * w
             act8_scaled8(bytes8(fb, c, valid), act8_lines(now_f[i], q.ratio, factor_f), n[i]);
-            u64 d[4], eg[4];
+            u64 d[4];
+            sums.get(kInner, i, d);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) eg[k] = e[i][k];
+            for (int k = 0; k < 4; ++k) d[k] = fma2(e[i][k], n[i][k], d[k]);
+            sums.set(kInner, i, d);
             if (q.a.gate) {
-                u64 gw[4];
-                weights8<VEC, T>(q.a.gate, q.wf32, gate * q.a.ldgate, c, valid, 0.0f, gw);
+                weights8<VEC, T>(q.a.gate, q.wf32, gate * q.a.ldgate, c, valid, 0.0f, w);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) eg[k] = mul2(e[i][k], gw[k]);
+                for (int k = 0; k < 4; ++k) e[i][k] = mul2(e[i][k], w[k]);
             }
             if (post) {
-                sums.get(kDpost, i, d);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) d[k] = fma2(eg[k], n[i][k], d[k]);
-                sums.set(kDpost, i, d);
                 weights8<VEC, T>(q.a.post_weight, q.wf32, 0, c, valid, q.offset, w);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     e[i][k] = mul2(e[i][k], w[k]);
-                    eg[k] = mul2(eg[k], w[k]);
+                    s = fma2(e[i][k], n[i][k], s);
                 }
-            }
-            if (q.a.gate) {
-                sums.get(kDgate, i, d);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) d[k] = fma2(e[i][k], n[i][k], d[k]);
-                sums.set(kDgate, i, d);
-            }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                e[i][k] = eg[k];
-                s = fma2(eg[k], n[i][k], s);
             }
         }
         float mean = 0.0f;
@@ -619,8 +615,7 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
         }
     }
     if (p.dpre) sums.template put<VEC>(kDpre, p.dpre + (int64_t)blockIdx.x * cols, cols);
-    if (p.dpost) sums.template put<VEC>(kDpost, p.dpost + (int64_t)blockIdx.x * cols, cols);
-    if (p.dgate) sums.template put<VEC>(kDgate, p.dgate + (blockIdx.x + gate) * cols, cols);
+    if (p.inner) sums.template put<VEC>(kInner, p.inner + (blockIdx.x + gate) * cols, cols);
 }
 
 // A thread's 32 bytes of columns times `factor`, from its bytes.
@@ -638,7 +633,7 @@ __device__ __forceinline__ void held32(const unsigned char* bytes, float m, floa
 
 // Backward with a ring: 32 bytes of columns per thread, sums in registers.
 template <typename T, bool WF32>
-__global__ void __launch_bounds__(sizeof(T) == 2 ? 512 : 1024)
+__global__ void __launch_bounds__(512)
 block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     constexpr int kP = kPairs32<T>;
     __shared__ float buf[2][32];
@@ -667,7 +662,8 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
                    at_fb = ring.stage_bytes - q.code_bytes + c;
     int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
-    u64 dpre[kP] = {}, dpost[kP] = {}, dgate[kP] = {};
+    u64 dpre[kP] = {}, inner[kP] = {};
+    allow_dependents();
     auto put = [&](const u64* v, float* to) {
         if (!live) return;
 #pragma unroll
@@ -687,9 +683,9 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
 
     for (int64_t row = first; row < last; ++row) {
         if (q.a.gate && row == gate_end) {
-            if (p.dgate) put(dgate, p.dgate + (blockIdx.x + gate) * q.a.cols);
+            if (p.inner) put(inner, p.inner + (blockIdx.x + gate) * q.a.cols);
 #pragma unroll
-            for (int k = 0; k < kP; ++k) dgate[k] = 0ull;
+            for (int k = 0; k < kP; ++k) inner[k] = 0ull;
             ++gate;
             gate_end += q.a.gate_tokens;
         }
@@ -713,11 +709,14 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
                 e[k] = mul2(e[k], w[k]);
                 s = fma2(e[k], n[k], s);
             }
-            const float mean = cta_sum(live ? sum8(s) : 0.0f) * q.inv_cols;
+            cta_sum.post(live ? sum8(s) : 0.0f);
+            Raw32 raw_dr;
+            if (has_dr) raw_dr = load32(at + at_dr);
+            const float mean = cta_sum.total() * q.inv_cols;
 #pragma unroll
             for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rr));
             if (has_dr) {
-                pairs32(load32(at + at_dr), w, T());
+                pairs32(raw_dr, w, T());
 #pragma unroll
                 for (int k = 0; k < kP; ++k) e[k] = add2(e[k], w[k]);
             }
@@ -735,32 +734,18 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         float mean = 0.0f;
         if (has_f) {
             held32<T>(at + at_fb, mf, q.ratio, rf, n);
-            u64 s = 0ull;
+#pragma unroll
+            for (int k = 0; k < kP; ++k) inner[k] = fma2(e[k], n[k], inner[k]);
             if (q.a.gate) {
-                u64 g[kP];
-                gt.get(g);
-                if (post) {
-                    wt.get(w, q.offset);
+                gt.get(w);
 #pragma unroll
-                    for (int k = 0; k < kP; ++k) {
-                        const u64 en = mul2(e[k], n[k]);
-                        dpost[k] = fma2(en, g[k], dpost[k]);
-                        dgate[k] = fma2(en, w[k], dgate[k]);
-                        e[k] = mul2(e[k], mul2(g[k], w[k]));
-                        s = fma2(e[k], n[k], s);
-                    }
-                } else {
-#pragma unroll
-                    for (int k = 0; k < kP; ++k) {
-                        dgate[k] = fma2(e[k], n[k], dgate[k]);
-                        e[k] = mul2(e[k], g[k]);
-                    }
-                }
-            } else {                      // f was kept for its norm
+                for (int k = 0; k < kP; ++k) e[k] = mul2(e[k], w[k]);
+            }
+            u64 s = 0ull;
+            if (post) {
                 wt.get(w, q.offset);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) {
-                    dpost[k] = fma2(e[k], n[k], dpost[k]);
                     e[k] = mul2(e[k], w[k]);
                     s = fma2(e[k], n[k], s);
                 }
@@ -779,44 +764,100 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(e, T()));
     }
     if (p.dpre) put(dpre, p.dpre + (int64_t)blockIdx.x * q.a.cols);
-    if (p.dpost) put(dpost, p.dpost + (int64_t)blockIdx.x * q.a.cols);
-    if (p.dgate) put(dgate, p.dgate + (blockIdx.x + gate) * q.a.cols);
+    if (p.inner) put(inner, p.inner + (blockIdx.x + gate) * q.a.cols);
 }
 
-// Adds the CTAs' sums of one column per thread: sixteen parts of the CTAs side by side, then the
-// parts.  blockIdx.y: 0 dpre, 1 dpost, 2 + g gate g.
-constexpr int kSumCols = 32, kSumParts = 16;
-template <typename W>
-__global__ void __launch_bounds__(kSumCols * kSumParts)
-block_norm_sums_kernel(const __grid_constant__ GradParams p, int64_t ctas, W* dpre, W* dpost, W* dgate) {
-    __shared__ float part[kSumParts][kSumCols];
-    const int cols = (int)p.q.a.cols;
-    const int c = blockIdx.x * kSumCols + threadIdx.x;
-    for (int64_t which = blockIdx.y; which < 2 + (dgate ? p.q.a.gate_rows : 0); which += gridDim.y) {
+// Adds the CTAs' sums of V columns per thread (4 where the columns allow it): 64 parts of the CTAs side
+// by side, eight loads of a part in flight, then the parts.  blockIdx.y: 0 dpre, 1 dpost, 2 + g gate g.
+constexpr int kSumLanes = 8, kSumParts = 64;
+template <int V> struct alignas(4 * V) Columns { float v[V]; };
+template <typename W, int V>
+__device__ __forceinline__ void gate_columns(const W* gate, float* w) {
+    struct alignas(V * sizeof(W)) Vec { W v[V]; };
+    if (((uintptr_t)gate & (V * sizeof(W) - 1)) == 0) {
+        const Vec x = *reinterpret_cast<const Vec*>(gate);
+#pragma unroll
+        for (int k = 0; k < V; ++k) w[k] = to_f32(x.v[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) w[k] = to_f32(gate[k]);
+    }
+}
+template <typename W, int V>
+__global__ void __launch_bounds__(kSumLanes * kSumParts)
+block_norm_sums_kernel(const __grid_constant__ GradParams p, int ctas, W* dpre, W* dpost, W* dgate) {
+    __shared__ Columns<V> part[kSumParts][kSumLanes];
+    const pwlq_block_norm_args& a = p.q.a;
+    const int cols = (int)a.cols;
+    const int c = (blockIdx.x * kSumLanes + threadIdx.x) * V;
+    const W* const gates = static_cast<const W*>(a.gate);
+    const W* const post = static_cast<const W*>(a.post_weight);
+    // rows and their quotients fit 32 bits
+    const unsigned rows = (unsigned)a.rows, per_cta = (unsigned)p.rows_per_cta;
+    const unsigned every = (unsigned)min(a.gate_tokens, (int64_t)0x7fffffff);
+    await_previous();
+    for (int64_t which = blockIdx.y; which < 2 + (dgate ? a.gate_rows : 0); which += gridDim.y) {
         W* out = which == 0 ? dpre : which == 1 ? dpost : dgate + (which - 2) * cols;
         if (which < 2 && !out) continue;
-        const float* src = which == 0 ? p.dpre : which == 1 ? p.dpost : p.dgate;
-        int64_t lo = 0, hi = ctas;
-        if (which >= 2) {
-            const int64_t g = which - 2, r0 = g * p.q.a.gate_tokens;
-            const int64_t r1 = min(r0 + p.q.a.gate_tokens, p.q.a.rows);
-            lo = r0 / p.rows_per_cta;
-            hi = r1 > r0 ? (r1 - 1) / p.rows_per_cta + 1 : lo;
-            src += g * cols;                       // slot of CTA b: b + g
-        }
-        float s = 0.0f;
-        if (c < cols) {
+        const float* src = (which == 0 ? p.dpre : p.inner) + c;
+        Columns<V> s = {};
+        if (c < cols && which == 1 && gates) {
+            // dpost: every slot times its gate; a CTA's first gate, then those that it went on to
+#pragma unroll 4
+            for (int b = threadIdx.y; b < ctas; b += kSumParts) {
+                const unsigned g = b * per_cta / every;
+                const Columns<V> x = *reinterpret_cast<const Columns<V>*>(src + (int64_t)(b + g) * cols);
+                float w[V];
+                gate_columns<W, V>(gates + (int64_t)g * a.ldgate + c, w);
+#pragma unroll
+                for (int k = 0; k < V; ++k) s.v[k] = fmaf(x.v[k], w[k], s.v[k]);
+            }
+            for (int b = threadIdx.y; b < ctas; b += kSumParts) {
+                const unsigned last = (min(b * per_cta + per_cta, rows) - 1) / every;
+                for (unsigned g = b * per_cta / every + 1; g <= last; ++g) {
+                    const Columns<V> x = *reinterpret_cast<const Columns<V>*>(src + (int64_t)(b + g) * cols);
+                    float w[V];
+                    gate_columns<W, V>(gates + (int64_t)g * a.ldgate + c, w);
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s.v[k] = fmaf(x.v[k], w[k], s.v[k]);
+                }
+            }
+        } else if (c < cols) {
+            int lo = 0, hi = ctas;
+            if (which >= 2) {
+                const int64_t g = which - 2, r0 = g * a.gate_tokens, r1 = min(r0 + a.gate_tokens, a.rows);
+                lo = (int)min(r0 / p.rows_per_cta, (int64_t)ctas);
+                hi = r1 > r0 ? (int)((r1 - 1) / p.rows_per_cta) + 1 : lo;
+                src += g * cols;                       // slot of CTA b: b + g
+            }
 #pragma unroll 8
-            for (int64_t b = lo + threadIdx.y; b < hi; b += kSumParts) s += src[b * cols + c];
+            for (int b = lo + threadIdx.y; b < hi; b += kSumParts) {
+                const Columns<V> x = *reinterpret_cast<const Columns<V>*>(src + (int64_t)b * cols);
+#pragma unroll
+                for (int k = 0; k < V; ++k) s.v[k] += x.v[k];
+            }
         }
         part[threadIdx.y][threadIdx.x] = s;
         __syncthreads();
+        // eight parts each, then the eight
+#pragma unroll
+        for (int step = 1; step < kSumParts; step *= 8) {
+            if (threadIdx.y % (8 * step) == 0) {
+#pragma unroll
+                for (int j = 1; j < 8; ++j)
+#pragma unroll
+                    for (int k = 0; k < V; ++k) s.v[k] += part[threadIdx.y + j * step][threadIdx.x].v[k];
+                part[threadIdx.y][threadIdx.x] = s;
+            }
+            __syncthreads();
+        }
         if (threadIdx.y == 0 && c < cols) {
 #pragma unroll
-            for (int k = 1; k < kSumParts; ++k) s += part[k][threadIdx.x];
-            out[c] = from_f32<W>(s);
+            for (int k = 0; k < V; ++k) {
+                const float w = which >= 2 && post ? to_f32(post[c + k]) + p.q.offset : 1.0f;
+                out[c + k] = from_f32<W>(s.v[k] * w);
+            }
         }
-        __syncthreads();
     }
 }
 
@@ -942,14 +983,14 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
                      a.cols % 4 == 0 && weights_aligned(a);
     if (a.cols > 8192) {
         const int threads = threads_for(a.cols, 32);
-        const size_t sums = (size_t)3 * 4 * 8 * sizeof(float) * threads;          // at most 192 KB
+        const size_t sums = (size_t)2 * 4 * 8 * sizeof(float) * threads;          // at most 128 KB
         return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, sums, stream, p)
                    : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, sums, stream, p);
     }
     const size_t stage = (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (g.dr ? p.q.row_bytes : 0) +
                          (a.f_codes ? p.q.code_bytes : 0);
-    const RingPlan ring = ring_plan(a.cols, kSize, kSize == 2 ? 512 : 1024, stage);
-    if (a.cols <= kRingCols && a.cols % (32 / kSize) == 0 && ring.stages >= 2 && (a.pre_weight || g.dr) &&
+    const RingPlan ring = ring_plan(a.cols, kSize, 512, stage);
+    if (ring.threads <= 512 && a.cols % (32 / kSize) == 0 && ring.stages >= 2 && (a.pre_weight || g.dr) &&
         rows_aligned32(g.dh, g.lddh, kSize) && rows_aligned32(g.dr, g.lddr, kSize) &&
         rows_aligned32(g.dx, g.lddx, kSize) && rows_aligned32(g.df, g.lddf, kSize) && weights_aligned(a)) {
         p.q.stages = ring.stages;
@@ -959,14 +1000,17 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
     return vec ? run(block_norm_backward_kernel<T, 1, true, false>, ctas, threads_for(a.cols, 8), 0, stream, p)
                : run(block_norm_backward_kernel<T, 1, false, false>, ctas, threads_for(a.cols, 8), 0, stream, p);
 }
+template <typename W, int V>
+cudaError_t sums(const GradParams& p, int64_t ctas, cudaStream_t stream) {
+    const int64_t kinds = 2 + (p.g.dgate ? p.q.a.gate_rows : 0);
+    const dim3 grid((unsigned)((p.q.a.cols + kSumLanes * V - 1) / (kSumLanes * V)),
+                    (unsigned)(kinds < 65535 ? kinds : 65535));
+    return launch_dependent(block_norm_sums_kernel<W, V>, grid, dim3(kSumLanes, kSumParts), 0, stream, p, (int)ctas,
+                            static_cast<W*>(p.g.dpre), static_cast<W*>(p.g.dpost), static_cast<W*>(p.g.dgate));
+}
 template <typename W>
 cudaError_t sums(const GradParams& p, int64_t ctas, cudaStream_t stream) {
-    const int64_t kinds = 2 + (p.dgate ? p.q.a.gate_rows : 0);
-    const dim3 grid((unsigned)((p.q.a.cols + kSumCols - 1) / kSumCols),
-                    (unsigned)(kinds < 65535 ? kinds : 65535));
-    block_norm_sums_kernel<W><<<grid, dim3(kSumCols, kSumParts), 0, stream>>>(
-        p, ctas, static_cast<W*>(p.g.dpre), static_cast<W*>(p.g.dpost), static_cast<W*>(p.g.dgate));
-    return cudaGetLastError();
+    return p.q.a.cols % 4 == 0 ? sums<W, 4>(p, ctas, stream) : sums<W, 1>(p, ctas, stream);
 }
 template <typename T>
 cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads& g, cudaStream_t stream) {
@@ -979,8 +1023,7 @@ cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
     ctas = (a.rows + p.rows_per_cta - 1) / p.rows_per_cta;
     float* ws = static_cast<float*>(g.workspace);
     p.dpre = g.dpre ? ws : nullptr;
-    p.dpost = g.dpost ? ws + ctas * a.cols : nullptr;
-    p.dgate = g.dgate ? ws + 2 * ctas * a.cols : nullptr;
+    p.inner = g.dpost || g.dgate ? ws + ctas * a.cols : nullptr;
     if (ctas)
         if (const cudaError_t e = backward_rows<T>(p, (unsigned)ctas, stream)) return e;
     if (!g.dpre && !g.dpost && !g.dgate) return cudaSuccess;
@@ -997,7 +1040,7 @@ cudaError_t launch_block_norm(const pwlq_block_norm_args& a, cudaStream_t stream
 
 size_t block_norm_backward_workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
     const int64_t ctas = backward_ctas(rows, cols);
-    return (size_t)(3 * ctas + gate_rows) * (size_t)cols * sizeof(float);
+    return (size_t)(2 * ctas + gate_rows) * (size_t)cols * sizeof(float);
 }
 
 cudaError_t launch_block_norm_backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads& g,

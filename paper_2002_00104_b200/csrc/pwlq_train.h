@@ -30,6 +30,24 @@ inline bool rows_aligned(const void* p, int64_t ld, size_t size) {
     return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)size)) & 15) == 0;
 }
 
+// Launches a kernel that may begin while the one before it in the stream still runs (it waits for that
+// one's end itself, await_previous).
+template <typename... P, typename... A>
+cudaError_t launch_dependent(void (*kernel)(P...), dim3 blocks, dim3 threads, size_t smem, cudaStream_t stream,
+                             const A&... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = blocks;
+    config.blockDim = threads;
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = &attr;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
+}
+
 cudaError_t launch_act8_encode(const void* x, int dtype, int64_t ldx, const Act8Tensor& a,
                                cudaStream_t stream);
 cudaError_t launch_act8_decode(const Act8Tensor& a, void* y, int dtype, int64_t ldy,

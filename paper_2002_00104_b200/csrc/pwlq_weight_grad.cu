@@ -385,24 +385,6 @@ inline size_t piece_bytes(int64_t rows, int64_t outputs, int64_t cols) {
     return (size_t)(s.units - s.whole) * kTile * kTile * sizeof(float);
 }
 
-// Launches a kernel that may begin while the one before it in the stream still runs (it waits for that
-// one's end itself).
-template <typename... P, typename... A>
-cudaError_t launch_dependent(void (*kernel)(P...), unsigned blocks, int threads, size_t smem, cudaStream_t stream,
-                             const A&... args) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t config = {};
-    config.gridDim = dim3(blocks);
-    config.blockDim = dim3((unsigned)threads);
-    config.dynamicSmemBytes = smem;
-    config.stream = stream;
-    config.attrs = &attr;
-    config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, kernel, args...);
-}
-
 // cuTensorMapEncodeTiled, through the runtime: the library does not link the driver.
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -480,12 +462,12 @@ cudaError_t launch(const WeightGrad& w, void* workspace, cudaStream_t stream) {
                                              (int)kSmemBytes))
         return e;
     const int64_t ctas = 2 * (p.s.units < pairs ? p.s.units : pairs);
-    if (cudaError_t e = launch_dependent(weight_grad_kernel<T>, (unsigned)ctas, kThreads, kSmemBytes, stream, map,
+    if (cudaError_t e = launch_dependent(weight_grad_kernel<T>, dim3((unsigned)ctas), dim3(kThreads), kSmemBytes, stream, map,
                                          xmap, p))
         return e;
     const int64_t cut = (int64_t)p.s.tiles_n * p.s.tiles_k - p.s.whole;
     if (!cut) return cudaSuccess;
-    return launch_dependent(weight_grad_pieces_kernel<T>, (unsigned)(cut * (kTile / 32) * (kTile / 32)), 256, 0,
+    return launch_dependent(weight_grad_pieces_kernel<T>, dim3((unsigned)(cut * (kTile / 32) * (kTile / 32))), dim3(256), 0,
                             stream, p);
 }
 
