@@ -78,6 +78,13 @@ __device__ __forceinline__ void store_pairs(const u64* v, T* p, int valid) {
     store8<VEC>(f, p, valid);
 }
 
+// Eight values of one thread, not of a warp that works together.
+template <bool VEC, typename T>
+__device__ __forceinline__ void put8(const float* v, T* p, int valid) {
+    if (VEC) store8<true>(v, p, valid);
+    else store8_each(v, p, valid);
+}
+
 // Eight weights (or gates) from column c on, as binary32, plus `offset`.
 template <bool VEC, typename T>
 __device__ __forceinline__ void weights8(const void* p, bool f32, int64_t at, int c, int valid, float offset,
@@ -382,18 +389,61 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
 // Backward.  CTA b owns the rows [b * rows_per_cta, ...) and its columns' sums over them; the sums
 // go to the workspace and a second kernel adds them in a fixed order.  Within the rows of one gate g,
 // the gate and the weight w are the same in every row, so one sum A = sum of e * n serves both
-// gradients: dgate_g = w * A_g and dpost = sum over the gates of g * A_g.  A goes out where the gate
-// changes and at the CTA's end.  The sums live in registers up to 8192 columns (16 per thread and
-// chunk); wider rows keep them in shared memory (WIDE), where every thread touches its own columns
-// only.
-// Workspace: [ctas][cols] of dpre, [ctas + gate_rows][cols] of A, whose slot b + g holds CTA b's share
-// of gate g (every CTA and every gate moves on by at least one).
+// gradients: dgate_g = w * A_g and dpost = sum over the gates of g * A_g.  Where the gate changes, and
+// at the CTA's end, A is turned into them: dgate_g goes out at once if all its rows are this CTA's
+// (a gate per token, say), dpost gathers in shared memory.  The running sums live in registers up to
+// 8192 columns (16 per thread and chunk); wider rows keep them in shared memory too (WIDE), where
+// every thread touches its own columns only.
+// Workspace: [ctas][cols] of dpre, [ctas][cols] of dpost, [2 * ctas][cols] of dgate: CTA b's share of
+// the gate of its first row, and of its last one if that is another.
 struct GradParams {
     NormParams q;
     pwlq_block_norm_grads g;
     int64_t rows_per_cta;
-    float *dpre, *inner;                  // workspace; nullptr: not wanted
+    float *dpre, *dpost, *dgate;          // workspace; nullptr: not wanted
+    unsigned gathered;                    // where dpost gathers in shared memory (with a gate)
 };
+
+// What a CTA does with A of eight columns from c on (the first `valid` of which exist) once it is past
+// the rows of `gate`.
+template <bool VEC, typename T>
+__device__ __forceinline__ void finish_gate(const GradParams& p, int64_t gate, int64_t first, int64_t last, int c,
+                                            int valid, const u64* A, float* gathered) {
+    const pwlq_block_norm_args& a = p.q.a;
+    if (valid <= 0) return;
+    u64 w[4], v[4];
+    float f[8];
+    if (p.dgate) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = A[k];
+        if (a.post_weight) {
+            weights8<VEC, T>(a.post_weight, p.q.wf32, 0, c, valid, p.q.offset, w);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], w[k]);
+        }
+        floats8(v, f);
+        const int64_t from = gate * a.gate_tokens, to = min(from + a.gate_tokens, a.rows);
+        if (from < first || to > last) {
+            const int64_t slot = 2 * (int64_t)blockIdx.x + (from > first);
+            put8<VEC>(f, p.dgate + slot * a.cols + c, valid);
+        } else if (p.q.wf32) {
+            put8<VEC>(f, static_cast<float*>(p.g.dgate) + gate * a.cols + c, valid);
+        } else {
+            put8<VEC>(f, static_cast<T*>(p.g.dgate) + gate * a.cols + c, valid);
+        }
+    }
+    if (p.dpost) {
+        weights8<VEC, T>(a.gate, p.q.wf32, gate * a.ldgate, c, valid, 0.0f, w);
+        ulonglong2* at = reinterpret_cast<ulonglong2*>(gathered + c);
+        ulonglong2 x = at[0], y = at[1];
+        x.x = fma2(A[0], w[0], x.x);
+        x.y = fma2(A[1], w[1], x.y);
+        y.x = fma2(A[2], w[2], y.x);
+        y.y = fma2(A[3], w[3], y.y);
+        at[0] = x;
+        at[1] = y;
+    }
+}
 
 enum { kDpre, kInner };
 
@@ -436,11 +486,20 @@ struct ColumnSums {
             get(which, i, v);
             float f[8];
             floats8(v, f);
-            if (VEC) store8<true>(f, to + c, cols - c);
-            else store8_each(f, to + c, cols - c);       // once per CTA or gate
+            put8<VEC>(f, to + c, cols - c);
         }
     }
 };
+
+// The columns of `gathered` that a thread looks after.
+template <int VC>
+__device__ __forceinline__ void clear_gathered(float* gathered) {
+#pragma unroll
+    for (int i = 0; i < VC; ++i) {
+        float4* at = reinterpret_cast<float4*>(gathered + (threadIdx.x + i * blockDim.x) * 8);
+        at[0] = at[1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+}
 
 template <typename T>
 __device__ __forceinline__ void request_backward(const GradParams& p, Ring& ring, int stage, int64_t row) {
@@ -490,6 +549,19 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
         sums.smem = reinterpret_cast<ulonglong2*>(smem);
         for (int which = 0; which < 2; ++which) sums.clear(which);
     }
+    float* const gathered = reinterpret_cast<float*>(smem + p.gathered);
+    const bool gates = q.a.gate && (p.dpost || p.dgate);
+    if (gates && p.dpost) clear_gathered<VC>(gathered);
+    auto finish = [&](int64_t gate) {
+#pragma unroll
+        for (int i = 0; i < VC; ++i) {
+            const int c = (threadIdx.x + i * blockDim.x) * 8;
+            u64 A[4];
+            sums.get(kInner, i, A);
+            finish_gate<VEC, T>(p, gate, first, last, c, cols - c, A, gathered);
+        }
+        sums.clear(kInner);
+    };
     int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
 
@@ -513,8 +585,7 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
 
     for (int64_t row = first; row < last; ++row) {
         if (q.a.gate && row == gate_end) {
-            if (p.inner) sums.template put<VEC>(kInner, p.inner + (blockIdx.x + gate) * cols, cols);
-            sums.clear(kInner);
+            if (gates) finish(gate);
             ++gate;
             gate_end += q.a.gate_tokens;
         }
@@ -615,7 +686,18 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
         }
     }
     if (p.dpre) sums.template put<VEC>(kDpre, p.dpre + (int64_t)blockIdx.x * cols, cols);
-    if (p.inner) sums.template put<VEC>(kInner, p.inner + (blockIdx.x + gate) * cols, cols);
+    if (gates) finish(gate);
+    if (!p.dpost) return;
+    float* const to = p.dpost + (int64_t)blockIdx.x * cols;
+    if (!gates) {
+        sums.template put<VEC>(kInner, to, cols);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < VC; ++i) {
+        const int c = (threadIdx.x + i * blockDim.x) * 8;
+        put8<VEC>(gathered + c, to + c, cols - c);
+    }
 }
 
 // A thread's 32 bytes of columns times `factor`, from its bytes.
@@ -664,6 +746,19 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
     u64 dpre[kP] = {}, inner[kP] = {};
     allow_dependents();
+    float* const gathered = reinterpret_cast<float*>(smem + p.gathered);
+    const bool gates = q.a.gate && (p.dpost || p.dgate);
+    if (gates && p.dpost && live)
+#pragma unroll
+        for (int k = 0; k < 2 * kP; ++k) gathered[c + k] = 0.0f;
+    auto finish = [&](int64_t gate) {
+        if (live)
+#pragma unroll
+            for (int k = 0; k < kP; k += 4)
+                finish_gate<true, T>(p, gate, first, last, c + 2 * k, 8, inner + k, gathered);
+#pragma unroll
+        for (int k = 0; k < kP; ++k) inner[k] = 0ull;
+    };
     auto put = [&](const u64* v, float* to) {
         if (!live) return;
 #pragma unroll
@@ -683,9 +778,7 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
 
     for (int64_t row = first; row < last; ++row) {
         if (q.a.gate && row == gate_end) {
-            if (p.inner) put(inner, p.inner + (blockIdx.x + gate) * q.a.cols);
-#pragma unroll
-            for (int k = 0; k < kP; ++k) inner[k] = 0ull;
+            if (gates) finish(gate);
             ++gate;
             gate_end += q.a.gate_tokens;
         }
@@ -764,101 +857,102 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(e, T()));
     }
     if (p.dpre) put(dpre, p.dpre + (int64_t)blockIdx.x * q.a.cols);
-    if (p.inner) put(inner, p.inner + (blockIdx.x + gate) * q.a.cols);
+    if (gates) finish(gate);
+    if (!p.dpost) return;
+    if (gates && live)
+#pragma unroll
+        for (int k = 0; k < kP; ++k) inner[k] = pack2(gathered[c + 2 * k], gathered[c + 2 * k + 1]);
+    put(inner, p.dpost + (int64_t)blockIdx.x * q.a.cols);
 }
 
 // Adds the CTAs' sums of V columns per thread (4 where the columns allow it): 64 parts of the CTAs side
-// by side, eight loads of a part in flight, then the parts.  blockIdx.y: 0 dpre, 1 dpost, 2 + g gate g.
-constexpr int kSumLanes = 8, kSumParts = 64;
-template <int V> struct alignas(4 * V) Columns { float v[V]; };
-template <typename W, int V>
-__device__ __forceinline__ void gate_columns(const W* gate, float* w) {
-    struct alignas(V * sizeof(W)) Vec { W v[V]; };
-    if (((uintptr_t)gate & (V * sizeof(W) - 1)) == 0) {
-        const Vec x = *reinterpret_cast<const Vec*>(gate);
+// by side, eight loads of a part in flight, then the parts.  blockIdx.y 0: dpre, 1: dpost, 2: zeros for
+// the gates without rows and, where few CTAs share a gate (`few`), the gates that do not end in the CTA
+// they begin in, one per threadIdx.y; else 3 + g: gate g.
+constexpr int kSumLanes = 8, kSumParts = 64, kFewShares = 16;
+template <int V> struct alignas(4 * V) Columns {
+    float v[V];
+    __device__ __forceinline__ void add(const float* p) {
+        const Columns x = *reinterpret_cast<const Columns*>(p);
 #pragma unroll
-        for (int k = 0; k < V; ++k) w[k] = to_f32(x.v[k]);
-    } else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) w[k] = to_f32(gate[k]);
+        for (int k = 0; k < V; ++k) v[k] += x.v[k];
     }
-}
+    template <typename W> __device__ __forceinline__ void put(W* to) const {
+#pragma unroll
+        for (int k = 0; k < V; ++k) to[k] = from_f32<W>(v[k]);
+    }
+};
 template <typename W, int V>
 __global__ void __launch_bounds__(kSumLanes * kSumParts)
-block_norm_sums_kernel(const __grid_constant__ GradParams p, int ctas, W* dpre, W* dpost, W* dgate) {
+block_norm_sums_kernel(const __grid_constant__ GradParams p, int ctas, bool few, W* dpre, W* dpost, W* dgate) {
     __shared__ Columns<V> part[kSumParts][kSumLanes];
     const pwlq_block_norm_args& a = p.q.a;
     const int cols = (int)a.cols;
     const int c = (blockIdx.x * kSumLanes + threadIdx.x) * V;
-    const W* const gates = static_cast<const W*>(a.gate);
-    const W* const post = static_cast<const W*>(a.post_weight);
     // rows and their quotients fit 32 bits
     const unsigned rows = (unsigned)a.rows, per_cta = (unsigned)p.rows_per_cta;
     const unsigned every = (unsigned)min(a.gate_tokens, (int64_t)0x7fffffff);
     await_previous();
-    for (int64_t which = blockIdx.y; which < 2 + (dgate ? a.gate_rows : 0); which += gridDim.y) {
-        W* out = which == 0 ? dpre : which == 1 ? dpost : dgate + (which - 2) * cols;
-        if (which < 2 && !out) continue;
-        const float* src = (which == 0 ? p.dpre : p.inner) + c;
-        Columns<V> s = {};
-        if (c < cols && which == 1 && gates) {
-            // dpost: every slot times its gate; a CTA's first gate, then those that it went on to
-#pragma unroll 4
-            for (int b = threadIdx.y; b < ctas; b += kSumParts) {
-                const unsigned g = b * per_cta / every;
-                const Columns<V> x = *reinterpret_cast<const Columns<V>*>(src + (int64_t)(b + g) * cols);
-                float w[V];
-                gate_columns<W, V>(gates + (int64_t)g * a.ldgate + c, w);
-#pragma unroll
-                for (int k = 0; k < V; ++k) s.v[k] = fmaf(x.v[k], w[k], s.v[k]);
+    if (blockIdx.y == 2) {
+        if (c >= cols) return;
+        const int64_t used = (a.rows + a.gate_tokens - 1) / a.gate_tokens;
+        for (int64_t g = used + threadIdx.y; g < a.gate_rows; g += kSumParts) Columns<V>{}.put(dgate + g * cols + c);
+        if (!few) return;
+        const float* src = p.dgate + c;
+        if (every < per_cta) {             // a gate goes on into the next CTA, and ends there
+            for (unsigned b = 1 + threadIdx.y; b < (unsigned)ctas; b += kSumParts) {
+                if (b * per_cta % every == 0) continue;
+                Columns<V> s = {};
+                s.add(src + (int64_t)(2 * b - 1) * cols);
+                s.add(src + (int64_t)(2 * b) * cols);
+                s.put(dgate + (int64_t)(b * per_cta / every) * cols + c);
             }
-            for (int b = threadIdx.y; b < ctas; b += kSumParts) {
-                const unsigned last = (min(b * per_cta + per_cta, rows) - 1) / every;
-                for (unsigned g = b * per_cta / every + 1; g <= last; ++g) {
-                    const Columns<V> x = *reinterpret_cast<const Columns<V>*>(src + (int64_t)(b + g) * cols);
-                    float w[V];
-                    gate_columns<W, V>(gates + (int64_t)g * a.ldgate + c, w);
-#pragma unroll
-                    for (int k = 0; k < V; ++k) s.v[k] = fmaf(x.v[k], w[k], s.v[k]);
-                }
-            }
-        } else if (c < cols) {
-            int lo = 0, hi = ctas;
-            if (which >= 2) {
-                const int64_t g = which - 2, r0 = g * a.gate_tokens, r1 = min(r0 + a.gate_tokens, a.rows);
-                lo = (int)min(r0 / p.rows_per_cta, (int64_t)ctas);
-                hi = r1 > r0 ? (int)((r1 - 1) / p.rows_per_cta) + 1 : lo;
-                src += g * cols;                       // slot of CTA b: b + g
-            }
-#pragma unroll 8
-            for (int b = lo + threadIdx.y; b < hi; b += kSumParts) {
-                const Columns<V> x = *reinterpret_cast<const Columns<V>*>(src + (int64_t)b * cols);
-#pragma unroll
-                for (int k = 0; k < V; ++k) s.v[k] += x.v[k];
-            }
+            return;
         }
-        part[threadIdx.y][threadIdx.x] = s;
-        __syncthreads();
-        // eight parts each, then the eight
-#pragma unroll
-        for (int step = 1; step < kSumParts; step *= 8) {
-            if (threadIdx.y % (8 * step) == 0) {
-#pragma unroll
-                for (int j = 1; j < 8; ++j)
-#pragma unroll
-                    for (int k = 0; k < V; ++k) s.v[k] += part[threadIdx.y + j * step][threadIdx.x].v[k];
-                part[threadIdx.y][threadIdx.x] = s;
-            }
-            __syncthreads();
+        for (unsigned g = threadIdx.y; g < (unsigned)used; g += kSumParts) {
+            const unsigned from = g * every, lo = from / per_cta;
+            const unsigned hi = (unsigned)((min((uint64_t)from + every, (uint64_t)rows) - 1) / per_cta);
+            if (lo == hi) continue;
+            Columns<V> s = {};
+            s.add(src + (int64_t)(2 * lo + (from > lo * per_cta)) * cols);
+            for (unsigned b = lo + 1; b <= hi; ++b) s.add(src + (int64_t)(2 * b) * cols);
+            s.put(dgate + (int64_t)g * cols + c);
         }
-        if (threadIdx.y == 0 && c < cols) {
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float w = which >= 2 && post ? to_f32(post[c + k]) + p.q.offset : 1.0f;
-                out[c + k] = from_f32<W>(s.v[k] * w);
-            }
-        }
+        return;
     }
+    W* out = blockIdx.y == 0 ? dpre : dpost;
+    const float* src = (blockIdx.y == 0 ? p.dpre : p.dpost) + c;
+    int lo = 0, hi = ctas;
+    int64_t pitch = cols, first = 0;               // how far the first share lies beyond its CTA's others
+    if (blockIdx.y > 2) {
+        const unsigned g = blockIdx.y - 3, from = g * every;
+        lo = (int)(from / per_cta);
+        hi = (int)((min((uint64_t)from + every, (uint64_t)rows) - 1) / per_cta) + 1;
+        if (hi == lo + 1) return;                  // written by that CTA
+        out = dgate + (int64_t)g * cols;
+        src = p.dgate + c;
+        pitch = 2 * (int64_t)cols;
+        first = from > lo * per_cta ? cols : 0;
+    }
+    if (!out) return;
+    Columns<V> s = {};
+    if (c < cols) {
+#pragma unroll 8
+        for (int b = lo + threadIdx.y; b < hi; b += kSumParts) s.add(src + b * pitch + (b == lo ? first : 0));
+    }
+    part[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    // eight parts each, then the eight
+#pragma unroll
+    for (int step = 1; step < kSumParts; step *= 8) {
+        if (threadIdx.y % (8 * step) == 0) {
+#pragma unroll
+            for (int j = 1; j < 8; ++j) s.add(part[threadIdx.y + j * step][threadIdx.x].v);
+            part[threadIdx.y][threadIdx.x] = s;
+        }
+        __syncthreads();
+    }
+    if (threadIdx.y == 0 && c < cols) s.put(out + c);
 }
 
 // ------------------------------------------------------------------------------ launching
@@ -908,7 +1002,7 @@ inline int threads_for(int64_t cols, int per_thread) {
 
 template <typename K, typename P>
 cudaError_t run(K* kernel, unsigned ctas, int threads, size_t smem, cudaStream_t stream, const P& p) {
-    if (smem > 40 * 1024) {             // with the static part, possibly above the default 48 KB
+    if (smem > 12 * 1024) {             // with the static part, possibly above the default 48 KB
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
@@ -978,35 +1072,48 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
     const pwlq_block_norm_grads& g = p.g;
     const pwlq_block_norm_args& a = p.q.a;
     constexpr size_t kSize = sizeof(T);
+    const size_t wsize = type_size((int)a.wtype);
     const bool vec = rows_aligned(g.dh, g.lddh, kSize) && rows_aligned(g.dr, g.lddr, kSize) &&
                      rows_aligned(g.dx, g.lddx, kSize) && rows_aligned(g.df, g.lddf, kSize) &&
-                     a.cols % 4 == 0 && weights_aligned(a);
+                     rows_aligned(g.dgate, a.cols, wsize) && a.cols % 4 == 0 && weights_aligned(a);
+    const bool gathers = a.gate && g.dpost;
     if (a.cols > 8192) {
         const int threads = threads_for(a.cols, 32);
-        const size_t sums = (size_t)2 * 4 * 8 * sizeof(float) * threads;          // at most 128 KB
-        return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, sums, stream, p)
-                   : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, sums, stream, p);
+        p.gathered = (unsigned)((size_t)2 * 4 * 8 * sizeof(float) * threads);     // at most 128 KB of sums
+        const size_t smem = p.gathered + (gathers ? (size_t)threads * 32 * sizeof(float) : 0);
+        return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, smem, stream, p)
+                   : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, smem, stream, p);
     }
     const size_t stage = (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (g.dr ? p.q.row_bytes : 0) +
                          (a.f_codes ? p.q.code_bytes : 0);
     const RingPlan ring = ring_plan(a.cols, kSize, 512, stage);
     if (ring.threads <= 512 && a.cols % (32 / kSize) == 0 && ring.stages >= 2 && (a.pre_weight || g.dr) &&
         rows_aligned32(g.dh, g.lddh, kSize) && rows_aligned32(g.dr, g.lddr, kSize) &&
-        rows_aligned32(g.dx, g.lddx, kSize) && rows_aligned32(g.df, g.lddf, kSize) && weights_aligned(a)) {
+        rows_aligned32(g.dx, g.lddx, kSize) && rows_aligned32(g.df, g.lddf, kSize) &&
+        rows_aligned(g.dgate, a.cols, wsize) && weights_aligned(a)) {
         p.q.stages = ring.stages;
+        p.gathered = (unsigned)(ring.stages * stage);
+        const size_t smem = p.gathered + (gathers ? (size_t)a.cols * sizeof(float) : 0);
         return run(p.q.wf32 ? block_norm_backward_ring_kernel<T, true> : block_norm_backward_ring_kernel<T, kSize == 4>,
-                   ctas, ring.threads, ring.stages * stage, stream, p);
+                   ctas, ring.threads, smem, stream, p);
     }
-    return vec ? run(block_norm_backward_kernel<T, 1, true, false>, ctas, threads_for(a.cols, 8), 0, stream, p)
-               : run(block_norm_backward_kernel<T, 1, false, false>, ctas, threads_for(a.cols, 8), 0, stream, p);
+    const int threads = threads_for(a.cols, 8);
+    const size_t smem = gathers ? (size_t)threads * 8 * sizeof(float) : 0;
+    return vec ? run(block_norm_backward_kernel<T, 1, true, false>, ctas, threads, smem, stream, p)
+               : run(block_norm_backward_kernel<T, 1, false, false>, ctas, threads, smem, stream, p);
 }
 template <typename W, int V>
 cudaError_t sums(const GradParams& p, int64_t ctas, cudaStream_t stream) {
-    const int64_t kinds = 2 + (p.g.dgate ? p.q.a.gate_rows : 0);
-    const dim3 grid((unsigned)((p.q.a.cols + kSumLanes * V - 1) / (kSumLanes * V)),
-                    (unsigned)(kinds < 65535 ? kinds : 65535));
+    const pwlq_block_norm_args& a = p.q.a;
+    int64_t kinds = 2;
+    bool few = true;
+    if (p.g.dgate) {
+        few = a.gate_tokens / p.rows_per_cta + 2 <= kFewShares;
+        kinds = few ? 3 : 3 + (a.rows + a.gate_tokens - 1) / a.gate_tokens;
+    }
+    const dim3 grid((unsigned)((a.cols + kSumLanes * V - 1) / (kSumLanes * V)), (unsigned)kinds);
     return launch_dependent(block_norm_sums_kernel<W, V>, grid, dim3(kSumLanes, kSumParts), 0, stream, p, (int)ctas,
-                            static_cast<W*>(p.g.dpre), static_cast<W*>(p.g.dpost), static_cast<W*>(p.g.dgate));
+                            few, static_cast<W*>(p.g.dpre), static_cast<W*>(p.g.dpost), static_cast<W*>(p.g.dgate));
 }
 template <typename W>
 cudaError_t sums(const GradParams& p, int64_t ctas, cudaStream_t stream) {
@@ -1023,7 +1130,9 @@ cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
     ctas = (a.rows + p.rows_per_cta - 1) / p.rows_per_cta;
     float* ws = static_cast<float*>(g.workspace);
     p.dpre = g.dpre ? ws : nullptr;
-    p.inner = g.dpost || g.dgate ? ws + ctas * a.cols : nullptr;
+    p.dpost = g.dpost ? ws + ctas * a.cols : nullptr;
+    p.dgate = g.dgate ? ws + 2 * ctas * a.cols : nullptr;
+    p.gathered = 0;
     if (ctas)
         if (const cudaError_t e = backward_rows<T>(p, (unsigned)ctas, stream)) return e;
     if (!g.dpre && !g.dpost && !g.dgate) return cudaSuccess;
@@ -1040,7 +1149,7 @@ cudaError_t launch_block_norm(const pwlq_block_norm_args& a, cudaStream_t stream
 
 size_t block_norm_backward_workspace(int64_t rows, int64_t cols, int64_t gate_rows) {
     const int64_t ctas = backward_ctas(rows, cols);
-    return (size_t)(2 * ctas + gate_rows) * (size_t)cols * sizeof(float);
+    return (size_t)((gate_rows ? 4 : 2) * ctas) * (size_t)cols * sizeof(float);
 }
 
 cudaError_t launch_block_norm_backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads& g,
