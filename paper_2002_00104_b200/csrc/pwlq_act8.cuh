@@ -202,6 +202,13 @@ __device__ __forceinline__ void store32(void* p, const Raw32& r) {
                  ::"l"(p), "r"(r.w[0]), "r"(r.w[1]), "r"(r.w[2]), "r"(r.w[3]), "r"(r.w[4]), "r"(r.w[5]),
                    "r"(r.w[6]), "r"(r.w[7]) : "memory");
 }
+__device__ __forceinline__ Raw32 load32_global(const void* p) {   // on a 32-byte boundary
+    Raw32 r;
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r.w[0]), "=r"(r.w[1]), "=r"(r.w[2]), "=r"(r.w[3]), "=r"(r.w[4]), "=r"(r.w[5]),
+                   "=r"(r.w[6]), "=r"(r.w[7]) : "l"(p) : "memory");
+    return r;
+}
 __device__ __forceinline__ Raw32 load32(const void* p) {          // two 16-byte reads: any memory
     const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
     return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};

@@ -386,6 +386,90 @@ __global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(con
     }
 }
 
+// Sum over the aligned `lanes` (a power of two) lanes that share a row.
+__device__ __forceinline__ float lanes_sum(float v, int lanes) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1)
+        if (o < lanes) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// Forward, rows of up to 32 lanes' columns: `lanes` lanes own a row, a warp 32 / lanes rows at a time,
+// and nothing waits for another warp (one CTA per row left most of a warp idle below 512 columns: at
+// 64 columns it ran at a tenth of the copy rate).  The next rows' values are requested before the
+// current ones are worked on.
+constexpr int kNarrowThreads = 256;
+template <typename T, bool SAVE, bool WF32>
+__global__ void __launch_bounds__(kNarrowThreads, 2)
+block_norm_narrow_kernel(const __grid_constant__ NormParams q, int lanes) {
+    constexpr int kP = kPairs32<T>;
+    const int lane = threadIdx.x & 31, in = lane & (lanes - 1);
+    const bool inside = in * 2 * kP < (int)q.a.cols, post = q.a.post_weight, pre = q.a.pre_weight;
+    const int c = inside ? in * 2 * kP : (int)q.a.cols - 2 * kP;       // idle lanes repeat the last columns
+    const int64_t per_step = (int64_t)gridDim.x * kNarrowThreads / lanes;
+    Weights<T, WF32> post_w, pre_w;
+    if (post) post_w.load(q.a.post_weight, c);
+    if (pre) pre_w.load(q.a.pre_weight, c);
+    const unsigned every = (unsigned)min(q.a.gate_tokens, (int64_t)0x7fffffff);
+    int64_t row = ((int64_t)blockIdx.x * kNarrowThreads + threadIdx.x) / lanes;
+    Raw32 next_x, next_f;
+    auto fetch = [&](int64_t r) {
+        const int64_t at = min(r, q.a.rows - 1);
+        next_x = load32_global(static_cast<const T*>(q.a.x) + at * q.a.ldx + c);
+        if (q.a.f) next_f = load32_global(static_cast<const T*>(q.a.f) + at * q.a.ldf + c);
+    };
+    // a warp's lanes go round together, with rows past the end masked
+    const int64_t warp_row = row - lane / lanes;
+    fetch(row);
+    for (int64_t at = warp_row; at < q.a.rows; at += per_step, row += per_step) {
+        const Raw32 raw_x = next_x, raw_f = next_f;
+        fetch(row + per_step);
+        const bool live = inside && row < q.a.rows;
+        u64 r[kP], w[kP], s;
+        pairs32(raw_x, r, T());
+#pragma unroll
+        for (int k = 0; k < kP; ++k) r[k] = mul2(r[k], both(q.scale));
+        if (q.a.f) {
+            u64 f[kP];
+            pairs32(raw_f, f, T());
+            if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+            if (post) {
+                s = 0ull;
+#pragma unroll
+                for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
+                const float rstd_f =
+                    rsqrtf(fmaf(lanes_sum(inside ? sum8(s) : 0.0f, lanes), q.inv_cols, q.eps));
+                if (SAVE && in == 0 && live && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
+                post_w.get(w, q.offset);
+#pragma unroll
+                for (int k = 0; k < kP; ++k) f[k] = mul2(mul2(f[k], both(rstd_f)), w[k]);
+            }
+            if (q.a.gate) {
+                Weights<T, WF32> g;
+                g.load(q.a.gate, (int64_t)((unsigned)min(row, q.a.rows - 1) / every) * q.a.ldgate + c);
+                g.get(w);
+#pragma unroll
+                for (int k = 0; k < kP; ++k) r[k] = fma2(f[k], w[k], r[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < kP; ++k) r[k] = add2(r[k], f[k]);
+            }
+        }
+        if (live && q.a.r) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
+        if (SAVE && q.a.r_codes) save32<T>(r, q, live, row, c, q.a.r_codes, q.a.r_ranges);
+        if (!pre) continue;
+        s = 0ull;
+#pragma unroll
+        for (int k = 0; k < kP; ++k) s = fma2(r[k], r[k], s);
+        const float rstd_r = rsqrtf(fmaf(lanes_sum(inside ? sum8(s) : 0.0f, lanes), q.inv_cols, q.eps));
+        if (SAVE && in == 0 && live && q.a.r_rstd) q.a.r_rstd[row] = rstd_r;
+        pre_w.get(w, q.offset);
+#pragma unroll
+        for (int k = 0; k < kP; ++k) w[k] = mul2(mul2(r[k], both(rstd_r)), w[k]);
+        if (live) store32(static_cast<T*>(q.a.h) + row * q.a.ldh + c, raw32(w, T()));
+    }
+}
+
 // Backward.  CTA b owns the rows [b * rows_per_cta, ...) and its columns' sums over them; the sums
 // go to the workspace and a second kernel adds them in a fixed order.  Within the rows of one gate g,
 // the gate and the weight w are the same in every row, so one sum A = sum of e * n serves both
@@ -865,6 +949,170 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     put(inner, p.dpost + (int64_t)blockIdx.x * q.a.cols);
 }
 
+// Backward of narrow rows (see block_norm_narrow_kernel), for one gate at most.  The CTA's rows are not
+// neighbours here, but its sums are those of one CTA all the same.
+template <typename T, bool WF32>
+__global__ void __launch_bounds__(kNarrowThreads, 2)
+block_norm_backward_narrow_kernel(const __grid_constant__ GradParams p, int lanes) {
+    constexpr int kP = kPairs32<T>, kWarps = kNarrowThreads / 32;
+    __shared__ __align__(16) float part[kWarps][32 * 2 * kP];
+    const NormParams& q = p.q;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, in = lane & (lanes - 1);
+    const bool pre = q.a.pre_weight, post = q.a.post_weight, has_f = q.a.f_codes, has_dr = p.g.dr;
+    const bool inside = in * 2 * kP < (int)q.a.cols;
+    const int c = inside ? in * 2 * kP : (int)q.a.cols - 2 * kP;
+    const int64_t per_step = (int64_t)gridDim.x * kNarrowThreads / lanes;
+    Weights<T, WF32> post_w, pre_w, gate_w;
+    if (post) post_w.load(q.a.post_weight, c);
+    if (pre) pre_w.load(q.a.pre_weight, c);
+    if (q.a.gate) gate_w.load(q.a.gate, c);
+    allow_dependents();
+    u64 dpre[kP] = {}, inner[kP] = {};
+    int64_t row = ((int64_t)blockIdx.x * kNarrowThreads + threadIdx.x) / lanes;
+    for (int64_t at = row - lane / lanes; at < q.a.rows; at += per_step, row += per_step) {
+        const bool live = inside && row < q.a.rows;
+        const int64_t t = min(row, q.a.rows - 1), range = t * q.groups + (c >> q.group_shift);
+        Raw32 raw_dh, raw_dr;
+        float mr = 0.0f, mf = 0.0f, rr = 0.0f, rf = 1.0f;
+        uint4 rb, fb;
+        auto bytes = [&](const uint8_t* codes) {
+            const uint8_t* from = codes + t * q.a.ldc + c;
+            if (kP == 8) return *reinterpret_cast<const uint4*>(from);
+            const uint2 b = *reinterpret_cast<const uint2*>(from);
+            return make_uint4(b.x, b.y, 0u, 0u);
+        };
+        if (pre) {
+            raw_dh = load32_global(static_cast<const T*>(p.g.dh) + t * p.g.lddh + c);
+            rb = bytes(q.a.r_codes);
+            mr = q.a.r_ranges[range];
+            rr = q.a.r_rstd[t];
+        }
+        if (has_dr) raw_dr = load32_global(static_cast<const T*>(p.g.dr) + t * p.g.lddr + c);
+        if (has_f) {
+            fb = bytes(q.a.f_codes);
+            mf = q.a.f_ranges[range];
+            if (post) rf = q.a.f_rstd[t];
+        }
+        u64 e[kP], n[kP], w[kP], s = 0ull;
+        if (pre) {
+            pairs32(raw_dh, e, T());
+            held32<T>(reinterpret_cast<const unsigned char*>(&rb), mr, q.ratio, rr, n);
+            pre_w.get(w, q.offset);
+            if (live)
+#pragma unroll
+                for (int k = 0; k < kP; ++k) dpre[k] = fma2(e[k], n[k], dpre[k]);
+#pragma unroll
+            for (int k = 0; k < kP; ++k) {
+                e[k] = mul2(e[k], w[k]);
+                s = fma2(e[k], n[k], s);
+            }
+            const float mean = lanes_sum(inside ? sum8(s) : 0.0f, lanes) * q.inv_cols;
+#pragma unroll
+            for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rr));
+            if (has_dr) {
+                pairs32(raw_dr, w, T());
+#pragma unroll
+                for (int k = 0; k < kP; ++k) e[k] = add2(e[k], w[k]);
+            }
+        } else {
+            pairs32(raw_dr, e, T());
+        }
+        if (p.g.dx && live) {
+#pragma unroll
+            for (int k = 0; k < kP; ++k) w[k] = mul2(e[k], both(q.scale));
+            store32(static_cast<T*>(p.g.dx) + row * p.g.lddx + c, raw32(w, T()));
+        }
+        float mean = 0.0f;
+        if (has_f) {
+            held32<T>(reinterpret_cast<const unsigned char*>(&fb), mf, q.ratio, rf, n);
+            if (live)
+#pragma unroll
+                for (int k = 0; k < kP; ++k) inner[k] = fma2(e[k], n[k], inner[k]);
+            if (q.a.gate) {
+                gate_w.get(w);
+#pragma unroll
+                for (int k = 0; k < kP; ++k) e[k] = mul2(e[k], w[k]);
+            }
+            if (post) {
+                post_w.get(w, q.offset);
+                s = 0ull;
+#pragma unroll
+                for (int k = 0; k < kP; ++k) {
+                    e[k] = mul2(e[k], w[k]);
+                    s = fma2(e[k], n[k], s);
+                }
+                mean = lanes_sum(inside ? sum8(s) : 0.0f, lanes) * q.inv_cols;
+            }
+        }
+        if (!p.g.df || !live) continue;
+        if (post)
+#pragma unroll
+            for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rf));
+        store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(e, T()));
+    }
+    // a warp's rows, then the warps, in a fixed order
+    auto reduce = [&](u64* v) {
+        for (int o = lanes; o < 32; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < kP; ++k) v[k] = add2(v[k], __shfl_xor_sync(0xffffffffu, v[k], o));
+        __syncthreads();
+        if (lane < lanes)
+#pragma unroll
+            for (int k = 0; k < kP; k += 2)
+                *reinterpret_cast<ulonglong2*>(&part[warp][in * 2 * kP + 2 * k]) = make_ulonglong2(v[k], v[k + 1]);
+        __syncthreads();
+        if (warp == 0 && lane < lanes)
+            for (int j = 1; j < kWarps; ++j)
+#pragma unroll
+                for (int k = 0; k < kP; k += 2) {
+                    const ulonglong2 x = *reinterpret_cast<const ulonglong2*>(&part[j][in * 2 * kP + 2 * k]);
+                    v[k] = add2(v[k], x.x);
+                    v[k + 1] = add2(v[k + 1], x.y);
+                }
+    };
+    const bool mine = warp == 0 && lane < lanes && inside;
+    if (p.dpre) {
+        reduce(dpre);
+        if (mine)
+#pragma unroll
+            for (int k = 0; k < kP; k += 4)
+                store32(p.dpre + (int64_t)blockIdx.x * q.a.cols + c + 2 * k, raw32(dpre + k, 0.0f));
+    }
+    if (!p.dpost && !p.dgate) return;
+    reduce(inner);
+    if (!mine) return;
+    if (!q.a.gate) {
+#pragma unroll
+        for (int k = 0; k < kP; k += 4)
+            store32(p.dpost + (int64_t)blockIdx.x * q.a.cols + c + 2 * k, raw32(inner + k, 0.0f));
+        return;
+    }
+    // the gate's rows are everybody's: shares of the CTAs' first gate, unless there is one CTA
+    u64 w[kP], v[kP];
+    if (p.dgate) {
+        if (post) post_w.get(w, q.offset);
+#pragma unroll
+        for (int k = 0; k < kP; ++k) v[k] = post ? mul2(inner[k], w[k]) : inner[k];
+        float f[2 * kP];
+#pragma unroll
+        for (int k = 0; k < kP; ++k) unpack2(v[k], f[2 * k], f[2 * k + 1]);
+#pragma unroll
+        for (int k = 0; k < 2 * kP; k += 8) {
+            if (gridDim.x > 1) put8<true>(f + k, p.dgate + 2 * (int64_t)blockIdx.x * q.a.cols + c + k, 8);
+            else if (q.wf32) put8<true>(f + k, static_cast<float*>(p.g.dgate) + c + k, 8);
+            else put8<true>(f + k, static_cast<T*>(p.g.dgate) + c + k, 8);
+        }
+    }
+    if (p.dpost) {
+        gate_w.get(w);
+#pragma unroll
+        for (int k = 0; k < kP; ++k) v[k] = mul2(inner[k], w[k]);
+#pragma unroll
+        for (int k = 0; k < kP; k += 4)
+            store32(p.dpost + (int64_t)blockIdx.x * q.a.cols + c + 2 * k, raw32(v + k, 0.0f));
+    }
+}
+
 // Adds the CTAs' sums of V columns per thread (4 where the columns allow it): 64 parts of the CTAs side
 // by side, eight loads of a part in flight, then the parts.  blockIdx.y 0: dpre, 1: dpost, 2: zeros for
 // the gates without rows and, where few CTAs share a gate (`few`), the gates that do not end in the CTA
@@ -1028,16 +1276,37 @@ inline bool rows_aligned32(const void* p, int64_t ld, size_t size) {
     return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * (int64_t)size)) & 31) == 0;
 }
 
+// Lanes per row of the narrow kernels; 0: the rows are too wide for them.
+inline int narrow_lanes(int64_t cols, size_t size) {
+    const int64_t n = (cols * (int64_t)size + 31) / 32;
+    int lanes = 2;                        // a pair of lanes shares the reciprocals of a range
+    while (lanes < n) lanes *= 2;
+    return lanes <= 32 ? lanes : 0;
+}
+// CTAs of a narrow kernel: four per multiprocessor at most, whole rounds of rows where there are few.
+inline int64_t narrow_ctas(int64_t rows, int lanes) {
+    const int64_t per_cta = kNarrowThreads / lanes;
+    return std::min<int64_t>((rows + per_cta - 1) / per_cta, 4 * (int64_t)sm_count());
+}
+
 template <typename T, bool SAVE>
 cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
     NormParams q = params(a);
     constexpr size_t kSize = sizeof(T);
+    const bool rows32 = a.cols % (32 / kSize) == 0 && rows_aligned32(a.x, a.ldx, kSize) &&
+                        rows_aligned32(a.f, a.ldf, kSize) && rows_aligned32(a.r, a.ldr, kSize) &&
+                        rows_aligned32(a.h, a.ldh, kSize) && weights_aligned(a);
+    const int lanes = narrow_lanes(a.cols, kSize);
+    if (rows32 && lanes) {
+        q.group_lanes = std::min((int)(a.group * kSize / 32), lanes);
+        auto* kernel = q.wf32 ? block_norm_narrow_kernel<T, SAVE, true> : block_norm_narrow_kernel<T, SAVE, kSize == 4>;
+        kernel<<<(unsigned)narrow_ctas(a.rows, lanes), kNarrowThreads, 0, stream>>>(q, lanes);
+        return cudaGetLastError();
+    }
     const RingPlan ring = ring_plan(a.cols, kSize, kSize == 2 ? 768 : 1024, (a.f ? 2 : 1) * (size_t)q.row_bytes);
     const int64_t resident = (int64_t)ring.ctas * sm_count();
     // a ring pays once every CTA has a few rows to walk
-    if (a.cols <= kRingCols && a.cols % (32 / kSize) == 0 && ring.stages >= 2 && a.rows >= 2 * resident &&
-        rows_aligned32(a.x, a.ldx, kSize) && rows_aligned32(a.f, a.ldf, kSize) &&
-        rows_aligned32(a.r, a.ldr, kSize) && rows_aligned32(a.h, a.ldh, kSize) && weights_aligned(a)) {
+    if (a.cols <= kRingCols && rows32 && ring.stages >= 2 && a.rows >= 2 * resident) {
         q.stages = ring.stages;
         q.group_lanes = (int)(a.group * kSize / 32);
         if (a.gate) {
@@ -1067,6 +1336,16 @@ inline int64_t backward_ctas(int64_t rows, int64_t cols) {
     return std::min<int64_t>(rows, per_sm * sm_count());
 }
 
+// Whether the kernels that read 32 bytes of columns at a time do.
+template <typename T>
+bool rows32_backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads& g) {
+    constexpr size_t kSize = sizeof(T);
+    return a.cols % (32 / kSize) == 0 && (a.pre_weight || g.dr) && rows_aligned32(g.dh, g.lddh, kSize) &&
+           rows_aligned32(g.dr, g.lddr, kSize) && rows_aligned32(g.dx, g.lddx, kSize) &&
+           rows_aligned32(g.df, g.lddf, kSize) && rows_aligned(g.dgate, a.cols, type_size((int)a.wtype)) &&
+           weights_aligned(a);
+}
+
 template <typename T>
 cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
     const pwlq_block_norm_grads& g = p.g;
@@ -1087,10 +1366,7 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
     const size_t stage = (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (g.dr ? p.q.row_bytes : 0) +
                          (a.f_codes ? p.q.code_bytes : 0);
     const RingPlan ring = ring_plan(a.cols, kSize, 512, stage);
-    if (ring.threads <= 512 && a.cols % (32 / kSize) == 0 && ring.stages >= 2 && (a.pre_weight || g.dr) &&
-        rows_aligned32(g.dh, g.lddh, kSize) && rows_aligned32(g.dr, g.lddr, kSize) &&
-        rows_aligned32(g.dx, g.lddx, kSize) && rows_aligned32(g.df, g.lddf, kSize) &&
-        rows_aligned(g.dgate, a.cols, wsize) && weights_aligned(a)) {
+    if (ring.threads <= 512 && ring.stages >= 2 && rows32_backward<T>(a, g)) {
         p.q.stages = ring.stages;
         p.gathered = (unsigned)(ring.stages * stage);
         const size_t smem = p.gathered + (gathers ? (size_t)a.cols * sizeof(float) : 0);
@@ -1126,6 +1402,9 @@ cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
     if (!a.gate && !a.post_weight) p.q.a.f_codes = nullptr;      // f enters as it is: nothing of it is needed
     p.g = g;
     int64_t ctas = backward_ctas(a.rows, a.cols);
+    const int lanes = !a.gate || a.gate_tokens >= a.rows ? narrow_lanes(a.cols, sizeof(T)) : 0;
+    const bool narrow = lanes && rows32_backward<T>(a, g);
+    if (narrow) ctas = std::min(ctas, narrow_ctas(a.rows, lanes));
     p.rows_per_cta = ctas ? (a.rows + ctas - 1) / ctas : 1;
     ctas = (a.rows + p.rows_per_cta - 1) / p.rows_per_cta;
     float* ws = static_cast<float*>(g.workspace);
@@ -1133,8 +1412,14 @@ cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
     p.dpost = g.dpost ? ws + ctas * a.cols : nullptr;
     p.dgate = g.dgate ? ws + 2 * ctas * a.cols : nullptr;
     p.gathered = 0;
-    if (ctas)
+    if (ctas && narrow) {
+        auto* kernel = p.q.wf32 ? block_norm_backward_narrow_kernel<T, true>
+                                : block_norm_backward_narrow_kernel<T, sizeof(T) == 4>;
+        kernel<<<(unsigned)ctas, kNarrowThreads, 0, stream>>>(p, lanes);
+        if (const cudaError_t e = cudaGetLastError()) return e;
+    } else if (ctas) {
         if (const cudaError_t e = backward_rows<T>(p, (unsigned)ctas, stream)) return e;
+    }
     if (!g.dpre && !g.dpost && !g.dgate) return cudaSuccess;
     return p.q.wf32 ? sums<float>(p, ctas, stream) : sums<T>(p, ctas, stream);
 }
