@@ -1,0 +1,91 @@
+"""PyTorch autograd functions over the training calls: what they keep between the forward and the
+backward pass is 8-bit checkpoints, one byte per activation and one range per group.
+
+``ratio`` is the breakpoint of the checkpoints' quantizer as a part of a group's range; ``best_ratio``
+finds it with the library's breakpoint search on a sample of the activations.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import pwlq
+
+
+class Checkpoints:
+    """Settings of the checkpoints of a model: group length, breakpoint ratio."""
+
+    def __init__(self, group: int = 128, ratio: float = 0.5):
+        self.group, self.ratio = group, ratio
+
+
+def best_ratio(x: torch.Tensor, group: int = 128, candidates: int = 32) -> float:
+    """The breakpoint ratio with the smallest total squared error on x [rows, cols] (every group a
+    row of the 7-bit search); candidates are k / candidates, the last one (no tail) left out."""
+    cols = x.shape[1] // group * group
+    rows = x[:, :cols].float().reshape(-1, group).contiguous()
+    ratios = torch.arange(1, candidates, device=x.device, dtype=torch.float32) / candidates
+    sse = pwlq.search(rows, 7, ratios, want_sse=True)["sse"]
+    return float(ratios[sse.double().sum(dim=0).argmin()])
+
+
+class _Linear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, settings):
+        ctx.saved = pwlq.act8_encode(x, group=settings.group, ratio=settings.ratio)
+        ctx.save_for_backward(weight)
+        return x @ weight.t()
+
+    @staticmethod
+    def backward(ctx, dy):
+        weight, = ctx.saved_tensors
+        dx = dy @ weight if ctx.needs_input_grad[0] else None
+        dw = pwlq.act8_weight_grad(dy.contiguous(), ctx.saved) if ctx.needs_input_grad[1] else None
+        return dx, dw, None
+
+
+def linear(x, weight, settings: Checkpoints):
+    """x @ weight.T for x [rows, cols] in bf16 or fp16; x is kept as an 8-bit checkpoint."""
+    return _Linear.apply(x, weight, settings)
+
+
+class _Silu(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, settings):
+        ctx.saved = pwlq.act8_encode(x, group=settings.group, ratio=settings.ratio)
+        return torch.nn.functional.silu(x)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x = pwlq.act8_decode(ctx.saved, dtype=dy.dtype)
+        s = torch.sigmoid(x)
+        return dy * s * (1 + x * (1 - s)), None
+
+
+def silu(x, settings: Checkpoints):
+    """x * sigmoid(x); x is kept as an 8-bit checkpoint."""
+    return _Silu.apply(x, settings)
+
+
+class _BlockNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps, settings):
+        r, h, ctx.saved = pwlq.block_norm(x, f, pre_weight, post_weight, gate, gate_tokens,
+                                          residual_scale, eps, save=(settings.group, settings.ratio))
+        ctx.set_materialize_grads(False)
+        return r, h
+
+    @staticmethod
+    def backward(ctx, dr, dh):
+        if dh is None:
+            dh = torch.zeros_like(dr)
+        g = pwlq.block_norm_backward(ctx.saved, dh.contiguous(),
+                                     dr.contiguous() if dr is not None else None)
+        return (g["dx"], g["df"], g["dpre"], g["dpost"], g["dgate"]) + (None,) * 4
+
+
+def block_norm(x, f, pre_weight, post_weight=None, gate=None, gate_tokens=None, residual_scale=1.0,
+               eps=1e-6, settings=Checkpoints()):
+    """(r, h): r = residual_scale * x + gate * N(f; post_weight), h = N(r; pre_weight).  f may be None
+    (the norm before the first block).  r and f are kept as 8-bit checkpoints."""
+    return _BlockNorm.apply(x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps,
+                            settings)
