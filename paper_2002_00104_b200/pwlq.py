@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import struct
-from typing import NamedTuple, Optional
+from typing import Optional
 
 import torch
 
@@ -820,14 +820,46 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-class Act8(NamedTuple):
+class Act8:
     """An 8-bit checkpoint of a [rows, cols] tensor: one byte per value in ``codes`` [rows, pitch]
     (pitch a multiple of 16), one range per group of a row in ``ranges`` [rows, groups]."""
-    codes: torch.Tensor
-    ranges: torch.Tensor
-    cols: int
-    group: int
-    ratio: float
+    __slots__ = ("rows", "cols", "group", "ratio", "_memory", "_at", "_codes", "_ranges")
+
+    def __init__(self, codes: torch.Tensor, ranges: torch.Tensor, cols: int, group: int, ratio: float):
+        self.rows, self.cols, self.group, self.ratio = codes.shape[0], cols, group, ratio
+        self._memory, self._codes, self._ranges = None, codes, ranges
+
+    @classmethod
+    def _inside(cls, memory: torch.Tensor, at: int, rows: int, cols: int, group: int, ratio: float):
+        """The checkpoint that lies in a byte tensor from offset ``at`` on (see ``_act8_bytes``); its
+        two tensors are made when somebody asks for them."""
+        a = cls.__new__(cls)
+        a.rows, a.cols, a.group, a.ratio = rows, cols, group, ratio
+        a._memory, a._at, a._codes, a._ranges = memory, at, None, None
+        return a
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            pitch = -(-self.cols // 16) * 16
+            self._codes = self._memory[self._at:self._at + self.rows * pitch].view(self.rows, pitch)
+        return self._codes
+
+    @property
+    def ranges(self) -> torch.Tensor:
+        if self._ranges is None:
+            at = self._at + self.rows * (-(-self.cols // 16) * 16)
+            groups = -(-self.cols // self.group)
+            self._ranges = (self._memory[at:at + 4 * self.rows * groups].view(torch.float32)
+                            .view(self.rows, groups))
+        return self._ranges
+
+
+def _act8_bytes(rows: int, cols: int, group: int) -> int:
+    """Size of a checkpoint in one piece: the codes, then the ranges, to the next multiple of 32."""
+    if group < 1 or cols < 1:
+        raise PwlqError(ERR_INVALID_ARG, f"checkpoint of {cols} columns in groups of {group}")
+    return (rows * (-(-cols // 16) * 16 + 4 * -(-cols // group)) + 31) // 32 * 32
 
 
 def _home(t: torch.Tensor, what: str) -> int:
@@ -884,6 +916,13 @@ def _on(stream):
 
 def _act8(a: Act8, device, rows=None, cols=None):
     """(codes pointer, pitch, ranges pointer) of a checkpoint, checked against its own layout."""
+    if rows is not None and (a.rows != rows or (cols is not None and a.cols != cols)):
+        raise ValueError(f"the checkpoint is of [{a.rows}, {a.cols}], not [{rows}, {cols}]")
+    memory = a._memory
+    if memory is not None and memory.get_device() == device:
+        pitch = -(-a.cols // 16) * 16
+        at = memory.data_ptr() + a._at
+        return at, pitch, at + a.rows * pitch
     codes, ranges = a.codes, a.ranges
     if (codes.dtype != torch.uint8 or codes.dim() != 2 or codes.get_device() != device or
             not codes.is_contiguous() or codes.shape[1] < a.cols or codes.shape[1] % 16 or
@@ -892,16 +931,13 @@ def _act8(a: Act8, device, rows=None, cols=None):
         raise ValueError(f"not a checkpoint on cuda:{device}: codes must be contiguous uint8 "
                          "[rows, pitch] with a pitch that is a multiple of 16, ranges float32 "
                          "[rows, groups]")
-    if rows is not None and (codes.shape[0] != rows or (cols is not None and a.cols != cols)):
-        raise ValueError(f"the checkpoint is of [{codes.shape[0]}, {a.cols}], not [{rows}, {cols}]")
     return codes.data_ptr(), codes.shape[1], ranges.data_ptr()
 
 
 def act8_empty(rows: int, cols: int, group: int = 128, ratio: float = 0.5, device=None) -> Act8:
     """An uninitialised checkpoint of a [rows, cols] tensor."""
-    return Act8(torch.empty((rows, -(-cols // 16) * 16), dtype=torch.uint8, device=device),
-                torch.empty((rows, -(-cols // group)), dtype=torch.float32, device=device),
-                cols, group, ratio)
+    memory = torch.empty(_act8_bytes(rows, cols, group), dtype=torch.uint8, device=device)
+    return Act8._inside(memory, 0, rows, cols, group, ratio)
 
 
 def act8_encode(x, group=128, ratio=0.5, out: Optional[Act8] = None, stream=None) -> Act8:
@@ -914,9 +950,7 @@ def act8_encode(x, group=128, ratio=0.5, out: Optional[Act8] = None, stream=None
     ptr, pitch = _matrix(x, "x", shape, x.dtype, device)
     if out is None:
         out = act8_empty(rows, cols, group, ratio, x.device)
-        codes, ldc, ranges = out.codes.data_ptr(), -(-cols // 16) * 16, out.ranges.data_ptr()
-    else:
-        codes, ldc, ranges = _act8(out, device, rows, cols)
+    codes, ldc, ranges = _act8(out, device, rows, cols)
     _check(load_library().pwlq_act8_encode(ptr, _DTYPES[x.dtype], rows, cols, pitch, out.group,
                                            out.ratio, codes, ldc, ranges, _raw_stream(device)),
            "pwlq_act8_encode")
@@ -928,11 +962,12 @@ def act8_decode(saved: Act8, dtype=torch.float32, out=None, stream=None):
     if stream is not None:
         with _on(stream):
             return act8_decode(saved, dtype, out)
-    device = _home(saved.codes, "the checkpoint")
+    memory = saved._memory if saved._memory is not None else saved.codes
+    device = _home(memory, "the checkpoint")
     codes, ldc, ranges = _act8(saved, device)
-    shape = rows, cols = saved.codes.shape[0], saved.cols
+    shape = rows, cols = saved.rows, saved.cols
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=saved.codes.device)
+        out = torch.empty(shape, dtype=dtype, device=memory.device)
         ptr, pitch = out.data_ptr(), cols
     else:
         dtype = out.dtype
@@ -945,20 +980,36 @@ def act8_decode(saved: Act8, dtype=torch.float32, out=None, stream=None):
     return out
 
 
-class BlockNormSaved(NamedTuple):
-    """What ``block_norm`` keeps for ``block_norm_backward``: the checkpoints, the norms' factors,
-    the weights and gate it was given, and its settings."""
-    r: Optional[Act8]
-    f: Optional[Act8]
-    r_rstd: Optional[torch.Tensor]
-    f_rstd: Optional[torch.Tensor]
-    pre_weight: Optional[torch.Tensor]
-    post_weight: Optional[torch.Tensor]
-    gate: Optional[torch.Tensor]
-    shape: tuple
-    dtype: torch.dtype
-    has_f: bool
-    block: bytes                     # pwlq_block_norm_args of the forward call
+class BlockNormSaved:
+    """What ``block_norm`` keeps for ``block_norm_backward``: the checkpoints ``r`` and ``f`` and the
+    norms' factors ``r_rstd`` and ``f_rstd`` (None where the call needs none), all in one piece of
+    memory, and the weights and gate it was given."""
+    __slots__ = ("pre_weight", "post_weight", "gate", "shape", "dtype", "has_f", "group", "ratio",
+                 "_memory", "_block", "_f_at", "_rstd_at")
+
+    def _checkpoint(self, at: int) -> Act8:
+        return Act8._inside(self._memory, at, *self.shape, self.group, self.ratio)
+
+    def _factors(self, at: int) -> torch.Tensor:
+        return self._memory[at:at + 4 * self.shape[0]].view(torch.float32)
+
+    @property
+    def r(self) -> Optional[Act8]:
+        return self._checkpoint(0) if self.pre_weight is not None else None
+
+    @property
+    def f(self) -> Optional[Act8]:
+        some = self.post_weight is not None or self.gate is not None
+        return self._checkpoint(self._f_at) if some else None
+
+    @property
+    def r_rstd(self) -> Optional[torch.Tensor]:
+        return self._factors(self._rstd_at) if self.pre_weight is not None else None
+
+    @property
+    def f_rstd(self) -> Optional[torch.Tensor]:
+        at = self._rstd_at + 4 * self.shape[0]
+        return self._factors(at) if self.post_weight is not None else None
 
 
 # pwlq_block_norm_args and pwlq_block_norm_grads of include/pwlq.h
@@ -1019,29 +1070,28 @@ def block_norm(x, f=None, pre_weight=None, post_weight=None, gate=None, gate_tok
                                  rp, ldr, hp, ldh, 0, 0.0, 0, 0, 0, 0, 0, 0, 0)
         _check(load_library().pwlq_block_norm(block, _raw_stream(device)), "pwlq_block_norm")
         return r, h, None
-    group, ratio = int(save[0]), float(save[1])
-    ldc = -(-cols // 16) * 16
-    r8 = f8 = rs = fs = None
-    rc = rr = fc = fr = rsp = fsp = 0
+    kept = BlockNormSaved()
+    kept.pre_weight, kept.post_weight, kept.gate = pre_weight, post_weight, gate
+    kept.shape, kept.dtype, kept.has_f = shape, dtype, f is not None
+    kept.group, kept.ratio = group, ratio = int(save[0]), float(save[1])
+    size, ldc = _act8_bytes(rows, cols, group), -(-cols // 16) * 16
+    kept._f_at = f_at = size if pre_weight is not None else 0
+    kept._rstd_at = rstd_at = f_at + (size if gate is not None or post_weight is not None else 0)
+    kept._memory = torch.empty(rstd_at + 8 * rows, dtype=torch.uint8, device=x.device)
+    base = kept._memory.data_ptr()
+    rc = rr = rsp = fc = fr = fsp = 0
     if pre_weight is not None:
-        r8 = act8_empty(rows, cols, group, ratio, x.device)
-        rs = r8.ranges.new_empty(rows)
-        rc, rr, rsp = r8.codes.data_ptr(), r8.ranges.data_ptr(), rs.data_ptr()
+        rc, rr, rsp = base, base + rows * ldc, base + rstd_at
     if gate is not None or post_weight is not None:
-        if r8 is None:
-            f8 = act8_empty(rows, cols, group, ratio, x.device)
-        else:
-            f8 = Act8(torch.empty_like(r8.codes), torch.empty_like(r8.ranges), cols, group, ratio)
-        fc, fr = f8.codes.data_ptr(), f8.ranges.data_ptr()
+        fc, fr = base + f_at, base + f_at + rows * ldc
         if post_weight is not None:
-            fs = f8.ranges.new_empty(rows)
-            fsp = fs.data_ptr()
-    block = _BLOCK_ARGS.pack(rows, cols, _DTYPES[dtype], _DTYPES[wtype], xp, ldx, fp, ldf, post, pre,
-                             gp, ldg, gate_rows, every, residual_scale, eps, weight_offset, rp, ldr,
-                             hp, ldh, group, ratio, ldc, rc, rr, rsp, fc, fr, fsp)
+            fsp = base + rstd_at + 4 * rows
+    kept._block = block = _BLOCK_ARGS.pack(
+        rows, cols, _DTYPES[dtype], _DTYPES[wtype], xp, ldx, fp, ldf, post, pre, gp, ldg, gate_rows,
+        every, residual_scale, eps, weight_offset, rp, ldr, hp, ldh, group, ratio, ldc, rc, rr, rsp,
+        fc, fr, fsp)
     _check(load_library().pwlq_block_norm(block, _raw_stream(device)), "pwlq_block_norm")
-    return r, h, BlockNormSaved(r8, f8, rs, fs, pre_weight, post_weight, gate, shape, dtype,
-                                f is not None, block)
+    return r, h, kept
 
 
 def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None, stream=None):
@@ -1058,9 +1108,9 @@ def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None,
     shape, dtype = saved.shape, saved.dtype
     cols = shape[1]
     device = _home(some, "the gradient")
-    kept = saved.r.codes if pre is not None else saved.f.codes if saved.f is not None else some
-    if kept.get_device() != device:
-        raise ValueError(f"the forward call ran on {kept.device}, the gradient is on {some.device}")
+    memory = saved._memory
+    if memory.get_device() != device:
+        raise ValueError(f"the forward call ran on {memory.device}, the gradient is on {some.device}")
     dhp = lddh = drp = lddr = dfp = dprep = dpostp = dgatep = wsp = need = gate_rows = 0
     if dh is not None:
         dhp, lddh = _matrix(dh, "dh", shape, dtype, device)
@@ -1083,13 +1133,12 @@ def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None,
     lib = load_library()
     if dprep or dpostp or dgatep:
         if workspace is None:
-            workspace = torch.empty(
-                lib.pwlq_block_norm_backward_workspace_bytes(shape[0], cols, gate_rows),
-                dtype=torch.uint8, device=some.device)
+            workspace = memory.new_empty(
+                lib.pwlq_block_norm_backward_workspace_bytes(shape[0], cols, gate_rows))
         wsp, need = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
     grads = _BLOCK_GRADS.pack(dhp, lddh, drp, lddr, dx.data_ptr(), cols, dfp, cols, dprep, dpostp,
                               dgatep, wsp, need)
-    _check(lib.pwlq_block_norm_backward(saved.block, grads, _raw_stream(device)),
+    _check(lib.pwlq_block_norm_backward(saved._block, grads, _raw_stream(device)),
            "pwlq_block_norm_backward")
     return {"dx": dx, "df": df, "dpre": dpre, "dpost": dpost, "dgate": dgate}
 
@@ -1127,7 +1176,7 @@ def act8_weight_grad(dy, saved: Act8, dtype=None, out=None, accumulate=False, wo
     if workspace is None:
         need = lib.pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols,
                                                          int((dyp | lddy * 2) % 16 == 0))
-        workspace = torch.empty(need, dtype=torch.uint8, device=dy.device)
+        workspace = (saved._memory if saved._memory is not None else saved.codes).new_empty(need)
     _check(lib.pwlq_act8_weight_grad(dyp, _DTYPES[dy.dtype], rows, outputs, lddy, codes, ldc, ranges,
                                      cols, saved.group, saved.ratio, dwp, _DTYPES[dtype], lddw,
                                      int(accumulate), _dev(workspace, torch.uint8, "workspace"),

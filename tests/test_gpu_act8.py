@@ -91,6 +91,8 @@ def test_no_rows_reuse_of_a_checkpoint_and_another_stream():
     y = pwlq.act8_decode(saved, dtype=torch.bfloat16, stream=side)
     side.synchronize()
     assert saved is out
+    again = pwlq.Act8(saved.codes, saved.ranges, 300, 128, 0.5)       # the same, from its two tensors
+    assert torch.equal(pwlq.act8_decode(again, dtype=torch.bfloat16), y)
     want_b, _, want_y = act8_reference(x.float().numpy(), 128, 0.5)
     assert np.array_equal(saved.codes.cpu().numpy()[:, :300], want_b)
     assert torch.equal(y.cpu(), torch.from_numpy(want_y).to(torch.bfloat16))
@@ -140,6 +142,8 @@ def test_refusals():
         pwlq.act8_encode(x, out=pwlq.act8_empty(4, 128, device="cuda"))
     saved = pwlq.act8_encode(x)
     with pytest.raises(ValueError):
-        pwlq.act8_decode(saved._replace(codes=saved.codes[:, :60]))
+        pwlq.act8_decode(pwlq.Act8(saved.codes[:, :60], saved.ranges, 64, 128, 0.5))
+    with pytest.raises(ValueError):
+        pwlq.act8_decode(pwlq.Act8(saved.codes, saved.ranges[:3], 64, 128, 0.5))
     with pytest.raises(ValueError):
         pwlq.act8_decode(saved, out=torch.empty(4, 63, device="cuda"))

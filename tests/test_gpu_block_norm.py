@@ -9,8 +9,8 @@ import numpy as np
 import pytest
 import torch
 
-from train_util import (TYPES, U, act8_reference, act8_values64, backward64, check, forward64,
-                        gate_rows, on_grid)
+from train_util import (TYPES, U, act8_reference, act8_values64, backward64, check, forward64, held64,
+                        on_grid)
 
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA device")]
@@ -59,8 +59,8 @@ def _check_forward(s, every, scale, eps, offset, r, h):
 
 def _check_backward(s, every, scale, offset, saved, grads, rows_per_sum):
     w = {k: _d(s[k]) for k in ("pre", "post", "gate", "dh", "dr")}
-    R = act8_values64(saved.r.codes, saved.r.ranges, *saved.r[2:]) if saved.r else None
-    F = act8_values64(saved.f.codes, saved.f.ranges, *saved.f[2:]) if saved.f else None
+    R = held64(saved.r) if saved.r else None
+    F = held64(saved.f) if saved.f else None
     rr = saved.r_rstd.double()[:, None] if saved.r_rstd is not None else None
     rf = saved.f_rstd.double()[:, None] if saved.f_rstd is not None else None
     want, mag = backward64(R, F, rr, rf, w["dh"], w["dr"], w["pre"], w["post"], w["gate"], every, scale,

@@ -9,7 +9,7 @@ import numpy as np
 import pytest
 import torch
 
-from train_util import HALF_ULP, TYPES, act8_values64, check
+from train_util import HALF_ULP, TYPES, check, held64
 
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA device")]
@@ -30,7 +30,7 @@ def _held(saved, dt):
     is tested on its own)."""
     from paper_2002_00104_b200 import pwlq
     v = pwlq.act8_decode(saved, dtype=dt).double()
-    exact = act8_values64(saved.codes, saved.ranges, *saved[2:])
+    exact = held64(saved)
     assert ((v - exact).abs() <= (HALF_ULP[dt] + 2.0 ** -22) * exact.abs() + 2.0 ** -25).all()
     return v
 

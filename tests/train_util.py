@@ -59,6 +59,10 @@ def act8_values64(codes, ranges, cols, group, ratio):
     return torch.where((c & 128) != 0, -v, v)
 
 
+def held64(saved):
+    return act8_values64(saved.codes, saved.ranges, saved.cols, saved.group, saved.ratio)
+
+
 def on_grid(rng, rows, cols, group, step):
     """Values that a checkpoint at ratio 0.5 holds exactly: multiples of `step` up to 126, one of
     which is 126 in every group."""
