@@ -4,6 +4,8 @@
 // (or 8) consecutive values, the 2 ... 32 threads of a group are neighbours in a warp and find the
 // group's range with shuffles, so the values are read once although the range must be known before
 // the first byte.
+#include <algorithm>
+
 #include "pwlq_act8.cuh"
 #include "pwlq_train.h"
 
@@ -14,6 +16,22 @@ constexpr int kThreads = 256;
 // Values per thread: 16, so that every access to the bytes is 16 bytes wide; 8 where the rows of the
 // values are off their alignment, since neighbouring threads then join their values (store8).
 __host__ __device__ constexpr int chunk_of(bool vec) { return vec ? 16 : 8; }
+
+// A matrix of 16-bit values whose rows do not start on 16-byte boundaries is copied to one whose rows
+// do by extra blocks of a decode launch, from block `first` on: a launch of its own cost 3.7 us.
+__device__ __forceinline__ void realign(const Realigned& r) {
+    typedef __nv_bfloat16 T;                     // 16 bits, whatever they mean
+    const unsigned per_row = (unsigned)(r.pitch / 8);
+    const int64_t row0 = (int64_t)(blockIdx.x - r.first) * r.rows_per_block;
+    const unsigned rows = (unsigned)min((int64_t)r.rows_per_block, r.rows - row0);
+    for (unsigned i = threadIdx.x; i < rows * per_row; i += blockDim.x) {
+        const unsigned row = i / per_row, c = (i - row * per_row) * 8;
+        const T* from = reinterpret_cast<const T*>(r.from) + (row0 + row) * r.ld + c;
+        Raw8<T> v;
+        load8<false>(v, from, (int)r.cols - (int)c, (int)c);
+        v.store(reinterpret_cast<T*>(r.to) + (row0 + row) * r.pitch + c);
+    }
+}
 
 // Which chunk of which row a thread owns.  Rows of up to 256 chunks share a block (rows_per_block of
 // them), longer ones take blocks_per_row equal blocks; a row's chunks are counted in whole groups, so
@@ -77,12 +95,13 @@ act8_encode_kernel(const T* x, int64_t ldx, Act8Grid g, int group_shift, float r
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads)
 act8_decode_kernel(const uint8_t* codes, int64_t ldc, const float* ranges, int64_t groups,
-                   Act8Grid g, int group_shift, float ratio, T* y, int64_t ldy) {
+                   Act8Grid g, int group_shift, float ratio, T* y, int64_t ldy, Realigned beside) {
+    allow_dependents();
+    if (blockIdx.x >= beside.first) return realign(beside);
     constexpr int kChunk = chunk_of(VEC), kParts = kChunk / 8;
     int64_t row, col;
     int valid;
     const bool live = locate(g, kChunk, row, col, valid);
-    allow_dependents();
     if (!__any_sync(0xffffffffu, live)) return;
     uint2 w[kParts] = {};
     float m = 0.0f;
@@ -143,8 +162,9 @@ act8_encode_flat_kernel(const T* x, int64_t chunks, int group_shift, float ratio
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 act8_decode_flat_kernel(const uint8_t* codes, const float* ranges, int64_t chunks, int group_shift, float ratio,
-                        T* y) {
+                        T* y, Realigned beside) {
     allow_dependents();
+    if (blockIdx.x >= beside.first) return realign(beside);
     const int64_t first = (int64_t)blockIdx.x * (kThreads * kFlatChunks) + threadIdx.x;
     uint4 w[kFlatChunks];
     float m[kFlatChunks];
@@ -175,7 +195,7 @@ inline unsigned flat_blocks(const Act8Tensor& a) {
     return (unsigned)((a.rows * a.cols + per_block - 1) / per_block);
 }
 
-cudaError_t plan(int64_t rows, int64_t cols, int group, bool vec, Act8Grid& g, unsigned& blocks) {
+void plan(int64_t rows, int64_t cols, int group, bool vec, Act8Grid& g, unsigned& blocks) {
     const int per_group = group / chunk_of(vec);
     const int64_t chunks = (cols + group - 1) / group * per_group;
     g.rows = rows;
@@ -191,10 +211,8 @@ cudaError_t plan(int64_t rows, int64_t cols, int group, bool vec, Act8Grid& g, u
     }
     g.magic = (unsigned)(65536 / g.chunks_lo + 1);
     const int64_t n = (rows + g.rows_per_block - 1) / g.rows_per_block * per_row;
-    if (n > ((int64_t)1 << 31) - 1) return cudaErrorInvalidConfiguration;
     g.blocks_per_row = (unsigned)per_row;
-    blocks = (unsigned)n;
-    return cudaSuccess;
+    blocks = (unsigned)n;                // at most 2^31 - 1: the entry points check it
 }
 
 template <typename T>
@@ -207,7 +225,7 @@ cudaError_t encode(const void* x, const Act8Tensor& a, int64_t ldx, cudaStream_t
         return cudaGetLastError();
     }
     const bool vec = rows_aligned(x, ldx, sizeof(T));
-    if (cudaError_t e = plan(a.rows, a.cols, a.group, vec, g, blocks)) return e;
+    plan(a.rows, a.cols, a.group, vec, g, blocks);
     const T* p = static_cast<const T*>(x);
     auto* kernel = vec ? act8_encode_kernel<T, true>
                                                    : act8_encode_kernel<T, false>;
@@ -215,22 +233,32 @@ cudaError_t encode(const void* x, const Act8Tensor& a, int64_t ldx, cudaStream_t
                                             a.ldc, a.ranges, a.groups());
     return cudaGetLastError();
 }
+// Where the extra blocks begin, and how many they are.
+unsigned place(Realigned& r, unsigned blocks) {
+    r.first = blocks;
+    if (!r.from) return 0;
+    r.rows_per_block = (unsigned)std::max<int64_t>(1, 2048 / (r.pitch / 8));
+    return (unsigned)((r.rows + r.rows_per_block - 1) / r.rows_per_block);
+}
+
 template <typename T>
-cudaError_t decode(const Act8Tensor& a, void* y, int64_t ldy, cudaStream_t stream) {
+cudaError_t decode(const Act8Tensor& a, void* y, int64_t ldy, Realigned beside, cudaStream_t stream) {
     Act8Grid g;
     unsigned blocks;
     if (is_flat(y, ldy, a)) {
-        act8_decode_flat_kernel<T><<<flat_blocks(a), kThreads, 0, stream>>>(
-            a.codes, a.ranges, a.rows * a.cols / 16, group_shift(a.group), a.ratio, static_cast<T*>(y));
+        const unsigned extra = place(beside, flat_blocks(a));
+        act8_decode_flat_kernel<T><<<beside.first + extra, kThreads, 0, stream>>>(
+            a.codes, a.ranges, a.rows * a.cols / 16, group_shift(a.group), a.ratio, static_cast<T*>(y), beside);
         return cudaGetLastError();
     }
     const bool vec = rows_aligned(y, ldy, sizeof(T));
-    if (cudaError_t e = plan(a.rows, a.cols, a.group, vec, g, blocks)) return e;
+    plan(a.rows, a.cols, a.group, vec, g, blocks);
     T* p = static_cast<T*>(y);
     auto* kernel = vec ? act8_decode_kernel<T, true>
                                                    : act8_decode_kernel<T, false>;
-    kernel<<<blocks, g.threads, 0, stream>>>(a.codes, a.ldc, a.ranges, a.groups(), g,
-                                            group_shift(a.group), a.ratio, p, ldy);
+    const unsigned extra = place(beside, blocks);
+    kernel<<<beside.first + extra, g.threads, 0, stream>>>(a.codes, a.ldc, a.ranges, a.groups(), g,
+                                                           group_shift(a.group), a.ratio, p, ldy, beside);
     return cudaGetLastError();
 }
 
@@ -242,11 +270,11 @@ cudaError_t launch_act8_encode(const void* x, int dtype, int64_t ldx, const Act8
     if (dtype == kBf16) return encode<__nv_bfloat16>(x, a, ldx, stream);
     return encode<__half>(x, a, ldx, stream);
 }
-cudaError_t launch_act8_decode(const Act8Tensor& a, void* y, int dtype, int64_t ldy,
-                               cudaStream_t stream) {
-    if (dtype == kF32) return decode<float>(a, y, ldy, stream);
-    if (dtype == kBf16) return decode<__nv_bfloat16>(a, y, ldy, stream);
-    return decode<__half>(a, y, ldy, stream);
+cudaError_t launch_act8_decode(const Act8Tensor& a, void* y, int dtype, int64_t ldy, cudaStream_t stream,
+                               const Realigned& beside) {
+    if (dtype == kF32) return decode<float>(a, y, ldy, beside, stream);
+    if (dtype == kBf16) return decode<__nv_bfloat16>(a, y, ldy, beside, stream);
+    return decode<__half>(a, y, ldy, beside, stream);
 }
 
 }  // namespace pwlq

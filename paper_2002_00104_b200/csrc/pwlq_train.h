@@ -50,8 +50,17 @@ cudaError_t launch_dependent(void (*kernel)(P...), dim3 blocks, dim3 threads, si
 
 cudaError_t launch_act8_encode(const void* x, int dtype, int64_t ldx, const Act8Tensor& a,
                                cudaStream_t stream);
-cudaError_t launch_act8_decode(const Act8Tensor& a, void* y, int dtype, int64_t ldy,
-                               cudaStream_t stream);
+// A copy of [rows, cols] 16-bit values to rows of `pitch` (a multiple of 8) values, zeros past cols, that
+// a decode launch makes beside its own work (from null: none; first and rows_per_block are its own).
+struct Realigned {
+    const void* from = nullptr;
+    int64_t ld = 0;
+    void* to = nullptr;
+    int64_t pitch = 8, cols = 0, rows = 0;
+    unsigned first = 0, rows_per_block = 1;
+};
+cudaError_t launch_act8_decode(const Act8Tensor& a, void* y, int dtype, int64_t ldy, cudaStream_t stream,
+                               const Realigned& beside = Realigned());
 
 cudaError_t launch_block_norm(const pwlq_block_norm_args& a, cudaStream_t stream);
 size_t block_norm_backward_workspace(int64_t rows, int64_t cols, int64_t gate_rows);

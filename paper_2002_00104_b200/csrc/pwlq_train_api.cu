@@ -169,7 +169,7 @@ int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outpu
     if (int rc = check_size(rows, cols)) return rc;
     if (!is_dtype(dtype) || !is_dtype(dw_dtype) || (dw_dtype != PWLQ_F32 && dw_dtype != dtype))
         return PWLQ_ERR_INVALID_ARG;
-    if (dtype == PWLQ_F32 || rows * ((cols + 2047) / 2048) > kMaxRows) return PWLQ_ERR_UNSUPPORTED;
+    if (dtype == PWLQ_F32 || rows * ((cols + 2047) / 2048 + 1) > kMaxRows) return PWLQ_ERR_UNSUPPORTED;
     if (bad_tensor(dy, dtype, lddy, rows, outputs) || bad_format(group, ratio) ||
         bad_codes(codes, ldc, ranges, rows, cols) || bad_tensor(dw, dw_dtype, lddw, outputs, cols))
         return PWLQ_ERR_INVALID_ARG;

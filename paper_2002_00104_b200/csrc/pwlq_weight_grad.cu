@@ -185,6 +185,7 @@ __device__ __forceinline__ void put_block(float* v, float (*turn)[33], W* to, in
 #pragma unroll
     for (int i = 0; i < 32; ++i) turn[lane][i] = v[i];
     __syncwarp();
+#pragma unroll 8
     for (int i = 0; i < 32; ++i) {
         const float r = turn[i][lane];
         if (i < rows && lane < cols) {
@@ -337,14 +338,6 @@ __global__ void __launch_bounds__(256) weight_grad_pieces_kernel(const __grid_co
         put4(r, static_cast<T*>(p.w.dw) + n * p.w.lddw + k, valid, p.vec_out, p.w.accumulate);
 }
 
-// dy with rows that start on 16-byte boundaries, for a dy whose rows do not (TMA's condition).
-__global__ void __launch_bounds__(256)
-realign_kernel(const uint16_t* from, int64_t ld, uint16_t* to, int64_t pitch, int64_t cols) {
-    const int64_t row = blockIdx.x;
-    for (int64_t c = threadIdx.x; c < pitch; c += 256)
-        to[row * pitch + c] = c < cols ? from[row * ld + c] : (uint16_t)0;
-}
-
 // dw without rows: zeros, or left as it is.
 template <typename W>
 __global__ void clear_kernel(W* dw, int64_t ld, int64_t cols) {
@@ -443,20 +436,25 @@ cudaError_t launch(const WeightGrad& w, void* workspace, cudaStream_t stream) {
     p.pieces = static_cast<float*>(workspace);
 
     unsigned char* at = static_cast<unsigned char*>(workspace) + piece_bytes(w.rows, w.outputs, w.x.cols);
+    // TMA wants rows on 16-byte boundaries: a dy without is copied while the checkpoint is decoded
     const void* dy = w.dy;
     int64_t pitch = w.lddy;
+    Realigned copy;
     if (!rows_aligned(w.dy, w.lddy, sizeof(T))) {
         pitch = realigned_pitch(w.outputs);
-        realign_kernel<<<(unsigned)w.rows, 256, 0, stream>>>(static_cast<const uint16_t*>(w.dy), w.lddy,
-                                                             reinterpret_cast<uint16_t*>(at), pitch, w.outputs);
-        if (cudaError_t e = cudaGetLastError()) return e;
+        copy.from = w.dy;
+        copy.ld = w.lddy;
+        copy.to = at;
+        copy.pitch = pitch;
+        copy.cols = w.outputs;
+        copy.rows = w.rows;
         dy = at;
         at += copy_bytes(w.rows, w.outputs);
     }
     CUtensorMap map, xmap;
     if (cudaError_t e = map_columns<T>(map, dy, w.outputs, w.rows, pitch)) return e;
     const int64_t xpitch = realigned_pitch(w.x.cols);
-    if (cudaError_t e = launch_act8_decode(w.x, at, w.dtype, xpitch, stream)) return e;
+    if (cudaError_t e = launch_act8_decode(w.x, at, w.dtype, xpitch, stream, copy)) return e;
     if (cudaError_t e = map_columns<T>(xmap, at, w.x.cols, w.rows, xpitch)) return e;
     if (cudaError_t e = cudaFuncSetAttribute(weight_grad_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              (int)kSmemBytes))
