@@ -1,4 +1,5 @@
-"""Builds ``libpwlq.so`` (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds ``libpwlq.so`` (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and the PyTorch module of
+the training calls with the host compiler."""
 from __future__ import annotations
 
 import os
@@ -10,6 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpwlq.so")
 PEAK_LIB = os.path.join(HERE, "libpwlq_peak.so")     # FP32 micro-benchmark, loaded by bench.py only
 PEAK_SOURCES = ["fp32_peak.cu"]
+CALLS_LIB = os.path.join(HERE, "_pwlq_calls.so")     # imported as a Python module
+CALLS_SOURCE = "pwlq_calls.cpp"
 SOURCES = ["pwlq_api.cu", "pwlq_absmax.cu", "pwlq_search.cu", "pwlq_quantize.cu",
            "pwlq_noalloc.cu", "pwlq_select.cu", "pwlq_search2.cu", "pwlq_bias.cu", "pwlq_rowmap.cu",
            "pwlq_act8.cu", "pwlq_block_norm.cu", "pwlq_weight_grad.cu", "pwlq_train_api.cu"]
@@ -41,12 +44,35 @@ def _nvcc(sources, lib: str, verbose: bool) -> None:
         print(res.stderr)
 
 
+def _calls(verbose: bool) -> None:
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")), "..")
+    include = [os.path.join(root, "include"), os.path.join(root, "include/torch/csrc/api/include"),
+               sysconfig.get_paths()["include"], os.path.join(cuda, "include")]
+    # the system compiler: the module has to share one libstdc++ with PyTorch
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+    cmd += [a for i in include for a in ("-isystem", i)]
+    cmd += [os.path.join(CSRC, CALLS_SOURCE), "-o", CALLS_LIB, "-L" + os.path.join(root, "lib"),
+            "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
+    if verbose:
+        print(res.stderr)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compiles the library (and the benchmark's FP32 micro-benchmark) if a source is newer."""
     if force or _stale(LIB):
         _nvcc(SOURCES, LIB, verbose)
     if force or _stale(PEAK_LIB):
         _nvcc(PEAK_SOURCES, PEAK_LIB, verbose)
+    if force or _stale(CALLS_LIB):
+        _calls(verbose)
     return LIB
 
 

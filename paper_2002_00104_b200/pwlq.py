@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import os
-import struct
 from typing import Optional
 
 import torch
@@ -122,7 +121,7 @@ class PwlqError(RuntimeError):
 
 def load_library(path: Optional[str] = None) -> ctypes.CDLL:
     """Loads the C-ABI library; raises if it has not been built (no fallback exists)."""
-    global _lib
+    global _lib, _calls_module
     if _lib is None or path is not None:
         path = path or _LIB_PATH
         if not os.path.exists(path):
@@ -133,7 +132,7 @@ def load_library(path: Optional[str] = None) -> ctypes.CDLL:
         for name, (res, args) in {**_SIGNATURES, **_TEST_HOOKS}.items():
             fn = getattr(lib, name)
             fn.restype, fn.argtypes = res, args
-        _lib = lib
+        _lib, _calls_module = lib, None
     return _lib
 
 
@@ -812,12 +811,32 @@ def encode_host_unsigned(x_host, row_offsets_host, C, max_n, bits, ratios_host, 
 
 
 # ---------------------------------------------------------------- training on 8-bit checkpoints
-# These calls are made once per layer and step, often on few rows, so what they do on the host is
-# kept short: one look at each tensor's attributes, and argument blocks packed in one go.
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
-    lambda device: torch.cuda.current_stream(device).cuda_stream)
+_calls_module = None
+
+
+def _calls():
+    """The compiled module that takes these calls' tensors apart (``csrc/pwlq_calls.cpp``)."""
+    global _calls_module
+    if _calls_module is None:
+        lib = load_library()
+        try:
+            from . import _pwlq_calls as module
+        except ImportError as e:
+            raise RuntimeError("_pwlq_calls.so is missing or does not fit this PyTorch: build it with "
+                               "`python -m paper_2002_00104_b200.build`") from e
+        entries = ("pwlq_act8_encode", "pwlq_act8_decode", "pwlq_block_norm",
+                   "pwlq_block_norm_backward_workspace_bytes", "pwlq_block_norm_backward",
+                   "pwlq_act8_weight_grad_workspace_bytes", "pwlq_act8_weight_grad")
+        module.init(tuple(ctypes.cast(getattr(lib, name), _P).value for name in entries), PwlqError)
+        _calls_module = module
+    return _calls_module
+
+
+def _dtype_code(dtype) -> int:
+    if dtype not in _DTYPES:
+        raise ValueError("values are float32, bfloat16 or float16")
+    return _DTYPES[dtype]
 
 
 class Act8:
@@ -862,76 +881,28 @@ def _act8_bytes(rows: int, cols: int, group: int) -> int:
     return (rows * (-(-cols // 16) * 16 + 4 * -(-cols // group)) + 31) // 32 * 32
 
 
-def _home(t: torch.Tensor, what: str) -> int:
-    """Device index of a call's first tensor, which has to be the current device: the library
-    launches there."""
-    device = t.get_device()
-    if device < 0 or device != _device():
-        raise ValueError(f"{what} must be on the current CUDA device (cuda:{_device()}), "
-                         f"it is on {t.device}")
-    return device
-
-
-def _matrix(t: torch.Tensor, what: str, shape, dtype, device):
-    """(data pointer, row pitch) of a tensor of this shape, type and device with adjacent values in
-    its rows."""
-    if t.shape != shape or t.dtype != dtype or t.get_device() != device:
-        raise ValueError(f"{what} must be {list(shape)} of {dtype} on cuda:{device}, "
-                         f"got {list(t.shape)} of {t.dtype} on {t.device}")
-    if t.is_contiguous():
-        return t.data_ptr(), shape[1]
-    pitch, step = t.stride()
-    if shape[1] > 1 and step != 1:
-        raise ValueError(f"{what}: the values of a row must be adjacent")
-    if shape[0] < 2:
-        pitch = shape[1]
-    elif pitch < shape[1]:
-        raise ValueError(f"{what}: rows overlap (a broadcast tensor must be made whole first)")
-    return t.data_ptr(), pitch
-
-
-def _shape2(t: torch.Tensor, what: str):
-    if t.dim() != 2 or t.dtype not in _DTYPES:
-        raise ValueError(f"{what} must be a [rows, cols] tensor of float32, bfloat16 or float16")
-    return t.shape
-
-
-def _vector(t: torch.Tensor, what: str, shape, dtype, device):
-    if t.shape != shape or t.dtype != dtype or t.get_device() != device or not t.is_contiguous():
-        raise ValueError(f"{what} must be contiguous {list(shape)} of {dtype} on cuda:{device}, "
-                         f"got {list(t.shape)} of {t.dtype} on {t.device}")
-    return t.data_ptr()
-
-
-def _like(t: torch.Tensor):
-    """Uninitialised contiguous tensor of t's shape and type."""
-    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
-
-
 def _on(stream):
     """What a call does on a stream other than the current one: its outputs and workspaces then
     belong to that stream too, so that their memory is not handed on before it has run."""
     return torch.cuda.stream(stream)
 
 
-def _act8(a: Act8, device, rows=None, cols=None):
-    """(codes pointer, pitch, ranges pointer) of a checkpoint, checked against its own layout."""
-    if rows is not None and (a.rows != rows or (cols is not None and a.cols != cols)):
-        raise ValueError(f"the checkpoint is of [{a.rows}, {a.cols}], not [{rows}, {cols}]")
+def _act8(a: Act8):
+    """(a tensor of the checkpoint's, codes pointer, pitch, ranges pointer), checked against its own
+    layout."""
     memory = a._memory
-    if memory is not None and memory.get_device() == device:
+    if memory is not None:
         pitch = -(-a.cols // 16) * 16
         at = memory.data_ptr() + a._at
-        return at, pitch, at + a.rows * pitch
-    codes, ranges = a.codes, a.ranges
-    if (codes.dtype != torch.uint8 or codes.dim() != 2 or codes.get_device() != device or
+        return memory, at, pitch, at + a.rows * pitch
+    codes, ranges = a._codes, a._ranges
+    if (codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_cuda or
             not codes.is_contiguous() or codes.shape[1] < a.cols or codes.shape[1] % 16 or
-            ranges.dtype != torch.float32 or ranges.get_device() != device or
+            ranges.dtype != torch.float32 or ranges.device != codes.device or
             not ranges.is_contiguous() or ranges.shape != (codes.shape[0], -(-a.cols // a.group))):
-        raise ValueError(f"not a checkpoint on cuda:{device}: codes must be contiguous uint8 "
-                         "[rows, pitch] with a pitch that is a multiple of 16, ranges float32 "
-                         "[rows, groups]")
-    return codes.data_ptr(), codes.shape[1], ranges.data_ptr()
+        raise ValueError("not a checkpoint: codes must be contiguous uint8 [rows, pitch] on a CUDA "
+                         "device with a pitch that is a multiple of 16, ranges float32 [rows, groups]")
+    return codes, codes.data_ptr(), codes.shape[1], ranges.data_ptr()
 
 
 def act8_empty(rows: int, cols: int, group: int = 128, ratio: float = 0.5, device=None) -> Act8:
@@ -945,15 +916,14 @@ def act8_encode(x, group=128, ratio=0.5, out: Optional[Act8] = None, stream=None
     if stream is not None:
         with _on(stream):
             return act8_encode(x, group, ratio, out)
-    device = _home(x, "x")
-    shape = rows, cols = _shape2(x, "x")
-    ptr, pitch = _matrix(x, "x", shape, x.dtype, device)
     if out is None:
-        out = act8_empty(rows, cols, group, ratio, x.device)
-    codes, ldc, ranges = _act8(out, device, rows, cols)
-    _check(load_library().pwlq_act8_encode(ptr, _DTYPES[x.dtype], rows, cols, pitch, out.group,
-                                           out.ratio, codes, ldc, ranges, _raw_stream(device)),
-           "pwlq_act8_encode")
+        memory = _calls().encode(x, group, ratio, 0, 0, 0, 0)
+        return Act8._inside(memory, 0, *x.shape, group, ratio)
+    kept, codes, ldc, ranges = _act8(out)
+    if x.shape != (out.rows, out.cols) or x.device != kept.device:
+        raise ValueError(f"the checkpoint is of [{out.rows}, {out.cols}] on {kept.device}, x is "
+                         f"{list(x.shape)} on {x.device}")
+    _calls().encode(x, out.group, out.ratio, codes, ldc, ranges, 1)
     return out
 
 
@@ -962,30 +932,17 @@ def act8_decode(saved: Act8, dtype=torch.float32, out=None, stream=None):
     if stream is not None:
         with _on(stream):
             return act8_decode(saved, dtype, out)
-    memory = saved._memory if saved._memory is not None else saved.codes
-    device = _home(memory, "the checkpoint")
-    codes, ldc, ranges = _act8(saved, device)
-    shape = rows, cols = saved.rows, saved.cols
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=memory.device)
-        ptr, pitch = out.data_ptr(), cols
-    else:
-        dtype = out.dtype
-        ptr, pitch = _matrix(out, "out", shape, dtype, device)
-    if dtype not in _DTYPES:
-        raise ValueError("values are float32, bfloat16 or float16")
-    _check(load_library().pwlq_act8_decode(codes, ldc, ranges, rows, cols, saved.group, saved.ratio,
-                                           ptr, _DTYPES[dtype], pitch, _raw_stream(device)),
-           "pwlq_act8_decode")
-    return out
+    memory, codes, ldc, ranges = _act8(saved)
+    return _calls().decode(memory, codes, ldc, ranges, saved.rows, saved.cols, saved.group,
+                           saved.ratio, _dtype_code(dtype), out)
 
 
 class BlockNormSaved:
     """What ``block_norm`` keeps for ``block_norm_backward``: the checkpoints ``r`` and ``f`` and the
     norms' factors ``r_rstd`` and ``f_rstd`` (None where the call needs none), all in one piece of
     memory, and the weights and gate it was given."""
-    __slots__ = ("pre_weight", "post_weight", "gate", "shape", "dtype", "has_f", "group", "ratio",
-                 "_memory", "_block", "_f_at", "_rstd_at")
+    __slots__ = ("pre_weight", "post_weight", "gate", "shape", "has_f", "group", "ratio", "_memory",
+                 "_block", "_f_at", "_rstd_at")
 
     def _checkpoint(self, at: int) -> Act8:
         return Act8._inside(self._memory, at, *self.shape, self.group, self.ratio)
@@ -1012,11 +969,6 @@ class BlockNormSaved:
         return self._factors(at) if self.post_weight is not None else None
 
 
-# pwlq_block_norm_args and pwlq_block_norm_grads of include/pwlq.h
-_BLOCK_ARGS = struct.Struct("4q QqQqQQQqqq 3d QqQq qdq QQQQQQ")
-_BLOCK_GRADS = struct.Struct("QqQqQqQq QQQ Qq")
-
-
 def block_norm(x, f=None, pre_weight=None, post_weight=None, gate=None, gate_tokens=None,
                residual_scale=1.0, eps=1e-6, weight_offset=0.0, save=None, out=None, stream=None):
     """``pwlq_block_norm``: r = residual_scale * x + gate * N(f; post_weight), h = N(r; pre_weight).
@@ -1029,68 +981,19 @@ def block_norm(x, f=None, pre_weight=None, post_weight=None, gate=None, gate_tok
         with _on(stream):
             return block_norm(x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps,
                               weight_offset, save, out)
-    device = _home(x, "x")
-    shape = rows, cols = _shape2(x, "x")
-    dtype = x.dtype
-    xp, ldx = _matrix(x, "x", shape, dtype, device)
-    fp = ldf = pre = post = gp = ldg = gate_rows = every = hp = ldh = 0
-    if f is not None:
-        fp, ldf = _matrix(f, "f", shape, dtype, device)
-    some = pre_weight if pre_weight is not None else post_weight if post_weight is not None else gate
-    wtype = dtype
-    if some is not None:
-        wtype = some.dtype
-        if wtype != dtype and wtype != torch.float32:
-            raise ValueError("weights and gate must be of x's type or float32")
-        wshape = (cols,)
-        if pre_weight is not None:
-            pre = _vector(pre_weight, "pre_weight", wshape, wtype, device)
-        if post_weight is not None:
-            post = _vector(post_weight, "post_weight", wshape, wtype, device)
-        if gate is not None:
-            gate_rows = gate.shape[0]
-            gp, ldg = _matrix(gate, "gate", (gate_rows, cols), wtype, device)
-            every = int(gate_tokens) if gate_tokens else max(-(-rows // max(gate_rows, 1)), 1)
+    group, ratio = save if save is not None else (0, 0.0)
     r, h = out if out is not None else (None, None)
-    if r is None:
-        r = _like(x)
-        rp, ldr = r.data_ptr(), cols
-    else:
-        rp, ldr = _matrix(r, "r", shape, dtype, device)
-    if pre_weight is None:
-        h = None
-    elif h is None:
-        h = _like(x)
-        hp, ldh = h.data_ptr(), cols
-    else:
-        hp, ldh = _matrix(h, "h", shape, dtype, device)
+    if save is not None and group < 1:
+        raise PwlqError(ERR_INVALID_ARG, "checkpoint group")
+    r, h, memory, block, f_at, rstd_at = _calls().block_norm(
+        x, f, pre_weight, post_weight, gate, gate_tokens or 0, residual_scale, eps, weight_offset,
+        group, ratio, r, h)
     if save is None:
-        block = _BLOCK_ARGS.pack(rows, cols, _DTYPES[dtype], _DTYPES[wtype], xp, ldx, fp, ldf, post,
-                                 pre, gp, ldg, gate_rows, every, residual_scale, eps, weight_offset,
-                                 rp, ldr, hp, ldh, 0, 0.0, 0, 0, 0, 0, 0, 0, 0)
-        _check(load_library().pwlq_block_norm(block, _raw_stream(device)), "pwlq_block_norm")
         return r, h, None
     kept = BlockNormSaved()
     kept.pre_weight, kept.post_weight, kept.gate = pre_weight, post_weight, gate
-    kept.shape, kept.dtype, kept.has_f = shape, dtype, f is not None
-    kept.group, kept.ratio = group, ratio = int(save[0]), float(save[1])
-    size, ldc = _act8_bytes(rows, cols, group), -(-cols // 16) * 16
-    kept._f_at = f_at = size if pre_weight is not None else 0
-    kept._rstd_at = rstd_at = f_at + (size if gate is not None or post_weight is not None else 0)
-    kept._memory = torch.empty(rstd_at + 8 * rows, dtype=torch.uint8, device=x.device)
-    base = kept._memory.data_ptr()
-    rc = rr = rsp = fc = fr = fsp = 0
-    if pre_weight is not None:
-        rc, rr, rsp = base, base + rows * ldc, base + rstd_at
-    if gate is not None or post_weight is not None:
-        fc, fr = base + f_at, base + f_at + rows * ldc
-        if post_weight is not None:
-            fsp = base + rstd_at + 4 * rows
-    kept._block = block = _BLOCK_ARGS.pack(
-        rows, cols, _DTYPES[dtype], _DTYPES[wtype], xp, ldx, fp, ldf, post, pre, gp, ldg, gate_rows,
-        every, residual_scale, eps, weight_offset, rp, ldr, hp, ldh, group, ratio, ldc, rc, rr, rsp,
-        fc, fr, fsp)
-    _check(load_library().pwlq_block_norm(block, _raw_stream(device)), "pwlq_block_norm")
+    kept.shape, kept.has_f, kept.group, kept.ratio = x.shape, f is not None, group, ratio
+    kept._memory, kept._block, kept._f_at, kept._rstd_at = memory, block, f_at, rstd_at
     return r, h, kept
 
 
@@ -1100,46 +1003,9 @@ def block_norm_backward(saved: BlockNormSaved, dh=None, dr=None, workspace=None,
     if stream is not None:
         with _on(stream):
             return block_norm_backward(saved, dh, dr, workspace)
-    some = dh if dh is not None else dr
-    pre, post, gate = saved.pre_weight, saved.post_weight, saved.gate
-    if some is None or (dh is None) != (pre is None):
-        raise ValueError("dh is needed exactly where the forward call had a pre_weight, dr where it "
-                         "had none")
-    shape, dtype = saved.shape, saved.dtype
-    cols = shape[1]
-    device = _home(some, "the gradient")
-    memory = saved._memory
-    if memory.get_device() != device:
-        raise ValueError(f"the forward call ran on {memory.device}, the gradient is on {some.device}")
-    dhp = lddh = drp = lddr = dfp = dprep = dpostp = dgatep = wsp = need = gate_rows = 0
-    if dh is not None:
-        dhp, lddh = _matrix(dh, "dh", shape, dtype, device)
-    if dr is not None:
-        drp, lddr = _matrix(dr, "dr", shape, dtype, device)
-    df = dpre = dpost = dgate = None
-    dx = _like(some)
-    if saved.has_f:
-        df = _like(some)
-        dfp = df.data_ptr()
-    if pre is not None:
-        dpre = _like(pre)
-        dprep = dpre.data_ptr()
-    if post is not None:
-        dpost = _like(post)
-        dpostp = dpost.data_ptr()
-    if gate is not None:
-        dgate = _like(gate)
-        dgatep, gate_rows = dgate.data_ptr(), gate.shape[0]
-    lib = load_library()
-    if dprep or dpostp or dgatep:
-        if workspace is None:
-            workspace = memory.new_empty(
-                lib.pwlq_block_norm_backward_workspace_bytes(shape[0], cols, gate_rows))
-        wsp, need = _dev(workspace, torch.uint8, "workspace"), workspace.numel()
-    grads = _BLOCK_GRADS.pack(dhp, lddh, drp, lddr, dx.data_ptr(), cols, dfp, cols, dprep, dpostp,
-                              dgatep, wsp, need)
-    _check(lib.pwlq_block_norm_backward(saved._block, grads, _raw_stream(device)),
-           "pwlq_block_norm_backward")
+    dx, df, dpre, dpost, dgate = _calls().block_norm_backward(
+        saved._block, saved._memory, saved.has_f, dh, dr, saved.pre_weight, saved.post_weight,
+        saved.gate, workspace)
     return {"dx": dx, "df": df, "dpre": dpre, "dpost": dpost, "dgate": dgate}
 
 
@@ -1156,30 +1022,7 @@ def act8_weight_grad(dy, saved: Act8, dtype=None, out=None, accumulate=False, wo
     if stream is not None:
         with _on(stream):
             return act8_weight_grad(dy, saved, dtype, out, accumulate, workspace)
-    device = _home(dy, "dy")
-    shape = rows, outputs = _shape2(dy, "dy")
-    dyp, lddy = _matrix(dy, "dy", shape, dy.dtype, device)
-    codes, ldc, ranges = _act8(saved, device, rows)
-    cols = saved.cols
-    if out is None:
-        if accumulate:
-            raise ValueError("accumulate needs out")
-        dtype = dtype or dy.dtype
-        out = torch.empty((outputs, cols), dtype=dtype, device=dy.device)
-        dwp, lddw = out.data_ptr(), cols
-    else:
-        dtype = out.dtype
-        dwp, lddw = _matrix(out, "out", (outputs, cols), dtype, device)
-    if dtype not in _DTYPES:
-        raise ValueError("dw is float32, bfloat16 or float16")
-    lib = load_library()
-    if workspace is None:
-        need = lib.pwlq_act8_weight_grad_workspace_bytes(rows, outputs, cols,
-                                                         int((dyp | lddy * 2) % 16 == 0))
-        workspace = (saved._memory if saved._memory is not None else saved.codes).new_empty(need)
-    _check(lib.pwlq_act8_weight_grad(dyp, _DTYPES[dy.dtype], rows, outputs, lddy, codes, ldc, ranges,
-                                     cols, saved.group, saved.ratio, dwp, _DTYPES[dtype], lddw,
-                                     int(accumulate), _dev(workspace, torch.uint8, "workspace"),
-                                     workspace.numel(), _raw_stream(device)),
-           "pwlq_act8_weight_grad")
-    return out
+    memory, codes, ldc, ranges = _act8(saved)
+    return _calls().weight_grad(dy, memory, codes, ldc, ranges, saved.rows, saved.cols, saved.group,
+                                saved.ratio, -1 if dtype is None else _dtype_code(dtype), out,
+                                accumulate, workspace)

@@ -1,5 +1,6 @@
 """Arguments of the training operators are checked on the host, before any CUDA call."""
 import os
+import struct
 
 import pytest
 
@@ -12,6 +13,10 @@ def lib():
     build.build()
     return pwlq.load_library()
 
+
+# pwlq_block_norm_args and pwlq_block_norm_grads of include/pwlq.h
+BLOCK_ARGS = struct.Struct("4q QqQqQQQqqq 3d QqQq qdq QQQQQQ")
+BLOCK_GRADS = struct.Struct("QqQqQqQq QQQ Qq")
 
 A, B, C = (0x10000 * i for i in (1, 2, 3))
 
@@ -41,12 +46,11 @@ FIELDS = ("rows cols dtype wtype x ldx f ldf post pre gate ldgate gate_rows gate
 
 
 def _block(**kw):
-    from paper_2002_00104_b200 import pwlq
     v = dict(rows=4, cols=100, dtype=0, wtype=0, x=A, ldx=100, f=B, ldf=100, post=C, pre=C, gate=A, ldgate=100,
              gate_rows=2, gate_tokens=2, scale=1.0, eps=1e-6, offset=0.0, r=A, ldr=100, h=B, ldh=100, group=64,
              ratio=0.5, ldc=112, r_codes=A, r_ranges=A, r_rstd=A, f_codes=A, f_ranges=A, f_rstd=A)
     v.update(kw)
-    return pwlq._BLOCK_ARGS.pack(*(v[k] for k in FIELDS))
+    return BLOCK_ARGS.pack(*(v[k] for k in FIELDS))
 
 
 def test_block_norm(lib):
@@ -74,7 +78,7 @@ def test_block_norm_backward(lib):
         v = dict(dh=A, lddh=100, dr=B, lddr=100, dx=A, lddx=100, df=B, lddf=100, dpre=C, dpost=C, dgate=C,
                  ws=A, bytes=need)
         v.update(kw)
-        return lib.pwlq_block_norm_backward(block or _block(), pwlq._BLOCK_GRADS.pack(*(v[k] for k in names)),
+        return lib.pwlq_block_norm_backward(block or _block(), BLOCK_GRADS.pack(*(v[k] for k in names)),
                                             None)
 
     assert lib.pwlq_block_norm_backward(_block(), None, None) == pwlq.ERR_INVALID_ARG
@@ -105,10 +109,23 @@ def test_weight_grad(lib):
     assert rc(16, need - 1) == rc(15, None) == pwlq.ERR_WORKSPACE
 
 
+def test_the_compiled_calls_refuse_what_is_no_cuda_tensor(lib):
+    import torch
+    from paper_2002_00104_b200 import pwlq
+    x = torch.zeros(4, 64)
+    for bad in (lambda: pwlq.act8_encode(x), lambda: pwlq.act8_encode(None),
+                lambda: pwlq.block_norm(x, x, pre_weight=x[0]),
+                lambda: pwlq.act8_weight_grad(x, pwlq.Act8(torch.zeros(4, 64, dtype=torch.uint8), x, 64, 64, 0.5)),
+                lambda: pwlq.act8_decode(pwlq.Act8(torch.zeros(4, 64, dtype=torch.uint8), x, 64, 64, 0.5))):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises((TypeError, ValueError)):
+        pwlq._calls().encode(x)
+
+
 def test_packed_blocks_have_the_header_s_size(lib, tmp_path):
     import shutil
     import subprocess
-    from paper_2002_00104_b200 import pwlq
     cc = shutil.which("gcc") or pytest.skip("no C compiler")
     src = tmp_path / "size.c"
     src.write_text('#include "pwlq.h"\n#include <stdio.h>\nint main(void) { printf("%zu %zu", '
@@ -116,4 +133,4 @@ def test_packed_blocks_have_the_header_s_size(lib, tmp_path):
     exe = str(tmp_path / "size")
     subprocess.run([cc, "-I", os.path.join(ROOT, "include"), str(src), "-o", exe], check=True)
     sizes = subprocess.run([exe], capture_output=True, text=True, check=True).stdout.split()
-    assert [int(v) for v in sizes] == [pwlq._BLOCK_ARGS.size, pwlq._BLOCK_GRADS.size]
+    assert [int(v) for v in sizes] == [BLOCK_ARGS.size, BLOCK_GRADS.size]
