@@ -485,7 +485,9 @@ struct GradParams {
     pwlq_block_norm_grads g;
     int64_t rows_per_cta;
     float *dpre, *dpost, *dgate;          // workspace; nullptr: not wanted
-    unsigned gathered;                    // where dpost gathers in shared memory (with a gate)
+    unsigned gathered;                    // where dpost gathers in shared memory (with gates)
+    bool gates;                           // several gates; one gate for all rows is dealt with where A
+                                          // has been added up, and `dpost` holds A then
 };
 
 // What a CTA does with A of eight columns from c on (the first `valid` of which exist) once it is past
@@ -634,7 +636,7 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
         for (int which = 0; which < 2; ++which) sums.clear(which);
     }
     float* const gathered = reinterpret_cast<float*>(smem + p.gathered);
-    const bool gates = q.a.gate && (p.dpost || p.dgate);
+    const bool gates = p.gates && (p.dpost || p.dgate);
     if (gates && p.dpost) clear_gathered<VC>(gathered);
     auto finish = [&](int64_t gate) {
 #pragma unroll
@@ -831,7 +833,7 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     u64 dpre[kP] = {}, inner[kP] = {};
     allow_dependents();
     float* const gathered = reinterpret_cast<float*>(smem + p.gathered);
-    const bool gates = q.a.gate && (p.dpost || p.dgate);
+    const bool gates = p.gates && (p.dpost || p.dgate);
     if (gates && p.dpost && live)
 #pragma unroll
         for (int k = 0; k < 2 * kP; ++k) gathered[c + k] = 0.0f;
@@ -1078,39 +1080,12 @@ block_norm_backward_narrow_kernel(const __grid_constant__ GradParams p, int lane
             for (int k = 0; k < kP; k += 4)
                 store32(p.dpre + (int64_t)blockIdx.x * q.a.cols + c + 2 * k, raw32(dpre + k, 0.0f));
     }
-    if (!p.dpost && !p.dgate) return;
+    if (!p.dpost) return;
     reduce(inner);
-    if (!mine) return;
-    if (!q.a.gate) {
+    if (mine)
 #pragma unroll
         for (int k = 0; k < kP; k += 4)
             store32(p.dpost + (int64_t)blockIdx.x * q.a.cols + c + 2 * k, raw32(inner + k, 0.0f));
-        return;
-    }
-    // the gate's rows are everybody's: shares of the CTAs' first gate, unless there is one CTA
-    u64 w[kP], v[kP];
-    if (p.dgate) {
-        if (post) post_w.get(w, q.offset);
-#pragma unroll
-        for (int k = 0; k < kP; ++k) v[k] = post ? mul2(inner[k], w[k]) : inner[k];
-        float f[2 * kP];
-#pragma unroll
-        for (int k = 0; k < kP; ++k) unpack2(v[k], f[2 * k], f[2 * k + 1]);
-#pragma unroll
-        for (int k = 0; k < 2 * kP; k += 8) {
-            if (gridDim.x > 1) put8<true>(f + k, p.dgate + 2 * (int64_t)blockIdx.x * q.a.cols + c + k, 8);
-            else if (q.wf32) put8<true>(f + k, static_cast<float*>(p.g.dgate) + c + k, 8);
-            else put8<true>(f + k, static_cast<T*>(p.g.dgate) + c + k, 8);
-        }
-    }
-    if (p.dpost) {
-        gate_w.get(w);
-#pragma unroll
-        for (int k = 0; k < kP; ++k) v[k] = mul2(inner[k], w[k]);
-#pragma unroll
-        for (int k = 0; k < kP; k += 4)
-            store32(p.dpost + (int64_t)blockIdx.x * q.a.cols + c + 2 * k, raw32(v + k, 0.0f));
-    }
 }
 
 // Adds the CTAs' sums of V columns per thread (4 where the columns allow it): 64 parts of the CTAs side
@@ -1124,6 +1099,11 @@ template <int V> struct alignas(4 * V) Columns {
         const Columns x = *reinterpret_cast<const Columns*>(p);
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] += x.v[k];
+    }
+    template <typename W> __device__ __forceinline__ void times(const W* w, int c, float offset) {
+        if (!w) return;
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] *= to_f32(w[c + k]) + offset;
     }
     template <typename W> __device__ __forceinline__ void put(W* to) const {
 #pragma unroll
@@ -1182,7 +1162,7 @@ block_norm_sums_kernel(const __grid_constant__ GradParams p, int ctas, bool few,
         pitch = 2 * (int64_t)cols;
         first = from > lo * per_cta ? cols : 0;
     }
-    if (!out) return;
+    if (blockIdx.y == 0 ? !out : !p.dpost && blockIdx.y == 1) return;
     Columns<V> s = {};
     if (c < cols) {
 #pragma unroll 8
@@ -1200,7 +1180,14 @@ block_norm_sums_kernel(const __grid_constant__ GradParams p, int ctas, bool few,
         }
         __syncthreads();
     }
-    if (threadIdx.y == 0 && c < cols) s.put(out + c);
+    if (threadIdx.y != 0 || c >= cols) return;
+    if (blockIdx.y == 1 && a.gate && !p.gates) {   // s is A, of all rows
+        Columns<V> x = s;
+        x.times(static_cast<const W*>(a.post_weight), c, p.q.offset);
+        if (dgate) x.put(dgate + c);
+        s.times(static_cast<const W*>(a.gate), c, 0.0f);
+    }
+    if (out) s.put(out + c);
 }
 
 // ------------------------------------------------------------------------------ launching
@@ -1355,7 +1342,7 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
     const bool vec = rows_aligned(g.dh, g.lddh, kSize) && rows_aligned(g.dr, g.lddr, kSize) &&
                      rows_aligned(g.dx, g.lddx, kSize) && rows_aligned(g.df, g.lddf, kSize) &&
                      rows_aligned(g.dgate, a.cols, wsize) && a.cols % 4 == 0 && weights_aligned(a);
-    const bool gathers = a.gate && g.dpost;
+    const bool gathers = p.gates && g.dpost;
     if (a.cols > 8192) {
         const int threads = threads_for(a.cols, 32);
         p.gathered = (unsigned)((size_t)2 * 4 * 8 * sizeof(float) * threads);     // at most 128 KB of sums
@@ -1383,9 +1370,12 @@ cudaError_t sums(const GradParams& p, int64_t ctas, cudaStream_t stream) {
     const pwlq_block_norm_args& a = p.q.a;
     int64_t kinds = 2;
     bool few = true;
-    if (p.g.dgate) {
+    if (p.g.dgate && p.gates) {
         few = a.gate_tokens / p.rows_per_cta + 2 <= kFewShares;
         kinds = few ? 3 : 3 + (a.rows + a.gate_tokens - 1) / a.gate_tokens;
+    } else if (p.g.dgate && a.gate_rows > 1) {
+        kinds = 3;                                 // zeros for the others
+        few = false;
     }
     const dim3 grid((unsigned)((a.cols + kSumLanes * V - 1) / (kSumLanes * V)), (unsigned)kinds);
     return launch_dependent(block_norm_sums_kernel<W, V>, grid, dim3(kSumLanes, kSumParts), 0, stream, p, (int)ctas,
@@ -1409,8 +1399,9 @@ cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
     ctas = (a.rows + p.rows_per_cta - 1) / p.rows_per_cta;
     float* ws = static_cast<float*>(g.workspace);
     p.dpre = g.dpre ? ws : nullptr;
-    p.dpost = g.dpost ? ws + ctas * a.cols : nullptr;
-    p.dgate = g.dgate ? ws + 2 * ctas * a.cols : nullptr;
+    p.gates = a.gate && a.gate_tokens < a.rows;
+    p.dpost = g.dpost || (g.dgate && !p.gates) ? ws + ctas * a.cols : nullptr;
+    p.dgate = g.dgate && p.gates ? ws + 2 * ctas * a.cols : nullptr;
     p.gathered = 0;
     if (ctas && narrow) {
         auto* kernel = p.q.wf32 ? block_norm_backward_narrow_kernel<T, true>
