@@ -14,6 +14,7 @@
 // the boundary).
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 #include "pwlq_act8.cuh"
 #include "pwlq_pipeline.cuh"
@@ -52,6 +53,30 @@ struct CtaSum {
         v += __shfl_xor_sync(0xffffffffu, v, 1);
         half ^= 1;
         return __shfl_sync(0xffffffffu, v, 0);
+    }
+    __device__ __forceinline__ float operator()(float v) {
+        post(v);
+        return total();
+    }
+};
+// The same over a pair of CTAs of up to 16 warps each that share a row: every warp's part goes to both,
+// and the barrier is the cluster's.
+struct PairSum {
+    float (*buf)[32];                     // zero at first
+    uint32_t rank;
+    int half = 0;
+    __device__ __forceinline__ void post(float v) {
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        const int lane = threadIdx.x & 31;
+        if (lane < 2) store_cluster(peer_addr(&buf[half][rank * 16 + (threadIdx.x >> 5)], (uint32_t)lane), v);
+    }
+    __device__ __forceinline__ float total() {
+        __syncwarp();
+        cluster_sync();
+        float v = buf[half][threadIdx.x & 31];
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        half ^= 1;
+        return v;
     }
     __device__ __forceinline__ float operator()(float v) {
         post(v);
@@ -297,7 +322,7 @@ __device__ __forceinline__ void save32(const u64* v, const NormParams& q, bool l
 
 // Forward with a ring: 32 bytes of columns per thread.
 template <typename T, bool SAVE, bool WF32>
-__global__ void __maxnreg__(sizeof(T) == 2 ? 80 : 64) block_norm_ring_kernel(const __grid_constant__ NormParams q) {
+__global__ void __maxnreg__(64) block_norm_ring_kernel(const __grid_constant__ NormParams q) {
     constexpr int kP = kPairs32<T>;
     __shared__ float buf[2][32];
     __shared__ uint64_t full[kMaxStages];
@@ -493,8 +518,8 @@ struct GradParams {
 // What a CTA does with A of eight columns from c on (the first `valid` of which exist) once it is past
 // the rows of `gate`.
 template <bool VEC, typename T>
-__device__ __forceinline__ void finish_gate(const GradParams& p, int64_t gate, int64_t first, int64_t last, int c,
-                                            int valid, const u64* A, float* gathered) {
+__device__ __forceinline__ void finish_gate(const GradParams& p, int64_t cta, int64_t gate, int64_t first,
+                                            int64_t last, int c, int valid, const u64* A, float* gathered) {
     const pwlq_block_norm_args& a = p.q.a;
     if (valid <= 0) return;
     u64 w[4], v[4];
@@ -510,7 +535,7 @@ __device__ __forceinline__ void finish_gate(const GradParams& p, int64_t gate, i
         floats8(v, f);
         const int64_t from = gate * a.gate_tokens, to = min(from + a.gate_tokens, a.rows);
         if (from < first || to > last) {
-            const int64_t slot = 2 * (int64_t)blockIdx.x + (from > first);
+            const int64_t slot = 2 * cta + (from > first);
             put8<VEC>(f, p.dgate + slot * a.cols + c, valid);
         } else if (p.q.wf32) {
             put8<VEC>(f, static_cast<float*>(p.g.dgate) + gate * a.cols + c, valid);
@@ -588,22 +613,22 @@ __device__ __forceinline__ void clear_gathered(float* gathered) {
 }
 
 template <typename T>
-__device__ __forceinline__ void request_backward(const GradParams& p, Ring& ring, int stage, int64_t row) {
+__device__ __forceinline__ void request_backward(const GradParams& p, Ring& ring, int stage, int64_t row, int base) {
     const NormParams& q = p.q;
     unsigned char* to = ring.stage0 + (size_t)stage * ring.stage_bytes;
     uint64_t* bar = &ring.full[stage];
     mbar_expect_tx(bar, ring.stage_bytes);
     if (q.a.pre_weight) {
-        bulk_copy_g2s(to, static_cast<const T*>(p.g.dh) + row * p.g.lddh, q.row_bytes, bar);
+        bulk_copy_g2s(to, static_cast<const T*>(p.g.dh) + row * p.g.lddh + base, q.row_bytes, bar);
         to += q.row_bytes;
-        bulk_copy_g2s(to, q.a.r_codes + row * q.a.ldc, q.code_bytes, bar);
+        bulk_copy_g2s(to, q.a.r_codes + row * q.a.ldc + base, q.code_bytes, bar);
         to += q.code_bytes;
     }
     if (p.g.dr) {
-        bulk_copy_g2s(to, static_cast<const T*>(p.g.dr) + row * p.g.lddr, q.row_bytes, bar);
+        bulk_copy_g2s(to, static_cast<const T*>(p.g.dr) + row * p.g.lddr + base, q.row_bytes, bar);
         to += q.row_bytes;
     }
-    if (q.a.f_codes) bulk_copy_g2s(to, q.a.f_codes + row * q.a.ldc, q.code_bytes, bar);
+    if (q.a.f_codes) bulk_copy_g2s(to, q.a.f_codes + row * q.a.ldc + base, q.code_bytes, bar);
 }
 
 // Eight bytes of a row from column c on; those past the row read as 0.
@@ -644,7 +669,7 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
             const int c = (threadIdx.x + i * blockDim.x) * 8;
             u64 A[4];
             sums.get(kInner, i, A);
-            finish_gate<VEC, T>(p, gate, first, last, c, cols - c, A, gathered);
+            finish_gate<VEC, T>(p, blockIdx.x, gate, first, last, c, cols - c, A, gathered);
         }
         sums.clear(kInner);
     };
@@ -799,40 +824,52 @@ __device__ __forceinline__ void held32(const unsigned char* bytes, float m, floa
     }
 }
 
-// Backward with a ring: 32 bytes of columns per thread, sums in registers.
-template <typename T, bool WF32>
+__device__ __forceinline__ void set_rank(CtaSum&, uint32_t) {}
+__device__ __forceinline__ void set_rank(PairSum& s, uint32_t rank) { s.rank = rank; }
+
+// Backward with a ring: 32 bytes of columns per thread, sums in registers.  PAIR: a cluster of two CTAs
+// shares the rows, half the columns each (rows too wide for one CTA's registers).
+template <typename T, bool WF32, bool PAIR>
 __global__ void __launch_bounds__(512)
 block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     constexpr int kP = kPairs32<T>;
     __shared__ float buf[2][32];
     __shared__ uint64_t full[kMaxStages];
     extern __shared__ __align__(16) unsigned char smem[];
-    CtaSum cta_sum{buf};
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
+    typename std::conditional<PAIR, PairSum, CtaSum>::type cta_sum{buf};
     const NormParams& q = p.q;
-    const int64_t first = blockIdx.x * p.rows_per_cta, last = min(first + p.rows_per_cta, q.a.rows);
+    const int64_t cta = PAIR ? blockIdx.x >> 1 : blockIdx.x;
+    const int cols = PAIR ? (int)q.a.cols / 2 : (int)q.a.cols, base = (int)rank * cols;
+    const int64_t first = cta * p.rows_per_cta, last = min(first + p.rows_per_cta, q.a.rows);
     const bool pre = q.a.pre_weight, post = q.a.post_weight, has_f = q.a.f_codes, has_dr = p.g.dr;
     Ring ring{full, smem,
               (pre ? q.row_bytes + q.code_bytes : 0) + (has_dr ? q.row_bytes : 0) + (has_f ? q.code_bytes : 0),
               q.stages};
+    if (PAIR && threadIdx.x < 64) buf[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
     if (threadIdx.x == 0) {
         for (int s = 0; s < q.stages; ++s) mbar_init(&full[s], 1);
         fence_barrier_init();
         for (int s = 0; s < q.stages; ++s)
-            if (first + s < last) request_backward<T>(p, ring, s, first + s);
+            if (first + s < last) request_backward<T>(p, ring, s, first + s, base);
     }
     __syncthreads();
+    if (PAIR) {
+        set_rank(cta_sum, rank);
+        cluster_sync();                   // the other CTA writes to this one's sums
+    }
     // threads past the row repeat its last columns and neither store nor count
-    const bool live = (int)threadIdx.x * 2 * kP < (int)q.a.cols;
-    const int c = live ? (int)threadIdx.x * 2 * kP : (int)q.a.cols - 2 * kP;
+    const bool live = (int)threadIdx.x * 2 * kP < cols;
+    const int local = live ? (int)threadIdx.x * 2 * kP : cols - 2 * kP, c = base + local;
     // where this thread's part of each operand lies in a stage
-    const unsigned at_dh = c * (int)sizeof(T), at_rb = q.row_bytes + c,
-                   at_dr = (pre ? q.row_bytes + q.code_bytes : 0) + c * (int)sizeof(T),
-                   at_fb = ring.stage_bytes - q.code_bytes + c;
+    const unsigned at_dh = local * (int)sizeof(T), at_rb = q.row_bytes + local,
+                   at_dr = (pre ? q.row_bytes + q.code_bytes : 0) + local * (int)sizeof(T),
+                   at_fb = ring.stage_bytes - q.code_bytes + local;
     int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
     u64 dpre[kP] = {}, inner[kP] = {};
     allow_dependents();
-    float* const gathered = reinterpret_cast<float*>(smem + p.gathered);
+    float* const gathered = reinterpret_cast<float*>(smem + p.gathered) - base;
     const bool gates = p.gates && (p.dpost || p.dgate);
     if (gates && p.dpost && live)
 #pragma unroll
@@ -841,7 +878,7 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         if (live)
 #pragma unroll
             for (int k = 0; k < kP; k += 4)
-                finish_gate<true, T>(p, gate, first, last, c + 2 * k, 8, inner + k, gathered);
+                finish_gate<true, T>(p, cta, gate, first, last, c + 2 * k, 8, inner + k, gathered);
 #pragma unroll
         for (int k = 0; k < kP; ++k) inner[k] = 0ull;
     };
@@ -934,7 +971,7 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         if (!post) __syncthreads();
         // every thread has its values of this stage
         const int64_t ahead = row + q.stages;
-        if (threadIdx.x == 0 && ahead < last && !ring.dead) request_backward<T>(p, ring, ring.stage, ahead);
+        if (threadIdx.x == 0 && ahead < last && !ring.dead) request_backward<T>(p, ring, ring.stage, ahead, base);
         ring.next();
         if (!p.g.df || !live) continue;
         if (post)
@@ -942,13 +979,13 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
             for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rf));
         store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(e, T()));
     }
-    if (p.dpre) put(dpre, p.dpre + (int64_t)blockIdx.x * q.a.cols);
+    if (p.dpre) put(dpre, p.dpre + cta * q.a.cols);
     if (gates) finish(gate);
     if (!p.dpost) return;
     if (gates && live)
 #pragma unroll
         for (int k = 0; k < kP; ++k) inner[k] = pack2(gathered[c + 2 * k], gathered[c + 2 * k + 1]);
-    put(inner, p.dpost + (int64_t)blockIdx.x * q.a.cols);
+    put(inner, p.dpost + cta * q.a.cols);
 }
 
 // Backward of narrow rows (see block_norm_narrow_kernel), for one gate at most.  The CTA's rows are not
@@ -1248,7 +1285,6 @@ cudaError_t run(K* kernel, unsigned ctas, int threads, size_t smem, cudaStream_t
 // A ring kernel's launch: threads of 32 bytes of columns each; CTAs that share a multiprocessor, as
 // far as their registers allow (`threads_per_sm`); stages of `bytes` for each of them.
 struct RingPlan { int threads, ctas, stages; };
-constexpr int64_t kRingCols = 8192;
 // what is left of the 228 KB is cache for the weights, which every row reads again
 constexpr size_t kSmemBudget = 160 * 1024;
 RingPlan ring_plan(int64_t cols, size_t size, int threads_per_sm, size_t bytes) {
@@ -1290,10 +1326,10 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
         kernel<<<(unsigned)narrow_ctas(a.rows, lanes), kNarrowThreads, 0, stream>>>(q, lanes);
         return cudaGetLastError();
     }
-    const RingPlan ring = ring_plan(a.cols, kSize, kSize == 2 ? 768 : 1024, (a.f ? 2 : 1) * (size_t)q.row_bytes);
+    const RingPlan ring = ring_plan(a.cols, kSize, 1024, (a.f ? 2 : 1) * (size_t)q.row_bytes);
     const int64_t resident = (int64_t)ring.ctas * sm_count();
     // a ring pays once every CTA has a few rows to walk
-    if (a.cols <= kRingCols && rows32 && ring.stages >= 2 && a.rows >= 2 * resident) {
+    if (ring.threads <= 1024 && rows32 && ring.stages >= 2 && a.rows >= 2 * resident) {
         q.stages = ring.stages;
         q.group_lanes = (int)(a.group * kSize / 32);
         if (a.gate) {
@@ -1333,6 +1369,48 @@ bool rows32_backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
            weights_aligned(a);
 }
 
+// The ring's stage of a row of `cols` columns.
+inline size_t backward_stage(const GradParams& p) {
+    const pwlq_block_norm_args& a = p.q.a;
+    return (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (p.g.dr ? p.q.row_bytes : 0) +
+           (a.f_codes ? p.q.code_bytes : 0);
+}
+
+// Rows that one CTA's registers cannot sum: a pair of CTAs, where the halves are whole threads'.
+template <typename T>
+bool pairs_backward(const GradParams& p) {
+    const pwlq_block_norm_args& a = p.q.a;
+    return threads_for(a.cols, 32 / sizeof(T)) > 512 && threads_for(a.cols, 64 / sizeof(T)) <= 512 &&
+           a.cols % 32 == 0 && rows32_backward<T>(a, p.g);
+}
+template <typename T>
+cudaError_t backward_pairs(GradParams& p, unsigned pairs, cudaStream_t stream) {
+    const pwlq_block_norm_args& a = p.q.a;
+    p.q.row_bytes /= 2;
+    p.q.code_bytes = (unsigned)(a.cols / 2);
+    const size_t stage = backward_stage(p);
+    const RingPlan ring = ring_plan(a.cols / 2, sizeof(T), 512, stage);
+    p.q.stages = ring.stages;
+    p.gathered = (unsigned)(ring.stages * stage);
+    const size_t smem = p.gathered + (p.gates && p.g.dpost ? (size_t)a.cols / 2 * sizeof(float) : 0);
+    auto* kernel = p.q.wf32 ? block_norm_backward_ring_kernel<T, true, true>
+                            : block_norm_backward_ring_kernel<T, sizeof(T) == 4, true>;
+    if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem))
+        return e;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = 2;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t config = {};
+    config.gridDim = dim3(2 * pairs);
+    config.blockDim = dim3((unsigned)ring.threads);
+    config.dynamicSmemBytes = smem;
+    config.stream = stream;
+    config.attrs = &attr;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, p);
+}
+
 template <typename T>
 cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
     const pwlq_block_norm_grads& g = p.g;
@@ -1350,14 +1428,14 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
         return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, smem, stream, p)
                    : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, smem, stream, p);
     }
-    const size_t stage = (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (g.dr ? p.q.row_bytes : 0) +
-                         (a.f_codes ? p.q.code_bytes : 0);
+    const size_t stage = backward_stage(p);
     const RingPlan ring = ring_plan(a.cols, kSize, 512, stage);
     if (ring.threads <= 512 && ring.stages >= 2 && rows32_backward<T>(a, g)) {
         p.q.stages = ring.stages;
         p.gathered = (unsigned)(ring.stages * stage);
         const size_t smem = p.gathered + (gathers ? (size_t)a.cols * sizeof(float) : 0);
-        return run(p.q.wf32 ? block_norm_backward_ring_kernel<T, true> : block_norm_backward_ring_kernel<T, kSize == 4>,
+        return run(p.q.wf32 ? block_norm_backward_ring_kernel<T, true, false>
+                            : block_norm_backward_ring_kernel<T, kSize == 4, false>,
                    ctas, ring.threads, smem, stream, p);
     }
     const int threads = threads_for(a.cols, 8);
@@ -1393,8 +1471,9 @@ cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
     p.g = g;
     int64_t ctas = backward_ctas(a.rows, a.cols);
     const int lanes = !a.gate || a.gate_tokens >= a.rows ? narrow_lanes(a.cols, sizeof(T)) : 0;
-    const bool narrow = lanes && rows32_backward<T>(a, g);
+    const bool narrow = lanes && rows32_backward<T>(a, g), pairs = pairs_backward<T>(p);
     if (narrow) ctas = std::min(ctas, narrow_ctas(a.rows, lanes));
+    if (pairs) ctas = std::min<int64_t>(ctas, std::max(1, sm_count() / 2));
     p.rows_per_cta = ctas ? (a.rows + ctas - 1) / ctas : 1;
     ctas = (a.rows + p.rows_per_cta - 1) / p.rows_per_cta;
     float* ws = static_cast<float*>(g.workspace);
@@ -1408,6 +1487,8 @@ cudaError_t backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
                                 : block_norm_backward_narrow_kernel<T, sizeof(T) == 4>;
         kernel<<<(unsigned)ctas, kNarrowThreads, 0, stream>>>(p, lanes);
         if (const cudaError_t e = cudaGetLastError()) return e;
+    } else if (ctas && pairs) {
+        if (const cudaError_t e = backward_pairs<T>(p, (unsigned)ctas, stream)) return e;
     } else if (ctas) {
         if (const cudaError_t e = backward_rows<T>(p, (unsigned)ctas, stream)) return e;
     }

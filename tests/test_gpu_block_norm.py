@@ -95,14 +95,16 @@ def test_every_combination_of_operands(kind, dtype):
 
 # rows a few lanes wide, rows enough for CTAs that walk them, rows too wide for registers
 @pytest.mark.parametrize("kind", KINDS)
-@pytest.mark.parametrize("rows,cols", [(301, 48), (77, 512), (2400, 1280), (7, 8400)])
+@pytest.mark.parametrize("rows,cols", [(301, 48), (77, 512), (2400, 1280), (7, 8400),
+                                       (150, 8704)])
 @pytest.mark.parametrize("dtype,wtype", [("bf16", "fp32"), ("fp32", "fp32")])
 def test_every_combination_of_operands_in_every_form(kind, rows, cols, dtype, wtype):
     _round(rows, cols, TYPES[dtype], TYPES[wtype], kind, rows, 64, 0.4375)
 
 
 @pytest.mark.parametrize("rows,cols,every", [(1, 64, 1), (5, 16, 3), (2000, 32, 2000), (1000, 96, 7),
-                                             (2500, 1024, 300), (3000, 1040, 1), (2400, 2048, 2399)])
+                                             (2500, 1024, 300), (3000, 1040, 1), (2400, 2048, 2399),
+                                             (300, 12288, 7), (200, 8224, 150)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_gates_in_every_form(rows, cols, every, dtype):
     _round(rows, cols, TYPES[dtype], TYPES[dtype], "fogpd", every, 256, 0.5)
