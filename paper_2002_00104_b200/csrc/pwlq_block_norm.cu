@@ -134,7 +134,8 @@ struct NormParams {
     int group_lanes, group_shift;
     bool wf32;
     int stages;
-    unsigned row_bytes, code_bytes;       // of a row in a stage
+    unsigned row_bytes, code_bytes;       // of a row
+    unsigned slot_bytes;                  // what a row of values takes in a stage
     int64_t gate_step, gate_rest;         // gridDim.x / gate_tokens and the remainder (forward)
 };
 
@@ -165,6 +166,9 @@ __device__ __forceinline__ void save8(const u64* pairs, const NormParams& q, int
                                       int valid, uint8_t* codes, float* ranges) {
     float v[8], top = 0.0f;
     floats8(pairs, v);
+    if (valid < 8)                        // bytes of 0 past the row, where x * scale may be -0
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < valid ? v[i] : 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max_abs(top, v[i]);
     top = group_max(top, q.group_lanes);
@@ -178,15 +182,133 @@ __device__ __forceinline__ void save8(const u64* pairs, const NormParams& q, int
     if ((c & ((1 << q.group_shift) - 1)) == 0) ranges[row * q.groups + (c >> q.group_shift)] = m;
 }
 
+// A row of values on its way to a stage.  ODD: rows of 16-bit values that start anywhere.  The copy then
+// takes the aligned words that hold the row, so that the row begins as far past the slot's beginning
+// as past the boundary; bytes outside the matrix are not touched: the ends of its first and last row
+// that no aligned word inside the matrix holds are moved value by value.
 template <typename T>
+struct RowCopy {
+    const unsigned char *from, *lo, *hi;   // the row; the words copied
+    unsigned bytes, skip;                  // of the row; from the slot's beginning to it
+    __device__ __forceinline__ RowCopy(const void* base, int64_t rows, int64_t ld, int64_t row, unsigned row_bytes) {
+        const unsigned char* first = static_cast<const unsigned char*>(base);
+        from = first + row * ld * (int64_t)sizeof(T);
+        bytes = row_bytes;
+        skip = (unsigned)((uintptr_t)from & 15);
+        const uintptr_t in_lo = ((uintptr_t)first + 15) & ~(uintptr_t)15;
+        const uintptr_t in_hi = ((uintptr_t)first + (rows - 1) * ld * (int64_t)sizeof(T) + bytes) & ~(uintptr_t)15;
+        lo = reinterpret_cast<const unsigned char*>(max((uintptr_t)from - skip, in_lo));
+        hi = reinterpret_cast<const unsigned char*>(min(((uintptr_t)from + bytes + 15) & ~(uintptr_t)15, in_hi));
+        if (hi < lo) hi = lo;
+    }
+    __device__ __forceinline__ unsigned size() const { return (unsigned)(hi - lo); }
+    // the ends, before the barrier is told of the copy
+    __device__ __forceinline__ void ends(unsigned char* slot) const {
+        const unsigned char* origin = from - skip;
+        for (const unsigned char* p = from; p < from + bytes; p += sizeof(T)) {
+            if (p >= lo && p < hi) p = hi;                   // words end between values
+            if (p >= from + bytes) break;
+            *reinterpret_cast<T*>(slot + (p - origin)) = *reinterpret_cast<const T*>(p);
+        }
+    }
+    __device__ __forceinline__ void start(unsigned char* slot, uint64_t* bar) const {
+        if (hi > lo) bulk_copy_g2s(slot + (lo - (from - skip)), lo, size(), bar);
+    }
+};
+
+template <typename T, bool ODD>
 __device__ __forceinline__ void request_forward(const NormParams& q, Ring& ring, int stage, int64_t row) {
     unsigned char* to = ring.stage0 + (size_t)stage * ring.stage_bytes;
-    mbar_expect_tx(&ring.full[stage], q.a.f ? 2 * q.row_bytes : q.row_bytes);
-    bulk_copy_g2s(to, static_cast<const T*>(q.a.x) + row * q.a.ldx, q.row_bytes, &ring.full[stage]);
-    if (q.a.f)
-        bulk_copy_g2s(to + q.row_bytes, static_cast<const T*>(q.a.f) + row * q.a.ldf, q.row_bytes,
-                      &ring.full[stage]);
+    uint64_t* bar = &ring.full[stage];
+    if (ODD) {
+        const RowCopy<T> x(q.a.x, q.a.rows, q.a.ldx, row, q.row_bytes),
+            f(q.a.f ? q.a.f : q.a.x, q.a.rows, q.a.f ? q.a.ldf : q.a.ldx, row, q.row_bytes);
+        x.ends(to);
+        if (q.a.f) f.ends(to + q.slot_bytes);
+        mbar_expect_tx(bar, x.size() + (q.a.f ? f.size() : 0));
+        x.start(to, bar);
+        if (q.a.f) f.start(to + q.slot_bytes, bar);
+        return;
+    }
+    mbar_expect_tx(bar, ring.stage_bytes);
+    bulk_copy_g2s(to, static_cast<const T*>(q.a.x) + row * q.a.ldx, q.row_bytes, bar);
+    if (q.a.f) bulk_copy_g2s(to + q.slot_bytes, static_cast<const T*>(q.a.f) + row * q.a.ldf, q.row_bytes, bar);
 }
+
+// How far past a 16-byte boundary a row starts.
+template <typename T, bool ODD>
+__device__ __forceinline__ unsigned row_skip(const void* base, int64_t ld, int64_t row) {
+    return ODD ? (unsigned)(((uintptr_t)base + row * ld * (int64_t)sizeof(T)) & 15) : 0;
+}
+// The 32 bytes that begin `bytes` (the same in a whole warp, below 16) past the first of twelve words:
+// a branch over the word, then one operation a word.
+template <int K>
+__device__ __forceinline__ void words_from(const uint32_t (&w)[12], uint32_t pick, Raw32& r) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.w[i] = __byte_perm(w[i + K], w[i + K + 1], pick);
+}
+__device__ __forceinline__ Raw32 window32(const uint4* q, unsigned bytes) {
+    uint32_t w[12];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const uint4 x = q[i];
+        w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
+    }
+    const uint32_t pick = bytes & 2 ? 0x5432 : 0x3210;
+    Raw32 r;
+    switch (bytes >> 2) {
+        case 0: words_from<0>(w, pick, r); break;
+        case 1: words_from<1>(w, pick, r); break;
+        case 2: words_from<2>(w, pick, r); break;
+        default: words_from<3>(w, pick, r);
+    }
+    return r;
+}
+
+// A thread's 32 bytes of a row in shared memory; the values from `valid` on read as 0.
+template <typename T, bool ODD>
+__device__ __forceinline__ Raw32 ring32(const unsigned char* at, int valid) {
+    if (!ODD) return load32(at);
+    const unsigned o = smem_addr(at) & 15;
+    Raw32 r = window32(reinterpret_cast<const uint4*>(at - o), o);
+    if (valid < 2 * kPairs32<T>)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int n = valid - 2 * i;  // values of this word that exist
+            r.w[i] = n <= 0 ? 0u : n == 1 ? r.w[i] & 0xffffu : r.w[i];
+        }
+    return r;
+}
+// A warp's 32 bytes per lane to a row.  ODD: the first lane's go to `row0`, where `rest` values of the row
+// exist from there on; they are turned in shared memory, so that whole aligned 16-byte words are written
+// and only the ends of the warp's stretch go value by value.  Every lane calls.
+constexpr int kTurn = 65;                // words of a warp's turn: the last window ends one past them
+template <typename T, bool ODD>
+__device__ __forceinline__ void put32(T* to, const Raw32& v, bool live, uint4* turn, T* row0, int rest) {
+    if (!ODD) {
+        if (live) store32(to, v);
+        return;
+    }
+    constexpr int kSize = sizeof(T);
+    const int lane = threadIdx.x & 31;
+    const int bytes = min(rest * kSize, 1024), head = min((int)(-(uintptr_t)row0 & 15), bytes);
+    const int words = (bytes - head) >> 4;
+    uint4* const mine = turn + (threadIdx.x >> 5) * kTurn;
+    __syncwarp();
+    mine[2 * lane] = make_uint4(v.w[0], v.w[1], v.w[2], v.w[3]);
+    mine[2 * lane + 1] = make_uint4(v.w[4], v.w[5], v.w[6], v.w[7]);
+    __syncwarp();
+    const Raw32 x = window32(mine + 2 * lane, head);
+    uint4* const out = reinterpret_cast<uint4*>(reinterpret_cast<unsigned char*>(row0) + head) + 2 * lane;
+    if (2 * lane < words) out[0] = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+    if (2 * lane + 1 < words) out[1] = make_uint4(x.w[4], x.w[5], x.w[6], x.w[7]);
+    const T* from = reinterpret_cast<const T*>(mine);
+    const int tail = (head + 16 * words) / kSize + lane;
+    if (lane * kSize < head) row0[lane] = from[lane];
+    if (tail * kSize < bytes) row0[tail] = from[tail];
+}
+template <bool ODD>
+__device__ __forceinline__ unsigned turn_bytes() { return ODD ? blockDim.x / 32 * kTurn * 16 : 0; }
 
 // Forward, every thread loading its values itself, one row per CTA.  VC: chunks of eight columns per
 // thread.
@@ -270,6 +392,32 @@ template <typename T, bool WF32>
 struct Weights {
     static constexpr bool kWide = WF32 && sizeof(T) == 2;
     Raw32 raw[kWide ? 2 : 1];
+    // rows of weights that need not be aligned, and of which `valid` values from there on exist
+    __device__ __forceinline__ void load_odd(const void* p, int64_t row, int c, int valid) {
+        if (kWide) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                Raw8<float> r;
+                load8<false>(r, static_cast<const float*>(p) + row + c + 8 * i, valid - 8 * i, c + 8 * i);
+                float v[8];
+                r.get(v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) raw[kWide ? i : 0].w[k] = __float_as_uint(v[k]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                Raw8<T> r;
+                load8<false>(r, static_cast<const T*>(p) + row + c + 8 * i, valid - 8 * i, c + 8 * i);
+                const uint4 w = *reinterpret_cast<const uint4*>(&r);
+                raw[0].w[4 * i] = w.x; raw[0].w[4 * i + 1] = w.y; raw[0].w[4 * i + 2] = w.z; raw[0].w[4 * i + 3] = w.w;
+            }
+        }
+    }
+    template <bool ODD> __device__ __forceinline__ void load(const void* p, int64_t row, int c, int valid) {
+        if (ODD) load_odd(p, row, c, valid);
+        else load(p, row + c);
+    }
     __device__ __forceinline__ void load(const void* p, int64_t at) {
         if (kWide) {
             raw[0] = load32(static_cast<const float*>(p) + at);
@@ -294,13 +442,16 @@ struct Weights {
 };
 
 // Bytes of a thread's 32 bytes of values, and the range of their group.
-template <typename T>
+template <typename T, bool ODD = false>
 __device__ __forceinline__ void save32(const u64* v, const NormParams& q, bool live, int64_t row, int c,
                                        uint8_t* codes, float* ranges) {
     constexpr int kP = kPairs32<T>;
     float f[2 * kP], top = 0.0f;
 #pragma unroll
     for (int k = 0; k < kP; ++k) unpack2(v[k], f[2 * k], f[2 * k + 1]);
+    if (ODD && c + 2 * kP > (int)q.a.cols)
+#pragma unroll
+        for (int k = 0; k < 2 * kP; ++k) f[k] = c + k < (int)q.a.cols ? f[k] : 0.0f;     // bytes of 0 past the row
 #pragma unroll
     for (int k = 0; k < 2 * kP; ++k) top = max_abs(top, f[k]);
     top = group_max(top, q.group_lanes);
@@ -321,20 +472,21 @@ __device__ __forceinline__ void save32(const u64* v, const NormParams& q, bool l
 }
 
 // Forward with a ring: 32 bytes of columns per thread.
-template <typename T, bool SAVE, bool WF32>
-__global__ void __maxnreg__(64) block_norm_ring_kernel(const __grid_constant__ NormParams q) {
+template <typename T, bool SAVE, bool WF32, bool ODD>
+__global__ void __maxnreg__(ODD ? 80 : 64) block_norm_ring_kernel(const __grid_constant__ NormParams q) {
     constexpr int kP = kPairs32<T>;
     __shared__ float buf[2][32];
     __shared__ uint64_t full[kMaxStages];
     extern __shared__ __align__(16) unsigned char smem[];
     CtaSum cta_sum{buf};
-    Ring ring{full, smem, q.a.f ? 2 * q.row_bytes : q.row_bytes, q.stages};
+    uint4* const turn = reinterpret_cast<uint4*>(smem);
+    Ring ring{full, smem + turn_bytes<ODD>(), q.a.f ? 2 * q.slot_bytes : q.slot_bytes, q.stages};
     if (threadIdx.x == 0) {
         for (int s = 0; s < q.stages; ++s) mbar_init(&full[s], 1);
         fence_barrier_init();
         for (int s = 0; s < q.stages; ++s) {
             const int64_t row = blockIdx.x + (int64_t)s * gridDim.x;
-            if (row < q.a.rows) request_forward<T>(q, ring, s, row);
+            if (row < q.a.rows) request_forward<T, ODD>(q, ring, s, row);
         }
     }
     __syncthreads();
@@ -347,32 +499,34 @@ __global__ void __maxnreg__(64) block_norm_ring_kernel(const __grid_constant__ N
     // threads past the row repeat its last columns (so that a group's range stays its own) and
     // neither store nor count
     const bool live = (int)threadIdx.x * 2 * kP < (int)q.a.cols, post = q.a.post_weight, pre = q.a.pre_weight;
-    const int c = live ? (int)threadIdx.x * 2 * kP : (int)q.a.cols - 2 * kP;
+    const int cols = (int)q.a.cols, c = live ? (int)threadIdx.x * 2 * kP : ODD ? (cols - 1) / (2 * kP) * (2 * kP) : cols - 2 * kP;
+    const int valid = ODD ? cols - c : 2 * kP;
+    const int warp_c = (int)(threadIdx.x & ~31u) * 2 * kP;       // of the warp's first lane
     for (int64_t row = blockIdx.x; row < q.a.rows; row += gridDim.x) {
         u64 r[kP], w[kP], s = 0ull;
         Weights<T, WF32> wt;
-        if (post) wt.load(q.a.post_weight, c);
+        if (post) wt.template load<ODD>(q.a.post_weight, 0, c, valid);
         const unsigned char* at = ring.wait() + c * (int)sizeof(T);
-        pairs32(load32(at), r, T());
+        pairs32(ring32<T, ODD>(at + row_skip<T, ODD>(q.a.x, q.a.ldx, row), valid), r, T());
 #pragma unroll
         for (int k = 0; k < kP; ++k) r[k] = mul2(r[k], both(q.scale));
         if (q.a.f) {
             u64 f[kP];
-            pairs32(load32(at + q.row_bytes), f, T());
+            pairs32(ring32<T, ODD>(at + q.slot_bytes + row_skip<T, ODD>(q.a.f, q.a.ldf, row), valid), f, T());
             if (post) {
 #pragma unroll
                 for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
                 cta_sum.post(live ? sum8(s) : 0.0f);
-                if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+                if (SAVE && q.a.f_codes) save32<T, ODD>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
                 const float rstd_f = rsqrtf(fmaf(cta_sum.total(), q.inv_cols, q.eps));
                 if (SAVE && threadIdx.x == 0 && q.a.f_rstd) q.a.f_rstd[row] = rstd_f;
                 wt.get(w, q.offset);
-                if (q.a.gate) wt.load(q.a.gate, gate * q.a.ldgate + c);
+                if (q.a.gate) wt.template load<ODD>(q.a.gate, gate * q.a.ldgate, c, valid);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) f[k] = mul2(mul2(f[k], both(rstd_f)), w[k]);
             } else {
-                if (q.a.gate) wt.load(q.a.gate, gate * q.a.ldgate + c);
-                if (SAVE && q.a.f_codes) save32<T>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
+                if (q.a.gate) wt.template load<ODD>(q.a.gate, gate * q.a.ldgate, c, valid);
+                if (SAVE && q.a.f_codes) save32<T, ODD>(f, q, live, row, c, q.a.f_codes, q.a.f_ranges);
             }
             if (q.a.gate) {
                 wt.get(w);
@@ -391,23 +545,27 @@ __global__ void __maxnreg__(64) block_norm_ring_kernel(const __grid_constant__ N
         for (int k = 0; k < kP; ++k) s = fma2(r[k], r[k], s);
         if (pre) {
             cta_sum.post(live ? sum8(s) : 0.0f);
-            wt.load(q.a.pre_weight, c);
+            wt.template load<ODD>(q.a.pre_weight, 0, c, valid);
         }
-        if (live && q.a.r) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
-        if (SAVE && q.a.r_codes) save32<T>(r, q, live, row, c, q.a.r_codes, q.a.r_ranges);
+        if (q.a.r && (ODD || live)) {
+            T* const to = static_cast<T*>(q.a.r) + row * q.a.ldr;
+            put32<T, ODD>(to + c, raw32(r, T()), live, turn, to + warp_c, cols - warp_c);
+        }
+        if (SAVE && q.a.r_codes) save32<T, ODD>(r, q, live, row, c, q.a.r_codes, q.a.r_ranges);
         float rstd_r = 0.0f;
         if (pre) rstd_r = rsqrtf(fmaf(cta_sum.total(), q.inv_cols, q.eps));
         else __syncthreads();
         // every thread has its values of this stage
         const int64_t ahead = row + (int64_t)q.stages * gridDim.x;
-        if (threadIdx.x == 0 && ahead < q.a.rows && !ring.dead) request_forward<T>(q, ring, ring.stage, ahead);
+        if (threadIdx.x == 0 && ahead < q.a.rows && !ring.dead) request_forward<T, ODD>(q, ring, ring.stage, ahead);
         ring.next();
         if (!pre) continue;
         if (SAVE && threadIdx.x == 0 && q.a.r_rstd) q.a.r_rstd[row] = rstd_r;
         wt.get(w, q.offset);
 #pragma unroll
         for (int k = 0; k < kP; ++k) w[k] = mul2(mul2(r[k], both(rstd_r)), w[k]);
-        if (live) store32(static_cast<T*>(q.a.h) + row * q.a.ldh + c, raw32(w, T()));
+        T* const to = static_cast<T*>(q.a.h) + row * q.a.ldh;
+        put32<T, ODD>(to + c, raw32(w, T()), live, turn, to + warp_c, cols - warp_c);
     }
 }
 
@@ -612,23 +770,32 @@ __device__ __forceinline__ void clear_gathered(float* gathered) {
     }
 }
 
-template <typename T>
+template <typename T, bool ODD>
 __device__ __forceinline__ void request_backward(const GradParams& p, Ring& ring, int stage, int64_t row, int base) {
     const NormParams& q = p.q;
     unsigned char* to = ring.stage0 + (size_t)stage * ring.stage_bytes;
     uint64_t* bar = &ring.full[stage];
-    mbar_expect_tx(bar, ring.stage_bytes);
-    if (q.a.pre_weight) {
-        bulk_copy_g2s(to, static_cast<const T*>(p.g.dh) + row * p.g.lddh + base, q.row_bytes, bar);
-        to += q.row_bytes;
-        bulk_copy_g2s(to, q.a.r_codes + row * q.a.ldc + base, q.code_bytes, bar);
-        to += q.code_bytes;
+    unsigned char* const at_dr = to + (q.a.pre_weight ? q.slot_bytes + q.code_bytes : 0);
+    if (ODD) {
+        const bool pre = q.a.pre_weight, has_dr = p.g.dr;
+        const RowCopy<T> dh(pre ? p.g.dh : p.g.dr, q.a.rows, pre ? p.g.lddh : p.g.lddr, row, q.row_bytes),
+            dr(has_dr ? p.g.dr : p.g.dh, q.a.rows, has_dr ? p.g.lddr : p.g.lddh, row, q.row_bytes);
+        if (pre) dh.ends(to);
+        if (has_dr) dr.ends(at_dr);
+        mbar_expect_tx(bar, (pre ? dh.size() + q.code_bytes : 0) + (has_dr ? dr.size() : 0) +
+                                (q.a.f_codes ? q.code_bytes : 0));
+        if (pre) dh.start(to, bar);
+        if (has_dr) dr.start(at_dr, bar);
+    } else {
+        mbar_expect_tx(bar, ring.stage_bytes);
+        if (q.a.pre_weight)
+            bulk_copy_g2s(to, static_cast<const T*>(p.g.dh) + row * p.g.lddh + base, q.row_bytes, bar);
+        if (p.g.dr) bulk_copy_g2s(at_dr, static_cast<const T*>(p.g.dr) + row * p.g.lddr + base, q.row_bytes, bar);
     }
-    if (p.g.dr) {
-        bulk_copy_g2s(to, static_cast<const T*>(p.g.dr) + row * p.g.lddr + base, q.row_bytes, bar);
-        to += q.row_bytes;
-    }
-    if (q.a.f_codes) bulk_copy_g2s(to, q.a.f_codes + row * q.a.ldc + base, q.code_bytes, bar);
+    if (q.a.pre_weight)
+        bulk_copy_g2s(to + q.slot_bytes, q.a.r_codes + row * q.a.ldc + base, q.code_bytes, bar);
+    if (q.a.f_codes)
+        bulk_copy_g2s(to + ring.stage_bytes - q.code_bytes, q.a.f_codes + row * q.a.ldc + base, q.code_bytes, bar);
 }
 
 // Eight bytes of a row from column c on; those past the row read as 0.
@@ -812,16 +979,28 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
 }
 
 // A thread's 32 bytes of columns times `factor`, from its bytes.
+// The bytes from `valid` on read as 0.
 template <typename T>
-__device__ __forceinline__ void held32(const unsigned char* bytes, float m, float ratio, float factor, u64* n) {
+__device__ __forceinline__ void held32(const unsigned char* bytes, int valid, float m, float ratio, float factor,
+                                       u64* n) {
     const Act8Lines L = act8_lines(m, ratio, factor);
-    if (kPairs32<T> == 8) {
-        const uint4 b = *reinterpret_cast<const uint4*>(bytes);
-        act8_scaled8(make_uint2(b.x, b.y), L, n);
-        act8_scaled8(make_uint2(b.z, b.w), L, n + kPairs32<T> - 4);
+    constexpr int kWords = kPairs32<T> / 2;
+    uint32_t b[4];
+    if (kWords == 4) {
+        const uint4 x = *reinterpret_cast<const uint4*>(bytes);
+        b[0] = x.x; b[1] = x.y; b[2] = x.z; b[3] = x.w;
     } else {
-        act8_scaled8(*reinterpret_cast<const uint2*>(bytes), L, n);
+        const uint2 x = *reinterpret_cast<const uint2*>(bytes);
+        b[0] = x.x; b[1] = x.y; b[2] = b[3] = 0u;
     }
+    if (valid < 4 * kWords)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const int k = valid - 4 * i;  // bytes of this word that exist
+            b[i] = k >= 4 ? b[i] : k <= 0 ? 0u : b[i] & (0xffffffffu >> (32 - 8 * k));
+        }
+    act8_scaled8(make_uint2(b[0], b[1]), L, n);
+    if (kWords == 4) act8_scaled8(make_uint2(b[2], b[3]), L, n + kPairs32<T> - 4);
 }
 
 __device__ __forceinline__ void set_rank(CtaSum&, uint32_t) {}
@@ -829,7 +1008,7 @@ __device__ __forceinline__ void set_rank(PairSum& s, uint32_t rank) { s.rank = r
 
 // Backward with a ring: 32 bytes of columns per thread, sums in registers.  PAIR: a cluster of two CTAs
 // shares the rows, half the columns each (rows too wide for one CTA's registers).
-template <typename T, bool WF32, bool PAIR>
+template <typename T, bool WF32, bool PAIR, bool ODD>
 __global__ void __launch_bounds__(512)
 block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     constexpr int kP = kPairs32<T>;
@@ -843,15 +1022,16 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     const int cols = PAIR ? (int)q.a.cols / 2 : (int)q.a.cols, base = (int)rank * cols;
     const int64_t first = cta * p.rows_per_cta, last = min(first + p.rows_per_cta, q.a.rows);
     const bool pre = q.a.pre_weight, post = q.a.post_weight, has_f = q.a.f_codes, has_dr = p.g.dr;
-    Ring ring{full, smem,
-              (pre ? q.row_bytes + q.code_bytes : 0) + (has_dr ? q.row_bytes : 0) + (has_f ? q.code_bytes : 0),
+    uint4* const turn = reinterpret_cast<uint4*>(smem);
+    Ring ring{full, smem + turn_bytes<ODD>(),
+              (pre ? q.slot_bytes + q.code_bytes : 0) + (has_dr ? q.slot_bytes : 0) + (has_f ? q.code_bytes : 0),
               q.stages};
     if (PAIR && threadIdx.x < 64) buf[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
     if (threadIdx.x == 0) {
         for (int s = 0; s < q.stages; ++s) mbar_init(&full[s], 1);
         fence_barrier_init();
         for (int s = 0; s < q.stages; ++s)
-            if (first + s < last) request_backward<T>(p, ring, s, first + s, base);
+            if (first + s < last) request_backward<T, ODD>(p, ring, s, first + s, base);
     }
     __syncthreads();
     if (PAIR) {
@@ -860,10 +1040,12 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     }
     // threads past the row repeat its last columns and neither store nor count
     const bool live = (int)threadIdx.x * 2 * kP < cols;
-    const int local = live ? (int)threadIdx.x * 2 * kP : cols - 2 * kP, c = base + local;
+    const int local = live ? (int)threadIdx.x * 2 * kP : (cols - 1) / (2 * kP) * (2 * kP), c = base + local;
+    const int valid = ODD ? cols - local : 2 * kP;
+    const int warp_c = (int)(threadIdx.x & ~31u) * 2 * kP;       // of the warp's first lane
     // where this thread's part of each operand lies in a stage
-    const unsigned at_dh = local * (int)sizeof(T), at_rb = q.row_bytes + local,
-                   at_dr = (pre ? q.row_bytes + q.code_bytes : 0) + local * (int)sizeof(T),
+    const unsigned at_dh = local * (int)sizeof(T), at_rb = q.slot_bytes + local,
+                   at_dr = (pre ? q.slot_bytes + q.code_bytes : 0) + local * (int)sizeof(T),
                    at_fb = ring.stage_bytes - q.code_bytes + local;
     int64_t gate = q.a.gate ? first / q.a.gate_tokens : 0;
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
@@ -878,14 +1060,22 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         if (live)
 #pragma unroll
             for (int k = 0; k < kP; k += 4)
-                finish_gate<true, T>(p, cta, gate, first, last, c + 2 * k, 8, inner + k, gathered);
+                finish_gate<!ODD, T>(p, cta, gate, first, last, c + 2 * k, valid - 2 * k, inner + k, gathered);
 #pragma unroll
         for (int k = 0; k < kP; ++k) inner[k] = 0ull;
     };
     auto put = [&](const u64* v, float* to) {
         if (!live) return;
 #pragma unroll
-        for (int k = 0; k < kP; k += 4) store32(to + c + 2 * k, raw32(v + k, 0.0f));
+        for (int k = 0; k < kP; k += 4) {
+            if (!ODD) {
+                store32(to + c + 2 * k, raw32(v + k, 0.0f));
+                continue;
+            }
+            float f[8];
+            floats8(v + k, f);
+            put8<false>(f, to + c + 2 * k, valid - 2 * k);
+        }
     };
 
     // a row's ranges and factors, requested one row ahead
@@ -909,15 +1099,15 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         if (row + 1 < last) fetch(row + 1);
         u64 e[kP], n[kP], w[kP];
         Weights<T, WF32> wt, gt;
-        if (pre) wt.load(q.a.pre_weight, c);
+        if (pre) wt.template load<ODD>(q.a.pre_weight, 0, c, valid);
         const unsigned char* at = ring.wait();
         // outer norm: e = dr + rstd * (u - n * mean(u n))
         if (pre) {
-            pairs32(load32(at + at_dh), e, T());
-            held32<T>(at + at_rb, mr, q.ratio, rr, n);
+            pairs32(ring32<T, ODD>(at + at_dh + row_skip<T, ODD>(p.g.dh, p.g.lddh, row), valid), e, T());
+            held32<T>(at + at_rb, valid, mr, q.ratio, rr, n);
             wt.get(w, q.offset);
-            if (post) wt.load(q.a.post_weight, c);
-            if (q.a.gate) gt.load(q.a.gate, gate * q.a.ldgate + c);
+            if (post) wt.template load<ODD>(q.a.post_weight, 0, c, valid);
+            if (q.a.gate) gt.template load<ODD>(q.a.gate, gate * q.a.ldgate, c, valid);
             u64 s = 0ull;
 #pragma unroll
             for (int k = 0; k < kP; ++k) {
@@ -927,7 +1117,7 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
             }
             cta_sum.post(live ? sum8(s) : 0.0f);
             Raw32 raw_dr;
-            if (has_dr) raw_dr = load32(at + at_dr);
+            if (has_dr) raw_dr = ring32<T, ODD>(at + at_dr + row_skip<T, ODD>(p.g.dr, p.g.lddr, row), valid);
             const float mean = cta_sum.total() * q.inv_cols;
 #pragma unroll
             for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rr));
@@ -937,19 +1127,20 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
                 for (int k = 0; k < kP; ++k) e[k] = add2(e[k], w[k]);
             }
         } else {                          // without the outer norm dr is all there is
-            if (post) wt.load(q.a.post_weight, c);
-            if (q.a.gate) gt.load(q.a.gate, gate * q.a.ldgate + c);
-            pairs32(load32(at + at_dr), e, T());
+            if (post) wt.template load<ODD>(q.a.post_weight, 0, c, valid);
+            if (q.a.gate) gt.template load<ODD>(q.a.gate, gate * q.a.ldgate, c, valid);
+            pairs32(ring32<T, ODD>(at + at_dr + row_skip<T, ODD>(p.g.dr, p.g.lddr, row), valid), e, T());
         }
-        if (p.g.dx && live) {
+        if (p.g.dx && (ODD || live)) {
 #pragma unroll
             for (int k = 0; k < kP; ++k) w[k] = mul2(e[k], both(q.scale));
-            store32(static_cast<T*>(p.g.dx) + row * p.g.lddx + c, raw32(w, T()));
+            T* const to = static_cast<T*>(p.g.dx) + row * p.g.lddx;
+            put32<T, ODD>(to + c, raw32(w, T()), live, turn, to + warp_c, cols - warp_c);
         }
         // inner norm and gate; e becomes v = e * gate * w
         float mean = 0.0f;
         if (has_f) {
-            held32<T>(at + at_fb, mf, q.ratio, rf, n);
+            held32<T>(at + at_fb, valid, mf, q.ratio, rf, n);
 #pragma unroll
             for (int k = 0; k < kP; ++k) inner[k] = fma2(e[k], n[k], inner[k]);
             if (q.a.gate) {
@@ -971,13 +1162,14 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
         if (!post) __syncthreads();
         // every thread has its values of this stage
         const int64_t ahead = row + q.stages;
-        if (threadIdx.x == 0 && ahead < last && !ring.dead) request_backward<T>(p, ring, ring.stage, ahead, base);
+        if (threadIdx.x == 0 && ahead < last && !ring.dead) request_backward<T, ODD>(p, ring, ring.stage, ahead, base);
         ring.next();
-        if (!p.g.df || !live) continue;
+        if (!p.g.df || (!ODD && !live)) continue;
         if (post)
 #pragma unroll
             for (int k = 0; k < kP; ++k) e[k] = mul2(fma2(n[k], both(-mean), e[k]), both(rf));
-        store32(static_cast<T*>(p.g.df) + row * p.g.lddf + c, raw32(e, T()));
+        T* const to = static_cast<T*>(p.g.df) + row * p.g.lddf;
+        put32<T, ODD>(to + c, raw32(e, T()), live, turn, to + warp_c, cols - warp_c);
     }
     if (p.dpre) put(dpre, p.dpre + cta * q.a.cols);
     if (gates) finish(gate);
@@ -1035,7 +1227,7 @@ block_norm_backward_narrow_kernel(const __grid_constant__ GradParams p, int lane
         u64 e[kP], n[kP], w[kP], s = 0ull;
         if (pre) {
             pairs32(raw_dh, e, T());
-            held32<T>(reinterpret_cast<const unsigned char*>(&rb), mr, q.ratio, rr, n);
+            held32<T>(reinterpret_cast<const unsigned char*>(&rb), 2 * kP, mr, q.ratio, rr, n);
             pre_w.get(w, q.offset);
             if (live)
 #pragma unroll
@@ -1063,7 +1255,7 @@ block_norm_backward_narrow_kernel(const __grid_constant__ GradParams p, int lane
         }
         float mean = 0.0f;
         if (has_f) {
-            held32<T>(reinterpret_cast<const unsigned char*>(&fb), mf, q.ratio, rf, n);
+            held32<T>(reinterpret_cast<const unsigned char*>(&fb), 2 * kP, mf, q.ratio, rf, n);
             if (live)
 #pragma unroll
                 for (int k = 0; k < kP; ++k) inner[k] = fma2(e[k], n[k], inner[k]);
@@ -1258,8 +1450,14 @@ NormParams params(const pwlq_block_norm_args& a) {
     q.gate_step = q.gate_rest = 0;
     q.row_bytes = (unsigned)(a.cols * type_size((int)a.dtype));
     q.code_bytes = (unsigned)((a.cols + 15) / 16 * 16);
+    q.slot_bytes = q.row_bytes;
     return q;
 }
+
+// Rows that the kernels of 32 bytes per thread cannot take as they lie (ODD): a slot for the aligned
+// words that hold one and for the 16 bytes after its last thread's part.
+inline void odd_slots(NormParams& q) { q.slot_bytes = (q.row_bytes + 31) / 32 * 32 + 32; }
+inline size_t turn_bytes(bool odd, int threads) { return odd ? (size_t)threads / 32 * kTurn * 16 : 0; }
 
 inline bool weights_aligned(const pwlq_block_norm_args& a) {
     const size_t ws = type_size((int)a.wtype);
@@ -1326,21 +1524,33 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
         kernel<<<(unsigned)narrow_ctas(a.rows, lanes), kNarrowThreads, 0, stream>>>(q, lanes);
         return cudaGetLastError();
     }
-    const RingPlan ring = ring_plan(a.cols, kSize, 1024, (a.f ? 2 : 1) * (size_t)q.row_bytes);
+    const bool vec = rows_aligned(a.x, a.ldx, kSize) && rows_aligned(a.f, a.ldf, kSize) &&
+                     rows_aligned(a.r, a.ldr, kSize) && rows_aligned(a.h, a.ldh, kSize) && weights_aligned(a);
+    // Rows that lie anywhere, 16-bit types: 16384 x 4095 234 -> 144 us (with checkpoints 305 -> 218) against
+    // threads that load for themselves.  Not binary32 (16384 x 2047: 122 against 133 us), nor rows on
+    // 16-byte boundaries that end inside a thread's part (16384 x 4104: 115 against 171 us).
+    const bool odd = kSize == 2 && !vec;
+    if (odd) odd_slots(q);
+    const size_t stage = (a.f ? 2 : 1) * (size_t)q.slot_bytes;
+    const RingPlan ring = ring_plan(a.cols, kSize, odd ? 768 : 1024, stage);
     const int64_t resident = (int64_t)ring.ctas * sm_count();
     // a ring pays once every CTA has a few rows to walk
-    if (ring.threads <= 1024 && rows32 && ring.stages >= 2 && a.rows >= 2 * resident) {
+    if ((rows32 || odd) && ring.threads <= (odd ? 768 : 1024) && ring.stages >= 2 && a.rows >= 2 * resident) {
         q.stages = ring.stages;
         q.group_lanes = (int)(a.group * kSize / 32);
         if (a.gate) {
             q.gate_step = resident / a.gate_tokens;
             q.gate_rest = resident % a.gate_tokens;
         }
-        return run(q.wf32 ? block_norm_ring_kernel<T, SAVE, true> : block_norm_ring_kernel<T, SAVE, kSize == 4>,
-                   (unsigned)resident, ring.threads, (size_t)ring.stages * (a.f ? 2 : 1) * q.row_bytes, stream, q);
+        auto* kernel = q.wf32 ? block_norm_ring_kernel<T, SAVE, true, false>
+                              : block_norm_ring_kernel<T, SAVE, kSize == 4, false>;
+        if constexpr (kSize == 2) {
+            if (odd) kernel = q.wf32 ? block_norm_ring_kernel<T, SAVE, true, true>
+                                     : block_norm_ring_kernel<T, SAVE, false, true>;
+        }
+        return run(kernel, (unsigned)resident, ring.threads, turn_bytes(odd, ring.threads) + ring.stages * stage,
+                   stream, q);
     }
-    const bool vec = rows_aligned(a.x, a.ldx, kSize) && rows_aligned(a.f, a.ldf, kSize) &&
-                     rows_aligned(a.r, a.ldr, kSize) && rows_aligned(a.h, a.ldh, kSize) && weights_aligned(a);
     const unsigned rows = (unsigned)a.rows;
     if (a.cols <= 8192)
         return vec ? run(block_norm_kernel<T, 1, true, SAVE>, rows, threads_for(a.cols, 8), 0, stream, q)
@@ -1372,7 +1582,7 @@ bool rows32_backward(const pwlq_block_norm_args& a, const pwlq_block_norm_grads&
 // The ring's stage of a row of `cols` columns.
 inline size_t backward_stage(const GradParams& p) {
     const pwlq_block_norm_args& a = p.q.a;
-    return (a.pre_weight ? p.q.row_bytes + p.q.code_bytes : 0) + (p.g.dr ? p.q.row_bytes : 0) +
+    return (a.pre_weight ? p.q.slot_bytes + p.q.code_bytes : 0) + (p.g.dr ? p.q.slot_bytes : 0) +
            (a.f_codes ? p.q.code_bytes : 0);
 }
 
@@ -1386,15 +1596,15 @@ bool pairs_backward(const GradParams& p) {
 template <typename T>
 cudaError_t backward_pairs(GradParams& p, unsigned pairs, cudaStream_t stream) {
     const pwlq_block_norm_args& a = p.q.a;
-    p.q.row_bytes /= 2;
+    p.q.slot_bytes = p.q.row_bytes /= 2;
     p.q.code_bytes = (unsigned)(a.cols / 2);
     const size_t stage = backward_stage(p);
     const RingPlan ring = ring_plan(a.cols / 2, sizeof(T), 512, stage);
     p.q.stages = ring.stages;
     p.gathered = (unsigned)(ring.stages * stage);
     const size_t smem = p.gathered + (p.gates && p.g.dpost ? (size_t)a.cols / 2 * sizeof(float) : 0);
-    auto* kernel = p.q.wf32 ? block_norm_backward_ring_kernel<T, true, true>
-                            : block_norm_backward_ring_kernel<T, sizeof(T) == 4, true>;
+    auto* kernel = p.q.wf32 ? block_norm_backward_ring_kernel<T, true, true, false>
+                            : block_norm_backward_ring_kernel<T, sizeof(T) == 4, true, false>;
     if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem))
         return e;
     cudaLaunchAttribute attr;
@@ -1428,15 +1638,25 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
         return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, smem, stream, p)
                    : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, smem, stream, p);
     }
+    const bool rows32 = rows32_backward<T>(a, g);
+    // Rows that lie anywhere, 16-bit types: 16384 x 4095 352 -> 254 us, 16384 x 4104 406 -> 356 us against
+    // threads that load for themselves.  Not binary32 (16384 x 2047: 190 against 192 us), nor gates of a few
+    // rows, whose gradients go value by value (8192 x 4095, a gate per row: 286 against 327 us).
+    const bool odd = !rows32 && kSize == 2 && (!p.dgate || a.gate_tokens >= 8);
+    if (odd) odd_slots(p.q);
     const size_t stage = backward_stage(p);
     const RingPlan ring = ring_plan(a.cols, kSize, 512, stage);
-    if (ring.threads <= 512 && ring.stages >= 2 && rows32_backward<T>(a, g)) {
+    if ((rows32 || odd) && ring.threads <= 512 && ring.stages >= 2 && (a.pre_weight || g.dr)) {
         p.q.stages = ring.stages;
-        p.gathered = (unsigned)(ring.stages * stage);
-        const size_t smem = p.gathered + (gathers ? (size_t)a.cols * sizeof(float) : 0);
-        return run(p.q.wf32 ? block_norm_backward_ring_kernel<T, true, false>
-                            : block_norm_backward_ring_kernel<T, kSize == 4, false>,
-                   ctas, ring.threads, smem, stream, p);
+        p.gathered = (unsigned)(turn_bytes(odd, ring.threads) + ring.stages * stage);
+        const size_t smem = p.gathered + (gathers ? (size_t)(a.cols + 15) / 16 * 16 * sizeof(float) : 0);
+        auto* kernel = p.q.wf32 ? block_norm_backward_ring_kernel<T, true, false, false>
+                                : block_norm_backward_ring_kernel<T, kSize == 4, false, false>;
+        if constexpr (kSize == 2) {
+            if (odd) kernel = p.q.wf32 ? block_norm_backward_ring_kernel<T, true, false, true>
+                                       : block_norm_backward_ring_kernel<T, false, false, true>;
+        }
+        return run(kernel, ctas, ring.threads, smem, stream, p);
     }
     const int threads = threads_for(a.cols, 8);
     const size_t smem = gathers ? (size_t)threads * 8 * sizeof(float) : 0;

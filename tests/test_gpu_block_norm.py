@@ -57,6 +57,22 @@ def _check_forward(s, every, scale, eps, offset, r, h):
     return r64, rr, rf, err_r
 
 
+def _check_saved(s, saved, r64, err_r, cols, group, ratio):
+    if saved.f:
+        b, m, _ = act8_reference(s["f"].float().cpu().numpy(), group, ratio)
+        assert np.array_equal(saved.f.codes.cpu().numpy()[:, :cols], b)
+        assert not saved.f.codes[:, cols:].any()
+        assert np.array_equal(saved.f.ranges.cpu().numpy(), m)
+    if saved.r:
+        # half a level of the piece, and what r was off in binary32
+        m = saved.r.ranges.double().repeat_interleave(group, dim=1)[:, :cols]
+        held = act8_values64(saved.r.codes, saved.r.ranges, cols, group, ratio)
+        half = torch.where(held.abs() > ratio * m * (1 - 1e-6), (1 - ratio) * m, ratio * m) / 126
+        half = torch.maximum(half, torch.where((held.abs() - ratio * m).abs() < 1e-3 * m, m / 126, 0.0))
+        assert ((held - r64).abs() <= half * (1 + 1e-5) + 2 * err_r + 1e-6 * m).all()
+        assert not saved.r.codes[:, cols:].any()
+
+
 def _check_backward(s, every, scale, offset, saved, grads, rows_per_sum):
     w = {k: _d(s[k]) for k in ("pre", "post", "gate", "dh", "dr")}
     R = held64(saved.r) if saved.r else None
@@ -96,7 +112,7 @@ def test_every_combination_of_operands(kind, dtype):
 # rows a few lanes wide, rows enough for CTAs that walk them, rows too wide for registers
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("rows,cols", [(301, 48), (77, 512), (2400, 1280), (7, 8400),
-                                       (150, 8704)])
+                                       (150, 8704), (4800, 75), (3000, 1283)])
 @pytest.mark.parametrize("dtype,wtype", [("bf16", "fp32"), ("fp32", "fp32")])
 def test_every_combination_of_operands_in_every_form(kind, rows, cols, dtype, wtype):
     _round(rows, cols, TYPES[dtype], TYPES[wtype], kind, rows, 64, 0.4375)
@@ -104,7 +120,9 @@ def test_every_combination_of_operands_in_every_form(kind, rows, cols, dtype, wt
 
 @pytest.mark.parametrize("rows,cols,every", [(1, 64, 1), (5, 16, 3), (2000, 32, 2000), (1000, 96, 7),
                                              (2500, 1024, 300), (3000, 1040, 1), (2400, 2048, 2399),
-                                             (300, 12288, 7), (200, 8224, 150)])
+                                             (300, 12288, 7), (200, 8224, 150), (4800, 333, 7),
+                                             (3000, 1283, 299), (700, 4104, 150), (600, 8191, 250),
+                                             (320, 9001, 20)])
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 def test_gates_in_every_form(rows, cols, every, dtype):
     _round(rows, cols, TYPES[dtype], TYPES[dtype], "fogpd", every, 256, 0.5)
@@ -127,21 +145,9 @@ def _round(rows, cols, dt, wt, kind, every, group, ratio):
     r2, h2, saved = pwlq.block_norm(s["x"], s["f"], save=(group, ratio), **args)
     assert torch.equal(r, r2) and (h is None or torch.equal(h, h2))
     r64, rr, rf, err_r = _check_forward(s, every, scale, eps, offset, r, h)
-    if saved.f:
-        b, m, _ = act8_reference(s["f"].float().cpu().numpy(), group, ratio)
-        assert np.array_equal(saved.f.codes.cpu().numpy()[:, :cols], b)
-        assert not saved.f.codes[:, cols:].any()
-        assert np.array_equal(saved.f.ranges.cpu().numpy(), m)
+    _check_saved(s, saved, r64, err_r, cols, group, ratio)
     if saved.f_rstd is not None:
         check(saved.f_rstd[:, None], rf, U * FACTOR * rf, "f_rstd")
-    if saved.r:
-        # half a level of the piece, and what r was off in binary32
-        m = saved.r.ranges.double().repeat_interleave(group, dim=1)[:, :cols]
-        held = act8_values64(saved.r.codes, saved.r.ranges, cols, group, ratio)
-        half = torch.where(held.abs() > ratio * m * (1 - 1e-6), (1 - ratio) * m, ratio * m) / 126
-        half = torch.maximum(half, torch.where((held.abs() - ratio * m).abs() < 1e-3 * m, m / 126, 0.0))
-        assert ((held - r64).abs() <= half * (1 + 1e-5) + 2 * err_r + 1e-6 * m).all()
-        assert not saved.r.codes[:, cols:].any()
     grads = pwlq.block_norm_backward(saved, s["dh"], s["dr"])
     _check_backward(s, every, scale, offset, saved, grads, -(-rows // 100) + 48)
     again = pwlq.block_norm_backward(saved, s["dh"], s["dr"])
@@ -168,6 +174,35 @@ def test_strides_in_place_and_unaligned():
         r, h, saved = pwlq.block_norm(x, f, save=(32, 0.5), out=(x, f), **args)
         assert r.data_ptr() == x.data_ptr() and torch.equal(r, want[0]) and torch.equal(h, want[1])
         assert torch.equal(saved.r.codes, want[2].r.codes) and torch.equal(saved.f.codes, want[2].f.codes)
+
+
+@pytest.mark.parametrize("kind", ["fogpd", "pd"])
+@pytest.mark.parametrize("dtype,wtype", [("bf16", "bf16"), ("fp16", "fp32"), ("fp32", "fp32")])
+@pytest.mark.parametrize("rows,cols", [(5000, 40), (1300, 2048), (700, 4095)])
+def test_column_slices_of_wider_tensors(rows, cols, dtype, wtype, kind):
+    """Every operand and result at its own offset and pitch; nothing around the results is written."""
+    from paper_2002_00104_b200 import pwlq
+    s = _inputs(rows + cols, rows, cols, TYPES[dtype], TYPES[wtype], kind, 130)
+
+    def sliced(t, at, pad):
+        if t is None:
+            return None, None
+        wide = torch.full((t.shape[0], at + t.shape[1] + pad), 7.0, dtype=t.dtype, device="cuda")
+        wide[:, at:at + t.shape[1]] = t
+        return wide[:, at:at + t.shape[1]], wide
+
+    x, f, gate = sliced(s["x"], 1, 0)[0], sliced(s["f"], 3, 6)[0], sliced(s["gate"], 2, 3)[0]
+    (r, wide_r), (h, wide_h) = (sliced(torch.zeros_like(s["x"]), at, pad) for at, pad in ((5, 4), (8, 1)))
+    scale, eps, offset = -0.5, 1e-5, 0.25
+    _, _, saved = pwlq.block_norm(x, f, gate=gate, gate_tokens=130, save=(64, 0.4375), out=(r, h),
+                                  pre_weight=s["pre"], post_weight=s["post"], residual_scale=scale, eps=eps,
+                                  weight_offset=offset)
+    r64, _, _, err_r = _check_forward(s, 130, scale, eps, offset, r, h)
+    for wide, at in ((wide_r, 5), (wide_h, 8)):
+        assert (wide[:, :at] == 7).all() and (wide[:, at + cols:] == 7).all()
+    _check_saved(s, saved, r64, err_r, cols, 64, 0.4375)
+    grads = pwlq.block_norm_backward(saved, sliced(s["dh"], 1, 2)[0], sliced(s["dr"], 7, 0)[0])
+    _check_backward(s, 130, scale, offset, saved, grads, -(-rows // 100) + 48)
 
 
 def test_rows_of_zeros_infinities_and_nan_stay_in_their_rows():
