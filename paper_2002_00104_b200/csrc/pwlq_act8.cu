@@ -1,9 +1,11 @@
 // 8-bit activation checkpoints: encode (values -> bytes and group ranges) and decode.
 //
-// Both directions move each value once and keep nothing: they are bound by HBM.  A thread owns 16
-// (or 8) consecutive values, the 2 ... 32 threads of a group are neighbours in a warp and find the
-// group's range with shuffles, so the values are read once although the range must be known before
-// the first byte.
+// Both directions move each value once and keep nothing.  A thread owns 16 (or 8) consecutive values, the
+// 2 ... 32 threads of a group are neighbours in a warp and find the group's range with shuffles, so the
+// values are read once although the range must be known before the first byte.  The bound is HBM with the
+// instructions close behind (15 and 11 per value): 16384 x 4096 bf16 in 35.8 and 33.2 us, 5670 and 6110 GB/s.
+// Rows with gaps between them, or off their alignment, take the kernels that find a value's row first:
+// 16384 x 4104 55 and 53 us, 16384 x 4095, whose values and results are shifted, 73 and 73 us.
 #include <algorithm>
 
 #include "pwlq_act8.cuh"

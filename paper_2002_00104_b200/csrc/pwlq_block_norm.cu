@@ -6,12 +6,18 @@
 // the two reductions that depend on one another (of f, then of r; of the outer norm, then of the
 // inner one), so every operand crosses HBM once.
 //
-// Where the rows start on 32-byte boundaries (and, forward, there are enough of them), persistent CTAs
-// walk the rows and a ring of shared-memory stages holds the next ones, brought in by bulk copies: the
-// loads of a row are then in flight during the reductions of the rows before it, at no cost in
-// registers, and a thread works on 32 bytes of columns at a time, which shares the reductions' and
-// the ranges' cost.  Else a thread loads its values itself, eight at a time (see load8 for rows off
-// the boundary).
+// Forms (the rules and both sides of each stand at the launches, at the end of this file):
+//   narrow   rows of at most 1024 bytes: a few lanes per row, no barrier (400000 x 64 bf16: forward 35 us, a CTA
+//            per row 236; backward 75 against 432)
+//   ring     persistent CTAs walk the rows, and a ring of shared-memory stages holds the next ones, brought in by
+//            bulk copies: a row's loads are in flight during the reductions of the rows before it, at no cost in
+//            registers, and a thread works on 32 bytes of columns, which shares the cost of reductions and ranges
+//            (16384 x 4096 bf16: with checkpoints 141 us = 4790 GB/s against 213, backward 152 us = 4420 GB/s against
+//            243).  Bound by instruction issue: 61 and 52 instructions per value at 3.1 and 2.5 a cycle of 4.
+//            Backward, a pair of CTAs shares rows too wide for one CTA's registers (4096 x 12288: 217 against 314 us).
+//   row      forward without checkpoints, one CTA per row, 32 bytes of columns per thread
+//   direct   a thread loads its values itself, eight at a time: few rows, and rows off their alignment that the
+//            ring does not take (see load8)
 #include <algorithm>
 #include <mutex>
 #include <type_traits>
@@ -567,6 +573,66 @@ __global__ void __maxnreg__(ODD ? 80 : 64) block_norm_ring_kernel(const __grid_c
         T* const to = static_cast<T*>(q.a.h) + row * q.a.ldh;
         put32<T, ODD>(to + c, raw32(w, T()), live, turn, to + warp_c, cols - warp_c);
     }
+}
+
+// Forward without checkpoints, weights of the values' type, a row per CTA and no ring: the arithmetic, and so
+// the bits, of block_norm_ring_kernel.  A row is then so little work that many CTAs, each with its own loads in
+// flight, keep the memory busier than a ring does (16384 x 4096 bf16, one norm: 80.5 us = 6670 GB/s).
+template <typename T>
+__global__ void __maxnreg__(64) block_norm_row_kernel(const __grid_constant__ NormParams q) {
+    constexpr bool WF32 = sizeof(T) == 4;
+    constexpr int kP = kPairs32<T>;
+    __shared__ float buf[2][32];
+    CtaSum cta_sum{buf};
+    const int64_t row = blockIdx.x;
+    const bool live = (int)threadIdx.x * 2 * kP < (int)q.a.cols, post = q.a.post_weight, pre = q.a.pre_weight;
+    const int c = live ? (int)threadIdx.x * 2 * kP : (int)q.a.cols - 2 * kP;
+    const Raw32 x = load32_global(static_cast<const T*>(q.a.x) + row * q.a.ldx + c);
+    u64 r[kP], w[kP], s = 0ull;
+    Weights<T, WF32> wt;
+    if (q.a.f) {
+        const Raw32 raw = load32_global(static_cast<const T*>(q.a.f) + row * q.a.ldf + c);
+        const int64_t gate = q.a.gate ? row / q.a.gate_tokens * q.a.ldgate + c : 0;
+        u64 f[kP];
+        if (post) {
+            wt.load(q.a.post_weight, c);
+            pairs32(raw, f, T());
+#pragma unroll
+            for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
+            const float rstd_f = rsqrtf(fmaf(cta_sum(live ? sum8(s) : 0.0f), q.inv_cols, q.eps));
+            wt.get(w, q.offset);
+            if (q.a.gate) wt.load(q.a.gate, gate);
+#pragma unroll
+            for (int k = 0; k < kP; ++k) f[k] = mul2(mul2(f[k], both(rstd_f)), w[k]);
+        } else {
+            if (q.a.gate) wt.load(q.a.gate, gate);
+            pairs32(raw, f, T());
+        }
+        pairs32(x, r, T());
+#pragma unroll
+        for (int k = 0; k < kP; ++k) r[k] = mul2(r[k], both(q.scale));
+        if (q.a.gate) wt.get(w);
+#pragma unroll
+        for (int k = 0; k < kP; ++k) r[k] = q.a.gate ? fma2(f[k], w[k], r[k]) : add2(r[k], f[k]);
+    } else {
+        pairs32(x, r, T());
+#pragma unroll
+        for (int k = 0; k < kP; ++k) r[k] = mul2(r[k], both(q.scale));
+    }
+    s = 0ull;
+#pragma unroll
+    for (int k = 0; k < kP; ++k) s = fma2(r[k], r[k], s);
+    if (pre) {
+        cta_sum.post(live ? sum8(s) : 0.0f);
+        wt.load(q.a.pre_weight, c);
+    }
+    if (q.a.r && live) store32(static_cast<T*>(q.a.r) + row * q.a.ldr + c, raw32(r, T()));
+    if (!pre) return;
+    const float rstd_r = rsqrtf(fmaf(cta_sum.total(), q.inv_cols, q.eps));
+    wt.get(w, q.offset);
+#pragma unroll
+    for (int k = 0; k < kP; ++k) w[k] = mul2(mul2(r[k], both(rstd_r)), w[k]);
+    if (live) store32(static_cast<T*>(q.a.h) + row * q.a.ldh + c, raw32(w, T()));
 }
 
 // Sum over the aligned `lanes` (a power of two) lanes that share a row.
@@ -1536,9 +1602,16 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
     const int64_t resident = (int64_t)ring.ctas * sm_count();
     // A ring pays once every CTA has a few rows to walk (with checkpoints, bf16 1776 x 4096 18.1 against 24.1 us,
     // 592 rows 7.7 against 9.2, but 148 rows 5.1 against 4.5; without them 592 rows 5.3 against 4.9).  The rule
-    // does not ask for checkpoints, since saving them must not change r and h; without them and without a gate
-    // one row per CTA would be the faster form up to 4096 columns (2048: 88.6 against 100 us).
+    // does not ask for checkpoints: saving them does not change r and h.
     if ((rows32 || odd) && ring.threads <= (odd ? 768 : 1024) && ring.stages >= 2 && a.rows >= 2 * resident) {
+        // Without checkpoints, up to how many columns a CTA per row is faster than the ring: with one reduction
+        // 8192 (bf16 83 against 96 us, binary32 169 against 184 us; 12288: 98 against 99), with two 4096 (88 against 96;
+        // 8192: 99 against 91) or, binary32, 5120 (172 against 181; 6144: 247 against 179), with a gate between them
+        // 2048 (88 against 91; 2560: 95 against 88) or 2560 (166 against 166; 4096: 192 against 171).
+        constexpr bool kF = kSize == 4;
+        const int64_t light = !a.f || !a.post_weight ? 8192 : a.gate ? (kF ? 2560 : 2048) : kF ? 5120 : 4096;
+        if (!SAVE && !odd && q.wf32 == kF && a.cols <= light)
+            return run(block_norm_row_kernel<T>, (unsigned)a.rows, ring.threads, 0, stream, q);
         q.stages = ring.stages;
         q.group_lanes = (int)(a.group * kSize / 32);
         if (a.gate) {

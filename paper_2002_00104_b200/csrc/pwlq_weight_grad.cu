@@ -8,6 +8,11 @@
 // memory: nothing is transposed.  The sums stay in tensor memory, two tiles of 256 columns, so that
 // a tile's results leave while the next one is summed.
 //
+// Bound by the tensor pipe: 94 % busy, 8192 x 4096 x 4096 bf16 in 176 us (1562 TFLOP/s), next to 19 us of
+// decoding and 9 of adding pieces.  Decoding inside the product instead, by warps that feed the tensor cores
+// from shared memory, took 843 us in all against 263; decoding beside it, with flags between the two kernels,
+// 262 against 211 (back to back on warm caches).
+//
 // The pairs are persistent.  Whole tiles go round the pairs first; the tiles of the last, partial
 // round are cut along t so that they fill it, their binary32 pieces go to the workspace, and a
 // second kernel adds them in the order of t.

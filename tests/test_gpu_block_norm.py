@@ -113,7 +113,7 @@ def test_every_combination_of_operands(kind, dtype):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("rows,cols", [(301, 48), (77, 512), (2400, 1280), (7, 8400),
                                        (150, 8704), (4800, 75), (3000, 1283)])
-@pytest.mark.parametrize("dtype,wtype", [("bf16", "fp32"), ("fp32", "fp32")])
+@pytest.mark.parametrize("dtype,wtype", [("bf16", "bf16"), ("bf16", "fp32"), ("fp32", "fp32")])
 def test_every_combination_of_operands_in_every_form(kind, rows, cols, dtype, wtype):
     _round(rows, cols, TYPES[dtype], TYPES[wtype], kind, rows, 64, 0.4375)
 
