@@ -505,7 +505,8 @@ __global__ void __maxnreg__(ODD ? 80 : 64) block_norm_ring_kernel(const __grid_c
     // threads past the row repeat its last columns (so that a group's range stays its own) and
     // neither store nor count
     const bool live = (int)threadIdx.x * 2 * kP < (int)q.a.cols, post = q.a.post_weight, pre = q.a.pre_weight;
-    const int cols = (int)q.a.cols, c = live ? (int)threadIdx.x * 2 * kP : ODD ? (cols - 1) / (2 * kP) * (2 * kP) : cols - 2 * kP;
+    const int cols = (int)q.a.cols, end = ODD ? (cols - 1) / (2 * kP) * (2 * kP) : cols - 2 * kP;
+    const int c = live ? (int)threadIdx.x * 2 * kP : end;
     const int valid = ODD ? cols - c : 2 * kP;
     const int warp_c = (int)(threadIdx.x & ~31u) * 2 * kP;       // of the warp's first lane
     for (int64_t row = blockIdx.x; row < q.a.rows; row += gridDim.x) {

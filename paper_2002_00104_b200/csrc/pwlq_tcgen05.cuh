@@ -24,11 +24,6 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, unsigned parity
     }
     return false;
 }
-// Orders this thread's generic-proxy writes before asynchronous-proxy reads of either CTA.
-__device__ __forceinline__ void fence_proxy_async_all() {
-    asm volatile("fence.proxy.async;" ::: "memory");
-}
-
 __device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }

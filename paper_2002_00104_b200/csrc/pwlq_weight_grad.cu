@@ -465,8 +465,8 @@ cudaError_t launch(const WeightGrad& w, void* workspace, cudaStream_t stream) {
                                              (int)kSmemBytes))
         return e;
     const int64_t ctas = 2 * (p.s.units < pairs ? p.s.units : pairs);
-    if (cudaError_t e = launch_dependent(weight_grad_kernel<T>, dim3((unsigned)ctas), dim3(kThreads), kSmemBytes, stream, map,
-                                         xmap, p))
+    if (cudaError_t e = launch_dependent(weight_grad_kernel<T>, dim3((unsigned)ctas), dim3(kThreads), kSmemBytes,
+                                         stream, map, xmap, p))
         return e;
     const int64_t cut = (int64_t)p.s.tiles_n * p.s.tiles_k - p.s.whole;
     if (!cut) return cudaSuccess;

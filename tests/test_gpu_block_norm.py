@@ -341,3 +341,29 @@ def test_refusals():
     with pytest.raises(pwlq.PwlqError) as e:
         pwlq.block_norm_backward(saved, x, workspace=small)
     assert e.value.status == pwlq.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("cols", [512, 1024, 4001])
+def test_offsets_beyond_32_bits(cols):
+    """Rows far apart: the last ones start more than 2^31 elements into their tensors.  The results are
+    those of contiguous rows."""
+    from paper_2002_00104_b200 import pwlq
+    rows, pitch = 2600, 1 << 20
+    s = _inputs(cols, rows, cols, torch.bfloat16, torch.bfloat16, "fogpd", 700)
+    store = torch.empty(rows * pitch, dtype=torch.bfloat16, device="cuda")
+    far = [store.as_strided((rows, cols), (pitch, 1), 16384 * i + cols % 2) for i in range(6)]
+    for to, k in zip(far, ("x", "f", "dh", "dr")):
+        to.copy_(s[k])
+    args = dict(pre_weight=s["pre"], post_weight=s["post"], gate=s["gate"], gate_tokens=700)
+    near = [torch.empty(rows, cols + 16, dtype=torch.bfloat16, device="cuda")[:, :cols] for _ in range(6)]
+    for to, k in zip(near, ("x", "f", "dh", "dr")):
+        to.copy_(s[k])
+    for save in (None, (64, 0.5)):
+        r, h, saved = pwlq.block_norm(far[0], far[1], save=save, out=(far[4], far[5]), **args)
+        r2, h2, saved2 = pwlq.block_norm(near[0], near[1], save=save, out=(near[4], near[5]), **args)
+        assert torch.equal(r, r2) and torch.equal(h, h2)
+    assert torch.equal(saved.r.codes, saved2.r.codes) and torch.equal(saved.f.codes, saved2.f.codes)
+    got = pwlq.block_norm_backward(saved, far[2], far[3])
+    want = pwlq.block_norm_backward(saved2, near[2], near[3])
+    for k in want:
+        assert torch.equal(got[k], want[k]), k

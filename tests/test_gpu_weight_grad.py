@@ -99,6 +99,19 @@ def test_same_bits_again_and_on_another_stream():
     assert pwlq.device_status() == 0
 
 
+def test_offsets_beyond_32_bits():
+    """Rows of dy far apart: the last ones start more than 2^31 elements into it; same bits."""
+    from paper_2002_00104_b200 import pwlq
+    dy, saved = _case(5, 2600, 264, 272, torch.bfloat16, 64, 0.5)
+    store = torch.empty(2600 << 20, dtype=torch.bfloat16, device="cuda")
+    far = store.as_strided((2600, 264), (1 << 20, 1), 128)
+    far.copy_(dy)
+    assert torch.equal(pwlq.act8_weight_grad(far, saved), pwlq.act8_weight_grad(dy, saved))
+    odd = store.as_strided((2600, 264), (1 << 20, 1), 129)
+    odd.copy_(dy)
+    assert torch.equal(pwlq.act8_weight_grad(odd, saved), pwlq.act8_weight_grad(dy, saved))
+
+
 def test_no_rows():
     from paper_2002_00104_b200 import pwlq
     dy, saved = _case(1, 0, 20, 30, torch.bfloat16, 32, 0.5)
