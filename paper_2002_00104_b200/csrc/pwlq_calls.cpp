@@ -125,6 +125,18 @@ PyObject* tuple(std::initializer_list<PyObject*> items) {
     return t;
 }
 
+// Weights and gate of a block norm, which both directions take from the tensors they are given.
+void weights_of(pwlq_block_norm_args& b, const at::Tensor& pre, const at::Tensor& post, const at::Tensor& gate,
+                at::ScalarType wtype, int device) {
+    b.pre_weight = pre.defined() ? vector(pre, "pre_weight", b.cols, wtype, device) : nullptr;
+    b.post_weight = post.defined() ? vector(post, "post_weight", b.cols, wtype, device) : nullptr;
+    b.gate = nullptr;
+    if (!gate.defined()) return;
+    const Matrix m = matrix(gate, "gate", b.gate_rows, b.cols, wtype, device);
+    b.gate = m.p;
+    b.ldgate = m.ld;
+}
+
 // A checkpoint in one piece: the codes, then the ranges, to the next multiple of 32.
 int64_t pitch_of(int64_t cols) { return (cols + 15) / 16 * 16; }
 int64_t act8_bytes(int64_t rows, int64_t cols, int64_t group) {
@@ -140,6 +152,31 @@ Codes codes_at(void* memory, int64_t rows, int64_t cols) {
     uint8_t* p = static_cast<uint8_t*>(memory);
     return {p, pitch_of(cols), reinterpret_cast<float*>(p + rows * pitch_of(cols))};
 }
+
+// What a block norm keeps for its backward pass, in one piece: r's checkpoint (with pre_weight), f's (with
+// post_weight or gate), the factors of both norms.
+struct Kept {
+    int64_t f_at = 0, rstd_at = 0, bytes = 0;
+    bool keeps_f = false;
+    Kept() = default;
+    Kept(const pwlq_block_norm_args& b, bool pre, bool post, bool gate) : keeps_f(post || gate) {
+        const int64_t size = act8_bytes(b.rows, b.cols, b.group);
+        f_at = pre ? size : 0;
+        rstd_at = f_at + (keeps_f ? size : 0);
+        bytes = rstd_at + 8 * b.rows;
+    }
+    void place(pwlq_block_norm_args& b, void* memory, bool pre, bool post) const {
+        uint8_t* const base = static_cast<uint8_t*>(memory);
+        float* const factors = reinterpret_cast<float*>(base + rstd_at);
+        const Codes r = codes_at(base, b.rows, b.cols), f = codes_at(base + f_at, b.rows, b.cols);
+        b.r_codes = pre ? r.codes : nullptr;
+        b.r_ranges = pre ? r.ranges : nullptr;
+        b.r_rstd = pre ? factors : nullptr;
+        b.f_codes = keeps_f ? f.codes : nullptr;
+        b.f_ranges = keeps_f ? f.ranges : nullptr;
+        b.f_rstd = post ? factors + b.rows : nullptr;
+    }
+};
 
 // (x, group, ratio, codes pointer or 0, pitch, ranges pointer) -> new memory, or None where given
 PyObject* encode(Args a) {
@@ -216,17 +253,13 @@ PyObject* block_norm(Args a) {
     const at::ScalarType wtype = some.defined() ? some.scalar_type() : type;
     TORCH_CHECK_VALUE(wtype == type || wtype == at::kFloat, "weights and gate must be of x's type or float32");
     b.wtype = dtype_code(wtype);
-    if (pre.defined()) b.pre_weight = vector(pre, "pre_weight", cols, wtype, device);
-    if (post.defined()) b.post_weight = vector(post, "post_weight", cols, wtype, device);
     if (gate.defined()) {
         TORCH_CHECK_VALUE(gate.dim() == 2, "gate must be [gate_rows, cols]");
         b.gate_rows = gate.size(0);
-        m = matrix(gate, "gate", b.gate_rows, cols, wtype, device);
-        b.gate = m.p;
-        b.ldgate = m.ld;
         const int64_t n = std::max<int64_t>(b.gate_rows, 1);
         b.gate_tokens = every ? every : std::max<int64_t>((rows + n - 1) / n, 1);
     }
+    weights_of(b, pre, post, gate, wtype, device);
     if (!r.defined()) r = like(x);
     m = matrix(r, "r", rows, cols, type, device);
     b.r = m.p;
@@ -240,37 +273,24 @@ PyObject* block_norm(Args a) {
         h = at::Tensor();
     }
     at::Tensor memory;
-    int64_t f_at = 0, rstd_at = 0;
+    Kept kept;
     if (group) {
-        const int64_t size = act8_bytes(rows, cols, group);
-        const bool keeps_f = post.defined() || gate.defined();
-        f_at = pre.defined() ? size : 0;
-        rstd_at = f_at + (keeps_f ? size : 0);
-        memory = bytes(rstd_at + 8 * rows, x);
-        uint8_t* base = static_cast<uint8_t*>(memory.data_ptr());
         b.group = group;
         b.ldc = pitch_of(cols);
-        if (pre.defined()) {
-            const Codes c = codes_at(base, rows, cols);
-            b.r_codes = c.codes;
-            b.r_ranges = c.ranges;
-            b.r_rstd = reinterpret_cast<float*>(base + rstd_at);
-        }
-        if (keeps_f) {
-            const Codes c = codes_at(base + f_at, rows, cols);
-            b.f_codes = c.codes;
-            b.f_ranges = c.ranges;
-            if (post.defined()) b.f_rstd = reinterpret_cast<float*>(base + rstd_at) + rows;
-        }
+        kept = Kept(b, pre.defined(), post.defined(), gate.defined());
+        memory = bytes(kept.bytes, x);
+        kept.place(b, memory.data_ptr(), pre.defined(), post.defined());
     }
     check(lib.block_norm(&b, stream_of(device)), "pwlq_block_norm");
     return tuple({wrap(r), wrap(h), wrap(memory),
                   PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&b), sizeof(b)),
-                  PyLong_FromLongLong(f_at), PyLong_FromLongLong(rstd_at)});
+                  PyLong_FromLongLong(kept.f_at), PyLong_FromLongLong(kept.rstd_at)});
 }
 
 // (argument block, memory, has_f, dh, dr, pre, post, gate, workspace or None)
 //   -> (dx, df, dpre, dpost, dgate)
+// Of the forward call's argument block only sizes, types and numbers are used: what the tensors' memory
+// holds now is what counts, wherever it lies (a parameter's storage may have been replaced in between).
 PyObject* block_norm_backward(Args a) {
     PyObject* block = a.next();
     pwlq_block_norm_args b;
@@ -288,6 +308,13 @@ PyObject* block_norm_backward(Args a) {
     TORCH_CHECK_VALUE(memory.get_device() == device, "the forward call ran on ", memory.device(),
                       ", the gradient is on ", some.device());
     const at::ScalarType type = dtype_of(b.dtype);
+    const Kept kept(b, pre.defined(), post.defined(), gate.defined());
+    TORCH_CHECK_VALUE(memory.scalar_type() == at::kByte && memory.is_contiguous() && memory.numel() == kept.bytes,
+                      "the kept memory is not that of a forward call with these weights");
+    kept.place(b, memory.data_ptr(), pre.defined(), post.defined());
+    weights_of(b, pre, post, gate, dtype_of(b.wtype), device);
+    b.x = b.f = nullptr;
+    b.r = b.h = nullptr;
     pwlq_block_norm_grads g = {};
     if (dh.defined()) {
         const Matrix m = matrix(dh, "dh", b.rows, b.cols, type, device);

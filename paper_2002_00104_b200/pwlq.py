@@ -940,7 +940,8 @@ def act8_decode(saved: Act8, dtype=torch.float32, out=None, stream=None):
 class BlockNormSaved:
     """What ``block_norm`` keeps for ``block_norm_backward``: the checkpoints ``r`` and ``f`` and the
     norms' factors ``r_rstd`` and ``f_rstd`` (None where the call needs none), all in one piece of
-    memory, and the weights and gate it was given."""
+    memory, and the weights and gate it was given.  The backward pass reads those three tensors
+    again, wherever their memory is by then: they have to hold what the forward pass saw."""
     __slots__ = ("pre_weight", "post_weight", "gate", "shape", "has_f", "group", "ratio", "_memory",
                  "_block", "_f_at", "_rstd_at")
 

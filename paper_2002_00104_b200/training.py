@@ -71,6 +71,8 @@ class _BlockNorm(torch.autograd.Function):
     def forward(ctx, x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps, settings):
         r, h, ctx.saved = pwlq.block_norm(x, f, pre_weight, post_weight, gate, gate_tokens,
                                           residual_scale, eps, save=(settings.group, settings.ratio))
+        # autograd's check that they still hold what the forward pass saw
+        ctx.save_for_backward(pre_weight, post_weight, gate)
         ctx.set_materialize_grads(False)
         return r, h
 
@@ -78,6 +80,7 @@ class _BlockNorm(torch.autograd.Function):
     def backward(ctx, dr, dh):
         if dh is None:
             dh = torch.zeros_like(dr)
+        ctx.saved.pre_weight, ctx.saved.post_weight, ctx.saved.gate = ctx.saved_tensors
         g = pwlq.block_norm_backward(ctx.saved, dh.contiguous(),
                                      dr.contiguous() if dr is not None else None)
         return (g["dx"], g["df"], g["dpre"], g["dpost"], g["dgate"]) + (None,) * 4
