@@ -64,7 +64,7 @@ def train(forward, student, x, target, steps, lr=2e-2):
     leaves = [t.requires_grad_() for group in student.values() for t in group]
     losses, kept, out, loss, grads = [], 0, None, None, None
     for step in range(steps):
-        del out, loss, grads                      # and with them what the last step kept
+        del out, loss, grads                      # so that what is counted below is this step's alone
         before = torch.cuda.memory_allocated()
         out = forward(student, x)
         loss = (out.float() - target).square().mean()

@@ -874,6 +874,21 @@ class Act8:
         return self._ranges
 
 
+    def detached(self):
+        """(the byte tensor that holds the checkpoint, a checkpoint without it): for keeping the two
+        apart.  Only of checkpoints in one piece, as ``act8_encode`` and ``act8_empty`` make them."""
+        if self._memory is None:
+            raise ValueError("the checkpoint was made from two tensors")
+        return self._memory, Act8._inside(None, self._at, self.rows, self.cols, self.group, self.ratio)
+
+    def attached(self, memory: torch.Tensor) -> "Act8":
+        """The checkpoint in ``memory``, which holds what ``detached`` gave, wherever it lies."""
+        need = self._at + _act8_bytes(self.rows, self.cols, self.group)
+        if memory.dtype != torch.uint8 or not memory.is_contiguous() or memory.numel() < need:
+            raise ValueError(f"the memory of this checkpoint is {need} contiguous bytes")
+        return Act8._inside(memory, self._at, self.rows, self.cols, self.group, self.ratio)
+
+
 def _act8_bytes(rows: int, cols: int, group: int) -> int:
     """Size of a checkpoint in one piece: the codes, then the ranges, to the next multiple of 32."""
     if group < 1 or cols < 1:
@@ -944,6 +959,21 @@ class BlockNormSaved:
     again, wherever their memory is by then: they have to hold what the forward pass saw."""
     __slots__ = ("pre_weight", "post_weight", "gate", "shape", "has_f", "group", "ratio", "_memory",
                  "_block", "_f_at", "_rstd_at")
+
+    def detached(self):
+        """(the byte tensor that holds it all, the rest without it and without weights and gate)."""
+        rest = BlockNormSaved()
+        rest.pre_weight = rest.post_weight = rest.gate = rest._memory = None
+        for name in ("shape", "has_f", "group", "ratio", "_block", "_f_at", "_rstd_at"):
+            setattr(rest, name, getattr(self, name))
+        return self._memory, rest
+
+    def attached(self, memory: torch.Tensor) -> "BlockNormSaved":
+        """The same with ``memory``, which holds what ``detached`` gave, wherever it lies; weights and
+        gate are the caller's to set."""
+        _, whole = self.detached()
+        whole._memory = memory
+        return whole
 
     def _checkpoint(self, at: int) -> Act8:
         return Act8._inside(self._memory, at, *self.shape, self.group, self.ratio)

@@ -28,18 +28,31 @@ def best_ratio(x: torch.Tensor, group: int = 128, candidates: int = 32) -> float
     return float(ratios[sse.double().sum(dim=0).argmin()])
 
 
+# Checkpoints and weights are kept through autograd: released when backward has used them, refused a
+# second time unless the graph is retained, seen by saved-tensor hooks (which may hand back other
+# memory), and weights checked for changes in place.
+def _keep(ctx, saved, *tensors):
+    memory, ctx.layout = saved.detached()
+    ctx.save_for_backward(memory, *tensors)
+
+
+def _kept(ctx):
+    memory, *tensors = ctx.saved_tensors
+    return (ctx.layout.attached(memory), *tensors)
+
+
 class _Linear(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, settings):
-        ctx.saved = pwlq.act8_encode(x, group=settings.group, ratio=settings.ratio)
-        ctx.save_for_backward(weight)
+        saved = pwlq.act8_encode(x, group=settings.group, ratio=settings.ratio)
+        _keep(ctx, saved, weight)
         return x @ weight.t()
 
     @staticmethod
     def backward(ctx, dy):
-        weight, = ctx.saved_tensors
+        saved, weight = _kept(ctx)
         dx = dy @ weight if ctx.needs_input_grad[0] else None
-        dw = pwlq.act8_weight_grad(dy.contiguous(), ctx.saved) if ctx.needs_input_grad[1] else None
+        dw = pwlq.act8_weight_grad(dy.contiguous(), saved) if ctx.needs_input_grad[1] else None
         return dx, dw, None
 
 
@@ -51,12 +64,13 @@ def linear(x, weight, settings: Checkpoints):
 class _Silu(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, settings):
-        ctx.saved = pwlq.act8_encode(x, group=settings.group, ratio=settings.ratio)
+        _keep(ctx, pwlq.act8_encode(x, group=settings.group, ratio=settings.ratio))
         return torch.nn.functional.silu(x)
 
     @staticmethod
     def backward(ctx, dy):
-        x = pwlq.act8_decode(ctx.saved, dtype=dy.dtype)
+        saved, = _kept(ctx)
+        x = pwlq.act8_decode(saved, dtype=dy.dtype)
         s = torch.sigmoid(x)
         return dy * s * (1 + x * (1 - s)), None
 
@@ -69,10 +83,9 @@ def silu(x, settings: Checkpoints):
 class _BlockNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps, settings):
-        r, h, ctx.saved = pwlq.block_norm(x, f, pre_weight, post_weight, gate, gate_tokens,
-                                          residual_scale, eps, save=(settings.group, settings.ratio))
-        # autograd's check that they still hold what the forward pass saw
-        ctx.save_for_backward(pre_weight, post_weight, gate)
+        r, h, saved = pwlq.block_norm(x, f, pre_weight, post_weight, gate, gate_tokens,
+                                      residual_scale, eps, save=(settings.group, settings.ratio))
+        _keep(ctx, saved, pre_weight, post_weight, gate)
         ctx.set_materialize_grads(False)
         return r, h
 
@@ -80,8 +93,9 @@ class _BlockNorm(torch.autograd.Function):
     def backward(ctx, dr, dh):
         if dh is None:
             dh = torch.zeros_like(dr)
-        ctx.saved.pre_weight, ctx.saved.post_weight, ctx.saved.gate = ctx.saved_tensors
-        g = pwlq.block_norm_backward(ctx.saved, dh.contiguous(),
+        saved, *weights = _kept(ctx)
+        saved.pre_weight, saved.post_weight, saved.gate = weights
+        g = pwlq.block_norm_backward(saved, dh.contiguous(),
                                      dr.contiguous() if dr is not None else None)
         return (g["dx"], g["df"], g["dpre"], g["dpost"], g["dgate"]) + (None,) * 4
 

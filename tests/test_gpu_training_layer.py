@@ -72,3 +72,67 @@ def test_kept_memory_of_other_weights_is_refused():
     saved.pre_weight = None
     with pytest.raises(ValueError):
         pwlq.block_norm_backward(saved, None, d)
+
+
+def _layers():
+    """(name, function of leaves, leaves) for each autograd function."""
+    from paper_2002_00104_b200 import training
+    settings = training.Checkpoints(group=64, ratio=0.4375)
+    inputs, _ = _norm_inputs(rows=512, cols=1024)
+    x, w = _rand(7, 512, 1024).requires_grad_(), _rand(8, 256, 1024, scale=0.03).requires_grad_()
+    return [("linear", lambda *t: training.linear(*t, settings), [x, w]),
+            ("silu", lambda t: training.silu(t, settings), [x]),
+            ("block_norm", lambda *t: sum(training.block_norm(*t, gate_tokens=171, settings=settings)), inputs)]
+
+
+@pytest.mark.parametrize("which", range(3), ids=["linear", "silu", "block_norm"])
+def test_checkpoints_are_released_when_backward_has_used_them(which):
+    """The output, and with it the graph, lives on; a byte per value of x does not."""
+    _, layer, leaves = _layers()[which]
+    out = layer(*leaves)
+    seed = torch.ones_like(out)
+    torch.autograd.grad(out, leaves, seed)        # the libraries' own workspaces
+    del out
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_allocated()
+    out = layer(*leaves)
+    with_graph = torch.cuda.memory_allocated()
+    assert with_graph - before >= out.numel() * 2 + 512 * 1024
+    grads = torch.autograd.grad(out, leaves, seed)
+    del grads
+    assert torch.cuda.memory_allocated() - before < out.numel() * 2 + 4096
+    with pytest.raises(RuntimeError, match="second time"):
+        torch.autograd.grad(out, leaves, seed)
+
+
+@pytest.mark.parametrize("which", range(3), ids=["linear", "silu", "block_norm"])
+def test_a_retained_graph_and_saved_tensor_hooks(which):
+    _, layer, leaves = _layers()[which]
+    out = layer(*leaves)
+    seed = torch.ones_like(out)
+    want = torch.autograd.grad(out, leaves, seed, retain_graph=True)
+    again = torch.autograd.grad(out, leaves, seed)
+    packed = []
+
+    def to_host(t):
+        packed.append(t.dtype)
+        return t.cpu()
+
+    with torch.autograd.graph.saved_tensors_hooks(to_host, lambda t: t.cuda()):
+        out = layer(*leaves)
+    assert torch.uint8 in packed
+    moved = torch.autograd.grad(out, leaves, seed)
+    for a, b, c in zip(want, again, moved):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_memory_of_another_size_is_refused():
+    from paper_2002_00104_b200 import pwlq
+    memory, layout = pwlq.act8_encode(_rand(1, 4, 64)).detached()
+    assert layout.attached(memory).codes.data_ptr() == memory.data_ptr()
+    for bad in (memory[:-1], memory.view(torch.int32), memory.repeat(2)[::2]):
+        with pytest.raises(ValueError):
+            layout.attached(bad)
+    with pytest.raises(ValueError):
+        pwlq.Act8(torch.zeros(4, 64, dtype=torch.uint8, device="cuda"), torch.zeros(4, 1, device="cuda"), 64, 64,
+                  0.5).detached()
