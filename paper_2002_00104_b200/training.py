@@ -3,10 +3,14 @@ backward pass is 8-bit checkpoints, one byte per activation and one range per gr
 
 ``ratio`` is the breakpoint of the checkpoints' quantizer as a part of a group's range; ``best_ratio``
 finds it with the library's breakpoint search on a sample of the activations.
+
+The functions are differentiable once: in their gradients the kept activations are constants, so a
+second derivative would lack terms, and asking for one raises.
 """
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import pwlq
 
@@ -49,6 +53,7 @@ class _Linear(torch.autograd.Function):
         return x @ weight.t()
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         saved, weight = _kept(ctx)
         dx = dy @ weight if ctx.needs_input_grad[0] else None
@@ -68,6 +73,7 @@ class _Silu(torch.autograd.Function):
         return torch.nn.functional.silu(x)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         saved, = _kept(ctx)
         x = pwlq.act8_decode(saved, dtype=dy.dtype)
@@ -90,6 +96,7 @@ class _BlockNorm(torch.autograd.Function):
         return r, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dr, dh):
         if dh is None:
             dh = torch.zeros_like(dr)

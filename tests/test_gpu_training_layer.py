@@ -136,3 +136,15 @@ def test_memory_of_another_size_is_refused():
     with pytest.raises(ValueError):
         pwlq.Act8(torch.zeros(4, 64, dtype=torch.uint8, device="cuda"), torch.zeros(4, 1, device="cuda"), 64, 64,
                   0.5).detached()
+
+
+@pytest.mark.parametrize("which", range(3), ids=["linear", "silu", "block_norm"])
+def test_second_derivatives_are_refused(which):
+    _, layer, leaves = _layers()[which]
+    out = layer(*leaves)
+    first = torch.autograd.grad(out.float().square().sum(), leaves, create_graph=True)
+    second = sum(g.float().square().sum() for g in first)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(second, leaves, retain_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        second.backward()
