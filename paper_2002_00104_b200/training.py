@@ -63,6 +63,8 @@ class _Linear(torch.autograd.Function):
 
 def linear(x, weight, settings: Checkpoints):
     """x @ weight.T for x [rows, cols] in bf16 or fp16; x is kept as an 8-bit checkpoint."""
+    if weight.requires_grad and torch.is_grad_enabled() and x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError(f"the weight's gradient needs x in bfloat16 or float16, not {x.dtype}")
     return _Linear.apply(x, weight, settings)
 
 

@@ -148,3 +148,18 @@ def test_second_derivatives_are_refused(which):
         torch.autograd.grad(second, leaves, retain_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         second.backward()
+
+
+def test_linear_refuses_types_without_a_weight_gradient_in_the_forward_pass():
+    from paper_2002_00104_b200 import training
+    x, w = _rand(1, 8, 64, dtype=torch.float32), _rand(2, 32, 64, dtype=torch.float32)
+    settings = training.Checkpoints()
+    with pytest.raises(ValueError, match="bfloat16 or float16"):
+        training.linear(x, w.requires_grad_(), settings)
+    with torch.no_grad():                                   # no gradient will be asked for
+        y = training.linear(x, w, settings)
+    assert torch.equal(y, x @ w.detach().t())
+    x.requires_grad_()
+    y = training.linear(x, w.detach(), settings)            # a frozen weight
+    dx, = torch.autograd.grad(y.sum(), x)
+    assert torch.allclose(dx, w.detach().sum(0).expand(8, 64), rtol=1e-5, atol=1e-5)
