@@ -100,18 +100,20 @@ class _BlockNorm(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dr, dh):
-        if dh is None:
-            dh = torch.zeros_like(dr)
+        if dr is None and dh is None:
+            return (None,) * 9
         saved, *weights = _kept(ctx)
         saved.pre_weight, saved.post_weight, saved.gate = weights
-        g = pwlq.block_norm_backward(saved, dh.contiguous(),
-                                     dr.contiguous() if dr is not None else None)
+        if dh is None and saved.pre_weight is not None:
+            dh = torch.zeros_like(dr)
+        g = pwlq.block_norm_backward(saved, *(d.contiguous() if d is not None else None for d in (dh, dr)))
         return (g["dx"], g["df"], g["dpre"], g["dpost"], g["dgate"]) + (None,) * 4
 
 
 def block_norm(x, f, pre_weight, post_weight=None, gate=None, gate_tokens=None, residual_scale=1.0,
                eps=1e-6, settings=Checkpoints()):
     """(r, h): r = residual_scale * x + gate * N(f; post_weight), h = N(r; pre_weight).  f may be None
-    (the norm before the first block).  r and f are kept as 8-bit checkpoints."""
+    (the norm before the first block), and so may ``pre_weight`` (after the last one; h is None then).
+    r and f are kept as 8-bit checkpoints, as far as the gradients need them."""
     return _BlockNorm.apply(x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps,
                             settings)

@@ -163,3 +163,33 @@ def test_linear_refuses_types_without_a_weight_gradient_in_the_forward_pass():
     y = training.linear(x, w.detach(), settings)            # a frozen weight
     dx, = torch.autograd.grad(y.sum(), x)
     assert torch.allclose(dx, w.detach().sum(0).expand(8, 64), rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_block_norm_without_the_outer_norm(dtype):
+    from paper_2002_00104_b200 import pwlq, training
+    (x, f, _, post, gate), d = _norm_inputs(dtype=dtype)
+    r, h = training.block_norm(x, f, None, post, gate, gate_tokens=16)
+    assert h is None
+    got = torch.autograd.grad(r, (x, f, post, gate), d)
+    with torch.no_grad():
+        r2, _, saved = pwlq.block_norm(x, f, None, post, gate, gate_tokens=16, save=(128, 0.5))
+        want = pwlq.block_norm_backward(saved, dr=d)
+    assert torch.equal(r, r2)
+    for g, k in zip(got, ("dx", "df", "dpost", "dgate")):
+        assert torch.equal(g, want[k])
+
+
+@pytest.mark.parametrize("used", ["r", "h", "both"])
+def test_block_norm_with_one_output_used(used):
+    from paper_2002_00104_b200 import pwlq, training
+    leaves, d = _norm_inputs()
+    r, h = training.block_norm(*leaves, gate_tokens=16)
+    outs = [t for t, n in ((r, "r"), (h, "h")) if used in (n, "both")]
+    got = torch.autograd.grad(outs, leaves, [d] * len(outs))
+    with torch.no_grad():
+        _, _, saved = pwlq.block_norm(*leaves, gate_tokens=16, save=(128, 0.5))
+        want = pwlq.block_norm_backward(saved, torch.zeros_like(d) if used == "r" else d,
+                                        None if used == "h" else d)
+    for g, k in zip(got, ("dx", "df", "dpre", "dpost", "dgate")):
+        assert torch.equal(g, want[k])
