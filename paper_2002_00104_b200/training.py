@@ -78,9 +78,9 @@ class _Silu(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         saved, = _kept(ctx)
-        x = pwlq.act8_decode(saved, dtype=dy.dtype)
-        s = torch.sigmoid(x)
-        return dy * s * (1 + x * (1 - s)), None
+        # dy * s * (1 + x * (1 - s)) in 32 bits, rounded once: 1 + x * (1 - s) cancels near x = -1.28
+        x = pwlq.act8_decode(saved)
+        return torch.ops.aten.silu_backward(dy, x).to(dy.dtype), None
 
 
 def silu(x, settings: Checkpoints):

@@ -193,3 +193,28 @@ def test_block_norm_with_one_output_used(used):
                                         None if used == "h" else d)
     for g, k in zip(got, ("dx", "df", "dpre", "dpost", "dgate")):
         assert torch.equal(g, want[k])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 77), (600, 1024)])
+def test_silu_gradient_is_rounded_once(rows, cols, dtype):
+    """Against dy * s * (1 + x * (1 - s)) in binary64 at the checkpoint's values.  In binary32 s is good
+    to about 8 roundings (exp to 2 ulp, a sum, a quotient), 1 - s to 9 of 1, the factor therefore to 12
+    of 1 + |x|, and the products with s and dy add 10."""
+    from paper_2002_00104_b200 import pwlq, training
+    from train_util import U, check, held64
+    settings = training.Checkpoints(group=64, ratio=0.4375)
+    x = _rand(rows, rows, cols, scale=3.0, dtype=dtype).requires_grad_()
+    dy = _rand(cols, rows, cols, dtype=dtype)
+    y = training.silu(x, settings)
+    assert torch.equal(y, torch.nn.functional.silu(x))
+    dx, = torch.autograd.grad(y, x, dy)
+    v = held64(pwlq.act8_encode(x.detach(), 64, 0.4375))
+    s = torch.sigmoid(v)
+    bound = 24 * U * dy.double().abs() * s * (1 + v.abs())
+    check(dx, dy.double() * s * (1 + v * (1 - s)), bound, "dx")
+    # a gradient that is broadcast or transposed
+    for d in (dy[:1].expand(rows, cols), dy.t().contiguous().t()):
+        y = training.silu(x, settings)
+        dx, = torch.autograd.grad(y, x, d)
+        check(dx, d.double() * s * (1 + v * (1 - s)), 24 * U * d.double().abs() * s * (1 + v.abs()), "dx")
