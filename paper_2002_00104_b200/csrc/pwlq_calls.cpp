@@ -35,6 +35,12 @@ void check(int status, const char* what) {
     if (status != PWLQ_OK) throw Failed{status, what};
 }
 
+// A group length as the C ABI takes it: memory is sized with it before the library sees it.
+int group_of(int64_t v) {
+    if (v < 1 || v > 256) throw Failed{PWLQ_ERR_INVALID_ARG, "checkpoint group"};
+    return (int)v;
+}
+
 struct Args {
     PyObject* const* a;
     int i = 0;
@@ -181,7 +187,7 @@ struct Kept {
 // (x, group, ratio, codes pointer or 0, pitch, ranges pointer) -> new memory, or None where given
 PyObject* encode(Args a) {
     const at::Tensor x = a.tensor("x");
-    const int64_t group = a.integer();
+    const int group = group_of(a.integer());
     const double ratio = a.real();
     Codes c;
     c.codes = static_cast<uint8_t*>(a.pointer());
@@ -197,7 +203,7 @@ PyObject* encode(Args a) {
         memory = bytes(act8_bytes(rows, cols, group), x);
         c = codes_at(memory.data_ptr(), rows, cols);
     }
-    check(lib.encode(m.p, dtype_code(x.scalar_type()), rows, cols, m.ld, (int)group, (float)ratio, c.codes, c.ld,
+    check(lib.encode(m.p, dtype_code(x.scalar_type()), rows, cols, m.ld, group, (float)ratio, c.codes, c.ld,
                      c.ranges, stream_of(device)),
           "pwlq_act8_encode");
     return wrap(memory);
@@ -209,14 +215,15 @@ PyObject* decode(Args a) {
     uint8_t* codes = static_cast<uint8_t*>(a.pointer());
     const int64_t ldc = a.integer();
     float* ranges = static_cast<float*>(a.pointer());
-    const int64_t rows = a.integer(), cols = a.integer(), group = a.integer();
+    const int64_t rows = a.integer(), cols = a.integer();
+    const int group = group_of(a.integer());
     const double ratio = a.real();
     const int64_t code = a.integer();
     at::Tensor out = a.maybe("out");
     const int device = home(beside, "the checkpoint");
     if (!out.defined()) out = at::empty({rows, cols}, beside.options().dtype(dtype_of(code)));
     const Matrix m = matrix(out, "out", rows, cols, out.scalar_type(), device);
-    check(lib.decode(codes, ldc, ranges, rows, cols, (int)group, (float)ratio, m.p, dtype_code(out.scalar_type()),
+    check(lib.decode(codes, ldc, ranges, rows, cols, group, (float)ratio, m.p, dtype_code(out.scalar_type()),
                      m.ld, stream_of(device)),
           "pwlq_act8_decode");
     return wrap(out);
@@ -365,7 +372,8 @@ PyObject* weight_grad(Args a) {
     uint8_t* codes = static_cast<uint8_t*>(a.pointer());
     const int64_t ldc = a.integer();
     float* ranges = static_cast<float*>(a.pointer());
-    const int64_t kept = a.integer(), cols = a.integer(), group = a.integer();
+    const int64_t kept = a.integer(), cols = a.integer();
+    const int group = group_of(a.integer());
     const double ratio = a.real();
     const int64_t code = a.integer();
     at::Tensor out = a.maybe("out");
@@ -388,7 +396,7 @@ PyObject* weight_grad(Args a) {
     TORCH_CHECK_VALUE(workspace.scalar_type() == at::kByte && workspace.is_contiguous() && workspace.is_cuda() &&
                           workspace.get_device() == device,
                       "workspace must be contiguous uint8 on cuda:", device);
-    check(lib.grad(y.p, dtype_code(dy.scalar_type()), rows, outputs, y.ld, codes, ldc, ranges, cols, (int)group,
+    check(lib.grad(y.p, dtype_code(dy.scalar_type()), rows, outputs, y.ld, codes, ldc, ranges, cols, group,
                    (float)ratio, w.p, dtype_code(out.scalar_type()), w.ld, accumulate, workspace.data_ptr(),
                    (size_t)workspace.numel(), stream_of(device)),
           "pwlq_act8_weight_grad");

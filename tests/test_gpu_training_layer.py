@@ -218,3 +218,16 @@ def test_silu_gradient_is_rounded_once(rows, cols, dtype):
         y = training.silu(x, settings)
         dx, = torch.autograd.grad(y, x, d)
         check(dx, d.double() * s * (1 + v * (1 - s)), 24 * U * d.double().abs() * s * (1 + v.abs()), "dx")
+
+
+def test_group_lengths_beyond_32_bits_are_refused():
+    from paper_2002_00104_b200 import pwlq
+    x = _rand(1, 4, 512)
+    saved = pwlq.act8_encode(x)
+    wrong = pwlq.Act8(saved.codes, saved.ranges[:, :1].contiguous(), 512, 2 ** 32 + 64, 0.5)
+    for call in (lambda: pwlq.act8_encode(x, group=2 ** 32 + 64), lambda: pwlq.act8_decode(wrong),
+                 lambda: pwlq.act8_weight_grad(x, wrong),
+                 lambda: pwlq.block_norm(x, pre_weight=x[0].contiguous(), save=(2 ** 32 + 64, 0.5))):
+        with pytest.raises(pwlq.PwlqError) as e:
+            call()
+        assert e.value.status == pwlq.ERR_INVALID_ARG

@@ -1,0 +1,26 @@
+"""Arguments of the Python training calls that are refused before any CUDA call."""
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def pwlq():
+    from paper_2002_00104_b200 import build, pwlq
+    build.build()
+    pwlq.load_library()
+    return pwlq
+
+
+@pytest.mark.parametrize("group", [2 ** 32 + 64, 2 ** 32 + 32, 2 ** 33 + 256, -2 ** 32 + 128, 257, 0, -64])
+def test_group_lengths_beyond_32_bits(pwlq, group):
+    """The low 32 bits of some of these are a valid group: taken for it, the call would write more ranges
+    than the memory holds.  Refused before the device of the tensors is looked at."""
+    x = torch.zeros(4, 512)
+    codes = torch.zeros(4, 512, dtype=torch.uint8)
+    calls = pwlq._calls()
+    for call in (lambda: calls.encode(x, group, 0.5, 0, 0, 0, 0),
+                 lambda: calls.decode(codes, 0, 512, 0, 4, 512, group, 0.5, 0, None),
+                 lambda: calls.weight_grad(x, codes, 0, 512, 0, 4, 512, group, 0.5, -1, None, 0, None)):
+        with pytest.raises(pwlq.PwlqError) as e:
+            call()
+        assert e.value.status == pwlq.ERR_INVALID_ARG
