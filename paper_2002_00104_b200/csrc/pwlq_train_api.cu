@@ -125,8 +125,8 @@ size_t pwlq_block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int6
 int pwlq_block_norm_backward(const pwlq_block_norm_args* fwd, const pwlq_block_norm_grads* grads,
                              void* stream) {
     if (!fwd || !grads) return PWLQ_ERR_INVALID_ARG;
-    const pwlq_block_norm_args& a = *fwd;
-    const pwlq_block_norm_grads& g = *grads;
+    pwlq_block_norm_args a = *fwd;
+    pwlq_block_norm_grads g = *grads;
     if (int rc = check_block(a)) return rc;
     const int64_t dt = a.dtype;
     const bool some = a.rows > 0;
@@ -151,6 +151,10 @@ int pwlq_block_norm_backward(const pwlq_block_norm_args* fwd, const pwlq_block_n
         if (!g.workspace || g.workspace_bytes < 0 || (size_t)g.workspace_bytes < need)
             return PWLQ_ERR_WORKSPACE;
         if (misaligned(g.workspace, 256)) return PWLQ_ERR_INVALID_ARG;
+    }
+    if (a.gate_rows == 0) {                              // rows is 0, too: neither has a row to touch
+        a.gate = nullptr;
+        g.dgate = nullptr;
     }
     return from_cuda(pwlq::launch_block_norm_backward(a, g, as_stream(stream)));
 }
