@@ -67,6 +67,14 @@ int check_block(const pwlq_block_norm_args& a) {
     return PWLQ_OK;
 }
 
+// A gate for more rows than there are is one for all of them; the kernels add the length to row numbers.
+pwlq_block_norm_args with_gate_length(const pwlq_block_norm_args& given) {
+    pwlq_block_norm_args a = given;
+    const int64_t most = a.rows > 0 ? a.rows : 1;
+    if (a.gate && a.gate_tokens > most) a.gate_tokens = most;
+    return a;
+}
+
 // A checkpoint of the block norm: all of its parts or none.
 bool bad_saved(const pwlq_block_norm_args& a, const uint8_t* codes, const float* ranges,
                const float* rstd) {
@@ -111,7 +119,7 @@ int pwlq_block_norm(const pwlq_block_norm_args* args, void* stream) {
     if (bad_saved(a, a.r_codes, a.r_ranges, a.r_rstd) || bad_saved(a, a.f_codes, a.f_ranges, a.f_rstd))
         return PWLQ_ERR_INVALID_ARG;
     if (a.rows == 0) return PWLQ_OK;
-    return from_cuda(pwlq::launch_block_norm(a, as_stream(stream)));
+    return from_cuda(pwlq::launch_block_norm(with_gate_length(a), as_stream(stream)));
 }
 
 size_t pwlq_block_norm_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t gate_rows) {
@@ -156,7 +164,7 @@ int pwlq_block_norm_backward(const pwlq_block_norm_args* fwd, const pwlq_block_n
         a.gate = nullptr;
         g.dgate = nullptr;
     }
-    return from_cuda(pwlq::launch_block_norm_backward(a, g, as_stream(stream)));
+    return from_cuda(pwlq::launch_block_norm_backward(with_gate_length(a), g, as_stream(stream)));
 }
 
 size_t pwlq_act8_weight_grad_workspace_bytes(int64_t rows, int64_t outputs, int64_t cols,

@@ -39,3 +39,36 @@ def test_the_gradient_of_no_gates_is_not_written():
     assert lib.pwlq_block_norm_backward(args, gradients(lddh=64, lddr=64, lddx=64, lddf=64, dpre=dpre, dpost=dpost,
                                                         dgate=dgate, ws=ws, bytes=1024), _stream()) == pwlq.OK
     assert (dpre == 0).all() and (dpost == 0).all() and (dgate == 3).all()
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 300, 5000])
+@pytest.mark.parametrize("tokens", [2 ** 63 - 1, 2 ** 63 - 2, 2 ** 62, 2 ** 31, 2 ** 32 + 1])
+@pytest.mark.parametrize("cols", [64, 1200])
+def test_gates_of_more_rows_than_there_are(rows, tokens, cols):
+    """As if the gate were for exactly the rows; the rows around the gate's gradient stay as they are."""
+    from paper_2002_00104_b200 import pwlq
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    x, f, dh, dr = (torch.randn(rows, cols, generator=g, device="cuda") for _ in range(4))
+    pre, post = (torch.rand(cols, generator=g, device="cuda") + 0.5 for _ in range(2))
+    gate = torch.rand(2, cols, generator=g, device="cuda")
+    want = pwlq.block_norm(x, f, pre, post, gate, gate_tokens=rows, save=(64, 0.5))
+    grads = pwlq.block_norm_backward(want[2], dh, dr)
+    got = pwlq.block_norm(x, f, pre, post, gate, gate_tokens=tokens, save=(64, 0.5))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    again = pwlq.block_norm_backward(got[2], dh, dr)
+    for k in grads:
+        assert torch.equal(grads[k], again[k]), k
+    assert (again["dgate"][1] == 0).all()
+
+    lib, saved = pwlq.load_library(), got[2]
+    around = torch.full((4, cols), 7.0, device="cuda")
+    ws = torch.empty(lib.pwlq_block_norm_backward_workspace_bytes(rows, cols, 2), dtype=torch.uint8, device="cuda")
+    args = block(rows=rows, cols=cols, pre=pre, post=post, gate=gate, ldgate=cols, gate_rows=2, gate_tokens=tokens,
+                 scale=1.0, eps=1e-6, group=64, ratio=0.5, ldc=saved.r.codes.shape[1], r_codes=saved.r.codes,
+                 r_ranges=saved.r.ranges, r_rstd=saved.r_rstd, f_codes=saved.f.codes, f_ranges=saved.f.ranges,
+                 f_rstd=saved.f_rstd)
+    out = gradients(dh=dh, lddh=cols, dr=dr, lddr=cols, dgate=around[1:], ws=ws, bytes=ws.numel())
+    assert lib.pwlq_block_norm_backward(args, out, _stream()) == pwlq.OK
+    assert torch.equal(around[1:3], grads["dgate"])
+    assert (around[0] == 7).all() and (around[3] == 7).all()
