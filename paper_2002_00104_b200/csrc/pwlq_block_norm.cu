@@ -1541,12 +1541,20 @@ inline int threads_for(int64_t cols, int per_thread) {
     return (int)((n + 31) / 32 * 32);
 }
 
+// Shared memory above the default 48 KB has to be allowed to a kernel before its launch.  It is allowed
+// the most that any call of its form asks for, never a call's own size: calls from several threads share
+// the attribute, and a smaller one set between another's setting and launch made that launch fail.
+constexpr size_t kSmemBudget = 160 * 1024;      // what a multiprocessor's rings may take for their stages
+constexpr size_t kRingMost = kSmemBudget + 24 * kTurn * 16 + 8192 * sizeof(float);   // stages, turns, gathered
+constexpr size_t kDirectMost = 512 * (2 * 4 * 8 + 32) * sizeof(float);               // sums, gathered
+template <typename K>
+cudaError_t allow_smem(K* kernel, size_t smem, size_t most) {
+    if (smem <= 12 * 1024) return cudaSuccess;  // with the static part below 48 KB
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
 template <typename K, typename P>
-cudaError_t run(K* kernel, unsigned ctas, int threads, size_t smem, cudaStream_t stream, const P& p) {
-    if (smem > 12 * 1024) {             // with the static part, possibly above the default 48 KB
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return e;
-    }
+cudaError_t run(K* kernel, unsigned ctas, int threads, size_t smem, size_t most, cudaStream_t stream, const P& p) {
+    if (const cudaError_t e = allow_smem(kernel, smem, most)) return e;
     kernel<<<ctas, threads, smem, stream>>>(p);
     return cudaGetLastError();
 }
@@ -1554,8 +1562,7 @@ cudaError_t run(K* kernel, unsigned ctas, int threads, size_t smem, cudaStream_t
 // A ring kernel's launch: threads of 32 bytes of columns each; CTAs that share a multiprocessor, as
 // far as their registers allow (`threads_per_sm`); stages of `bytes` for each of them.
 struct RingPlan { int threads, ctas, stages; };
-// what all of them may take for their stages: two of every width up to the ring's limits fit
-constexpr size_t kSmemBudget = 160 * 1024;
+// two stages of every width up to the ring's limits fit
 RingPlan ring_plan(int64_t cols, size_t size, int threads_per_sm, size_t bytes) {
     RingPlan r;
     r.threads = threads_for(cols, (int)(32 / size));
@@ -1616,7 +1623,7 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
         constexpr bool kF = kSize == 4;
         const int64_t light = !a.f || !a.post_weight ? 8192 : a.gate ? (kF ? 2560 : 2048) : kF ? 5120 : 4096;
         if (!SAVE && !odd && q.wf32 == kF && a.cols <= light)
-            return run(block_norm_row_kernel<T>, (unsigned)a.rows, ring.threads, 0, stream, q);
+            return run(block_norm_row_kernel<T>, (unsigned)a.rows, ring.threads, 0, 0, stream, q);
         q.stages = ring.stages;
         q.group_lanes = (int)(a.group * kSize / 32);
         if (a.gate) {
@@ -1630,14 +1637,14 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
                                      : block_norm_ring_kernel<T, SAVE, false, true>;
         }
         return run(kernel, (unsigned)resident, ring.threads, turn_bytes(odd, ring.threads) + ring.stages * stage,
-                   stream, q);
+                   kRingMost, stream, q);
     }
     const unsigned rows = (unsigned)a.rows;
     if (a.cols <= 8192)
-        return vec ? run(block_norm_kernel<T, 1, true, SAVE>, rows, threads_for(a.cols, 8), 0, stream, q)
-                   : run(block_norm_kernel<T, 1, false, SAVE>, rows, threads_for(a.cols, 8), 0, stream, q);
-    return vec ? run(block_norm_kernel<T, 2, true, SAVE>, rows, threads_for(a.cols, 16), 0, stream, q)
-               : run(block_norm_kernel<T, 2, false, SAVE>, rows, threads_for(a.cols, 16), 0, stream, q);
+        return vec ? run(block_norm_kernel<T, 1, true, SAVE>, rows, threads_for(a.cols, 8), 0, 0, stream, q)
+                   : run(block_norm_kernel<T, 1, false, SAVE>, rows, threads_for(a.cols, 8), 0, 0, stream, q);
+    return vec ? run(block_norm_kernel<T, 2, true, SAVE>, rows, threads_for(a.cols, 16), 0, 0, stream, q)
+               : run(block_norm_kernel<T, 2, false, SAVE>, rows, threads_for(a.cols, 16), 0, 0, stream, q);
 }
 template <typename T>
 cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
@@ -1686,8 +1693,7 @@ cudaError_t backward_pairs(GradParams& p, unsigned pairs, cudaStream_t stream) {
     const size_t smem = p.gathered + (p.gates && p.g.dpost ? (size_t)a.cols / 2 * sizeof(float) : 0);
     auto* kernel = p.q.wf32 ? block_norm_backward_ring_kernel<T, true, true, false>
                             : block_norm_backward_ring_kernel<T, sizeof(T) == 4, true, false>;
-    if (const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem))
-        return e;
+    if (const cudaError_t e = allow_smem(kernel, smem, kRingMost)) return e;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = 2;
@@ -1716,8 +1722,8 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
         const int threads = threads_for(a.cols, 32);
         p.gathered = (unsigned)((size_t)2 * 4 * 8 * sizeof(float) * threads);     // at most 128 KB of sums
         const size_t smem = p.gathered + (gathers ? (size_t)threads * 32 * sizeof(float) : 0);
-        return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, smem, stream, p)
-                   : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, smem, stream, p);
+        return vec ? run(block_norm_backward_kernel<T, 4, true, true>, ctas, threads, smem, kDirectMost, stream, p)
+                   : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, smem, kDirectMost, stream, p);
     }
     const bool rows32 = rows32_backward<T>(a, g);
     // Rows that lie anywhere, 16-bit types: 16384 x 4095 352 -> 254 us, 16384 x 4104 406 -> 356 us against
@@ -1737,12 +1743,12 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
             if (odd) kernel = p.q.wf32 ? block_norm_backward_ring_kernel<T, true, false, true>
                                        : block_norm_backward_ring_kernel<T, false, false, true>;
         }
-        return run(kernel, ctas, ring.threads, smem, stream, p);
+        return run(kernel, ctas, ring.threads, smem, kRingMost, stream, p);
     }
     const int threads = threads_for(a.cols, 8);
     const size_t smem = gathers ? (size_t)threads * 8 * sizeof(float) : 0;
-    return vec ? run(block_norm_backward_kernel<T, 1, true, false>, ctas, threads, smem, stream, p)
-               : run(block_norm_backward_kernel<T, 1, false, false>, ctas, threads, smem, stream, p);
+    return vec ? run(block_norm_backward_kernel<T, 1, true, false>, ctas, threads, smem, kDirectMost, stream, p)
+               : run(block_norm_backward_kernel<T, 1, false, false>, ctas, threads, smem, kDirectMost, stream, p);
 }
 template <typename W, int V>
 cudaError_t sums(const GradParams& p, int64_t ctas, cudaStream_t stream) {

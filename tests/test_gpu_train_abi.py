@@ -72,3 +72,43 @@ def test_gates_of_more_rows_than_there_are(rows, tokens, cols):
     assert lib.pwlq_block_norm_backward(args, out, _stream()) == pwlq.OK
     assert torch.equal(around[1:3], grads["dgate"])
     assert (around[0] == 7).all() and (around[3] == 7).all()
+
+
+def test_calls_of_different_widths_from_several_threads():
+    """Threads that share a kernel, whose calls need 24 to 192 KB of shared memory: every call is accepted
+    and gives what it gives alone."""
+    import threading
+
+    from paper_2002_00104_b200 import pwlq
+    lib, rows = pwlq.load_library(), 4
+    cases = []
+    for cols in (2048, 8192, 4096, 6144, 16384, 9000):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(cols)
+        x, dh, dr = (torch.randn(rows, cols, generator=g, device="cuda").bfloat16() for _ in range(3))
+        pre = torch.ones(cols, device="cuda").bfloat16()
+        _, _, saved = pwlq.block_norm(x, None, pre, save=(64, 0.5))
+        want = pwlq.block_norm_backward(saved, dh, dr)["dx"]
+        dx = torch.empty_like(x)
+        args = block(rows=rows, cols=cols, dtype=1, wtype=1, pre=pre, scale=1.0, eps=1e-6, group=64, ratio=0.5,
+                     ldc=saved.r.codes.shape[1], r_codes=saved.r.codes, r_ranges=saved.r.ranges, r_rstd=saved.r_rstd)
+        out = gradients(dh=dh, lddh=cols, dr=dr, lddr=cols, dx=dx, lddx=cols)
+        cases.append((args, out, dx, want, (saved, dh, dr, pre)))
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(args, out, stream):
+        for _ in range(3000):
+            if lib.pwlq_block_norm_backward(args, out, stream.cuda_stream) != pwlq.OK:
+                failed.append(1)
+
+    threads = [threading.Thread(target=work, args=(*c[:2], torch.cuda.Stream())) for c in cases]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed, f"{len(failed)} calls refused"
+    for _, _, dx, want, _ in cases:
+        assert torch.equal(dx, want)
+    assert pwlq.device_status() == 0
