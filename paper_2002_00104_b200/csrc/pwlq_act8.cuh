@@ -329,7 +329,8 @@ __device__ __forceinline__ uint2 act8_bytes8(const float* x, float m, const Piec
 
 // The eight values of eight bytes times a factor, in pairs, to within a few roundings (the gradients'
 // use; act8_values8 gives the format's own bits).  f = 128 + j from a byte permutation; the pieces are
-// the lines s1 * (f - 128) and p + s2 * (f - 192), one fused operation each.
+// the lines s1 * (f - 128) and p + s2 * (f - 192), one fused operation each.  192 steps of the tail must not
+// overflow: m * factor <= 1.1e38.
 struct Act8Lines { u64 s1, z1, s2, z2; };
 __device__ __forceinline__ Act8Lines act8_lines(float m, float ratio, float factor) {
     const float p = m * ratio, s1 = p * (1.0f / kAct8Levels) * factor, s2 = (m - p) * (1.0f / kAct8Levels) * factor;

@@ -734,6 +734,9 @@ block_norm_narrow_kernel(const __grid_constant__ NormParams q, int lanes) {
 // every thread touches its own columns only.
 // Workspace: [ctas][cols] of dpre, [ctas][cols] of dpost, [2 * ctas][cols] of dgate: CTA b's share of
 // the gate of its first row, and of its last one if that is another.
+// Factor on an f that enters without a norm, so that the lines of its values (act8_lines) stay in range up to
+// the largest: A is a quarter of the sum then, and dgate is multiplied back (both exact).
+constexpr float kAsItIs = 0.25f;
 struct GradParams {
     NormParams q;
     pwlq_block_norm_grads g;
@@ -760,6 +763,9 @@ __device__ __forceinline__ void finish_gate(const GradParams& p, int64_t cta, in
             weights8<VEC, T>(a.post_weight, p.q.wf32, 0, c, valid, p.q.offset, w);
 #pragma unroll
             for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], w[k]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], both(1.0f / kAsItIs));
         }
         floats8(v, f);
         const int64_t from = gate * a.gate_tokens, to = min(from + a.gate_tokens, a.rows);
@@ -915,7 +921,7 @@ block_norm_backward_kernel(const __grid_constant__ GradParams p) {
     int64_t gate_end = (gate + 1) * q.a.gate_tokens;
 
     // a row's ranges and factors, requested one row ahead
-    float mr[VC], mf[VC], rstd_r = 0.0f, rstd_f = 1.0f;
+    float mr[VC], mf[VC], rstd_r = 0.0f, rstd_f = kAsItIs;
     auto fetch = [&](int64_t row) {
         if (pre) rstd_r = q.a.r_rstd[row];
         if (post) rstd_f = q.a.f_rstd[row];
@@ -1150,7 +1156,7 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
     };
 
     // a row's ranges and factors, requested one row ahead
-    float next_mr = 0.0f, next_mf = 0.0f, next_rr = 0.0f, next_rf = 1.0f;
+    float next_mr = 0.0f, next_mf = 0.0f, next_rr = 0.0f, next_rf = kAsItIs;
     auto fetch = [&](int64_t row) {
         if (pre) next_rr = q.a.r_rstd[row];
         if (post) next_rf = q.a.f_rstd[row];
@@ -1275,7 +1281,7 @@ block_norm_backward_narrow_kernel(const __grid_constant__ GradParams p, int lane
         const bool live = inside && row < q.a.rows;
         const int64_t t = min(row, q.a.rows - 1), range = t * q.groups + (c >> q.group_shift);
         Raw32 raw_dh, raw_dr;
-        float mr = 0.0f, mf = 0.0f, rr = 0.0f, rf = 1.0f;
+        float mr = 0.0f, mf = 0.0f, rr = 0.0f, rf = kAsItIs;
         uint4 rb, fb;
         auto bytes = [&](const uint8_t* codes) {
             const uint8_t* from = codes + t * q.a.ldc + c;
@@ -1401,9 +1407,12 @@ template <int V> struct alignas(4 * V) Columns {
         for (int k = 0; k < V; ++k) v[k] += x.v[k];
     }
     template <typename W> __device__ __forceinline__ void times(const W* w, int c, float offset) {
-        if (!w) return;
 #pragma unroll
         for (int k = 0; k < V; ++k) v[k] *= to_f32(w[c + k]) + offset;
+    }
+    __device__ __forceinline__ void times(float w) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] *= w;
     }
     template <typename W> __device__ __forceinline__ void put(W* to) const {
 #pragma unroll
@@ -1483,7 +1492,8 @@ block_norm_sums_kernel(const __grid_constant__ GradParams p, int ctas, bool few,
     if (threadIdx.y != 0 || c >= cols) return;
     if (blockIdx.y == 1 && a.gate && !p.gates) {   // s is A, of all rows
         Columns<V> x = s;
-        x.times(static_cast<const W*>(a.post_weight), c, p.q.offset);
+        if (a.post_weight) x.times(static_cast<const W*>(a.post_weight), c, p.q.offset);
+        else x.times(1.0f / kAsItIs);
         if (dgate) x.put(dgate + c);
         s.times(static_cast<const W*>(a.gate), c, 0.0f);
     }
