@@ -229,12 +229,13 @@ PyObject* decode(Args a) {
     return wrap(out);
 }
 
-// (x, f, pre, post, gate, gate_tokens or 0, scale, eps, offset, group or 0, ratio, r or None, h or None)
+// (x, f, pre, post, gate, gate_tokens or None, scale, eps, offset, group or 0, ratio, r or None, h or None)
 //   -> (r, h, memory, argument block, offset of f's checkpoint, offset of the factors)
 PyObject* block_norm(Args a) {
     const at::Tensor x = a.tensor("x"), f = a.maybe("f"), pre = a.maybe("pre_weight"), post = a.maybe("post_weight"),
                      gate = a.maybe("gate");
-    const int64_t every = a.integer();
+    const bool given = !a.none();          // without a gate its length does not matter
+    const int64_t every = given ? a.integer() : (a.next(), 0);
     pwlq_block_norm_args b = {};
     b.residual_scale = a.real();
     b.eps = a.real();
@@ -264,7 +265,7 @@ PyObject* block_norm(Args a) {
         TORCH_CHECK_VALUE(gate.dim() == 2, "gate must be [gate_rows, cols]");
         b.gate_rows = gate.size(0);
         const int64_t n = std::max<int64_t>(b.gate_rows, 1);
-        b.gate_tokens = every ? every : std::max<int64_t>((rows + n - 1) / n, 1);
+        b.gate_tokens = given ? every : std::max<int64_t>((rows + n - 1) / n, 1);
     }
     weights_of(b, pre, post, gate, wtype, device);
     if (!r.defined()) r = like(x);

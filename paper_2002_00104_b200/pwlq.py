@@ -1017,7 +1017,7 @@ def block_norm(x, f=None, pre_weight=None, post_weight=None, gate=None, gate_tok
     if save is not None and group < 1:
         raise PwlqError(ERR_INVALID_ARG, "checkpoint group")
     r, h, memory, block, f_at, rstd_at = _calls().block_norm(
-        x, f, pre_weight, post_weight, gate, gate_tokens or 0, residual_scale, eps, weight_offset,
+        x, f, pre_weight, post_weight, gate, gate_tokens, residual_scale, eps, weight_offset,
         group, ratio, r, h)
     if save is None:
         return r, h, None

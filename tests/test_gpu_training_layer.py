@@ -231,3 +231,17 @@ def test_group_lengths_beyond_32_bits_are_refused():
         with pytest.raises(pwlq.PwlqError) as e:
             call()
         assert e.value.status == pwlq.ERR_INVALID_ARG
+
+
+def test_gates_of_no_tokens_are_refused():
+    from paper_2002_00104_b200 import pwlq
+    (x, f, pre, post, gate), _ = _norm_inputs()
+    with torch.no_grad():
+        for tokens in (0, -1, -2 ** 63):
+            with pytest.raises(pwlq.PwlqError) as e:
+                pwlq.block_norm(x, f, pre, post, gate, gate_tokens=tokens)
+            assert e.value.status == pwlq.ERR_INVALID_ARG
+            pwlq.block_norm(x, f, pre, post, gate_tokens=tokens)         # there is no gate
+        want = pwlq.block_norm(x, f, pre, post, gate, gate_tokens=16)
+        got = pwlq.block_norm(x, f, pre, post, gate)                     # 48 rows over 3 gates
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
