@@ -845,6 +845,7 @@ class Act8:
     __slots__ = ("rows", "cols", "group", "ratio", "_memory", "_at", "_codes", "_ranges")
 
     def __init__(self, codes: torch.Tensor, ranges: torch.Tensor, cols: int, group: int, ratio: float):
+        _checkpoint_size(cols, group)
         self.rows, self.cols, self.group, self.ratio = codes.shape[0], cols, group, ratio
         self._memory, self._codes, self._ranges = None, codes, ranges
 
@@ -889,10 +890,14 @@ class Act8:
         return Act8._inside(memory, self._at, self.rows, self.cols, self.group, self.ratio)
 
 
-def _act8_bytes(rows: int, cols: int, group: int) -> int:
-    """Size of a checkpoint in one piece: the codes, then the ranges, to the next multiple of 32."""
+def _checkpoint_size(cols: int, group: int) -> None:
     if group < 1 or cols < 1:
         raise PwlqError(ERR_INVALID_ARG, f"checkpoint of {cols} columns in groups of {group}")
+
+
+def _act8_bytes(rows: int, cols: int, group: int) -> int:
+    """Size of a checkpoint in one piece: the codes, then the ranges, to the next multiple of 32."""
+    _checkpoint_size(cols, group)
     return (rows * (-(-cols // 16) * 16 + 4 * -(-cols // group)) + 31) // 32 * 32
 
 

@@ -24,3 +24,13 @@ def test_group_lengths_beyond_32_bits(pwlq, group):
         with pytest.raises(pwlq.PwlqError) as e:
             call()
         assert e.value.status == pwlq.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("cols,group", [(64, 0), (64, -32), (0, 64), (-1, 64)])
+def test_checkpoints_of_no_columns_or_groups(pwlq, cols, group):
+    codes, ranges = torch.zeros(4, 64, dtype=torch.uint8), torch.zeros(4, 1)
+    for make in (lambda: pwlq.Act8(codes, ranges, cols, group, 0.5),
+                 lambda: pwlq.act8_empty(4, cols, group, 0.5, "cpu")):
+        with pytest.raises(pwlq.PwlqError) as e:
+            make()
+        assert e.value.status == pwlq.ERR_INVALID_ARG
