@@ -24,7 +24,11 @@ class Checkpoints:
 
 def best_ratio(x: torch.Tensor, group: int = 128, candidates: int = 32) -> float:
     """The breakpoint ratio with the smallest total squared error on x [rows, cols] (every group a
-    row of the 7-bit search); candidates are k / candidates, the last one (no tail) left out."""
+    row of the 7-bit search, the last values of a row that do not fill one left out; rows shorter than
+    a group are one each); candidates are k / candidates, the last one (no tail) left out."""
+    if x.numel() == 0 or candidates < 2:
+        raise ValueError(f"no candidates, or no values: x is {list(x.shape)}")
+    group = min(group, x.shape[1])
     cols = x.shape[1] // group * group
     rows = x[:, :cols].float().reshape(-1, group).contiguous()
     ratios = torch.arange(1, candidates, device=x.device, dtype=torch.float32) / candidates

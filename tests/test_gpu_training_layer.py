@@ -245,3 +245,15 @@ def test_gates_of_no_tokens_are_refused():
         want = pwlq.block_norm(x, f, pre, post, gate, gate_tokens=16)
         got = pwlq.block_norm(x, f, pre, post, gate)                     # 48 rows over 3 gates
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_best_ratio_of_rows_shorter_than_a_group():
+    from paper_2002_00104_b200 import training
+    x = _rand(3, 300, 96, dtype=torch.float32) ** 3
+    assert training.best_ratio(x, group=128) == training.best_ratio(x, group=96)
+    assert training.best_ratio(x[:1, :1]) < 1
+    for bad in (x[:0], x[:, :0]):
+        with pytest.raises(ValueError):
+            training.best_ratio(bad)
+    with pytest.raises(ValueError):
+        training.best_ratio(x, candidates=1)
