@@ -212,14 +212,17 @@ struct RowCopy {
         if (hi < lo) hi = lo;
     }
     __device__ __forceinline__ unsigned size() const { return (unsigned)(hi - lo); }
-    // the ends, before the barrier is told of the copy
+    // the ends, before the barrier is told of the copy; a later row's copy to the same bytes, which this thread
+    // starts too, comes after them
     __device__ __forceinline__ void ends(unsigned char* slot) const {
+        if (lo == from - skip && hi >= from + bytes) return;
         const unsigned char* origin = from - skip;
         for (const unsigned char* p = from; p < from + bytes; p += sizeof(T)) {
             if (p >= lo && p < hi) p = hi;                   // words end between values
             if (p >= from + bytes) break;
             *reinterpret_cast<T*>(slot + (p - origin)) = *reinterpret_cast<const T*>(p);
         }
+        fence_proxy_async();
     }
     __device__ __forceinline__ void start(unsigned char* slot, uint64_t* bar) const {
         if (hi > lo) bulk_copy_g2s(slot + (lo - (from - skip)), lo, size(), bar);

@@ -37,3 +37,29 @@ def test_gate_gradients_of_values_up_to_the_largest(rows, cols, dtype, wtype, ra
     _, size = backward64(None, m, None, None, None, dr.double(), None, None, gate.double(), every, 1.0, 0.0)
     check(got["df"], want["df"], 4 * U * mag["df"], "df")
     check(got["dgate"], want["dgate"], U * (6 + rows) * size["dgate"], "dgate")
+
+
+@pytest.mark.parametrize("at", [1, 3, 7])
+def test_first_rows_off_their_alignment_are_followed_by_others_in_their_place(at):
+    """Gapless rows of odd length from an odd address: the first row's beginning and the last one's end are
+    moved value by value, and further rows take the same bytes of shared memory.  The same results as from an
+    aligned address."""
+    from paper_2002_00104_b200 import pwlq
+    rows, cols = 5000, 1283
+    g = torch.Generator(device="cuda")
+    g.manual_seed(at)
+
+    def both(seed):
+        store = torch.randn(at + rows * cols, generator=g, device="cuda").bfloat16()
+        odd = store[at:].view(rows, cols)
+        return odd, odd.clone()
+
+    x, f, dh, dr = (both(i) for i in range(4))
+    w = torch.rand(cols, generator=g, device="cuda").bfloat16()
+    results = []
+    for i in range(2):
+        r, h, saved = pwlq.block_norm(x[i], f[i], w, w, save=(64, 0.5))
+        results.append([r, h, *(v for v in pwlq.block_norm_backward(saved, dh[i], dr[i]).values() if v is not None)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert pwlq.device_status() == 0
