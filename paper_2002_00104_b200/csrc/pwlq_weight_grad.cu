@@ -85,8 +85,6 @@ struct Params {
     WeightGrad w;
     Schedule s;
     float* pieces;                 // workspace: [slot][block of 32 x 32][four columns][row][4]
-    int64_t groups;
-    int group_shift;
     bool vec_out;                  // rows of dw start on 16-byte boundaries
 };
 
@@ -435,8 +433,6 @@ cudaError_t launch(const WeightGrad& w, void* workspace, cudaStream_t stream) {
     Params p;
     p.w = w;
     p.s = schedule(w.rows, w.outputs, w.x.cols, pairs);
-    p.groups = w.x.groups();
-    p.group_shift = group_shift(w.x.group);
     p.vec_out = rows_aligned(w.dw, w.lddw, type_size(w.dw_dtype));
     p.pieces = static_cast<float*>(workspace);
 
