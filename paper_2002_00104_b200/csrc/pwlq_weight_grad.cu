@@ -8,6 +8,12 @@
 // memory: nothing is transposed.  The sums stay in tensor memory, two tiles of 256 columns, so that
 // a tile's results leave while the next one is summed.
 //
+// Why xhat is rounded: both operands of a 16-bit product have one type, and dy has 16 bits.  A binary32 xhat
+// would be two products (its leading and its remaining bits), twice the tensor pipe's time, or tf32 operands at
+// half the rate, which round to 11 bits all the same.  What it costs, as a part of dw's norm, 8192 x 4096 x
+// 4096: bf16 0.0015 (fp16 8192 x 1000 x 2048: 0.00019), in a 16-bit dw 0.0023 (0.00028), where rounding the
+// exact sum gives 0.0017 (0.00021) and the checkpoint itself is off by 0.0073 (0.0072).
+//
 // Bound by the tensor pipe: 94 % busy, 8192 x 4096 x 4096 bf16 in 176 us (1562 TFLOP/s), next to 19 us of
 // decoding and 9 of adding pieces.  Decoding inside the product instead, by warps that feed the tensor cores
 // from shared memory, took 843 us in all against 263; decoding beside it, with flags between the two kernels,
