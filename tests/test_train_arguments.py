@@ -34,3 +34,22 @@ def test_checkpoints_of_no_columns_or_groups(pwlq, cols, group):
         with pytest.raises(pwlq.PwlqError) as e:
             make()
         assert e.value.status == pwlq.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("failure", ["no compiler", "no headers", "no torch"])
+def test_the_library_is_built_where_the_module_of_the_calls_cannot_be(monkeypatch, tmp_path, failure):
+    from paper_2002_00104_b200 import build
+    built, old = [], tmp_path / "_pwlq_calls.so"
+    old.write_bytes(b"of older sources")
+    monkeypatch.setattr(build, "CALLS_LIB", str(old))
+    monkeypatch.setattr(build, "_nvcc", lambda sources, lib, verbose: built.append(lib))
+
+    def calls(verbose):
+        raise {"no compiler": FileNotFoundError("g++"), "no headers": RuntimeError("Python.h: No such file"),
+               "no torch": ImportError("No module named 'torch'")}[failure]
+
+    monkeypatch.setattr(build, "_calls", calls)
+    with pytest.warns(UserWarning, match="training calls was not built"):
+        assert build.build(force=True) == build.LIB
+    assert built == [build.LIB, build.PEAK_LIB]
+    assert not old.exists()
