@@ -257,3 +257,74 @@ def test_best_ratio_of_rows_shorter_than_a_group():
             training.best_ratio(bad)
     with pytest.raises(ValueError):
         training.best_ratio(x, candidates=1)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,cols,outputs", [(1, 8, 3), (77, 200, 130), (600, 1024, 515)])
+def test_linear_against_the_formula(rows, cols, outputs, dtype):
+    """dx = dy W as PyTorch has it; dw = dy^T x_hat at the checkpoint's values (the bounds of the weight
+    gradient's own tests: half an ulp of x_hat, sums of 16 products at a time, the result's rounding)."""
+    from paper_2002_00104_b200 import pwlq, training
+    from train_util import HALF_ULP, SUBNORMAL, check, held64
+    settings = training.Checkpoints(group=32, ratio=0.375)
+    x = _rand(rows, rows, cols, dtype=dtype).requires_grad_()
+    w = _rand(cols, outputs, cols, scale=0.05, dtype=dtype).requires_grad_()
+    dy = _rand(outputs, rows, outputs, scale=0.1, dtype=dtype)
+    held, w64 = held64(pwlq.act8_encode(x.detach(), 32, 0.375)), w.detach().double()
+    for d in (dy, dy[:1].expand(rows, outputs), dy.t().contiguous().t()):
+        y = training.linear(x, w, settings)
+        assert torch.equal(y, x @ w.t())
+        dx, dw = torch.autograd.grad(y, (x, w), d)
+        assert torch.equal(dx, d @ w.detach())
+        want, mag = d.double().t() @ held, d.double().abs().t() @ held.abs()
+        slack = (2.0 ** -22 * (rows / 16 + 25) + HALF_ULP[dtype]) * mag
+        check(dw, want, slack + SUBNORMAL[dtype] * d.double().abs().sum(0)[:, None], "dw")
+
+
+# f: block output, o: norm after it, g: gate, p: norm before the next block
+@pytest.mark.parametrize("kind", ["fogp", "fop", "fgp", "fp", "p", "fog", "fo", "fg"])
+@pytest.mark.parametrize("dtype,wtype", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32),
+                                         (torch.float32, torch.float32)])
+def test_block_norm_is_the_calls_it_is_made_of(kind, dtype, wtype):
+    from paper_2002_00104_b200 import pwlq, training
+    rows, cols = 60, 304
+    x = _rand(1, rows, cols, dtype=dtype)
+    f = _rand(2, rows, cols, dtype=dtype) if "f" in kind else None
+    post = 1 + _rand(3, cols, scale=0.2, dtype=wtype) if "o" in kind else None
+    gate = _rand(4, 4, cols, scale=0.5, dtype=wtype) if "g" in kind else None
+    pre = 1 + _rand(5, cols, scale=0.2, dtype=wtype) if "p" in kind else None
+    dr, dh = _rand(6, rows, cols, scale=0.1, dtype=dtype), _rand(7, rows, cols, scale=0.1, dtype=dtype)
+    settings = training.Checkpoints(group=64, ratio=0.4375)
+    want_r, want_h, saved = pwlq.block_norm(x, f, pre, post, gate, residual_scale=0.5, eps=1e-5, save=(64, 0.4375))
+    want = pwlq.block_norm_backward(saved, dh if pre is not None else None, dr)
+    leaves = [t.requires_grad_() for t in (x, f, pre, post, gate) if t is not None]
+    r, h = training.block_norm(x, f, pre, post, gate, residual_scale=0.5, eps=1e-5, settings=settings)
+    assert torch.equal(r, want_r) and (h is None) == (want_h is None) and (h is None or torch.equal(h, want_h))
+    outs, seeds = ([r, h], [dr, dh]) if h is not None else ([r], [dr])
+    got = torch.autograd.grad(outs, leaves, seeds)
+    for g, w in zip(got, [v for v in want.values() if v is not None], strict=True):
+        assert torch.equal(g, w)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+@pytest.mark.parametrize("seed", [0, 1])
+def test_gradients_of_a_network_in_either_type(dtype, seed):
+    """The example's network against the same in PyTorch, in bf16 and fp16 (the reasons for 5 % are those of
+    the example's own test; fp16 rounds less)."""
+    import os
+    import sys
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import train_act8
+    from paper_2002_00104_b200 import training
+    dt = getattr(torch, dtype)
+    x, t = _rand(seed, 512, 256, dtype=dt), _rand(seed + 10, 512, 256, dtype=torch.float32)
+    settings = training.Checkpoints(group=64, ratio=0.5)
+
+    def grads(forward):
+        p = {k: [v.to(dt) for v in vs] for k, vs in train_act8.parameters(256, 2, seed).items()}
+        leaves = [v.requires_grad_() for group in p.values() for v in group]
+        return torch.autograd.grad((forward(p, x).float() * t).sum(), leaves)
+
+    for g, w in zip(grads(lambda p, v: train_act8.forward_act8(p, v, settings)), grads(train_act8.forward_plain)):
+        assert g.dtype == w.dtype == dt
+        assert (g.float() - w.float()).norm() <= 0.05 * w.float().norm()
