@@ -135,7 +135,7 @@ act8_decode_kernel(const uint8_t* codes, int64_t ldc, const float* ranges, int64
 // together.  Both directions issue three instructions a cycle of four and move 80 to 95 % of what a copy
 // moves (16384 x 4096 bf16: 35.8 and 33.2 us).  Two chunks per thread; of 16-bit values, once there are
 // kManyValues, three to encode and four to decode (there 37.9 -> 35.8 and 35.5 -> 33.2 us; 4096 x 4096
-// 10.4 against 10.8 and 7.6 against 7.9 us; binary32 50.0 against 50.4 and 52.3 against 53.2 us).
+// 10.4 against 10.8 and 7.6 against 7.9 us; binary32 16384 x 4096 50.0 against 50.4 and 52.3 against 53.2 us).
 constexpr int64_t kManyValues = (int64_t)1 << 25;
 template <typename T, int C>
 __global__ void __launch_bounds__(kThreads)

@@ -6,15 +6,22 @@
 // the two reductions that depend on one another (of f, then of r; of the outer norm, then of the
 // inner one), so every operand crosses HBM once.
 //
+// Times in this file are of whole calls (backward with its sums) in a CUDA graph of calls back to back, on
+// operands larger than the L2 cache together, which still holds some of the last call's writes.
+//
 // Forms (the rules and both sides of each stand at the launches, at the end of this file):
-//   narrow   rows of at most 1024 bytes: a few lanes per row, no barrier (400000 x 64 bf16: forward 35 us, a CTA
-//            per row 236; backward 75 against 432)
+//   narrow   rows of at most 1024 bytes: a few lanes per row, no barrier (400000 x 64 bf16: forward 36 us, a CTA
+//            per row 236; backward 76 against 432)
 //   ring     persistent CTAs walk the rows, and a ring of shared-memory stages holds the next ones, brought in by
 //            bulk copies: a row's loads are in flight during the reductions of the rows before it, at no cost in
 //            registers, and a thread works on 32 bytes of columns, which shares the cost of reductions and ranges
-//            (16384 x 4096 bf16: with checkpoints 141 us = 4790 GB/s against 213, backward 152 us = 4420 GB/s against
-//            243).  Bound by instruction issue: 61 and 52 instructions per value at 3.1 and 2.5 a cycle of 4.
-//            Backward, a pair of CTAs shares rows too wide for one CTA's registers (4096 x 12288: 217 against 314 us).
+//            (16384 x 4096 bf16: with checkpoints 142 us = 4750 GB/s against 213, backward 152 us = 4440 GB/s against
+//            243).  With checkpoints bound by instruction issue, 61 per value at 3.1 a cycle of 4.  Backward 52 per
+//            value at 2.5 a cycle: 122 registers a thread leave 16 warps a multiprocessor, too few to cover the
+//            latency of what they wait for, the barriers among it.
+//            Backward, a pair of CTAs shares rows too wide for one CTA's registers (4096 x 12288: 218 against 314 us).
+//            Binary32 weights beside 16-bit values take twice the registers and the loads (16384 x 4096 with a gate:
+//            189 and 221 us against 147 and 163), and 12 bytes a thread spill, 124 backward on unaligned rows.
 //   row      forward without checkpoints, one CTA per row, 32 bytes of columns per thread
 //   direct   a thread loads its values itself, eight at a time: few rows, and rows off their alignment that the
 //            ring does not take (see load8)
@@ -585,7 +592,8 @@ __global__ void __maxnreg__(ODD ? 80 : 64) block_norm_ring_kernel(const __grid_c
 
 // Forward without checkpoints, weights of the values' type, a row per CTA and no ring: the arithmetic, and so
 // the bits, of block_norm_ring_kernel.  A row is then so little work that many CTAs, each with its own loads in
-// flight, keep the memory busier than a ring does (16384 x 4096 bf16, one norm: 80.5 us = 6670 GB/s).
+// flight, keep the memory busier than a ring does (16384 x 4096 bf16, one norm: 80.5 us = 6670 GB/s, more than a
+// copy of that size moves, since the cache still holds part of the results).
 template <typename T>
 __global__ void __maxnreg__(64) block_norm_row_kernel(const __grid_constant__ NormParams q) {
     constexpr bool WF32 = sizeof(T) == 4;
@@ -1261,7 +1269,8 @@ block_norm_backward_ring_kernel(const __grid_constant__ GradParams p) {
 }
 
 // Backward of narrow rows (see block_norm_narrow_kernel), for one gate at most.  The CTA's rows are not
-// neighbours here, but its sums are those of one CTA all the same.
+// neighbours here, but its sums are those of one CTA all the same.  16-bit values: at the 128 registers that
+// two CTAs a multiprocessor leave, 200 bytes a thread spill (weights and sums of 16 columns live over the loop).
 template <typename T, bool WF32>
 __global__ void __launch_bounds__(kNarrowThreads, 2)
 block_norm_backward_narrow_kernel(const __grid_constant__ GradParams p, int lanes) {
@@ -1627,7 +1636,8 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
     const int64_t resident = (int64_t)ring.ctas * sm_count();
     // A ring pays once every CTA has a few rows to walk (with checkpoints, bf16 1776 x 4096 18.1 against 24.1 us,
     // 592 rows 7.7 against 9.2, but 148 rows 5.1 against 4.5; without them 592 rows 5.3 against 4.9).  The rule
-    // does not ask for checkpoints: saving them does not change r and h.
+    // does not ask for checkpoints, since saving them must not change r and h: it gives up the 592 rows with them.
+    // (block_norm_row_kernel has the ring's bits, too, and could take these sizes without checkpoints; not measured.)
     if ((rows32 || odd) && ring.threads <= (odd ? 768 : 1024) && ring.stages >= 2 && a.rows >= 2 * resident) {
         // Without checkpoints, up to how many columns a CTA per row is faster than the ring: with one reduction
         // 8192 (bf16 83 against 96 us, binary32 169 against 184 us; 12288: 98 against 99), with two 4096 (88 against 96;
@@ -1664,7 +1674,8 @@ cudaError_t forward(const pwlq_block_norm_args& a, cudaStream_t stream) {
     return a.r_codes || a.f_codes || a.r_rstd || a.f_rstd ? forward<T, true>(a, stream) : forward<T, false>(a, stream);
 }
 
-// CTAs of the backward pass: the rows are shared out evenly over at most this many.
+// CTAs of the backward pass: the rows are shared out evenly over at most this many.  As many as fit at once
+// where a thread has 16 columns (16-bit values); binary32 rings have 8, and so two rounds of CTAs.
 inline int64_t backward_ctas(int64_t rows, int64_t cols) {
     const int64_t per_sm = cols > 8192 ? 1 : std::max(1, std::min(16, 512 / threads_for(cols, 16)));
     return std::min<int64_t>(rows, per_sm * sm_count());
@@ -1739,7 +1750,7 @@ cudaError_t backward_rows(GradParams& p, unsigned ctas, cudaStream_t stream) {
                    : run(block_norm_backward_kernel<T, 4, false, true>, ctas, threads, smem, kDirectMost, stream, p);
     }
     const bool rows32 = rows32_backward<T>(a, g);
-    // Rows that lie anywhere, 16-bit types: 16384 x 4095 352 -> 254 us, 16384 x 4104 406 -> 356 us against
+    // Rows that lie anywhere, 16-bit types: 16384 x 4095 352 -> 254 us, 16384 x 4104 406 -> 382 us against
     // threads that load for themselves.  Not binary32 (16384 x 2047: 190 against 192 us), nor gates of a few
     // rows, whose gradients go value by value (8192 x 4095, a gate per row: 286 against 327 us).
     const bool odd = !rows32 && kSize == 2 && (!p.dgate || a.gate_tokens >= 8);

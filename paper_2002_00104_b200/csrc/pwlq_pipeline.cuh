@@ -4,8 +4,9 @@
 // spending registers on them.
 //
 // Rules kept here: source and destination 16-byte aligned, size a multiple of 16 bytes (spans
-// that do not qualify are staged with ordinary loads instead); no multicast, no cluster; every
-// wait is bounded and reports expiry instead of spinning forever.
+// that do not qualify are staged with ordinary loads instead); no multicast; every wait is bounded
+// and reports expiry instead of spinning forever.  The streaming kernels use no clusters; the few
+// operations on pairs of CTAs at the end serve the training kernels.
 #pragma once
 
 #include <cuda_runtime.h>

@@ -14,8 +14,9 @@
 // 4096: bf16 0.0015 (fp16 8192 x 1000 x 2048: 0.00019), in a 16-bit dw 0.0023 (0.00028), where rounding the
 // exact sum gives 0.0017 (0.00021) and the checkpoint itself is off by 0.0073 (0.0072).
 //
-// Bound by the tensor pipe: 94 % busy, 8192 x 4096 x 4096 bf16 in 176 us (1562 TFLOP/s), next to 19 us of
-// decoding and 9 of adding pieces.  Decoding inside the product instead, by warps that feed the tensor cores
+// Bound by the tensor pipe: 94 % busy, 8192 x 4096 x 4096 bf16 in 173 us (1589 TFLOP/s), next to 16 us of
+// decoding and 7 of adding pieces, at full clock.  The whole call takes 187 us at first and, once the power limit
+// lowers the clock, 217 us at 1530 MHz and 234 at 1372.  Decoding inside the product instead, by warps that feed the tensor cores
 // from shared memory, took 843 us in all against 263; decoding beside it, with flags between the two kernels,
 // 262 against 211 (back to back on warm caches).
 //
@@ -190,7 +191,8 @@ __device__ __forceinline__ void put_block(float* v, float (*turn)[33], W* to, in
         return;
     }
     // rows off their alignment, or the last columns: turned in shared memory, so that a warp writes
-    // 32 neighbours of a row (one value per lane and row took 42 us for 515 x 1283 results)
+    // 32 neighbours of a row (one value per lane and row took 42 us for 515 x 1283 results, against 15).
+    // Accumulating, each of them waits for what it adds to: 48 us a call against 18, rows of 333.
 #pragma unroll
     for (int i = 0; i < 32; ++i) turn[lane][i] = v[i];
     __syncwarp();
