@@ -58,3 +58,40 @@ def test_gapless_checkpoints_of_several_blocks(dtype, group, cols):
     saved = pwlq.act8_encode(x.cuda(), group=group, ratio=0.375)
     for out in ("fp32", dtype):
         check_checkpoint(x, group, 0.375, saved, pwlq.act8_decode(saved, dtype=TYPES[out]))
+
+
+@pytest.mark.parametrize("cols,dtype", [(48, "bf16"), (512, "fp32"), (1280, "bf16"), (1283, "bf16"), (2056, "fp32"),
+                                        (2047, "fp32"), (4104, "bf16"), (8704, "bf16"), (8399, "fp16")])
+def test_rows_of_infinities_and_nan_stay_in_their_rows_in_every_form(cols, dtype):
+    """What is not such a row has the bits that it has without them."""
+    from paper_2002_00104_b200 import pwlq
+    dt = TYPES[dtype]
+    rows = _ring_rows(cols, dt) if cols > 512 else 1000
+    g = torch.Generator(device="cuda")
+    g.manual_seed(cols)
+    x, f, dh, dr = (torch.randn(rows, cols, generator=g, device="cuda").to(dt) for _ in range(4))
+    pre, post = (torch.rand(cols, generator=g, device="cuda").add(0.5).to(dt) for _ in range(2))
+    gate = torch.rand(3, cols, generator=g, device="cuda").to(dt)
+    bad = torch.zeros(rows, dtype=torch.bool, device="cuda")
+
+    def passes():
+        plain = pwlq.block_norm(x, f, pre, post, gate)[:2]
+        r, h, saved = pwlq.block_norm(x, f, pre, post, gate, save=(64, 0.4375))
+        grads = pwlq.block_norm_backward(saved, dh, dr)
+        return [*plain, r, h, grads["dx"], grads["df"]]
+
+    want = passes()
+    for t, row, col, v in ((x, 1, 0, "inf"), (f, 3, cols - 1, "nan"), (x, rows // 2, cols // 2, "-inf"),
+                           (f, rows - 1, 1, "inf"), (x, rows - 3, cols - 1, "nan")):
+        t[row, col] = float(v)
+        bad[row] = True
+    got = passes()
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.equal(a[~bad], b[~bad])
+        assert i in (0, 2) or not torch.isfinite(a[bad]).all(dim=1).any()
+    dh[5, cols - 1] = float("nan")
+    dr[7, 0] = float("inf")
+    again = passes()
+    bad[[5, 7]] = True
+    for a, b in zip(again[4:], want[4:]):
+        assert torch.equal(a[~bad], b[~bad])
