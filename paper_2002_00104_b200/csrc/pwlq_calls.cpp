@@ -321,8 +321,6 @@ PyObject* block_norm_backward(Args a) {
                       "the kept memory is not that of a forward call with these weights");
     kept.place(b, memory.data_ptr(), pre.defined(), post.defined());
     weights_of(b, pre, post, gate, dtype_of(b.wtype), device);
-    b.x = b.f = nullptr;
-    b.r = b.h = nullptr;
     pwlq_block_norm_grads g = {};
     if (dh.defined()) {
         const Matrix m = matrix(dh, "dh", b.rows, b.cols, type, device);

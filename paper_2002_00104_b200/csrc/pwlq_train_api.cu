@@ -143,6 +143,7 @@ int pwlq_block_norm_backward(const pwlq_block_norm_args* fwd, const pwlq_block_n
         (g.dx && bad_tensor(g.dx, dt, g.lddx, a.rows, a.cols)) ||
         (g.df && bad_tensor(g.df, dt, g.lddf, a.rows, a.cols)))
         return PWLQ_ERR_INVALID_ARG;
+    if (some && g.df && !a.f) return PWLQ_ERR_INVALID_ARG;        // the gradient of what was not there
     const size_t ws = pwlq::type_size((int)a.wtype);
     if (misaligned(g.dpre, ws) || misaligned(g.dpost, ws) || misaligned(g.dgate, ws) ||
         (g.dpre && !a.pre_weight) || (g.dpost && !a.post_weight) || (g.dgate && !a.gate))

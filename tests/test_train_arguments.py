@@ -53,3 +53,11 @@ def test_the_library_is_built_where_the_module_of_the_calls_cannot_be(monkeypatc
         assert build.build(force=True) == build.LIB
     assert built == [build.LIB, build.PEAK_LIB]
     assert not old.exists()
+
+
+def test_the_gradient_of_a_block_that_was_not_there(pwlq):
+    """df without f: refused before any CUDA call (it was filled with the gradient of r)."""
+    from test_train_abi import A, B, BLOCK_GRADS, C, _block
+    args = _block(f=0, post=0, gate=0, f_codes=0, f_ranges=0, f_rstd=0)
+    grads = BLOCK_GRADS.pack(A, 100, B, 100, A, 100, B, 100, C, 0, 0, 0, 0)
+    assert pwlq.load_library().pwlq_block_norm_backward(args, grads, None) == pwlq.ERR_INVALID_ARG
