@@ -874,7 +874,6 @@ class Act8:
                             .view(self.rows, groups))
         return self._ranges
 
-
     def detached(self):
         """(the byte tensor that holds the checkpoint, a checkpoint without it): for keeping the two
         apart.  Only of checkpoints in one piece, as ``act8_encode`` and ``act8_empty`` make them."""
@@ -916,6 +915,8 @@ def _act8(a: Act8):
         at = memory.data_ptr() + a._at
         return memory, at, pitch, at + a.rows * pitch
     codes, ranges = a._codes, a._ranges
+    if codes is None:
+        raise ValueError("the checkpoint is detached from its memory")
     if (codes.dtype != torch.uint8 or codes.dim() != 2 or not codes.is_cuda or
             not codes.is_contiguous() or codes.shape[1] < a.cols or codes.shape[1] % 16 or
             ranges.dtype != torch.float32 or ranges.device != codes.device or

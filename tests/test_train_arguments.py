@@ -61,3 +61,10 @@ def test_the_gradient_of_a_block_that_was_not_there(pwlq):
     args = _block(f=0, post=0, gate=0, f_codes=0, f_ranges=0, f_rstd=0)
     grads = BLOCK_GRADS.pack(A, 100, B, 100, A, 100, B, 100, C, 0, 0, 0, 0)
     assert pwlq.load_library().pwlq_block_norm_backward(args, grads, None) == pwlq.ERR_INVALID_ARG
+
+
+def test_a_checkpoint_without_its_memory(pwlq):
+    memory, layout = pwlq.act8_empty(4, 64, device="cpu").detached()
+    with pytest.raises(ValueError, match="detached"):
+        pwlq.act8_decode(layout)
+    assert layout.attached(memory).codes.shape == (4, 64)
