@@ -912,8 +912,11 @@ def _act8(a: Act8):
     memory = a._memory
     if memory is not None:
         pitch = -(-a.cols // 16) * 16
-        at = memory.data_ptr() + a._at
-        return memory, at, pitch, at + a.rows * pitch
+        ranges = a._at + a.rows * pitch
+        if a.group < 1 or ranges + 4 * a.rows * -(-a.cols // a.group) > memory.numel():
+            raise ValueError(f"the checkpoint's memory does not hold [{a.rows}, {a.cols}] in groups of {a.group}")
+        at = memory.data_ptr()
+        return memory, at + a._at, pitch, at + ranges
     codes, ranges = a._codes, a._ranges
     if codes is None:
         raise ValueError("the checkpoint is detached from its memory")

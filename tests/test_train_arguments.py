@@ -68,3 +68,12 @@ def test_a_checkpoint_without_its_memory(pwlq):
     with pytest.raises(ValueError, match="detached"):
         pwlq.act8_decode(layout)
     assert layout.attached(memory).codes.shape == (4, 64)
+
+
+@pytest.mark.parametrize("field,value", [("group", 32), ("group", 0), ("rows", 5), ("cols", 600)])
+def test_checkpoints_whose_fields_were_changed(pwlq, field, value):
+    """More bytes or ranges than the memory holds would be read."""
+    saved = pwlq.act8_empty(4, 512, 128, device="cpu")
+    setattr(saved, field, value)
+    with pytest.raises(ValueError, match="does not hold"):
+        pwlq.act8_decode(saved)
