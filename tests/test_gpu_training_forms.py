@@ -95,3 +95,19 @@ def test_rows_of_infinities_and_nan_stay_in_their_rows_in_every_form(cols, dtype
     bad[[5, 7]] = True
     for a, b in zip(again[4:], want[4:]):
         assert torch.equal(a[~bad], b[~bad])
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("cols", [512, 333])
+def test_zeros_keep_their_sign_beside_other_values(dtype, cols):
+    """The byte's sign is the value's sign bit, -0's too, unless the group's range is 0."""
+    from paper_2002_00104_b200 import pwlq
+    x = _x(1, 9, cols, TYPES[dtype])
+    x[:, 1::3], x[:, 2::5], x[4, :64] = -0.0, 0.0, -0.0
+    saved = pwlq.act8_encode(x.cuda(), group=64, ratio=0.4375)
+    y = pwlq.act8_decode(saved, dtype=TYPES[dtype]).cpu()
+    held = (saved.ranges.cpu() > 0).repeat_interleave(64, dim=1)[:, :cols]
+    assert not held[4, :64].any() and held[5].all()
+    negative = torch.signbit(x) & held
+    assert torch.equal(saved.codes.cpu()[:, :cols] >= 128, negative)
+    assert torch.equal(torch.signbit(y), negative) and (y[x == 0] == 0).all()
