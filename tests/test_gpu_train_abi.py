@@ -112,3 +112,35 @@ def test_calls_of_different_widths_from_several_threads():
     for _, _, dx, want, _ in cases:
         assert torch.equal(dx, want)
     assert pwlq.device_status() == 0
+
+
+@pytest.mark.parametrize("rows,cols", [(1000, 48), (5000, 256), (700, 1040), (3000, 1283), (900, 4104), (300, 8192),
+                                       (200, 8704), (200, 8399), (3, 4096)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("norms", ["both", "inner", "outer"])
+def test_gradients_written_over_the_gradients_they_come_from(rows, cols, dtype, norms):
+    """dx in dr's place and df in dh's, in every form: the bits that separate results have."""
+    from paper_2002_00104_b200 import pwlq
+    lib, code = pwlq.load_library(), 1 if dtype == torch.bfloat16 else 0
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    x, f, dh, dr = (torch.randn(rows, cols, generator=g, device="cuda").to(dtype) for _ in range(4))
+    w, gate = torch.ones(cols, device="cuda").to(dtype), torch.rand(2, cols, generator=g, device="cuda").to(dtype)
+    pre, post = (w if norms != "inner" else None), (w if norms != "outer" else None)
+    _, _, saved = pwlq.block_norm(x, f, pre, post, gate, save=(64, 0.5))
+    want = pwlq.block_norm_backward(saved, dh if pre is not None else None, dr)
+    some = {"f_codes": saved.f.codes, "f_ranges": saved.f.ranges, "f_rstd": saved.f_rstd if post is not None else 0}
+    if pre is not None:
+        some.update(r_codes=saved.r.codes, r_ranges=saved.r.ranges, r_rstd=saved.r_rstd)
+    args = block(rows=rows, cols=cols, dtype=code, wtype=code, f=f, pre=0 if pre is None else pre,
+                 post=0 if post is None else post, gate=gate, ldgate=cols, gate_rows=2, gate_tokens=-(-rows // 2),
+                 scale=1.0, eps=1e-6, group=64, ratio=0.5, ldc=saved.f.codes.shape[1], **some)
+    dx, df = dr.clone(), dh.clone()
+    dgate = torch.empty_like(gate)
+    ws = torch.empty(lib.pwlq_block_norm_backward_workspace_bytes(rows, cols, 2), dtype=torch.uint8, device="cuda")
+    out = gradients(dh=df if pre is not None else 0, lddh=cols, dr=dx, lddr=cols, dx=dx, lddx=cols, df=df, lddf=cols,
+                    dgate=dgate, ws=ws, bytes=ws.numel())
+    assert lib.pwlq_block_norm_backward(args, out, _stream()) == pwlq.OK
+    for got, name in ((dx, "dx"), (df, "df"), (dgate, "dgate")):
+        assert torch.equal(got, want[name]), name
+    assert pwlq.device_status() == 0
