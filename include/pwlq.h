@@ -549,6 +549,77 @@ int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outpu
                           int group, float ratio, void* dw, int dw_dtype, int64_t lddw,
                           int accumulate, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------ products with 4-bit weights
+ * Weights in four bits each, by the 3-bit scheme with its region bit (L = 3), and the products that read
+ * them for a few tokens at a time: what a model costs then is reading its weights.
+ *
+ * Format.  `matrices` x [rows, cols] (experts; 1 for a single matrix); every row is cut into groups of
+ * `group` consecutive values (32, 64, 128 or 256; the last one may be shorter).  For each group
+ *     m = max |w|;  m < 2^-100 is held as 0, a group with an Inf or a NaN in it as NaN
+ *     s = m / 192 (one binary32 division), rounded up to bfloat16: the group's scale
+ * and with the breakpoint b, a whole number in 1..64 for the whole tensor (p = m * b / 64), the values are
+ * whole multiples of s:
+ *     tail = a > 3 b s;   n = tail ? 3 b + q (64 - b) : q b,   q in 0..3 the nearest level, ties to even
+ * (a = |w|).  Every bound between two levels is exact in binary32, and so is every value n * s: encoding and
+ * decoding round nothing but s.  n <= 192 has eight bits, so that n / 256 is exact in bf16 and fp16 as well and
+ * the products below take weights without rounding them.  |w| up to 2^126.
+ *   paired   1: the matrix is two of rows / 2 rows each, gate rows then up rows (rows even), which the
+ *            products take together: silu(gate) * up
+ *   codes    pwlq_w4_code_bytes() bytes, 16-byte aligned, in the order in which the products read them:
+ *            [matrices][tiles][ceil(cols / 64)] blocks of 512 bytes, 16 rows x 64 columns; a tile is 16
+ *            consecutive rows, of a paired matrix 8 gate rows and the 8 up rows that belong to them.  Rows and
+ *            columns behind the last one are held as 0
+ *   scales   pwlq_w4_scale_bytes() bytes, 4-byte aligned: [matrices][tiles][ceil(cols / group)][8][2]
+ * rows up to 2^24, cols up to 2^20, matrices up to 65535. */
+typedef struct {
+    int64_t matrices, rows, cols, group, breakpoint, paired;
+    void* codes;
+    void* scales;
+} pwlq_w4;
+size_t pwlq_w4_code_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t paired);
+size_t pwlq_w4_scale_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t group, int64_t paired);
+
+/* x, y [matrices, rows, cols] of type dtype; ldx / ldy the pitch of a row, ldm that of a matrix (ignored for one).
+ * Every byte of codes and scales is written. */
+int pwlq_w4_encode(const pwlq_w4* w, const void* x, int dtype, int64_t ldx, int64_t ldm, void* stream);
+int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ldm, void* stream);
+
+/* y[t, n] = sum over k of x[t, k] w[n, k], for a paired matrix y[t, n] = silu(gate) * up of the sums with gate row
+ * n and up row n, [tokens, rows / 2].  matrices = 1.  x [tokens, cols] and y of type dtype; made for few tokens (any
+ * number is taken; from some hundreds on decoding once and a dense product are faster).  Products are exact, the
+ * sums binary32 in a fixed order (bit-reproducible), y is rounded once.  tokens may be 0.  y must not overlap x. */
+int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, int64_t ldx, void* y,
+                   int64_t ldy, void* stream);
+
+/* A mixture-of-experts layer, y = sum over the chosen experts e of weight_e * D_e (silu(G_e x) * U_e x), for up to
+ * PWLQ_W4_MOE_MAX_TOKENS tokens:
+ *     score = router x;  the `top` largest are chosen, equal ones by lowest index, a NaN before everything
+ *     weights = softmax of the scores, over the chosen ones (normalize = 1) or over all (0)
+ *   up      paired [experts][2 hidden, features], G then U;   down   [experts][features, hidden]
+ *   x, y    [tokens, features] of type dtype; y may be x (same pitch)
+ *   router  [experts, features] of type router_dtype (PWLQ_F32 or dtype).  Scores are summed in twice binary32's
+ *           precision: which experts are chosen does not depend on the order of a sum
+ *   chosen, weights   [tokens, top] each, int32 and binary32, largest score first; or NULL
+ *   workspace         pwlq_w4_moe_workspace_bytes(...) bytes, 256-byte aligned; 0 for invalid arguments
+ * Sums are binary32 in a fixed order (bit-reproducible).  silu(gate) * up * weight lies in the workspace with 16
+ * bits of precision (24 for binary32 tokens) and binary32's range.  A token's values reach no other token's. */
+#define PWLQ_W4_MOE_MAX_TOKENS 64
+#define PWLQ_W4_MOE_MAX_EXPERTS 1024
+#define PWLQ_W4_MOE_MAX_TOP 32
+typedef struct {
+    int64_t tokens, top, dtype, router_dtype, normalize;
+    const void* x; int64_t ldx;
+    const void* router; int64_t ldrouter;
+    const pwlq_w4* up;
+    const pwlq_w4* down;
+    void* y; int64_t ldy;
+    int32_t* chosen;
+    float* weights;
+    void* workspace; int64_t workspace_bytes;
+} pwlq_w4_moe_args;
+size_t pwlq_w4_moe_workspace_bytes(int64_t tokens, int64_t top, int64_t hidden);
+int pwlq_w4_moe(const pwlq_w4_moe_args* args, void* stream);
+
 /* The streaming kernels (abs-max, quantize, dequantize) hand their data over through shared-memory
  * barriers that they await with a bounded number of polls; a wait that runs out makes the kernel
  * stop early and sets a flag on the current device.  This call reads the flags (it synchronises

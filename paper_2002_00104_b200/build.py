@@ -16,7 +16,8 @@ CALLS_LIB = os.path.join(HERE, "_pwlq_calls.so")     # imported as a Python modu
 CALLS_SOURCE = "pwlq_calls.cpp"
 SOURCES = ["pwlq_api.cu", "pwlq_absmax.cu", "pwlq_search.cu", "pwlq_quantize.cu",
            "pwlq_noalloc.cu", "pwlq_select.cu", "pwlq_search2.cu", "pwlq_bias.cu", "pwlq_rowmap.cu",
-           "pwlq_act8.cu", "pwlq_block_norm.cu", "pwlq_weight_grad.cu", "pwlq_train_api.cu"]
+           "pwlq_act8.cu", "pwlq_block_norm.cu", "pwlq_weight_grad.cu", "pwlq_train_api.cu",
+           "pwlq_w4.cu", "pwlq_w4_linear.cu", "pwlq_w4_moe.cu", "pwlq_w4_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
     "-fmad=false",            # no implicit FMA contraction: every fused op is an explicit fmaf

@@ -1,10 +1,11 @@
-// The training calls as PyTorch sees them: tensors in, tensors out.  These calls are made once per
-// layer and step, often on few rows, where marshalling in Python and a Python-level allocation per
+// The training calls and those on 4-bit weights as PyTorch sees them: tensors in, tensors out.  These calls are
+// made once per layer and step, often on few rows, where marshalling in Python and a Python-level allocation per
 // output took longer than the kernels; here a call looks at each tensor once, allocates, and enters
 // the C ABI.  Nothing is computed here.
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -23,6 +24,13 @@ struct Library {
     decltype(&pwlq_block_norm_backward) backward;
     decltype(&pwlq_act8_weight_grad_workspace_bytes) grad_bytes;
     decltype(&pwlq_act8_weight_grad) grad;
+    decltype(&pwlq_w4_code_bytes) w4_codes;
+    decltype(&pwlq_w4_scale_bytes) w4_scales;
+    decltype(&pwlq_w4_encode) w4_encode;
+    decltype(&pwlq_w4_decode) w4_decode;
+    decltype(&pwlq_w4_linear) w4_linear;
+    decltype(&pwlq_w4_moe_workspace_bytes) moe_bytes;
+    decltype(&pwlq_w4_moe) moe;
 } lib;
 PyObject* error_class = nullptr;
 
@@ -402,6 +410,168 @@ PyObject* weight_grad(Args a) {
     return wrap(out);
 }
 
+// A packed matrix from its fields (matrices, rows, cols, group, breakpoint, paired) and, where it has some, its
+// memory: the codes, then the scales.
+struct Packed {
+    pwlq_w4 w = {};
+    int64_t bytes = 0;
+    at::Tensor memory;
+    explicit Packed(PyObject* fields) {
+        TORCH_CHECK_VALUE(PyTuple_Check(fields) && PyTuple_GET_SIZE(fields) == 6, "not a packed matrix");
+        int64_t* const to[6] = {&w.matrices, &w.rows, &w.cols, &w.group, &w.breakpoint, &w.paired};
+        for (int i = 0; i < 6; ++i) {
+            *to[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(fields, i));
+            if (*to[i] == -1 && PyErr_Occurred()) throw python_error();
+        }
+        const size_t codes = lib.w4_codes(w.matrices, w.rows, w.cols, w.paired),
+                     scales = lib.w4_scales(w.matrices, w.rows, w.cols, w.group, w.paired);
+        if (!codes || !scales) throw Failed{PWLQ_ERR_INVALID_ARG, "packed matrix"};
+        bytes = (int64_t)(codes + scales);
+        code_bytes_ = (int64_t)codes;
+    }
+    void place(const at::Tensor& m, int device) {
+        TORCH_CHECK_VALUE(m.scalar_type() == at::kByte && m.is_contiguous() && m.is_cuda() && m.get_device() == device &&
+                              m.numel() == bytes,
+                          "the memory of this packed matrix is ", bytes, " contiguous bytes on cuda:", device, ", got ",
+                          m.numel(), " of ", m.scalar_type(), " on ", m.device());
+        memory = m;
+        w.codes = m.data_ptr();
+        w.scales = static_cast<uint8_t*>(w.codes) + code_bytes_;
+    }
+
+private:
+    int64_t code_bytes_ = 0;
+};
+Packed packed(Args& a, int device) {
+    Packed p(a.next());
+    p.place(a.tensor("the packed matrix's memory"), device);
+    return p;
+}
+
+// The values of a packed matrix: [rows, cols], or [matrices, rows, cols].
+struct Values {
+    void* p = nullptr;
+    int64_t ld = 0, ldm = 0;
+};
+Values values(const at::Tensor& t, const char* what, const pwlq_w4& w, int device) {
+    const int64_t d = t.dim();
+    dtype_code(t.scalar_type());
+    TORCH_CHECK_VALUE((d == 3 ? t.size(0) == w.matrices : d == 2 && w.matrices == 1) && t.size(d - 2) == w.rows &&
+                          t.size(d - 1) == w.cols && t.is_cuda() && t.get_device() == device,
+                      what, " must be ", w.matrices, " of [", w.rows, ", ", w.cols, "] on cuda:", device, ", got ", t.sizes(),
+                      " on ", t.device());
+    TORCH_CHECK_VALUE(w.cols < 2 || t.stride(d - 1) == 1, what, ": the values of a row must be adjacent");
+    Values v{t.data_ptr(), w.rows < 2 ? w.cols : t.stride(d - 2), w.matrices < 2 ? 0 : t.stride(0)};
+    TORCH_CHECK_VALUE(v.ld >= w.cols, what, ": rows overlap (a broadcast tensor must be made whole first)");
+    return v;
+}
+
+// (x, fields, memory or None) -> new memory, or None where given
+PyObject* w4_encode(Args a) {
+    const at::Tensor x = a.tensor("w");
+    Packed p(a.next());
+    const at::Tensor given = a.maybe("out");
+    const int device = home(x, "w");
+    const Values v = values(x, "w", p.w, device);
+    const at::Tensor memory = given.defined() ? given : bytes(p.bytes, x);
+    p.place(memory, device);
+    check(lib.w4_encode(&p.w, v.p, dtype_code(x.scalar_type()), v.ld, v.ldm, stream_of(device)), "pwlq_w4_encode");
+    return wrap(given.defined() ? at::Tensor() : memory);
+}
+
+// (fields, memory, type, three dimensions, out or None)
+PyObject* w4_decode(Args a) {
+    Packed p(a.next());
+    const at::Tensor memory = a.tensor("the packed matrix's memory");
+    const int64_t code = a.integer();
+    const bool three = a.integer() != 0;
+    at::Tensor out = a.maybe("out");
+    const int device = home(memory, "the packed matrix");
+    p.place(memory, device);
+    if (!out.defined()) {
+        const auto options = memory.options().dtype(dtype_of(code));
+        out = three ? at::empty({p.w.matrices, p.w.rows, p.w.cols}, options) : at::empty({p.w.rows, p.w.cols}, options);
+    }
+    const Values v = values(out, "out", p.w, device);
+    TORCH_CHECK_VALUE(p.w.matrices < 2 || v.ldm >= (p.w.rows - 1) * v.ld + p.w.cols, "out: matrices overlap");
+    check(lib.w4_decode(&p.w, v.p, dtype_code(out.scalar_type()), v.ld, v.ldm, stream_of(device)), "pwlq_w4_decode");
+    return wrap(out);
+}
+
+void no_gradient(const at::Tensor& t, const char* what) {
+    TORCH_CHECK_VALUE(!(t.requires_grad() && c10::GradMode::is_enabled()), what,
+                      " requires a gradient, and this call has no backward pass: call it under torch.no_grad()");
+}
+
+// (x, fields, memory, out or None) -> y
+PyObject* w4_linear(Args a) {
+    const at::Tensor x = a.tensor("x");
+    const int device = home(x, "x");
+    two_dimensions(x, "x");
+    no_gradient(x, "x");
+    const Packed p = packed(a, device);
+    at::Tensor y = a.maybe("out");
+    const int64_t tokens = x.size(0), outputs = p.w.paired ? p.w.rows / 2 : p.w.rows;
+    const Matrix mx = matrix(x, "x", tokens, p.w.cols, x.scalar_type(), device);
+    if (!y.defined()) y = at::empty({tokens, outputs}, x.options());
+    const Matrix my = matrix(y, "out", tokens, outputs, x.scalar_type(), device);
+    check(lib.w4_linear(&p.w, mx.p, dtype_code(x.scalar_type()), tokens, mx.ld, my.p, my.ld, stream_of(device)),
+          "pwlq_w4_linear");
+    return wrap(y);
+}
+
+// (x, router, fields and memory of up, of down, top, normalize, want the routing, out or None, workspace or None)
+//   -> (y, chosen, weights)
+PyObject* w4_moe(Args a) {
+    const at::Tensor x = a.tensor("x"), router = a.tensor("router");
+    const int device = home(x, "x");
+    two_dimensions(x, "x");
+    no_gradient(x, "x");
+    no_gradient(router, "router");
+    const Packed up = packed(a, device), down = packed(a, device);
+    pwlq_w4_moe_args m = {};
+    m.top = a.integer();
+    m.normalize = a.integer() != 0;
+    const bool want = a.integer() != 0;
+    at::Tensor y = a.maybe("out"), workspace = a.maybe("workspace");
+    const at::ScalarType type = x.scalar_type(), rtype = router.scalar_type();
+    TORCH_CHECK_VALUE(rtype == type || rtype == at::kFloat, "router must be of x's type or float32");
+    m.tokens = x.size(0);
+    m.dtype = dtype_code(type);
+    m.router_dtype = dtype_code(rtype);
+    Matrix t = matrix(x, "x", m.tokens, up.w.cols, type, device);
+    m.x = t.p;
+    m.ldx = t.ld;
+    t = matrix(router, "router", up.w.matrices, up.w.cols, rtype, device);
+    m.router = t.p;
+    m.ldrouter = t.ld;
+    m.up = &up.w;
+    m.down = &down.w;
+    if (!y.defined()) y = at::empty(x.sizes(), x.options());
+    t = matrix(y, "out", m.tokens, up.w.cols, type, device);
+    m.y = t.p;
+    m.ldy = t.ld;
+    // sizes that memory is made from, before the library sees them
+    const int64_t need = (int64_t)lib.moe_bytes(m.tokens, m.top, down.w.cols);
+    if (!need) throw Failed{m.tokens > PWLQ_W4_MOE_MAX_TOKENS || m.top > PWLQ_W4_MOE_MAX_TOP ? PWLQ_ERR_UNSUPPORTED
+                                                                                       : PWLQ_ERR_INVALID_ARG, "pwlq_w4_moe"};
+    at::Tensor chosen, weights;
+    if (want) {
+        chosen = at::empty({m.tokens, m.top}, x.options().dtype(at::kInt));
+        weights = at::empty({m.tokens, m.top}, x.options().dtype(at::kFloat));
+        m.chosen = static_cast<int32_t*>(chosen.data_ptr());
+        m.weights = static_cast<float*>(weights.data_ptr());
+    }
+    if (!workspace.defined()) workspace = bytes(need, x);
+    TORCH_CHECK_VALUE(workspace.scalar_type() == at::kByte && workspace.is_contiguous() && workspace.is_cuda() &&
+                          workspace.get_device() == device,
+                      "workspace must be contiguous uint8 on cuda:", device);
+    m.workspace = workspace.data_ptr();
+    m.workspace_bytes = workspace.numel();
+    check(lib.moe(&m, stream_of(device)), "pwlq_w4_moe");
+    return tuple({wrap(y), wrap(chosen), wrap(weights)});
+}
+
 template <PyObject* (*FN)(Args), int N>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
@@ -449,6 +619,10 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          PWLQ_CALL(block_norm, 13),
                          PWLQ_CALL(block_norm_backward, 9),
                          PWLQ_CALL(weight_grad, 13),
+                         PWLQ_CALL(w4_encode, 3),
+                         PWLQ_CALL(w4_decode, 5),
+                         PWLQ_CALL(w4_linear, 4),
+                         PWLQ_CALL(w4_moe, 11),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pwlq_calls", nullptr, -1, methods};
 

@@ -26,6 +26,7 @@ MAX_K = 4096
 MAX_K2 = 64
 F32, BF16, F16 = range(3)
 BLOCK_NORM_MAX_COLS = 16384
+W4_MOE_MAX_TOKENS, W4_MOE_MAX_EXPERTS, W4_MOE_MAX_TOP = 64, 1024, 32
 
 _P, _I64, _INT, _SZ = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_size_t
 _F32, _STRUCT = ctypes.c_float, ctypes.c_char_p     # _STRUCT: an argument block packed into bytes
@@ -103,6 +104,13 @@ _SIGNATURES = {
     "pwlq_act8_weight_grad_workspace_bytes": (_SZ, [_I64, _I64, _I64, _INT]),
     "pwlq_act8_weight_grad": (_INT, [_P, _INT, _I64, _I64, _I64, _P, _I64, _P, _I64, _INT, _F32, _P,
                                      _INT, _I64, _INT, _P, _SZ, _P]),
+    "pwlq_w4_code_bytes": (_SZ, [_I64, _I64, _I64, _I64]),
+    "pwlq_w4_scale_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
+    "pwlq_w4_encode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
+    "pwlq_w4_decode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
+    "pwlq_w4_linear": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P, _I64, _P]),
+    "pwlq_w4_moe_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
+    "pwlq_w4_moe": (_INT, [_STRUCT, _P]),
     "pwlq_device_status": (_INT, []),
     "pwlq_status_string": (ctypes.c_char_p, [_INT]),
     "pwlq_version": (ctypes.c_char_p, []),
@@ -827,7 +835,9 @@ def _calls():
                                "`python -m paper_2002_00104_b200.build`") from e
         entries = ("pwlq_act8_encode", "pwlq_act8_decode", "pwlq_block_norm",
                    "pwlq_block_norm_backward_workspace_bytes", "pwlq_block_norm_backward",
-                   "pwlq_act8_weight_grad_workspace_bytes", "pwlq_act8_weight_grad")
+                   "pwlq_act8_weight_grad_workspace_bytes", "pwlq_act8_weight_grad",
+                   "pwlq_w4_code_bytes", "pwlq_w4_scale_bytes", "pwlq_w4_encode", "pwlq_w4_decode",
+                   "pwlq_w4_linear", "pwlq_w4_moe_workspace_bytes", "pwlq_w4_moe")
         module.init(tuple(ctypes.cast(getattr(lib, name), _P).value for name in entries), PwlqError)
         _calls_module = module
     return _calls_module
@@ -1066,3 +1076,107 @@ def act8_weight_grad(dy, saved: Act8, dtype=None, out=None, accumulate=False, wo
     return _calls().weight_grad(dy, memory, codes, ldc, ranges, saved.rows, saved.cols, saved.group,
                                 saved.ratio, -1 if dtype is None else _dtype_code(dtype), out,
                                 accumulate, workspace)
+
+
+# ---------------------------------------------------------------- products with 4-bit weights
+def _w4_fields(shape, group: int, ratio: float, paired: bool):
+    """(matrices, rows, cols, group, breakpoint, paired) of a packed matrix of this shape, checked."""
+    if len(shape) not in (2, 3):
+        raise ValueError(f"a packed matrix is [rows, cols] or [matrices, rows, cols], not {list(shape)}")
+    matrices, rows, cols = (1, *shape) if len(shape) == 2 else shape
+    b = ratio * 64
+    if not 1 <= b <= 64 or b != int(b):
+        raise PwlqError(ERR_INVALID_ARG, f"breakpoint ratio {ratio}: a whole number of 64ths is needed")
+    if group not in (32, 64, 128, 256):
+        raise PwlqError(ERR_INVALID_ARG, f"group of {group} weights")
+    if paired and rows % 2:
+        raise PwlqError(ERR_INVALID_ARG, f"a pair of matrices in {rows} rows")
+    return int(matrices), int(rows), int(cols), int(group), int(b), int(bool(paired))
+
+
+def w4_bytes(shape, group: int = 128, paired: bool = False) -> int:
+    """Size of a packed matrix: the codes, then the scales."""
+    matrices, rows, cols, group, _, paired = _w4_fields(shape, group, 0.5, paired)
+    lib = load_library()
+    codes = lib.pwlq_w4_code_bytes(matrices, rows, cols, paired)
+    if not codes:
+        small = min(matrices, rows, cols) < 1
+        raise PwlqError(ERR_INVALID_ARG if small else ERR_UNSUPPORTED, f"packed matrix of {list(shape)}")
+    return int(codes + lib.pwlq_w4_scale_bytes(matrices, rows, cols, group, paired))
+
+
+class W4:
+    """A weight matrix [rows, cols], or several [matrices, rows, cols], in 4 bits a value with one scale per
+    group of a row, as ``w4_encode`` packs it: ``memory``, ``w4_bytes(shape, group, paired)`` bytes on one
+    device (what to save and load; aligned to 16 bytes), and what they stand for.  ``ratio`` is the
+    breakpoint as a part of a group's range, a whole number of 64ths.  ``paired``: gate rows, then as many up
+    rows, which the products take together."""
+    __slots__ = ("_memory", "_shape", "_fields")
+
+    def __init__(self, memory: torch.Tensor, shape, group: int = 128, ratio: float = 0.5, paired: bool = False):
+        self._fields = _w4_fields(shape, group, ratio, paired)
+        need = w4_bytes(shape, group, paired)
+        if memory.dtype != torch.uint8 or not memory.is_contiguous() or memory.numel() != need:
+            raise ValueError(f"the memory of this packed matrix is {need} contiguous bytes")
+        self._memory, self._shape = memory, tuple(int(v) for v in shape)
+
+    memory = property(lambda self: self._memory)
+    shape = property(lambda self: self._shape)
+    group = property(lambda self: self._fields[3])
+    ratio = property(lambda self: self._fields[4] / 64)
+    paired = property(lambda self: bool(self._fields[5]))
+
+
+def w4_encode(w, group=128, ratio=0.5, paired=False, out: Optional[W4] = None, stream=None) -> W4:
+    """``pwlq_w4_encode``: w [rows, cols] or [matrices, rows, cols] (fp32, bf16 or fp16) in 4 bits a value.
+    ``training.best_ratio(w, group, 64, bits=3)`` finds the ratio with the smallest squared error.  With
+    ``out`` its memory, group, ratio and pairing are used."""
+    if stream is not None:
+        with _on(stream):
+            return w4_encode(w, group, ratio, paired, out)
+    if out is not None:
+        if tuple(w.shape) != out.shape:
+            raise ValueError(f"the packed matrix is {list(out.shape)}, w is {list(w.shape)}")
+        _calls().w4_encode(w, out._fields, out._memory)
+        return out
+    packed = W4.__new__(W4)
+    packed._fields, packed._shape = _w4_fields(w.shape, group, ratio, paired), tuple(w.shape)
+    packed._memory = _calls().w4_encode(w, packed._fields, None)
+    return packed
+
+
+def w4_decode(packed: W4, dtype=torch.float32, out=None, stream=None):
+    """``pwlq_w4_decode``: the values of a packed matrix."""
+    if stream is not None:
+        with _on(stream):
+            return w4_decode(packed, dtype, out)
+    return _calls().w4_decode(packed._fields, packed._memory, _dtype_code(dtype), len(packed._shape) == 3, out)
+
+
+def w4_linear(x, packed: W4, out=None, stream=None):
+    """``pwlq_w4_linear``: x @ w.T for a few tokens x [tokens, cols], or for a paired matrix
+    silu(x @ gate.T) * (x @ up.T), [tokens, rows / 2].  No backward pass."""
+    if stream is not None:
+        with _on(stream):
+            return w4_linear(x, packed, out)
+    return _calls().w4_linear(x, packed._fields, packed._memory, out)
+
+
+def w4_moe_workspace_bytes(tokens: int, top: int, hidden: int) -> int:
+    return int(load_library().pwlq_w4_moe_workspace_bytes(tokens, top, hidden))
+
+
+def w4_moe(x, router, up: W4, down: W4, top: int, normalize=True, want_routing=False, out=None, workspace=None,
+           stream=None):
+    """``pwlq_w4_moe``: a mixture-of-experts layer for up to ``W4_MOE_MAX_TOKENS`` tokens x [tokens, features].
+    ``router`` is [experts, features], ``up`` a paired [experts, 2 * hidden, features], ``down``
+    [experts, features, hidden].  Every token takes the ``top`` experts with the largest scores x @ router.T,
+    weighted by the softmax over these (``normalize``) or over all scores.  Returns y, or with
+    ``want_routing`` (y, chosen experts int32 [tokens, top], weights float32 [tokens, top]), largest first.
+    ``out`` may be x.  No backward pass."""
+    if stream is not None:
+        with _on(stream):
+            return w4_moe(x, router, up, down, top, normalize, want_routing, out, workspace)
+    y, chosen, weights = _calls().w4_moe(x, router, up._fields, up._memory, down._fields, down._memory, top,
+                                         normalize, want_routing, out, workspace)
+    return (y, chosen, weights) if want_routing else y

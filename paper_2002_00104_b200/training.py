@@ -22,9 +22,9 @@ class Checkpoints:
         self.group, self.ratio = group, ratio
 
 
-def best_ratio(x: torch.Tensor, group: int = 128, candidates: int = 32) -> float:
+def best_ratio(x: torch.Tensor, group: int = 128, candidates: int = 32, bits: int = 7) -> float:
     """The breakpoint ratio with the smallest total squared error on x [rows, cols] (every group a
-    row of the 7-bit search, the last values of a row that do not fill one left out; rows shorter than
+    row of the search with this many bits: 7 for checkpoints, 3 for 4-bit weights; the last values of a row that do not fill one left out; rows shorter than
     a group are one each); candidates are k / candidates, the last one (no tail) left out."""
     if x.numel() == 0 or candidates < 2:
         raise ValueError(f"no candidates, or no values: x is {list(x.shape)}")
@@ -32,7 +32,7 @@ def best_ratio(x: torch.Tensor, group: int = 128, candidates: int = 32) -> float
     cols = x.shape[1] // group * group
     rows = x[:, :cols].float().reshape(-1, group).contiguous()
     ratios = torch.arange(1, candidates, device=x.device, dtype=torch.float32) / candidates
-    sse = pwlq.search(rows, 7, ratios, want_sse=True)["sse"]
+    sse = pwlq.search(rows, bits, ratios, want_sse=True)["sse"]
     return float(ratios[sse.double().sum(dim=0).argmin()])
 
 
