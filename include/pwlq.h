@@ -565,22 +565,20 @@ int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outpu
  * the products below take weights without rounding them.  |w| up to 2^126.
  *   paired   1: the matrix is two of rows / 2 rows each, gate rows then up rows (rows even), which the
  *            products take together: silu(gate) * up
- *   codes    pwlq_w4_code_bytes() bytes, 16-byte aligned, in the order in which the products read them:
- *            [matrices][tiles][ceil(cols / 64)] blocks of 512 bytes, 16 rows x 64 columns; a tile is 16
- *            consecutive rows, of a paired matrix 8 gate rows and the 8 up rows that belong to them.  Rows and
- *            columns behind the last one are held as 0
- *   scales   pwlq_w4_scale_bytes() bytes, 4-byte aligned: [matrices][tiles][ceil(cols / group)][8][2]
+ *   data     pwlq_w4_bytes() bytes, 16-byte aligned, in the order in which the products read them:
+ *            [matrices][tiles][ceil(cols / 128)] blocks of 16 rows x 128 columns, 1024 bytes of codes and then 16
+ *            scales for each of the block's groups (4, 2, 1 of 32, 64, 128 columns; a group of 256 has its
+ *            scales in both of its blocks).  A tile is 16 consecutive rows, of a paired matrix 8 gate rows
+ *            and the 8 up rows that belong to them.  Rows and columns behind the last one are held as 0
  * rows up to 2^24, cols up to 2^20, matrices up to 65535. */
 typedef struct {
     int64_t matrices, rows, cols, group, breakpoint, paired;
-    void* codes;
-    void* scales;
+    void* data;
 } pwlq_w4;
-size_t pwlq_w4_code_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t paired);
-size_t pwlq_w4_scale_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t group, int64_t paired);
+size_t pwlq_w4_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t group, int64_t paired);
 
 /* x, y [matrices, rows, cols] of type dtype; ldx / ldy the pitch of a row, ldm that of a matrix (ignored for one).
- * Every byte of codes and scales is written. */
+ * Every byte of data is written. */
 int pwlq_w4_encode(const pwlq_w4* w, const void* x, int dtype, int64_t ldx, int64_t ldm, void* stream);
 int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ldm, void* stream);
 

@@ -24,8 +24,7 @@ struct Library {
     decltype(&pwlq_block_norm_backward) backward;
     decltype(&pwlq_act8_weight_grad_workspace_bytes) grad_bytes;
     decltype(&pwlq_act8_weight_grad) grad;
-    decltype(&pwlq_w4_code_bytes) w4_codes;
-    decltype(&pwlq_w4_scale_bytes) w4_scales;
+    decltype(&pwlq_w4_bytes) w4_bytes;
     decltype(&pwlq_w4_encode) w4_encode;
     decltype(&pwlq_w4_decode) w4_decode;
     decltype(&pwlq_w4_linear) w4_linear;
@@ -411,7 +410,7 @@ PyObject* weight_grad(Args a) {
 }
 
 // A packed matrix from its fields (matrices, rows, cols, group, breakpoint, paired) and, where it has some, its
-// memory: the codes, then the scales.
+// memory.
 struct Packed {
     pwlq_w4 w = {};
     int64_t bytes = 0;
@@ -423,11 +422,8 @@ struct Packed {
             *to[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(fields, i));
             if (*to[i] == -1 && PyErr_Occurred()) throw python_error();
         }
-        const size_t codes = lib.w4_codes(w.matrices, w.rows, w.cols, w.paired),
-                     scales = lib.w4_scales(w.matrices, w.rows, w.cols, w.group, w.paired);
-        if (!codes || !scales) throw Failed{PWLQ_ERR_INVALID_ARG, "packed matrix"};
-        bytes = (int64_t)(codes + scales);
-        code_bytes_ = (int64_t)codes;
+        bytes = (int64_t)lib.w4_bytes(w.matrices, w.rows, w.cols, w.group, w.paired);
+        if (!bytes) throw Failed{PWLQ_ERR_INVALID_ARG, "packed matrix"};
     }
     void place(const at::Tensor& m, int device) {
         TORCH_CHECK_VALUE(m.scalar_type() == at::kByte && m.is_contiguous() && m.is_cuda() && m.get_device() == device &&
@@ -435,12 +431,8 @@ struct Packed {
                           "the memory of this packed matrix is ", bytes, " contiguous bytes on cuda:", device, ", got ",
                           m.numel(), " of ", m.scalar_type(), " on ", m.device());
         memory = m;
-        w.codes = m.data_ptr();
-        w.scales = static_cast<uint8_t*>(w.codes) + code_bytes_;
+        w.data = m.data_ptr();
     }
-
-private:
-    int64_t code_bytes_ = 0;
 };
 Packed packed(Args& a, int device) {
     Packed p(a.next());

@@ -5,15 +5,13 @@ namespace pwlq {
 
 W4View w4_view(const pwlq_w4& w, bool bf16) {
     W4View v = {};
-    v.codes = reinterpret_cast<const uint4*>(w.codes);
-    v.scales = reinterpret_cast<const uint32_t*>(w.scales);
+    v.data = static_cast<const uint8_t*>(w.data);
     v.rows = w.rows;
-    v.cols = w.cols;
+    v.cols = (int)w.cols;
     v.paired = w.paired != 0;
     v.tiles = w4_tiles(w.rows, v.paired);
-    v.blocks = w4_blocks(w.cols);
-    v.groups = w4_groups(w.cols, w.group);
-    v.group_shift = group_shift((int)w.group);
+    v.blocks = (int)w4_blocks(w.cols);
+    v.ends = w4_ends(w.group);
     const int b = (int)w.breakpoint;
     for (int i = 0; i < 8; ++i) {
         const int n = i < 4 ? i * b : 3 * b + (i - 4) * (64 - b);
@@ -35,10 +33,12 @@ namespace {
 constexpr float kInv192 = 192.0f;
 
 struct W4Write {
-    uint8_t* codes;
-    uint16_t* scales;
-    int64_t tiles, blocks, groups, rows, cols;
-    int group_shift, breakpoint, paired;
+    uint8_t* data;
+    int64_t tiles, blocks, rows, cols;
+    int group_shift, ends, breakpoint, paired;
+    __device__ __forceinline__ uint8_t* block(int64_t matrix, int64_t tile, int64_t b) const {
+        return data + ((matrix * tiles + tile) * blocks + b) * w4_block_bytes(ends);
+    }
     // row of the matrix that row r of a tile is, or -1
     __device__ __forceinline__ int64_t row_of(int64_t tile, int r) const {
         const int64_t half = rows / 2;
@@ -101,24 +101,26 @@ __global__ void __launch_bounds__(256) w4_encode_kernel(const T* __restrict__ x,
         }
         runs[r][c * 4 + i] = s > 0.0f ? (uint16_t)run : (uint16_t)0;
     }
-    const int64_t group = col >> w.group_shift;
-    if ((c & (lanes - 1)) == 0 && group < w.groups)
-        w.scales[(((matrix * w.tiles + tile) * w.groups + group) * 8 + (r & 7)) * 2 + (r >> 3)] = (uint16_t)(bits >> 16);
+    // a group's first thread writes its scale, of a group of 256 the first one of either block
+    if ((c & (min(lanes, 8) - 1)) == 0 && col / kBlockCols < w.blocks)
+        *reinterpret_cast<uint16_t*>(w.block(matrix, tile, col / kBlockCols) + kCodeBytes + ((c & 7) / lanes) * 32 +
+                                     (r & 7) * 4 + (r >> 3) * 2) = (uint16_t)(bits >> 16);
     __syncthreads();
-    const int64_t block = (int64_t)blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int64_t block = (int64_t)blockIdx.y * 2 + (threadIdx.x >> 7);
     if (block >= w.blocks) return;
-    const int lane = (threadIdx.x & 63) >> 1, half = threadIdx.x & 1;
+    const int lane = (threadIdx.x & 127) >> 2, h = threadIdx.x & 3;     // two words each, of a quarter of the block
     uint32_t word[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const int at = (threadIdx.x >> 6) * 16 + half * 8 + (lane & 3) * 2 + j;
+        const int at = (threadIdx.x >> 7) * 32 + h * 8 + (lane & 3) * 2 + j;
         const uint32_t a = runs[lane >> 2][at], e = runs[(lane >> 2) + 8][at];
         word[j] = (a & 0x7777u) | (e & 0x7777u) << 16 |
                   (a & 0x8u) << 4 | (a & 0x80u) << 8 | (a & 0x800u) << 12 | (a & 0x8000u) << 16 |
                   (e & 0x8u) | (e & 0x80u) << 4 | (e & 0x800u) << 8 | (e & 0x8000u) << 12;
     }
-    uint8_t* to = w.codes + ((matrix * w.tiles + tile) * w.blocks + block) * kBlockBytes;
-    *reinterpret_cast<uint2*>(to + lane * 16 + half * 8) = make_uint2(word[0], word[1]);
+    // a lane's words 0-3 in the block's first 512 bytes, 4-7 in the next
+    *reinterpret_cast<uint2*>(w.block(matrix, tile, block) + (h >> 1) * 512 + lane * 16 + (h & 1) * 8) =
+        make_uint2(word[0], word[1]);
 }
 
 // A warp per block; a lane has eight consecutive values of two rows in both halves of the block.
@@ -130,13 +132,14 @@ __global__ void __launch_bounds__(256) w4_decode_kernel(const W4View v, W4Write 
     const int64_t block = (int64_t)blockIdx.y * 8 + (threadIdx.x >> 5);
     await_previous();
     if (block >= v.blocks) return;
-    const uint4 c = v.tile_codes(matrix, tile)[block * 32 + lane];
-    const uint32_t words[4] = {c.x, c.y, c.z, c.w};
+    const uint8_t* const at = w.block(matrix, tile, block);
+    const uint4 c0 = *reinterpret_cast<const uint4*>(at + lane * 16);
+    const uint4 c1 = *reinterpret_cast<const uint4*>(at + 512 + lane * 16);
+    const uint32_t words[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        const int64_t first = block * kBlockCols + half * 32, col = first + q * 8;
-        const int64_t group = min(first >> v.group_shift, v.groups - 1);
-        const uint32_t s = v.tile_scales(matrix, tile)[group * 8 + g];
+    for (int half = 0; half < 4; ++half) {
+        const int64_t col = block * kBlockCols + half * 32 + q * 8;
+        const uint32_t s = *reinterpret_cast<const uint32_t*>(at + kCodeBytes + (half * w.ends / 4) * 32 + g * 4);
         float out[2][8];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -171,8 +174,8 @@ __global__ void __launch_bounds__(256) w4_decode_kernel(const W4View v, W4Write 
 
 W4Write writer(const pwlq_w4& w) {
     const bool paired = w.paired != 0;
-    return {static_cast<uint8_t*>(w.codes), static_cast<uint16_t*>(w.scales), w4_tiles(w.rows, paired), w4_blocks(w.cols),
-            w4_groups(w.cols, w.group), w.rows, w.cols, group_shift((int)w.group), (int)w.breakpoint, paired};
+    return {static_cast<uint8_t*>(w.data), w4_tiles(w.rows, paired), w4_blocks(w.cols), w.rows, w.cols,
+            group_shift((int)w.group), w4_ends(w.group), (int)w.breakpoint, paired};
 }
 
 template <typename T>
@@ -206,6 +209,13 @@ cudaError_t launch_w4_decode(const pwlq_w4& w, void* y, int dtype, int64_t ldy, 
     if (dtype == kF32) return decode(w, static_cast<float*>(y), ldy, ldm, stream);
     if (dtype == kBf16) return decode(w, static_cast<__nv_bfloat16*>(y), ldy, ldm, stream);
     return decode(w, static_cast<__half*>(y), ldy, ldm, stream);
+}
+
+cudaError_t launch_w4_linear(const pwlq_w4& w, const void* x, int dtype, int64_t tokens, int64_t ldx, void* y,
+                             int64_t ldy, cudaStream_t stream) {
+    if (dtype == kF32) return w4_linear_of<float>(w, x, tokens, ldx, y, ldy, stream);
+    if (dtype == kBf16) return w4_linear_of<__nv_bfloat16>(w, x, tokens, ldx, y, ldy, stream);
+    return w4_linear_of<__half>(w, x, tokens, ldx, y, ldy, stream);
 }
 
 }  // namespace pwlq

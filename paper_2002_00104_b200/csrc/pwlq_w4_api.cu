@@ -7,6 +7,7 @@ namespace {
 constexpr int64_t kMaxRows = (int64_t)1 << 24;
 constexpr int64_t kMaxCols = (int64_t)1 << 20;
 constexpr int64_t kMaxMatrices = 65535;
+constexpr int64_t kMaxBlocks = (int64_t)1 << 30;           // of 1 KB
 constexpr int64_t kMaxTokens = (int64_t)1 << 19;           // blocks of eight along a grid's second axis
 constexpr int64_t kMaxPitch = (int64_t)1 << 40;
 
@@ -17,7 +18,9 @@ inline bool is_dtype(int64_t d) { return d == PWLQ_F32 || d == PWLQ_BF16 || d ==
 
 int check_size(int64_t matrices, int64_t rows, int64_t cols, int64_t paired) {
     if (matrices < 1 || rows < 1 || cols < 1 || (paired != 0 && paired != 1) || (paired && rows % 2)) return PWLQ_ERR_INVALID_ARG;
-    if (matrices > kMaxMatrices || rows > kMaxRows || cols > kMaxCols) return PWLQ_ERR_UNSUPPORTED;
+    if (matrices > kMaxMatrices || rows > kMaxRows || cols > kMaxCols ||
+        matrices * pwlq::w4_tiles(rows, paired != 0) * pwlq::w4_blocks(cols) > kMaxBlocks)
+        return PWLQ_ERR_UNSUPPORTED;
     return PWLQ_OK;
 }
 bool bad_group(int64_t group) { return group != 32 && group != 64 && group != 128 && group != 256; }
@@ -25,8 +28,7 @@ bool bad_group(int64_t group) { return group != 32 && group != 64 && group != 12
 int check_w4(const pwlq_w4* w) {
     if (!w) return PWLQ_ERR_INVALID_ARG;
     if (int rc = check_size(w->matrices, w->rows, w->cols, w->paired)) return rc;
-    if (bad_group(w->group) || w->breakpoint < 1 || w->breakpoint > 64 || !w->codes || !w->scales ||
-        misaligned(w->codes, 16) || misaligned(w->scales, 4))
+    if (bad_group(w->group) || w->breakpoint < 1 || w->breakpoint > 64 || !w->data || misaligned(w->data, 16))
         return PWLQ_ERR_INVALID_ARG;
     return PWLQ_OK;
 }
@@ -50,14 +52,10 @@ bool bad_matrices(const pwlq_w4& w, const void* p, int dtype, int64_t ld, int64_
 
 extern "C" {
 
-size_t pwlq_w4_code_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t paired) {
-    if (check_size(matrices, rows, cols, paired)) return 0;
-    return (size_t)(matrices * pwlq::w4_tiles(rows, paired != 0) * pwlq::w4_blocks(cols) * pwlq::kBlockBytes);
-}
-
-size_t pwlq_w4_scale_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t group, int64_t paired) {
+size_t pwlq_w4_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t group, int64_t paired) {
     if (check_size(matrices, rows, cols, paired) || bad_group(group)) return 0;
-    return (size_t)(matrices * pwlq::w4_tiles(rows, paired != 0) * pwlq::w4_groups(cols, group) * 2 * pwlq::kTileRows);
+    return (size_t)(matrices * pwlq::w4_tiles(rows, paired != 0) * pwlq::w4_blocks(cols)) *
+           (size_t)pwlq::w4_block_bytes(pwlq::w4_ends(group));
 }
 
 int pwlq_w4_encode(const pwlq_w4* w, const void* x, int dtype, int64_t ldx, int64_t ldm, void* stream) {

@@ -1,0 +1,323 @@
+// Mixture of experts: the products of the chosen experts.  The files that include this one instantiate it for a type
+// each, so that they are compiled side by side.
+#pragma once
+
+#include "pwlq_w4_moe.h"
+
+namespace pwlq {
+namespace {
+
+constexpr int kUpWarps = 8, kDownWarps = 16;
+
+// Who goes where, made by every CTA for itself in shared memory: the experts that are chosen at all, and for each of
+// them its (token, place) pairs, token * top + place, in ascending order.
+struct Lists {
+    u64* mask;                                            // the tokens of an expert
+    uint16_t *index, *expert, *first, *pair;
+    int* active;
+    __device__ Lists(uint8_t* at, const Routing& r)
+        : mask(reinterpret_cast<u64*>(at)), index(reinterpret_cast<uint16_t*>(mask + r.experts)), expert(index + r.experts),
+          first(expert + r.experts), pair(first + r.experts + 1),
+          active(reinterpret_cast<int*>(at + (bytes(r) - 16))) {}
+    static __host__ __device__ int bytes(const Routing& r) {
+        return (r.experts * 14 + 2 + r.tokens * r.top * 2 + 15) / 16 * 16 + 16;
+    }
+};
+
+// Returns how many experts are active.
+__device__ __forceinline__ int build_lists(const Lists& l, const Routing& r) {
+    const int pairs = r.tokens * r.top, threads = blockDim.x;
+    for (int e = threadIdx.x; e < r.experts; e += threads) l.mask[e] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < pairs; i += threads) {
+        const int t = i / r.top;
+        atomicOr(reinterpret_cast<uint32_t*>(&l.mask[r.chosen[i]]) + (t >> 5), 1u << (t & 31));
+    }
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        int active = 0, before = 0;
+        for (int base = 0; base < r.experts; base += 32) {
+            const int e = base + lane;
+            const int count = e < r.experts ? __popcll(l.mask[e]) : 0;
+            const unsigned some = __ballot_sync(kAll, count > 0);
+            int sum = count;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(kAll, sum, o);
+                if (lane >= o) sum += v;
+            }
+            if (count > 0) {
+                const int at = active + __popc(some & ((1u << lane) - 1));
+                l.index[e] = (uint16_t)at;
+                l.expert[at] = (uint16_t)e;
+                l.first[at] = (uint16_t)(before + sum - count);
+            }
+            active += __popc(some);
+            before += __shfl_sync(kAll, sum, 31);
+        }
+        if (lane == 0) {
+            l.first[active] = (uint16_t)before;
+            *l.active = active;
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < pairs; i += threads) {
+        const int t = i / r.top, e = r.chosen[i];
+        l.pair[l.first[l.index[e]] + __popcll(l.mask[e] & ((1ull << t) - 1))] = (uint16_t)i;
+    }
+    __syncthreads();
+    return *l.active;
+}
+
+// What lies between the two products, a row for each pair: binary32, or two bf16 parts (16 bits of each value:
+// with them the result is rounded once, as if there were nothing between; one 16-bit value would add as much
+// error again).  Rows are padded with zeros to whole blocks.
+template <typename T> struct Hidden {
+    using Source = RowsSplit;
+    using Elem = __nv_bfloat16;
+    static __host__ __device__ int64_t pitch(int64_t padded) { return 2 * padded; }
+    static __device__ __forceinline__ void put(Elem* row, int64_t padded, int64_t i, float v) {
+        const __nv_bfloat16 high = __float2bfloat16_rn(v);
+        const float rest = v - __bfloat162float(high);
+        row[i] = high;
+        row[padded + i] = __float2bfloat16_rn(abs_bits(__bfloat162float(high)) < kInfBits ? rest : 0.0f);
+    }
+};
+template <> struct Hidden<float> {
+    using Source = RowsAny<float>;
+    using Elem = float;
+    static __host__ __device__ int64_t pitch(int64_t padded) { return padded; }
+    static __device__ __forceinline__ void put(float* row, int64_t, int64_t i, float v) { row[i] = v; }
+};
+
+template <typename T> struct UpArgs {
+    W4View w;                                             // [experts, 2 hidden, features], paired
+    Routing r;
+    const T* x;
+    int64_t ldx;
+    typename Hidden<T>::Elem* h;
+    int64_t padded;                                       // hidden in whole blocks
+    int team_shift;                                       // log2 of the warps of a team
+};
+
+// A warp's way through the items (tile of an expert) of its team, 8 NT of the expert's tokens at a time.
+struct UpTag { int tile, first, count; };                 // the expert's pairs of this pass
+template <int NT, typename T> struct UpSteps {
+    const Lists* l;
+    const UpArgs<T>* a;
+    int n_blocks, from, step, items, item, bytes;
+    int tile = 0, expert = 0, first = 0, count = 0;       // count: of the expert's pairs from `first` on
+    __device__ __forceinline__ bool next() {
+        first += 8 * NT;
+        count -= 8 * NT;
+        if (count > 0) return true;
+        item += step;
+        if (item >= items) return false;
+        const int at = item / (int)a->w.tiles;
+        tile = item - at * (int)a->w.tiles;
+        expert = l->expert[at];
+        first = l->first[at];
+        count = l->first[at + 1] - first;
+        return true;
+    }
+    __device__ __forceinline__ int blocks() const { return n_blocks; }
+    __device__ __forceinline__ const uint8_t* code(int) const {
+        return a->w.data + ((expert * a->w.tiles + tile) * a->w.blocks + from) * bytes;
+    }
+    __device__ __forceinline__ UpTag tag() const { return {tile, first, count}; }
+    __device__ __forceinline__ int column() const { return from * kBlockCols; }
+    // columns past the last token repeat it; nobody reads their sums
+    __device__ __forceinline__ const T* row(int n) const {
+        const int c = min(8 * n + ((int)(threadIdx.x & 31) >> 2), count - 1);
+        return a->x + (int64_t)(l->pair[first + c] / a->r.top) * a->ldx;
+    }
+};
+
+// A team of warps takes 8 gate rows and the 8 up rows that belong to them, of one expert, and shares the columns;
+// teams go on from one such item to the next.
+template <int NT, int ENDS, typename T, class S>
+__global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T> a) {
+    constexpr int kPitch = 8 * NT + 1, kRing = kRingBytes<1, ENDS>;
+    extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
+    float* const sums = reinterpret_cast<float*>(shared + kUpWarps * kRing);
+    const Lists l(reinterpret_cast<uint8_t*>(sums + kUpWarps * 16 * kPitch), a.r);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    await_previous();
+    const int active = build_lists(l, a.r);
+    const int team = 1 << a.team_shift, teams = kUpWarps >> a.team_shift, mine = warp >> a.team_shift;
+    const int part = warp & (team - 1), begin = (a.w.blocks * part) >> a.team_shift;
+    const int count = ((a.w.blocks * (part + 1)) >> a.team_shift) - begin, hidden = (int)(a.w.rows / 2);
+    auto meet = [&]() {                                   // the warps of a team
+        if (team == 1) __syncwarp();
+        else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(32 << a.team_shift) : "memory");
+    };
+    S source;
+    source.cols = a.w.cols;
+    const UpSteps<NT, T> steps = {&l, &a, count, begin, (int)gridDim.x * teams, active * (int)a.w.tiles,
+                                  ((int)blockIdx.x - (int)gridDim.x) * teams + mine, w4_block_bytes(ENDS)};
+    w4_stream<1, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
+                           [&](const UpTag& at, const float (&acc)[1][NT][4]) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sums[(warp * 16 + (lane >> 2) + (i & 2) * 4) * kPitch + 8 * n + 2 * (lane & 3) + (i & 1)] = acc[0][n][i];
+        meet();
+        for (int i = threadIdx.x & (32 * team - 1); i < 8 * min(at.count, 8 * NT); i += 32 * team) {
+            const int c = i >> 3, r = i & 7, pair = l.pair[at.first + c];
+            float gate = 0.0f, up = 0.0f;
+            for (int j = mine * team; j < (mine + 1) * team; ++j) {
+                gate += sums[(j * 16 + r) * kPitch + c];
+                up += sums[(j * 16 + r + 8) * kPitch + c];
+            }
+            const int f = at.tile * 8 + r;
+            typename Hidden<T>::Elem* const to = a.h + pair * Hidden<T>::pitch(a.padded);
+            Hidden<T>::put(to, a.padded, f,
+                           f < hidden ? silu_of(gate * 256.0f) * (up * 256.0f) * a.r.weights[pair] : 0.0f);
+            if (at.tile == a.w.tiles - 1)
+                for (int z = f + 8; z < a.padded; z += 8) Hidden<T>::put(to, a.padded, z, 0.0f);
+        }
+        meet();
+    });
+}
+
+template <typename T> struct DownArgs {
+    W4View w;                                             // [experts, features, hidden]
+    Routing r;
+    const typename Hidden<T>::Elem* h;
+    int64_t padded;
+    T* y;
+    int64_t ldy;
+};
+
+// A warp's way through its part of a tile's blocks, which are those of all chosen experts one after another.
+struct DownTag { int first, count; };
+template <int NT, typename T> struct DownSteps {
+    using H = Hidden<T>;
+    const Lists* l;
+    const DownArgs<T>* a;
+    int64_t tile;
+    int now, end, bytes;                                  // the block after this segment, the last one
+    int expert = 0, first = 0, count = 0, from = 0, n_blocks = 0;
+    __device__ __forceinline__ bool next() {
+        first += 8 * NT;
+        count -= 8 * NT;
+        if (count > 0) return true;
+        if (now >= end) return false;
+        const int at = now / a->w.blocks;
+        from = now - at * a->w.blocks;
+        n_blocks = min(a->w.blocks - from, end - now);
+        now += n_blocks;
+        expert = l->expert[at];
+        first = l->first[at];
+        count = l->first[at + 1] - first;
+        return true;
+    }
+    __device__ __forceinline__ int blocks() const { return n_blocks; }
+    __device__ __forceinline__ const uint8_t* code(int) const {
+        return a->w.data + ((expert * a->w.tiles + tile) * a->w.blocks + from) * bytes;
+    }
+    __device__ __forceinline__ DownTag tag() const { return {first, count}; }
+    __device__ __forceinline__ int column() const { return from * kBlockCols; }
+    __device__ __forceinline__ const typename H::Elem* row(int n) const {
+        const int c = min(8 * n + ((int)(threadIdx.x & 31) >> 2), count - 1);
+        return a->h + l->pair[first + c] * H::pitch(a->padded);
+    }
+};
+
+// A CTA per 16 features: the blocks of all chosen experts' rows are one list that the warps share; a warp adds what
+// an expert gives to its own sums, [16][tokens], and these are added in a fixed order at the end.
+template <int NT, int ENDS, typename T>
+__global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const DownArgs<T> a) {
+    using H = Hidden<T>;
+    constexpr int kRing = kRingBytes<1, ENDS>;
+    extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int pitch = a.r.tokens | 1;
+    float* const sums = reinterpret_cast<float*>(shared + kDownWarps * kRing);
+    float* const mine = sums + warp * 16 * pitch;
+    const Lists l(reinterpret_cast<uint8_t*>(sums + kDownWarps * 16 * pitch), a.r);
+    for (int i = lane; i < 16 * pitch; i += 32) mine[i] = 0.0f;
+    await_previous();
+    const int total = build_lists(l, a.r) * a.w.blocks;
+    typename H::Source source;
+    source.cols = (int)a.padded;
+    const DownSteps<NT, T> steps = {&l, &a, (int64_t)blockIdx.x, (int)((int64_t)total * warp / kDownWarps),
+                                    (int)((int64_t)total * (warp + 1) / kDownWarps), w4_block_bytes(ENDS)};
+    w4_stream<1, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
+                           [&](const DownTag& at, const float (&acc)[1][NT][4]) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = 8 * n + 2 * q + (i & 1);
+                if (c < at.count) mine[(g + (i & 2) * 4) * pitch + l.pair[at.first + c] / a.r.top] += acc[0][n][i];
+            }
+        __syncwarp();
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * a.r.tokens; i += kDownWarps * 32) {
+        const int r = i & 15, t = i >> 4;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kDownWarps; ++j) sum += sums[(j * 16 + r) * pitch + t];
+        const int64_t d = (int64_t)blockIdx.x * 16 + r;
+        if (d < a.w.rows) a.y[t * a.ldy + d] = from_f32<T>(sum * 256.0f);
+    }
+}
+
+template <typename F>
+cudaError_t with_ends(int ends, F f) {
+    if (ends == 4) return f(std::integral_constant<int, 4>());
+    return ends == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
+}
+
+template <int NT, typename T, class S>
+cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
+    const int64_t most = std::min<int64_t>(a.r.experts, (int64_t)a.r.tokens * a.r.top) * a.w.tiles;
+    a.team_shift = 0;
+    while (a.team_shift < 3 && most << a.team_shift < 24 * 148 && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
+    const int64_t ctas = ((most << a.team_shift) + kUpWarps - 1) / kUpWarps;
+    return with_ends(a.w.ends, [&](auto ends) {
+        constexpr int kEnds = decltype(ends)::value;
+        const size_t smem = kUpWarps * (kRingBytes<1, kEnds> + 16 * (8 * NT + 1) * 4) + Lists::bytes(a.r);
+        return launch_w4(moe_up_kernel<NT, kEnds, T, S>, a, dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
+                         smem, stream);
+    });
+}
+
+template <int NT, typename T>
+cudaError_t down_launch(const DownArgs<T>& a, cudaStream_t stream) {
+    return with_ends(a.w.ends, [&](auto ends) {
+        constexpr int kEnds = decltype(ends)::value;
+        const size_t smem = kDownWarps * (kRingBytes<1, kEnds> + 16 * (a.r.tokens | 1) * 4) + Lists::bytes(a.r);
+        return launch_w4(moe_down_kernel<NT, kEnds, T>, a, dim3((unsigned)a.w.tiles), kDownWarps * 32, smem, stream);
+    });
+}
+
+template <int NT, typename T>
+cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, void* hidden, cudaStream_t stream) {
+    const int64_t padded = w4_padded(a.down->cols);
+    auto* const h = static_cast<typename Hidden<T>::Elem*>(hidden);
+    const UpArgs<T> up = {w4_view(*a.up, !std::is_same<T, __half>::value), r, static_cast<const T*>(a.x), a.ldx, h, padded, 0};
+    cudaError_t err;
+    if constexpr (sizeof(T) == 2) {
+        err = a.up->cols % kBlockCols == 0 && rows_aligned(a.x, a.ldx, sizeof(T))
+                  ? up_launch<NT, T, RowsWhole<T>>(up, stream)
+                  : up_launch<NT, T, RowsAny<T>>(up, stream);
+    } else {
+        err = up_launch<NT, T, RowsAny<T>>(up, stream);
+    }
+    if (err != cudaSuccess) return err;
+    const DownArgs<T> down = {w4_view(*a.down, true), r, h, padded, static_cast<T*>(a.y), a.ldy};
+    return down_launch<NT, T>(down, stream);
+}
+
+}  // namespace
+
+template <typename T>
+cudaError_t launch_moe_products(const pwlq_w4_moe_args& a, const Routing& r, void* hidden, cudaStream_t stream) {
+    return a.tokens <= 8 ? products<1, T>(a, r, hidden, stream) : products<2, T>(a, r, hidden, stream);
+}
+
+}  // namespace pwlq

@@ -104,8 +104,7 @@ _SIGNATURES = {
     "pwlq_act8_weight_grad_workspace_bytes": (_SZ, [_I64, _I64, _I64, _INT]),
     "pwlq_act8_weight_grad": (_INT, [_P, _INT, _I64, _I64, _I64, _P, _I64, _P, _I64, _INT, _F32, _P,
                                      _INT, _I64, _INT, _P, _SZ, _P]),
-    "pwlq_w4_code_bytes": (_SZ, [_I64, _I64, _I64, _I64]),
-    "pwlq_w4_scale_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
+    "pwlq_w4_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
     "pwlq_w4_encode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
     "pwlq_w4_decode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
     "pwlq_w4_linear": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P, _I64, _P]),
@@ -836,7 +835,7 @@ def _calls():
         entries = ("pwlq_act8_encode", "pwlq_act8_decode", "pwlq_block_norm",
                    "pwlq_block_norm_backward_workspace_bytes", "pwlq_block_norm_backward",
                    "pwlq_act8_weight_grad_workspace_bytes", "pwlq_act8_weight_grad",
-                   "pwlq_w4_code_bytes", "pwlq_w4_scale_bytes", "pwlq_w4_encode", "pwlq_w4_decode",
+                   "pwlq_w4_bytes", "pwlq_w4_encode", "pwlq_w4_decode",
                    "pwlq_w4_linear", "pwlq_w4_moe_workspace_bytes", "pwlq_w4_moe")
         module.init(tuple(ctypes.cast(getattr(lib, name), _P).value for name in entries), PwlqError)
         _calls_module = module
@@ -1095,14 +1094,13 @@ def _w4_fields(shape, group: int, ratio: float, paired: bool):
 
 
 def w4_bytes(shape, group: int = 128, paired: bool = False) -> int:
-    """Size of a packed matrix: the codes, then the scales."""
+    """Size of a packed matrix."""
     matrices, rows, cols, group, _, paired = _w4_fields(shape, group, 0.5, paired)
-    lib = load_library()
-    codes = lib.pwlq_w4_code_bytes(matrices, rows, cols, paired)
-    if not codes:
+    need = load_library().pwlq_w4_bytes(matrices, rows, cols, group, paired)
+    if not need:
         small = min(matrices, rows, cols) < 1
         raise PwlqError(ERR_INVALID_ARG if small else ERR_UNSUPPORTED, f"packed matrix of {list(shape)}")
-    return int(codes + lib.pwlq_w4_scale_bytes(matrices, rows, cols, group, paired))
+    return int(need)
 
 
 class W4:
