@@ -560,7 +560,7 @@ int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outpu
  * and with the breakpoint b, a whole number in 1..64 for the whole tensor (p = m * b / 64), the values are
  * whole multiples of s:
  *     tail = a > 3 b s;   n = tail ? 3 b + q (64 - b) : q b,   q in 0..3 the nearest level, ties to even
- * (a = |w|).  Every bound between two levels is exact in binary32, and so is every value n * s: encoding and
+ * (a = |w|); a nibble is sign << 3 | tail << 2 | q, of a value held as 0 it is 0.  Every bound between two levels is exact in binary32, and so is every value n * s: encoding and
  * decoding round nothing but s.  n <= 192 has eight bits, so that n / 256 is exact in bf16 and fp16 as well and
  * the products below take weights without rounding them.  |w| up to 2^126.
  *   paired   1: the matrix is two of rows / 2 rows each, gate rows then up rows (rows even), which the
@@ -615,7 +615,7 @@ typedef struct {
     float* weights;
     void* workspace; int64_t workspace_bytes;
 } pwlq_w4_moe_args;
-size_t pwlq_w4_moe_workspace_bytes(int64_t tokens, int64_t top, int64_t hidden);
+size_t pwlq_w4_moe_workspace_bytes(int64_t tokens, int64_t top, int64_t features, int64_t hidden);
 int pwlq_w4_moe(const pwlq_w4_moe_args* args, void* stream);
 
 /* The streaming kernels (abs-max, quantize, dequantize) hand their data over through shared-memory

@@ -544,7 +544,7 @@ PyObject* w4_moe(Args a) {
     m.y = t.p;
     m.ldy = t.ld;
     // sizes that memory is made from, before the library sees them
-    const int64_t need = (int64_t)lib.moe_bytes(m.tokens, m.top, down.w.cols);
+    const int64_t need = (int64_t)lib.moe_bytes(m.tokens, m.top, down.w.rows, down.w.cols);
     if (!need) throw Failed{m.tokens > PWLQ_W4_MOE_MAX_TOKENS || m.top > PWLQ_W4_MOE_MAX_TOP ? PWLQ_ERR_UNSUPPORTED
                                                                                        : PWLQ_ERR_INVALID_ARG, "pwlq_w4_moe"};
     at::Tensor chosen, weights;

@@ -30,7 +30,7 @@ W4View w4_view(const pwlq_w4& w, bool bf16) {
 
 namespace {
 
-constexpr float kInv192 = 192.0f;
+constexpr float kUnits = 192.0f;         // scales to a range
 
 struct W4Write {
     uint8_t* data;
@@ -48,79 +48,112 @@ struct W4Write {
     }
 };
 
+// 1 where a > t, 0 elsewhere, for a and t in units of t's own size and 2^-40 times it or more: the sign of a - t is
+// that of the fused product's exact sum, and its size at least an ulp.  One instruction of the multiply-add pipe; a
+// comparison and a selection take four cycles of the integer pipe.
+__device__ __forceinline__ float above(float a, float minus_t) {
+    float r;
+    asm("fma.rn.sat.f32 %0, %1, 0f53800000, %2;" : "=f"(r) : "f"(a), "f"(minus_t));      // 2^40
+    return r;
+}
+
 // One CTA packs 16 rows x 256 columns, a multiple of every group length; a thread holds 16 values of a row, so
-// that a range is a few shuffles between neighbours.  Levels come from comparing |x| with halves of steps: a
-// bound is (a half-integer of at most 9 bits) * (a scale of 8 bits), exact in binary32, so that the level is the
-// nearest one, without a rounding on the way.
+// that a range is a few shuffles between neighbours.  A code counts the bounds below |x|, four between levels of the
+// center and the tail and the breakpoint itself.  A bound is (a half-integer of at most 9 bits) * (a scale of 8 bits),
+// exact in binary32, so that the level is the nearest one, without a rounding on the way.
+// It goes on to the tile below, so that what does not depend on the values is made once for several tiles.
 template <bool VEC, typename T>
-__global__ void __launch_bounds__(256) w4_encode_kernel(const T* __restrict__ x, int64_t ldx, int64_t ldm, W4Write w) {
-    __shared__ uint16_t runs[16][66];                     // four codes each; two columns of padding against conflicts
+__global__ void __launch_bounds__(256) w4_encode_kernel(const T* __restrict__ x, int64_t ldx, int64_t ldm, W4Write w,
+                                                        int tiles_each) {
+    __shared__ uint16_t runs[2][16][66];                  // four codes each; two columns of padding against conflicts
     const int r = threadIdx.x >> 4, c = threadIdx.x & 15;
-    const int64_t tile = blockIdx.x, matrix = blockIdx.z;
-    const int64_t col = (int64_t)blockIdx.y * 256 + c * 16;
-    const int64_t row = w.row_of(tile, r);
-    await_previous();
-    float v[16];
-    {
-        const T* p = x + matrix * ldm + (row < 0 ? 0 : row) * ldx + col;
-        const int64_t valid = row < 0 ? 0 : w.cols - col;
-        Raw8<T> a, b;
-        load8<VEC>(a, p, (int)max((int64_t)-8, min(valid, (int64_t)64)), (int)min(col, (int64_t)64));
-        load8<VEC>(b, p + 8, (int)max((int64_t)-8, min(valid - 8, (int64_t)64)), (int)min(col, (int64_t)64) + 8);
-        a.get(v);
-        b.get(v + 8);
-    }
-    uint32_t m = 0;                                       // as bits: a NaN is above infinity, infinity above the rest
-#pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, abs_bits(v[i]));
+    const int64_t first = (int64_t)blockIdx.x * tiles_each, matrix = blockIdx.z;
+    const int col = blockIdx.y * 256 + c * 16, cols = (int)w.cols;
     const int lanes = 1 << (w.group_shift - 4);           // threads of a group
-    for (int o = 1; o < lanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    uint32_t bits = 0;
-    if (m >= kInfBits) {
-        bits = 0x7fc00000u;
-    } else if (__uint_as_float(m) >= kAct8Tiny) {
-        bits = (__float_as_uint(__fdiv_rn(__uint_as_float(m), kInv192)) + 0xffffu) & 0xffff0000u;
-    }
-    const float s = m >= kInfBits ? 0.0f : __uint_as_float(bits);
-    const float b = (float)w.breakpoint, d = (float)(64 - w.breakpoint);
-    const float edge = 3.0f * b * s;
-    const float c1 = 0.5f * b * s, c2 = 1.5f * b * s, c3 = 2.5f * b * s;
-    const float t1 = (3.0f * b + 0.5f * d) * s, t2 = (3.0f * b + 1.5f * d) * s, t3 = (3.0f * b + 2.5f * d) * s;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint32_t run = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float value = v[4 * i + k], a = fabsf(value);
-            const bool tail = a > edge;
-            // halves go to the even level
-            uint32_t code = (a > (tail ? t1 : c1) ? 1u : 0u) + (a >= (tail ? t2 : c2) ? 1u : 0u) +
-                            (a > (tail ? t3 : c3) ? 1u : 0u) + (tail ? 4u : 0u);
-            if (value < 0.0f) code |= 8u;
-            run |= code << 4 * k;
-        }
-        runs[r][c * 4 + i] = s > 0.0f ? (uint16_t)run : (uint16_t)0;
-    }
+    // the row of the first tile that this thread has, and how many it has in all
+    const int64_t half = w.rows / 2, step = w.paired ? 8 : 16;
+    const int64_t row = w.paired && r >= 8 ? half + first * 8 + r - 8 : first * step + r;
+    const int64_t end = w.paired && r < 8 ? half : w.rows;
+    const T* p = x + matrix * ldm + row * ldx + col;
+    int rows = (int)min((int64_t)tiles_each, max((int64_t)0, (end - row + step - 1) / step));
+    int tiles = (int)min((int64_t)tiles_each, w.tiles - first);
+    uint8_t* to = w.block(matrix, first, (int64_t)blockIdx.y * 2);
+    const int64_t tile_bytes = w.blocks * w4_block_bytes(w.ends);
     // a group's first thread writes its scale, of a group of 256 the first one of either block
-    if ((c & (min(lanes, 8) - 1)) == 0 && col / kBlockCols < w.blocks)
-        *reinterpret_cast<uint16_t*>(w.block(matrix, tile, col / kBlockCols) + kCodeBytes + ((c & 7) / lanes) * 32 +
-                                     (r & 7) * 4 + (r >> 3) * 2) = (uint16_t)(bits >> 16);
-    __syncthreads();
-    const int64_t block = (int64_t)blockIdx.y * 2 + (threadIdx.x >> 7);
-    if (block >= w.blocks) return;
-    const int lane = (threadIdx.x & 127) >> 2, h = threadIdx.x & 3;     // two words each, of a quarter of the block
-    uint32_t word[2];
+    const bool scaling = (c & (min(lanes, 8) - 1)) == 0 && (c >> 3) + blockIdx.y * 2 < w.blocks;
+    const int scale_at = (c >> 3) * w4_block_bytes(w.ends) + kCodeBytes + ((c & 7) / lanes) * 32 + (r & 7) * 4 + (r >> 3) * 2;
+    // two words of a quarter of a block; a lane's words 0-3 are in the block's first 512 bytes, 4-7 in the next
+    const int block = threadIdx.x >> 7, lane = (threadIdx.x & 127) >> 2, h = threadIdx.x & 3;
+    const bool writing = blockIdx.y * 2 + block < w.blocks;
+    const int words_at = block * w4_block_bytes(w.ends) + (h >> 1) * 512 + lane * 16 + (h & 1) * 8;
+    const int runs_at = block * 32 + h * 8 + (lane & 3) * 2;
+    const float b = (float)w.breakpoint, d = (float)(64 - w.breakpoint);
+    const float center = -1099511627776.0f * b, tail = -1099511627776.0f * d;       // -2^40
+    await_previous();
+    for (int turn = 0; tiles > 0; --tiles, --rows, turn ^= 1, p += step * ldx, to += tile_bytes) {
+        float v[16];
+        {
+            const int valid = rows > 0 ? cols - col : 0;
+            Raw8<T> lo, hi;
+            load8<VEC>(lo, p, valid, col);
+            load8<VEC>(hi, p + 8, valid - 8, col + 8);
+            lo.get(v);
+            hi.get(v + 8);
+        }
+        uint32_t m = 0;                                   // as bits: a NaN is above infinity, infinity above the rest
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int at = (threadIdx.x >> 7) * 32 + h * 8 + (lane & 3) * 2 + j;
-        const uint32_t a = runs[lane >> 2][at], e = runs[(lane >> 2) + 8][at];
-        word[j] = (a & 0x7777u) | (e & 0x7777u) << 16 |
-                  (a & 0x8u) << 4 | (a & 0x80u) << 8 | (a & 0x800u) << 12 | (a & 0x8000u) << 16 |
-                  (e & 0x8u) | (e & 0x80u) << 4 | (e & 0x800u) << 8 | (e & 0x8000u) << 12;
+        for (int i = 0; i < 16; ++i) m = max(m, abs_bits(v[i]));
+        for (int o = 1; o < lanes; o <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        uint32_t bits = 0;
+        if (m >= kInfBits) {
+            bits = 0x7fc00000u;
+        } else if (__uint_as_float(m) >= kAct8Tiny) {
+            bits = (__float_as_uint(__fdiv_rn(__uint_as_float(m), kUnits)) + 0xffffu) & 0xffff0000u;
+        }
+        // s = unit * 2^e: bounds for values times 2^-e, so that no product leaves the range of binary32
+        const bool some = m < kInfBits && bits != 0;
+        const float unit = __uint_as_float((bits & 0x007fffffu) | 0x3f800000u);
+        const float scale = __uint_as_float(some ? 0x7f000000u - (bits & 0x7f800000u) : 0u);
+        const float bk = center * unit, dk = tail * unit;
+        // halves go to the even level: at 1.5 steps up, so that the bound there is the number before it (a tail without
+        // steps, at 64, has its bounds at the breakpoint)
+        const float edge = 3.0f * bk;
+        const float c1 = 0.5f * bk, c2 = __uint_as_float(__float_as_uint(1.5f * bk) - 1), c3 = 2.5f * bk;
+        const float t1 = edge + 0.5f * dk, t2 = __uint_as_float(__float_as_uint(edge + 1.5f * dk) - (d > 0.0f)),
+                    t3 = edge + 2.5f * dk;
+        const float bounds[6] = {c2, c3, edge, t1, t2, t3};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float run = 0.0f;
+#pragma unroll
+            for (int h2 = 2; h2 >= 0; h2 -= 2) {
+                const float x0 = v[4 * i + h2] * scale, x1 = v[4 * i + h2 + 1] * scale;
+                u64 count = pack2(above(fabsf(x0), c1), above(fabsf(x1), c1));
+#pragma unroll
+                for (int n = 0; n < 6; ++n) count = add2(count, pack2(above(fabsf(x0), bounds[n]), above(fabsf(x1), bounds[n])));
+                // the sign of what is not held as 0
+                run = fmaf(run, 16.0f, fmaf(above(-x1, c1), 8.0f, hi2(count)));
+                run = fmaf(run, 16.0f, fmaf(above(-x0, c1), 8.0f, lo2(count)));
+            }
+            runs[turn][r][c * 4 + i] = (uint16_t)(some ? __float_as_uint(run + 8388608.0f) : 0u);
+        }
+        if (scaling) *reinterpret_cast<uint16_t*>(to + scale_at) = (uint16_t)(bits >> 16);
+        __syncthreads();
+        if (!writing) continue;
+        uint32_t word[2];
+        const uint32_t a2 = *reinterpret_cast<const uint32_t*>(&runs[turn][lane >> 2][runs_at]);
+        const uint32_t e2 = *reinterpret_cast<const uint32_t*>(&runs[turn][(lane >> 2) + 8][runs_at]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            // magnitudes of row g below those of row g + 8; signs: bits 3, 7, 11, 15 go to 7, 15, 23, 31 for row g, to 3, 11,
+            // 19, 27 for row g + 8
+            const uint32_t both = permute(a2, e2, j ? 0x7632u : 0x5410u);
+            const uint32_t s = permute(a2, 0u, j ? 0x4342u : 0x4140u), q = permute(e2, 0u, j ? 0x4342u : 0x4140u);
+            word[j] = (both & 0x77777777u) | (s << 4 & 0x00800080u) | (s << 8 & 0x80008000u) | (q & 0x00080008u) |
+                      (q << 4 & 0x08000800u);
+        }
+        *reinterpret_cast<uint2*>(to + words_at) = make_uint2(word[0], word[1]);
     }
-    // a lane's words 0-3 in the block's first 512 bytes, 4-7 in the next
-    *reinterpret_cast<uint2*>(w.block(matrix, tile, block) + (h >> 1) * 512 + lane * 16 + (h & 1) * 8) =
-        make_uint2(word[0], word[1]);
 }
 
 // A warp per block; a lane has eight consecutive values of two rows in both halves of the block.
@@ -181,10 +214,13 @@ W4Write writer(const pwlq_w4& w) {
 template <typename T>
 cudaError_t encode(const pwlq_w4& w, const T* x, int64_t ldx, int64_t ldm, cudaStream_t stream) {
     const W4Write to = writer(w);
-    const dim3 grid((unsigned)to.tiles, (unsigned)((w.cols + 255) / 256), (unsigned)w.matrices);
+    // several tiles to a CTA where that leaves enough of them: 8192 x 8192 bf16 encode 82 -> 57 us with four
+    const int64_t columns = (w.cols + 255) / 256;
+    const int each = to.tiles * columns * w.matrices >= 4 * 8 * 148 ? 4 : 1;
+    const dim3 grid((unsigned)((to.tiles + each - 1) / each), (unsigned)columns, (unsigned)w.matrices);
     const bool aligned = rows_aligned(x, ldx, sizeof(T)) && (w.matrices == 1 || rows_aligned(x, ldm, sizeof(T)));
-    return aligned ? launch_dependent(w4_encode_kernel<true, T>, grid, dim3(256), 0, stream, x, ldx, ldm, to)
-                   : launch_dependent(w4_encode_kernel<false, T>, grid, dim3(256), 0, stream, x, ldx, ldm, to);
+    return aligned ? launch_dependent(w4_encode_kernel<true, T>, grid, dim3(256), 0, stream, x, ldx, ldm, to, each)
+                   : launch_dependent(w4_encode_kernel<false, T>, grid, dim3(256), 0, stream, x, ldx, ldm, to, each);
 }
 
 template <typename T>

@@ -157,20 +157,20 @@ template <> struct RowsAny<float> {
         }
     }
 };
-// Rows of two bf16 values each, high parts then low parts, whole blocks: 16 bits of a binary32 value.
-struct RowsSplit {
+// Rows of P bf16 parts, one after another, whose sum a value is; whole blocks.
+template <int P> struct RowsParts {
     using Elem = __nv_bfloat16;
     using Mma = __nv_bfloat16;
-    static constexpr int kPieces = 2;
-    struct Raw { uint4 w[2]; };
-    int cols;                                             // of each part
+    static constexpr int kPieces = P;
+    struct Raw { uint4 w[P]; };
+    int cols;                                             // of a part
     __device__ __forceinline__ void load(Raw& r, const __nv_bfloat16* row, int column, int offset, int) const {
-        r.w[0] = *reinterpret_cast<const uint4*>(row + column + offset);
-        r.w[1] = *reinterpret_cast<const uint4*>(row + cols + column + offset);
-    }
-    __device__ __forceinline__ void operand(const Raw& r, uint32_t (&b)[2][4]) const {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < P; ++i) r.w[i] = *reinterpret_cast<const uint4*>(row + i * cols + column + offset);
+    }
+    __device__ __forceinline__ void operand(const Raw& r, uint32_t (&b)[P][4]) const {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
             b[i][0] = r.w[i].x; b[i][1] = r.w[i].y; b[i][2] = r.w[i].z; b[i][3] = r.w[i].w;
         }
     }

@@ -22,7 +22,7 @@ cudaError_t w4_linear_of(const pwlq_w4& w, const void* x, int64_t tokens, int64_
                          cudaStream_t stream);
 cudaError_t launch_w4_linear(const pwlq_w4& w, const void* x, int dtype, int64_t tokens, int64_t ldx, void* y,
                              int64_t ldy, cudaStream_t stream);
-size_t w4_moe_workspace(int64_t tokens, int64_t top, int64_t hidden);
+size_t w4_moe_workspace(int64_t tokens, int64_t top, int64_t features, int64_t hidden);
 cudaError_t launch_w4_moe(const pwlq_w4_moe_args& a, cudaStream_t stream);
 
 }  // namespace pwlq

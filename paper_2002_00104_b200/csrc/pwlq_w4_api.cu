@@ -83,11 +83,11 @@ int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, i
     return from_cuda(pwlq::launch_w4_linear(*w, x, dtype, tokens, ldx, y, ldy, as_stream(stream)));
 }
 
-size_t pwlq_w4_moe_workspace_bytes(int64_t tokens, int64_t top, int64_t hidden) {
-    if (tokens < 0 || tokens > PWLQ_W4_MOE_MAX_TOKENS || top < 1 || top > PWLQ_W4_MOE_MAX_TOP || hidden < 1 ||
-        hidden > kMaxRows / 2)
+size_t pwlq_w4_moe_workspace_bytes(int64_t tokens, int64_t top, int64_t features, int64_t hidden) {
+    if (tokens < 0 || tokens > PWLQ_W4_MOE_MAX_TOKENS || top < 1 || top > PWLQ_W4_MOE_MAX_TOP || features < 1 ||
+        features > kMaxCols || hidden < 1 || hidden > kMaxCols)
         return 0;
-    const size_t bytes = pwlq::w4_moe_workspace(tokens, top, hidden);
+    const size_t bytes = pwlq::w4_moe_workspace(tokens, top, features, hidden);
     return bytes ? bytes : 256;
 }
 
@@ -108,7 +108,7 @@ int pwlq_w4_moe(const pwlq_w4_moe_args* args, void* stream) {
         bad_rows(a.router, a.router_dtype, a.ldrouter, up.cols) || misaligned(a.chosen, 4) || misaligned(a.weights, 4))
         return PWLQ_ERR_INVALID_ARG;
     if (!a.workspace || a.workspace_bytes < 0 ||
-        (size_t)a.workspace_bytes < pwlq_w4_moe_workspace_bytes(a.tokens, a.top, down.cols))
+        (size_t)a.workspace_bytes < pwlq_w4_moe_workspace_bytes(a.tokens, a.top, down.rows, down.cols))
         return PWLQ_ERR_WORKSPACE;
     if (misaligned(a.workspace, 256)) return PWLQ_ERR_INVALID_ARG;
     return from_cuda(pwlq::launch_w4_moe(a, as_stream(stream)));

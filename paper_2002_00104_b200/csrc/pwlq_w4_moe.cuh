@@ -27,6 +27,17 @@ struct Lists {
 // Returns how many experts are active.
 __device__ __forceinline__ int build_lists(const Lists& l, const Routing& r) {
     const int pairs = r.tokens * r.top, threads = blockDim.x;
+    if (r.tokens == 1) {                                  // every expert once, in the order of its choice
+        for (int i = threadIdx.x; i <= pairs; i += threads) {
+            l.first[i] = (uint16_t)i;
+            if (i < pairs) {
+                l.expert[i] = (uint16_t)r.chosen[i];
+                l.pair[i] = (uint16_t)i;
+            }
+        }
+        __syncthreads();
+        return pairs;
+    }
     for (int e = threadIdx.x; e < r.experts; e += threads) l.mask[e] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < pairs; i += threads) {
@@ -69,32 +80,37 @@ __device__ __forceinline__ int build_lists(const Lists& l, const Routing& r) {
     return *l.active;
 }
 
-// What lies between the two products, a row for each pair: binary32, or two bf16 parts (16 bits of each value:
-// with them the result is rounded once, as if there were nothing between; one 16-bit value would add as much
-// error again).  Rows are padded with zeros to whole blocks.
+// What lies between the two products, a row for each pair: bf16 parts, two of a 16-bit type (16 bits of each value:
+// with them the result is rounded once, as if there were nothing between; one 16-bit value would add as much error
+// again) or three of binary32.  Rows are padded with zeros to whole blocks.
 template <typename T> struct Hidden {
-    using Source = RowsSplit;
+    static constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
+    using Source = RowsParts<kParts>;
     using Elem = __nv_bfloat16;
-    static __host__ __device__ int64_t pitch(int64_t padded) { return 2 * padded; }
     static __device__ __forceinline__ void put(Elem* row, int64_t padded, int64_t i, float v) {
-        const __nv_bfloat16 high = __float2bfloat16_rn(v);
-        const float rest = v - __bfloat162float(high);
-        row[i] = high;
-        row[padded + i] = __float2bfloat16_rn(abs_bits(__bfloat162float(high)) < kInfBits ? rest : 0.0f);
+        if (kParts == 3) {
+            float p[3];
+            split3(v, p[0], p[1], p[2]);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) row[k * padded + i] = __float2bfloat16_rn(p[k]);
+        } else {
+            const __nv_bfloat16 high = __float2bfloat16_rn(v);
+            const float rest = v - __bfloat162float(high);
+            row[i] = high;
+            row[padded + i] = __float2bfloat16_rn(abs_bits(__bfloat162float(high)) < kInfBits ? rest : 0.0f);
+        }
     }
 };
-template <> struct Hidden<float> {
-    using Source = RowsAny<float>;
-    using Elem = float;
-    static __host__ __device__ int64_t pitch(int64_t padded) { return padded; }
-    static __device__ __forceinline__ void put(float* row, int64_t, int64_t i, float v) { row[i] = v; }
-};
+// The tokens: as they are given, or the copy that the first launch has made.
+template <typename T> struct Tokens { using Source = RowsWhole<T>; static constexpr int kParts = 1; };
+template <> struct Tokens<float> { using Source = RowsParts<3>; static constexpr int kParts = 3; };
 
 template <typename T> struct UpArgs {
     W4View w;                                             // [experts, 2 hidden, features], paired
     Routing r;
-    const T* x;
+    const typename Tokens<T>::Source::Elem* x;
     int64_t ldx;
+    int part;                                             // columns of a part of x
     typename Hidden<T>::Elem* h;
     int64_t padded;                                       // hidden in whole blocks
     int team_shift;                                       // log2 of the warps of a team
@@ -127,7 +143,7 @@ template <int NT, typename T> struct UpSteps {
     __device__ __forceinline__ UpTag tag() const { return {tile, first, count}; }
     __device__ __forceinline__ int column() const { return from * kBlockCols; }
     // columns past the last token repeat it; nobody reads their sums
-    __device__ __forceinline__ const T* row(int n) const {
+    __device__ __forceinline__ const typename Tokens<T>::Source::Elem* row(int n) const {
         const int c = min(8 * n + ((int)(threadIdx.x & 31) >> 2), count - 1);
         return a->x + (int64_t)(l->pair[first + c] / a->r.top) * a->ldx;
     }
@@ -135,7 +151,7 @@ template <int NT, typename T> struct UpSteps {
 
 // A team of warps takes 8 gate rows and the 8 up rows that belong to them, of one expert, and shares the columns;
 // teams go on from one such item to the next.
-template <int NT, int ENDS, typename T, class S>
+template <int NT, int ENDS, typename T>
 __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T> a) {
     constexpr int kPitch = 8 * NT + 1, kRing = kRingBytes<1, ENDS>;
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
@@ -143,6 +159,7 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
     const Lists l(reinterpret_cast<uint8_t*>(sums + kUpWarps * 16 * kPitch), a.r);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     await_previous();
+    allow_dependents();                                   // no CTA of this launch waits for a place
     const int active = build_lists(l, a.r);
     const int team = 1 << a.team_shift, teams = kUpWarps >> a.team_shift, mine = warp >> a.team_shift;
     const int part = warp & (team - 1), begin = (a.w.blocks * part) >> a.team_shift;
@@ -151,8 +168,8 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
         if (team == 1) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + mine), "r"(32 << a.team_shift) : "memory");
     };
-    S source;
-    source.cols = a.w.cols;
+    typename Tokens<T>::Source source;
+    source.cols = a.part;
     const UpSteps<NT, T> steps = {&l, &a, count, begin, (int)gridDim.x * teams, active * (int)a.w.tiles,
                                   ((int)blockIdx.x - (int)gridDim.x) * teams + mine, w4_block_bytes(ENDS)};
     w4_stream<1, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
@@ -171,7 +188,7 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
                 up += sums[(j * 16 + r + 8) * kPitch + c];
             }
             const int f = at.tile * 8 + r;
-            typename Hidden<T>::Elem* const to = a.h + pair * Hidden<T>::pitch(a.padded);
+            typename Hidden<T>::Elem* const to = a.h + pair * Hidden<T>::kParts * a.padded;
             Hidden<T>::put(to, a.padded, f,
                            f < hidden ? silu_of(gate * 256.0f) * (up * 256.0f) * a.r.weights[pair] : 0.0f);
             if (at.tile == a.w.tiles - 1)
@@ -221,7 +238,7 @@ template <int NT, typename T> struct DownSteps {
     __device__ __forceinline__ int column() const { return from * kBlockCols; }
     __device__ __forceinline__ const typename H::Elem* row(int n) const {
         const int c = min(8 * n + ((int)(threadIdx.x & 31) >> 2), count - 1);
-        return a->h + l->pair[first + c] * H::pitch(a->padded);
+        return a->h + l->pair[first + c] * H::kParts * a->padded;
     }
 };
 
@@ -272,7 +289,7 @@ cudaError_t with_ends(int ends, F f) {
     return ends == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
 }
 
-template <int NT, typename T, class S>
+template <int NT, typename T>
 cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
     const int64_t most = std::min<int64_t>(a.r.experts, (int64_t)a.r.tokens * a.r.top) * a.w.tiles;
     a.team_shift = 0;
@@ -281,7 +298,7 @@ cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
         const size_t smem = kUpWarps * (kRingBytes<1, kEnds> + 16 * (8 * NT + 1) * 4) + Lists::bytes(a.r);
-        return launch_w4(moe_up_kernel<NT, kEnds, T, S>, a, dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
+        return launch_w4(moe_up_kernel<NT, kEnds, T>, a, dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
                          smem, stream);
     });
 }
@@ -296,18 +313,14 @@ cudaError_t down_launch(const DownArgs<T>& a, cudaStream_t stream) {
 }
 
 template <int NT, typename T>
-cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, void* hidden, cudaStream_t stream) {
-    const int64_t padded = w4_padded(a.down->cols);
+cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* copy, void* hidden, cudaStream_t stream) {
+    const int64_t padded = w4_padded(a.down->cols), part = w4_padded(a.up->cols);
     auto* const h = static_cast<typename Hidden<T>::Elem*>(hidden);
-    const UpArgs<T> up = {w4_view(*a.up, !std::is_same<T, __half>::value), r, static_cast<const T*>(a.x), a.ldx, h, padded, 0};
-    cudaError_t err;
-    if constexpr (sizeof(T) == 2) {
-        err = a.up->cols % kBlockCols == 0 && rows_aligned(a.x, a.ldx, sizeof(T))
-                  ? up_launch<NT, T, RowsWhole<T>>(up, stream)
-                  : up_launch<NT, T, RowsAny<T>>(up, stream);
-    } else {
-        err = up_launch<NT, T, RowsAny<T>>(up, stream);
-    }
+    const bool copied = moe_copies(a);
+    const UpArgs<T> up = {w4_view(*a.up, !std::is_same<T, __half>::value), r,
+                          static_cast<const typename Tokens<T>::Source::Elem*>(copied ? copy : a.x),
+                          copied ? part * Tokens<T>::kParts : a.ldx, (int)part, h, padded, 0};
+    const cudaError_t err = up_launch<NT, T>(up, stream);
     if (err != cudaSuccess) return err;
     const DownArgs<T> down = {w4_view(*a.down, true), r, h, padded, static_cast<T*>(a.y), a.ldy};
     return down_launch<NT, T>(down, stream);
@@ -316,8 +329,11 @@ cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, void* hidden, 
 }  // namespace
 
 template <typename T>
-cudaError_t launch_moe_products(const pwlq_w4_moe_args& a, const Routing& r, void* hidden, cudaStream_t stream) {
-    return a.tokens <= 8 ? products<1, T>(a, r, hidden, stream) : products<2, T>(a, r, hidden, stream);
+cudaError_t launch_moe_products(const pwlq_w4_moe_args& a, const Routing& r, const void* copy, void* hidden,
+                                cudaStream_t stream) {
+    // tokens are taken eight or sixteen at a time: an expert's are, on average, few
+    return a.tokens <= 8 || a.tokens * a.top <= 6 * r.experts ? products<1, T>(a, r, copy, hidden, stream)
+                                                              : products<2, T>(a, r, copy, hidden, stream);
 }
 
 }  // namespace pwlq

@@ -108,7 +108,7 @@ _SIGNATURES = {
     "pwlq_w4_encode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
     "pwlq_w4_decode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
     "pwlq_w4_linear": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P, _I64, _P]),
-    "pwlq_w4_moe_workspace_bytes": (_SZ, [_I64, _I64, _I64]),
+    "pwlq_w4_moe_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64]),
     "pwlq_w4_moe": (_INT, [_STRUCT, _P]),
     "pwlq_device_status": (_INT, []),
     "pwlq_status_string": (ctypes.c_char_p, [_INT]),
@@ -1160,8 +1160,8 @@ def w4_linear(x, packed: W4, out=None, stream=None):
     return _calls().w4_linear(x, packed._fields, packed._memory, out)
 
 
-def w4_moe_workspace_bytes(tokens: int, top: int, hidden: int) -> int:
-    return int(load_library().pwlq_w4_moe_workspace_bytes(tokens, top, hidden))
+def w4_moe_workspace_bytes(tokens: int, top: int, features: int, hidden: int) -> int:
+    return int(load_library().pwlq_w4_moe_workspace_bytes(tokens, top, features, hidden))
 
 
 def w4_moe(x, router, up: W4, down: W4, top: int, normalize=True, want_routing=False, out=None, workspace=None,

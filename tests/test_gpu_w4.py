@@ -26,12 +26,12 @@ def _same(got, want):
 @pytest.mark.parametrize("rows,cols,group,ratio,paired", [
     (1, 1, 32, 0.5, False), (2, 1, 64, 0.25, True), (16, 128, 128, 0.421875, False), (17, 129, 64, 0.4375, False),
     (5, 31, 256, 1.0, False), (33, 700, 256, 1 / 64, False), (18, 333, 32, 0.5, True), (34, 257, 64, 0.375, True),
-    (64, 385, 128, 63 / 64, True), (100, 96, 32, 0.3125, False)])
+    (64, 385, 128, 63 / 64, True), (100, 96, 32, 0.3125, False), (40, 512, 32, 1.0, False)])
 def test_bytes_and_values(dtype, rows, cols, group, ratio, paired):
     from paper_2002_00104_b200 import pwlq
     w = _w(rows * 1009 + cols, rows, cols, dtype=TYPES[dtype])
     packed = pwlq.w4_encode(w.cuda(), group=group, ratio=ratio, paired=paired)
-    s, c, _ = U.codes(w.float(), group, ratio)
+    s, c = U.codes(w.float(), group, ratio)
     assert np.array_equal(packed.memory.cpu().numpy(), U.layout(s, c, group, paired))
     for out in ("fp32", dtype):
         _same(pwlq.w4_decode(packed, dtype=TYPES[out]), U.values(s, c, group, ratio))
@@ -50,6 +50,7 @@ def test_values_on_the_bounds_between_levels():
         w[:, 0] = 192 * s
         w = torch.from_numpy(w)
         packed = pwlq.w4_encode(w.cuda(), group=64, ratio=b / 64)
+        assert np.array_equal(packed.memory.cpu().numpy(), U.layout(*U.codes(w, 64, b / 64), 64, False))
         _same(pwlq.w4_decode(packed), U.held(w, 64, b / 64))
 
 

@@ -158,7 +158,7 @@ def test_workspaces_and_refusals():
     from paper_2002_00104_b200 import pwlq
     s, _, _ = _layer(71, 8, 128, 64, torch.bfloat16)
     x = _t(72, 4, 128, dtype=torch.bfloat16).cuda()
-    need = pwlq.w4_moe_workspace_bytes(4, 2, 64)
+    need = pwlq.w4_moe_workspace_bytes(4, 2, 128, 64)
     workspace = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
     want = _run(s, x, 2)
     assert torch.equal(_run(s, x, 2, workspace=workspace), want)

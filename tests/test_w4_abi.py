@@ -49,8 +49,9 @@ def test_sizes(pwlq):
                 (1, 16, (1 << 20) + 1, 128, 0), (65535, 1 << 20, 1 << 20, 128, 0), (1, 16, 128, 2 ** 32 + 64, 0)):
         assert lib.pwlq_w4_bytes(*bad) == 0, bad
     assert pwlq.w4_bytes((3, 17, 129), 64) == 3 * 2 * 2 * (1024 + 64)
-    assert lib.pwlq_w4_moe_workspace_bytes(64, 32, 1000) >= 64 * 32 * (1024 * 4 + 8)
-    for bad in ((65, 2, 100), (1, 33, 100), (1, 0, 100), (-1, 2, 100), (1, 2, 0)):
+    assert lib.pwlq_w4_moe_workspace_bytes(64, 32, 500, 1000) >= 64 * 32 * (1024 * 6 + 8) + 64 * 512 * 6
+    for bad in ((65, 2, 100, 100), (1, 33, 100, 100), (1, 0, 100, 100), (-1, 2, 100, 100), (1, 2, 0, 100), (1, 2, 100, 0),
+                (1, 2, 100, 2 ** 32)):
         assert lib.pwlq_w4_moe_workspace_bytes(*bad) == 0, bad
 
 
@@ -91,7 +92,7 @@ def test_linear(pwlq):
 def test_moe(pwlq):
     import ctypes
     lib = pwlq.load_library()
-    need = lib.pwlq_w4_moe_workspace_bytes(4, 2, 24)
+    need = lib.pwlq_w4_moe_workspace_bytes(4, 2, 100, 24)
     keep = []
 
     def block(**kw):

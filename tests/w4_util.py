@@ -25,21 +25,21 @@ def scales(w, group):
 
 
 def codes(w, group, ratio):
-    """(scales, codes) of w [n, k]: sign << 3 | region << 2 | level; decided in binary64."""
+    """(scales, codes) of w [n, k]: sign << 3 | region << 2 | level, 0 where the value is held as 0; decided in
+    binary64."""
     n, k = w.shape
     s = scales(w, group)
     b = ratio * 64
     each = s.double().repeat_interleave(group, 1)[:, :k]
-    a = w.double().abs() / torch.where(each > 0, each, 1.0)      # exact enough: bounds are halves of whole numbers
     tail = w.double().abs() > 3 * b * each
     step = torch.where(tail, 64 - b, b)
     z = torch.where(tail, 3 * b, 0.0)
-    # the bounds themselves, not a quotient, decide
     x = w.double().abs()
     q = ((x > (z + 0.5 * step) * each).long() + (x >= (z + 1.5 * step) * each).long()
          + (x > (z + 2.5 * step) * each).long())
-    c = (w < 0).long() * 8 + tail.long() * 4 + q
-    return s, torch.where(each > 0, c, 0), a
+    c = tail.long() * 4 + q
+    c = torch.where(c > 0, (w < 0).long() * 8 + c, 0)
+    return s, torch.where(each > 0, c, 0)
 
 
 def values(s, c, group, ratio):
@@ -54,7 +54,7 @@ def values(s, c, group, ratio):
 def held(w, group, ratio):
     """The values that w [n, k] or [e, n, k] is held as, binary64, on the CPU."""
     flat = w.cpu().flatten(0, -2)
-    s, c, _ = codes(flat, group, ratio)
+    s, c = codes(flat, group, ratio)
     return values(s, c, group, ratio).view(w.shape)
 
 
