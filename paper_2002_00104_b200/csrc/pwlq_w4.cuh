@@ -176,6 +176,9 @@ template <int P> struct RowsParts {
     }
 };
 
+// The warp's number as the same value in all lanes, so that branches on what follows from it need no convergence.
+__device__ __forceinline__ int warp_index() { return __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0); }
+
 // Sixteen bytes to shared memory where `yes`; they are there when the group that they belong to has been waited
 // for.
 __device__ __forceinline__ void copy16(uint32_t to, const uint8_t* from, bool yes) {

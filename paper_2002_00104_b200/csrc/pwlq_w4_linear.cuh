@@ -46,7 +46,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_linear_kernel(const LinearA
     constexpr int kCols = 8 * NT, kRing = kRingBytes<MT, ENDS>, kPitch = kCols + 1;
     static_assert(kRing >= 16 * MT * kPitch * 4 && kRing % 16 == 0, "sums are larger than a ring");
     extern __shared__ __align__(16) uint8_t shared[];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
     const int team = 1 << a.team_shift, teams = kWarps >> a.team_shift;
     const int64_t first = (int64_t)blockIdx.x * teams, mine = first + (warp >> a.team_shift);
     const int64_t token = (int64_t)blockIdx.y * kCols;

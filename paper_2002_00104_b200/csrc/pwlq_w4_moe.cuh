@@ -2,6 +2,8 @@
 // each, so that they are compiled side by side.
 #pragma once
 
+#include <cmath>
+
 #include "pwlq_w4_moe.h"
 
 namespace pwlq {
@@ -116,21 +118,31 @@ template <typename T> struct UpArgs {
     int team_shift;                                       // log2 of the warps of a team
 };
 
-// A warp's way through the items (tile of an expert) of its team, 8 NT of the expert's tokens at a time.
+// A warp's way through the items (tile of an expert) of its team, 8 NT of the expert's tokens at a time.  A team's items
+// are spread over all experts, some of which have more tokens than one pass takes.
 struct UpTag { int tile, first, count; };                 // the expert's pairs of this pass
 template <int NT, typename T> struct UpSteps {
     const Lists* l;
     const UpArgs<T>* a;
-    int n_blocks, from, step, items, item, bytes;
-    int tile = 0, expert = 0, first = 0, count = 0;       // count: of the expert's pairs from `first` on
+    int n_blocks, from, bytes;
+    int at, tile, experts;                                // of the next item: the expert's number, the tile
+    int step_at, step_tile;                               // from one item to the next
+    int expert = 0, first = 0, count = 0;                 // count: of the expert's pairs from `first` on
+    bool started = false;
     __device__ __forceinline__ bool next() {
         first += 8 * NT;
         count -= 8 * NT;
         if (count > 0) return true;
-        item += step;
-        if (item >= items) return false;
-        const int at = item / (int)a->w.tiles;
-        tile = item - at * (int)a->w.tiles;
+        if (started) {
+            at += step_at;
+            tile += step_tile;
+            if (tile >= (int)a->w.tiles) {
+                tile -= (int)a->w.tiles;
+                ++at;
+            }
+        }
+        started = true;
+        if (at >= experts) return false;
         expert = l->expert[at];
         first = l->first[at];
         count = l->first[at + 1] - first;
@@ -157,7 +169,7 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
     float* const sums = reinterpret_cast<float*>(shared + kUpWarps * kRing);
     const Lists l(reinterpret_cast<uint8_t*>(sums + kUpWarps * 16 * kPitch), a.r);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = warp_index(), lane = threadIdx.x & 31;
     await_previous();
     allow_dependents();                                   // no CTA of this launch waits for a place
     const int active = build_lists(l, a.r);
@@ -170,8 +182,9 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
     };
     typename Tokens<T>::Source source;
     source.cols = a.part;
-    const UpSteps<NT, T> steps = {&l, &a, count, begin, (int)gridDim.x * teams, active * (int)a.w.tiles,
-                                  ((int)blockIdx.x - (int)gridDim.x) * teams + mine, w4_block_bytes(ENDS)};
+    const int item = (int)blockIdx.x * teams + mine, step = (int)gridDim.x * teams, tiles = (int)a.w.tiles;
+    const UpSteps<NT, T> steps = {&l, &a, count, begin, w4_block_bytes(ENDS), item / tiles, item % tiles, active,
+                                  step / tiles, step % tiles};
     w4_stream<1, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
                            [&](const UpTag& at, const float (&acc)[1][NT][4]) {
 #pragma unroll
@@ -249,7 +262,7 @@ __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const Down
     using H = Hidden<T>;
     constexpr int kRing = kRingBytes<1, ENDS>;
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int pitch = a.r.tokens | 1;
     float* const sums = reinterpret_cast<float*>(shared + kDownWarps * kRing);
     float* const mine = sums + warp * 16 * pitch;
@@ -292,8 +305,13 @@ cudaError_t with_ends(int ends, F f) {
 template <int NT, typename T>
 cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
     const int64_t most = std::min<int64_t>(a.r.experts, (int64_t)a.r.tokens * a.r.top) * a.w.tiles;
-    a.team_shift = 0;
-    while (a.team_shift < 3 && most << a.team_shift < 24 * 148 && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
+    // Teams of two; larger ones where the items of as many experts as the tokens would choose at random leave
+    // multiprocessors empty.  4 tokens, 8 experts of 2 x 8192 x 4096: 72.5, 68.5, 73.4, 82.6 us with teams of 1, 2, 4, 8 (the
+    // last ones meet more often than they multiply); 5 tokens, 17 experts of 2 x 515 x 1287: 21.1, 14.2, 11.2, 12.4.
+    const double spared = std::pow(1.0 - (double)a.r.top / a.r.experts, a.r.tokens);
+    const double items = a.r.experts * (1.0 - spared) * (double)a.w.tiles;
+    a.team_shift = a.w.blocks >= 2;
+    while (a.team_shift < 3 && items * (1 << a.team_shift) < 12 * 148 && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
     const int64_t ctas = ((most << a.team_shift) + kUpWarps - 1) / kUpWarps;
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
