@@ -20,6 +20,9 @@ cudaError_t launch_w4_decode(const pwlq_w4& w, void* y, int dtype, int64_t ldy, 
 template <typename T>
 cudaError_t w4_linear_of(const pwlq_w4& w, const void* x, int64_t tokens, int64_t ldx, void* y, int64_t ldy,
                          cudaStream_t stream);
+template <typename T>
+cudaError_t w4_wide_of(const pwlq_w4& w, const void* x, int64_t tokens, int64_t ldx, void* y, int64_t ldy,
+                       cudaStream_t stream);
 cudaError_t launch_w4_linear(const pwlq_w4& w, const void* x, int dtype, int64_t tokens, int64_t ldx, void* y,
                              int64_t ldy, cudaStream_t stream);
 size_t w4_moe_workspace(int64_t tokens, int64_t top, int64_t features, int64_t hidden);

@@ -117,8 +117,7 @@ cudaError_t linear(const LinearArgs<T>& a, cudaStream_t stream) {
     if (a.tokens <= 8)
         return a.w.blocks >= 64 && a.w.tiles >= 256 ? launch<2, 1, ENDS, T, S>(a, stream)
                                                     : launch<1, 1, ENDS, T, S>(a, stream);
-    if (a.tokens <= 16) return launch<2, 2, ENDS, T, S>(a, stream);
-    return launch<1, 4, ENDS, T, S>(a, stream);
+    return launch<2, 2, ENDS, T, S>(a, stream);
 }
 
 template <typename T, class S>
@@ -132,6 +131,7 @@ cudaError_t linear(const LinearArgs<T>& a, cudaStream_t stream) {
 template <typename T>
 cudaError_t w4_linear_of(const pwlq_w4& w, const void* x, int64_t tokens, int64_t ldx, void* y, int64_t ldy,
                          cudaStream_t stream) {
+    if (tokens > 16) return w4_wide_of<T>(w, x, tokens, ldx, y, ldy, stream);
     const LinearArgs<T> a = {w4_view(w, !std::is_same<T, __half>::value), static_cast<const T*>(x), ldx, tokens,
                              static_cast<T*>(y), ldy};
     if constexpr (sizeof(T) == 2) {
