@@ -118,15 +118,15 @@ template <typename T> struct UpArgs {
     int team_shift;                                       // log2 of the warps of a team
 };
 
-// A warp's way through the items (tile of an expert) of its team, 8 NT of the expert's tokens at a time.  A team's items
+// A warp's way through the items (MT tiles of an expert) of its team, 8 NT of the expert's tokens at a time.  A team's items
 // are spread over all experts, some of which have more tokens than one pass takes.
 struct UpTag { int tile, first, count; };                 // the expert's pairs of this pass
-template <int NT, typename T> struct UpSteps {
+template <int MT, int NT, typename T> struct UpSteps {
     const Lists* l;
     const UpArgs<T>* a;
     int n_blocks, from, bytes;
     int at, tile, experts;                                // of the next item: the expert's number, the tile
-    int step_at, step_tile;                               // from one item to the next
+    int step_at, step_tile, units;                        // from one item to the next, items of an expert
     int expert = 0, first = 0, count = 0;                 // count: of the expert's pairs from `first` on
     bool started = false;
     __device__ __forceinline__ bool next() {
@@ -136,8 +136,8 @@ template <int NT, typename T> struct UpSteps {
         if (started) {
             at += step_at;
             tile += step_tile;
-            if (tile >= (int)a->w.tiles) {
-                tile -= (int)a->w.tiles;
+            if (tile >= units) {
+                tile -= units;
                 ++at;
             }
         }
@@ -149,8 +149,9 @@ template <int NT, typename T> struct UpSteps {
         return true;
     }
     __device__ __forceinline__ int blocks() const { return n_blocks; }
-    __device__ __forceinline__ const uint8_t* code(int) const {
-        return a->w.data + ((expert * a->w.tiles + tile) * a->w.blocks + from) * bytes;
+    // a tile past the last one repeats it; its sums go nowhere
+    __device__ __forceinline__ const uint8_t* code(int m) const {
+        return a->w.data + ((expert * a->w.tiles + min((int64_t)tile * MT + m, a->w.tiles - 1)) * a->w.blocks + from) * bytes;
     }
     __device__ __forceinline__ UpTag tag() const { return {tile, first, count}; }
     __device__ __forceinline__ int column() const { return from * kBlockCols; }
@@ -161,14 +162,14 @@ template <int NT, typename T> struct UpSteps {
     }
 };
 
-// A team of warps takes 8 gate rows and the 8 up rows that belong to them, of one expert, and shares the columns;
-// teams go on from one such item to the next.
-template <int NT, int ENDS, typename T>
+// A team of warps takes MT tiles, 8 gate rows and the 8 up rows that belong to them, of one expert, and shares the
+// columns; teams go on from one such item to the next.
+template <int MT, int NT, int ENDS, typename T>
 __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T> a) {
-    constexpr int kPitch = 8 * NT + 1, kRing = kRingBytes<1, ENDS>;
+    constexpr int kPitch = 8 * NT + 1, kRing = kRingBytes<MT, ENDS>;
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
     float* const sums = reinterpret_cast<float*>(shared + kUpWarps * kRing);
-    const Lists l(reinterpret_cast<uint8_t*>(sums + kUpWarps * 16 * kPitch), a.r);
+    const Lists l(reinterpret_cast<uint8_t*>(sums + kUpWarps * MT * 16 * kPitch), a.r);
     const int warp = warp_index(), lane = threadIdx.x & 31;
     await_previous();
     allow_dependents();                                   // no CTA of this launch waits for a place
@@ -182,29 +183,33 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
     };
     typename Tokens<T>::Source source;
     source.cols = a.part;
-    const int item = (int)blockIdx.x * teams + mine, step = (int)gridDim.x * teams, tiles = (int)a.w.tiles;
-    const UpSteps<NT, T> steps = {&l, &a, count, begin, w4_block_bytes(ENDS), item / tiles, item % tiles, active,
-                                  step / tiles, step % tiles};
-    w4_stream<1, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
-                           [&](const UpTag& at, const float (&acc)[1][NT][4]) {
+    const int item = (int)blockIdx.x * teams + mine, step = (int)gridDim.x * teams, units = (int)((a.w.tiles + MT - 1) / MT);
+    const UpSteps<MT, NT, T> steps = {&l, &a, count, begin, w4_block_bytes(ENDS), item / units, item % units, active,
+                                      step / units, step % units, units};
+    w4_stream<MT, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
+                            [&](const UpTag& at, const float (&acc)[MT][NT][4]) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                sums[(warp * 16 + (lane >> 2) + (i & 2) * 4) * kPitch + 8 * n + 2 * (lane & 3) + (i & 1)] = acc[0][n][i];
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    sums[((warp * MT + m) * 16 + (lane >> 2) + (i & 2) * 4) * kPitch + 8 * n + 2 * (lane & 3) + (i & 1)] =
+                        acc[m][n][i];
         meet();
-        for (int i = threadIdx.x & (32 * team - 1); i < 8 * min(at.count, 8 * NT); i += 32 * team) {
-            const int c = i >> 3, r = i & 7, pair = l.pair[at.first + c];
+        for (int i = threadIdx.x & (32 * team - 1); i < 8 * MT * min(at.count, 8 * NT); i += 32 * team) {
+            const int r = i % 8, m = i / 8 % MT, c = i / (8 * MT), pair = l.pair[at.first + c];
             float gate = 0.0f, up = 0.0f;
             for (int j = mine * team; j < (mine + 1) * team; ++j) {
-                gate += sums[(j * 16 + r) * kPitch + c];
-                up += sums[(j * 16 + r + 8) * kPitch + c];
+                gate += sums[((j * MT + m) * 16 + r) * kPitch + c];
+                up += sums[((j * MT + m) * 16 + r + 8) * kPitch + c];
             }
-            const int f = at.tile * 8 + r;
+            const int tile = at.tile * MT + m, f = tile * 8 + r;
+            if (tile >= a.w.tiles) continue;
             typename Hidden<T>::Elem* const to = a.h + pair * Hidden<T>::kParts * a.padded;
             Hidden<T>::put(to, a.padded, f,
                            f < hidden ? silu_of(gate * 256.0f) * (up * 256.0f) * a.r.weights[pair] : 0.0f);
-            if (at.tile == a.w.tiles - 1)
+            if (tile == a.w.tiles - 1)
                 for (int z = f + 8; z < a.padded; z += 8) Hidden<T>::put(to, a.padded, z, 0.0f);
         }
         meet();
@@ -222,11 +227,11 @@ template <typename T> struct DownArgs {
 
 // A warp's way through its part of a tile's blocks, which are those of all chosen experts one after another.
 struct DownTag { int first, count; };
-template <int NT, typename T> struct DownSteps {
+template <int MT, int NT, typename T> struct DownSteps {
     using H = Hidden<T>;
     const Lists* l;
     const DownArgs<T>* a;
-    int64_t tile;
+    int64_t tile;                                         // the first of MT
     int now, end, bytes;                                  // the block after this segment, the last one
     int expert = 0, first = 0, count = 0, from = 0, n_blocks = 0;
     __device__ __forceinline__ bool next() {
@@ -244,8 +249,9 @@ template <int NT, typename T> struct DownSteps {
         return true;
     }
     __device__ __forceinline__ int blocks() const { return n_blocks; }
-    __device__ __forceinline__ const uint8_t* code(int) const {
-        return a->w.data + ((expert * a->w.tiles + tile) * a->w.blocks + from) * bytes;
+    // a tile past the last one repeats it; its sums go nowhere
+    __device__ __forceinline__ const uint8_t* code(int m) const {
+        return a->w.data + ((expert * a->w.tiles + min(tile + m, a->w.tiles - 1)) * a->w.blocks + from) * bytes;
     }
     __device__ __forceinline__ DownTag tag() const { return {first, count}; }
     __device__ __forceinline__ int column() const { return from * kBlockCols; }
@@ -255,43 +261,49 @@ template <int NT, typename T> struct DownSteps {
     }
 };
 
-// A CTA per 16 features: the blocks of all chosen experts' rows are one list that the warps share; a warp adds what
-// an expert gives to its own sums, [16][tokens], and these are added in a fixed order at the end.
-template <int NT, int ENDS, typename T>
+// A CTA per MT tiles of 16 features: the blocks of all chosen experts' rows are one list that the warps share; a warp
+// adds what an expert gives to its own sums, [16 MT][tokens], and these are added in a fixed order at the end.
+template <int MT, int NT, int ENDS, typename T>
 __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const DownArgs<T> a) {
     using H = Hidden<T>;
-    constexpr int kRing = kRingBytes<1, ENDS>;
+    constexpr int kRing = kRingBytes<MT, ENDS>, kRows = 16 * MT;
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
     const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int pitch = a.r.tokens | 1;
     float* const sums = reinterpret_cast<float*>(shared + kDownWarps * kRing);
-    float* const mine = sums + warp * 16 * pitch;
-    const Lists l(reinterpret_cast<uint8_t*>(sums + kDownWarps * 16 * pitch), a.r);
-    for (int i = lane; i < 16 * pitch; i += 32) mine[i] = 0.0f;
+    float* const mine = sums + warp * kRows * pitch;
+    const Lists l(reinterpret_cast<uint8_t*>(sums + kDownWarps * kRows * pitch), a.r);
+    for (int i = lane; i < kRows * pitch; i += 32) mine[i] = 0.0f;
     await_previous();
     const int total = build_lists(l, a.r) * a.w.blocks;
     typename H::Source source;
     source.cols = (int)a.padded;
-    const DownSteps<NT, T> steps = {&l, &a, (int64_t)blockIdx.x, (int)((int64_t)total * warp / kDownWarps),
-                                    (int)((int64_t)total * (warp + 1) / kDownWarps), w4_block_bytes(ENDS)};
-    w4_stream<1, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
-                           [&](const DownTag& at, const float (&acc)[1][NT][4]) {
+    const DownSteps<MT, NT, T> steps = {&l, &a, (int64_t)blockIdx.x * MT, (int)((int64_t)total * warp / kDownWarps),
+                                        (int)((int64_t)total * (warp + 1) / kDownWarps), w4_block_bytes(ENDS)};
+    w4_stream<MT, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
+                            [&](const DownTag& at, const float (&acc)[MT][NT][4]) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = 8 * n + 2 * q + (i & 1);
-                if (c < at.count) mine[(g + (i & 2) * 4) * pitch + l.pair[at.first + c] / a.r.top] += acc[0][n][i];
+            for (int i = 0; i < 2; ++i) {
+                const int c = 8 * n + 2 * q + i;
+                if (c >= at.count) continue;
+                float* const to = mine + g * pitch + l.pair[at.first + c] / a.r.top;
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    to[16 * m * pitch] += acc[m][n][i];
+                    to[(16 * m + 8) * pitch] += acc[m][n][i + 2];
+                }
             }
         __syncwarp();
     });
     __syncthreads();
-    for (int i = threadIdx.x; i < 16 * a.r.tokens; i += kDownWarps * 32) {
-        const int r = i & 15, t = i >> 4;
+    for (int i = threadIdx.x; i < kRows * a.r.tokens; i += kDownWarps * 32) {
+        const int r = i % kRows, t = i / kRows;
         float sum = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kDownWarps; ++j) sum += sums[(j * 16 + r) * pitch + t];
-        const int64_t d = (int64_t)blockIdx.x * 16 + r;
+        for (int j = 0; j < kDownWarps; ++j) sum += sums[(j * kRows + r) * pitch + t];
+        const int64_t d = (int64_t)blockIdx.x * kRows + r;
         if (d < a.w.rows) a.y[t * a.ldy + d] = from_f32<T>(sum * 256.0f);
     }
 }
@@ -302,33 +314,38 @@ cudaError_t with_ends(int ends, F f) {
     return ends == 2 ? f(std::integral_constant<int, 2>()) : f(std::integral_constant<int, 1>());
 }
 
-template <int NT, typename T>
+template <int MT, int NT, typename T>
 cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
-    const int64_t most = std::min<int64_t>(a.r.experts, (int64_t)a.r.tokens * a.r.top) * a.w.tiles;
+    const int64_t units = (a.w.tiles + MT - 1) / MT, most = std::min<int64_t>(a.r.experts, (int64_t)a.r.tokens * a.r.top) * units;
     // Teams of two; larger ones where the items of as many experts as the tokens would choose at random leave
-    // multiprocessors empty.  4 tokens, 8 experts of 2 x 8192 x 4096: 72.5, 68.5, 73.4, 82.6 us with teams of 1, 2, 4, 8 (the
-    // last ones meet more often than they multiply); 5 tokens, 17 experts of 2 x 515 x 1287: 21.1, 14.2, 11.2, 12.4.
+    // multiprocessors empty.  4 tokens, 8 experts of 2 x 8192 x 4096, single tiles: 72.5, 68.5, 73.4, 82.6 us with teams of
+    // 1, 2, 4, 8 (the last ones meet more often than they multiply); 5 tokens, 17 experts of 2 x 515 x 1287: 21.1, 14.2, 11.2,
+    // 12.4.
     const double spared = std::pow(1.0 - (double)a.r.top / a.r.experts, a.r.tokens);
-    const double items = a.r.experts * (1.0 - spared) * (double)a.w.tiles;
+    const double items = a.r.experts * (1.0 - spared) * (double)units;
     a.team_shift = a.w.blocks >= 2;
     while (a.team_shift < 3 && items * (1 << a.team_shift) < 12 * 148 && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
     const int64_t ctas = ((most << a.team_shift) + kUpWarps - 1) / kUpWarps;
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
-        const size_t smem = kUpWarps * (kRingBytes<1, kEnds> + 16 * (8 * NT + 1) * 4) + Lists::bytes(a.r);
-        return launch_w4(moe_up_kernel<NT, kEnds, T>, a, dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
+        const size_t smem = kUpWarps * (kRingBytes<MT, kEnds> + MT * 16 * (8 * NT + 1) * 4) + Lists::bytes(a.r);
+        return launch_w4(moe_up_kernel<MT, NT, kEnds, T>, a, dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
                          smem, stream);
     });
 }
 
-template <int NT, typename T>
+template <int MT, int NT, typename T>
 cudaError_t down_launch(const DownArgs<T>& a, cudaStream_t stream) {
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
-        const size_t smem = kDownWarps * (kRingBytes<1, kEnds> + 16 * (a.r.tokens | 1) * 4) + Lists::bytes(a.r);
-        return launch_w4(moe_down_kernel<NT, kEnds, T>, a, dim3((unsigned)a.w.tiles), kDownWarps * 32, smem, stream);
+        const size_t smem = kDownWarps * (kRingBytes<MT, kEnds> + MT * 16 * (a.r.tokens | 1) * 4) + Lists::bytes(a.r);
+        return launch_w4(moe_down_kernel<MT, NT, kEnds, T>, a, dim3((unsigned)((a.w.tiles + MT - 1) / MT)), kDownWarps * 32, smem,
+                         stream);
     });
 }
+
+// How much of a last round of single CTAs to a multiprocessor is used.
+inline double filled(int64_t ctas) { return (double)ctas / (double)(148 * ((ctas + 147) / 148)); }
 
 template <int NT, typename T>
 cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* copy, void* hidden, cudaStream_t stream) {
@@ -338,10 +355,20 @@ cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* co
     const UpArgs<T> up = {w4_view(*a.up, !std::is_same<T, __half>::value), r,
                           static_cast<const typename Tokens<T>::Source::Elem*>(copied ? copy : a.x),
                           copied ? part * Tokens<T>::kParts : a.ldx, (int)part, h, padded, 0};
-    const cudaError_t err = up_launch<NT, T>(up, stream);
+    // two tiles at a time, eight tokens or fewer: as in the linear layer, where rows are long and many
+    cudaError_t err;
+    if constexpr (NT == 1) {
+        err = up.w.blocks >= 32 && up.w.tiles >= 256 ? up_launch<2, NT, T>(up, stream) : up_launch<1, NT, T>(up, stream);
+    } else {
+        err = up_launch<1, NT, T>(up, stream);
+    }
     if (err != cudaSuccess) return err;
     const DownArgs<T> down = {w4_view(*a.down, true), r, h, padded, static_cast<T*>(a.y), a.ldy};
-    return down_launch<NT, T>(down, stream);
+    if constexpr (NT == 1) {
+        // the warps' sums of many tokens leave no room for it
+        if (a.tokens <= 8 && filled((down.w.tiles + 1) / 2) >= filled(down.w.tiles)) return down_launch<2, NT, T>(down, stream);
+    }
+    return down_launch<1, NT, T>(down, stream);
 }
 
 }  // namespace

@@ -47,7 +47,8 @@ def _check(s, up, down, x, top, normalize):
 @pytest.mark.parametrize("tokens,features,hidden,experts,top,group,normalize", [
     (1, 64, 64, 4, 2, 32, True), (1, 256, 128, 64, 8, 128, True), (1, 1, 1, 1, 1, 64, False), (2, 300, 70, 3, 3, 64, False),
     (5, 129, 515, 17, 3, 32, False), (8, 512, 96, 8, 2, 256, True), (9, 130, 40, 5, 4, 64, True), (16, 384, 200, 100, 32, 64, False),
-    (33, 96, 129, 2, 1, 128, True), (64, 256, 64, 32, 4, 64, True), (64, 72, 24, 1024, 5, 32, True)])
+    (33, 96, 129, 2, 1, 128, True), (64, 256, 64, 32, 4, 64, True), (64, 72, 24, 1024, 5, 32, True),
+    (40, 4096, 24, 48, 4, 64, True), (3, 4100, 2056, 2, 1, 128, True), (8, 4096, 2050, 2, 2, 32, False)])
 def test_layers(dtype, tokens, features, hidden, experts, top, group, normalize):
     dt = TYPES[dtype]
     s, up, down = _layer(tokens * 31 + features, experts, features, hidden, dt, group)
