@@ -585,9 +585,13 @@ int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ld
 /* y[t, n] = sum over k of x[t, k] w[n, k], for a paired matrix y[t, n] = silu(gate) * up of the sums with gate row
  * n and up row n, [tokens, rows / 2].  matrices = 1.  x [tokens, cols] and y of type dtype; made for few tokens (any
  * number is taken; from some hundreds on decoding once and a dense product are faster).  Products are exact, the
- * sums binary32 in a fixed order (bit-reproducible), y is rounded once.  tokens may be 0.  y must not overlap x. */
+ * sums binary32 in a fixed order (bit-reproducible), y is rounded once.  tokens may be 0.  y must not overlap x.
+ *   workspace   pwlq_w4_linear_workspace_bytes(...) bytes, 256-byte aligned: for a large matrix, a copy of tokens
+ *               that are binary32 (in three bf16 parts whose sum they are), or whose rows do not start on 16-byte
+ *               boundaries (x_aligned) or are not whole eights; 0 bytes (workspace may be NULL) otherwise */
+size_t pwlq_w4_linear_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols, int dtype, int x_aligned);
 int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, int64_t ldx, void* y,
-                   int64_t ldy, void* stream);
+                   int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 
 /* A mixture-of-experts layer, y = sum over the chosen experts e of weight_e * D_e (silu(G_e x) * U_e x), for up to
  * PWLQ_W4_MOE_MAX_TOKENS tokens:

@@ -27,6 +27,7 @@ struct Library {
     decltype(&pwlq_w4_bytes) w4_bytes;
     decltype(&pwlq_w4_encode) w4_encode;
     decltype(&pwlq_w4_decode) w4_decode;
+    decltype(&pwlq_w4_linear_workspace_bytes) w4_linear_bytes;
     decltype(&pwlq_w4_linear) w4_linear;
     decltype(&pwlq_w4_moe_workspace_bytes) moe_bytes;
     decltype(&pwlq_w4_moe) moe;
@@ -495,19 +496,28 @@ void no_gradient(const at::Tensor& t, const char* what) {
                       " requires a gradient, and this call has no backward pass: call it under torch.no_grad()");
 }
 
-// (x, fields, memory, out or None) -> y
+// (x, fields, memory, out or None, workspace or None) -> y
 PyObject* w4_linear(Args a) {
     const at::Tensor x = a.tensor("x");
     const int device = home(x, "x");
     two_dimensions(x, "x");
     no_gradient(x, "x");
     const Packed p = packed(a, device);
-    at::Tensor y = a.maybe("out");
+    at::Tensor y = a.maybe("out"), workspace = a.maybe("workspace");
     const int64_t tokens = x.size(0), outputs = p.w.paired ? p.w.rows / 2 : p.w.rows;
     const Matrix mx = matrix(x, "x", tokens, p.w.cols, x.scalar_type(), device);
     if (!y.defined()) y = at::empty({tokens, outputs}, x.options());
     const Matrix my = matrix(y, "out", tokens, outputs, x.scalar_type(), device);
-    check(lib.w4_linear(&p.w, mx.p, dtype_code(x.scalar_type()), tokens, mx.ld, my.p, my.ld, stream_of(device)),
+    const int type = dtype_code(x.scalar_type());
+    const int64_t size = type == PWLQ_F32 ? 4 : 2;
+    const int64_t need = (int64_t)lib.w4_linear_bytes(tokens, p.w.rows, p.w.cols, type,
+                                                      (((uintptr_t)mx.p | (uintptr_t)(mx.ld * size)) & 15) == 0);
+    if (need && !workspace.defined()) workspace = bytes(need, x);
+    TORCH_CHECK_VALUE(!workspace.defined() || (workspace.scalar_type() == at::kByte && workspace.is_contiguous() &&
+                                               workspace.is_cuda() && workspace.get_device() == device),
+                      "workspace must be contiguous uint8 on cuda:", device);
+    check(lib.w4_linear(&p.w, mx.p, type, tokens, mx.ld, my.p, my.ld, workspace.defined() ? workspace.data_ptr() : nullptr,
+                        workspace.defined() ? (size_t)workspace.numel() : 0, stream_of(device)),
           "pwlq_w4_linear");
     return wrap(y);
 }
@@ -613,7 +623,7 @@ PyMethodDef methods[] = {{"init", init, METH_VARARGS, nullptr},
                          PWLQ_CALL(weight_grad, 13),
                          PWLQ_CALL(w4_encode, 3),
                          PWLQ_CALL(w4_decode, 5),
-                         PWLQ_CALL(w4_linear, 4),
+                         PWLQ_CALL(w4_linear, 5),
                          PWLQ_CALL(w4_moe, 11),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pwlq_calls", nullptr, -1, methods};

@@ -205,6 +205,31 @@ __global__ void __launch_bounds__(256) w4_decode_kernel(const W4View v, W4Write 
     }
 }
 
+// Rows of activations for the products: whole blocks of columns, zeros behind the last one; binary32 values in three
+// bf16 parts, one after another.  Made once, where every tile of the weights would make it for itself.
+template <typename T>
+__global__ void __launch_bounds__(128) w4_copy_kernel(const T* __restrict__ x, int64_t ldx, int64_t cols, void* __restrict__ copy,
+                                                      int64_t padded) {
+    const int64_t col = ((int64_t)blockIdx.x * 128 + threadIdx.x) * 8, token = blockIdx.y;
+    allow_dependents();                                   // few CTAs: the next launch may take its places
+    await_previous();
+    if (col >= padded) return;
+    Raw8<T> raw;
+    load8<false>(raw, x + token * ldx + col, (int)max((int64_t)-8, min(cols - col, (int64_t)64)), (int)min(col, (int64_t)64));
+    if constexpr (sizeof(T) == 4) {
+        float v[8];
+        uint32_t b[3][4];
+        raw.get(v);
+        parts3(v, b);
+#pragma unroll
+        for (int p = 0; p < 3; ++p)
+            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(copy) + (token * 3 + p) * padded + col) =
+                make_uint4(b[p][0], b[p][1], b[p][2], b[p][3]);
+    } else {
+        raw.store(static_cast<T*>(copy) + token * padded + col);
+    }
+}
+
 W4Write writer(const pwlq_w4& w) {
     const bool paired = w.paired != 0;
     return {static_cast<uint8_t*>(w.data), w4_tiles(w.rows, paired), w4_blocks(w.cols), w.rows, w.cols,
@@ -247,11 +272,29 @@ cudaError_t launch_w4_decode(const pwlq_w4& w, void* y, int dtype, int64_t ldy, 
     return decode(w, static_cast<__half*>(y), ldy, ldm, stream);
 }
 
+cudaError_t launch_w4_copy(const void* x, int dtype, int64_t tokens, int64_t cols, int64_t ldx, void* copy, cudaStream_t stream) {
+    const int64_t padded = w4_padded(cols);
+    const dim3 grid((unsigned)((padded / 8 + 127) / 128), (unsigned)tokens), threads(128);
+    if (dtype == kF32)
+        return launch_dependent(w4_copy_kernel<float>, grid, threads, 0, stream, static_cast<const float*>(x), ldx, cols, copy, padded);
+    if (dtype == kBf16)
+        return launch_dependent(w4_copy_kernel<__nv_bfloat16>, grid, threads, 0, stream, static_cast<const __nv_bfloat16*>(x),
+                                ldx, cols, copy, padded);
+    return launch_dependent(w4_copy_kernel<__half>, grid, threads, 0, stream, static_cast<const __half*>(x), ldx, cols, copy, padded);
+}
+
 cudaError_t launch_w4_linear(const pwlq_w4& w, const void* x, int dtype, int64_t tokens, int64_t ldx, void* y,
-                             int64_t ldy, cudaStream_t stream) {
-    if (dtype == kF32) return w4_linear_of<float>(w, x, tokens, ldx, y, ldy, stream);
-    if (dtype == kBf16) return w4_linear_of<__nv_bfloat16>(w, x, tokens, ldx, y, ldy, stream);
-    return w4_linear_of<__half>(w, x, tokens, ldx, y, ldy, stream);
+                             int64_t ldy, void* workspace, cudaStream_t stream) {
+    const bool copied = w4_copies(w.rows, w.cols, dtype, rows_aligned(x, ldx, type_size(dtype)));
+    if (copied) {
+        const cudaError_t err = launch_w4_copy(x, dtype, tokens, w.cols, ldx, workspace, stream);
+        if (err != cudaSuccess) return err;
+        x = workspace;
+        ldx = w4_padded(w.cols) * (dtype == kF32 ? 3 : 1);
+    }
+    if (dtype == kF32) return w4_linear_of<float>(w, x, copied, tokens, ldx, y, ldy, stream);
+    if (dtype == kBf16) return w4_linear_of<__nv_bfloat16>(w, x, copied, tokens, ldx, y, ldy, stream);
+    return w4_linear_of<__half>(w, x, copied, tokens, ldx, y, ldy, stream);
 }
 
 }  // namespace pwlq

@@ -102,7 +102,7 @@ __device__ __forceinline__ uint32_t top16(float lo, float hi) {
     return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
 
-// Activations as operands: eight consecutive values of a row, from column + offset + within on (`row` points `within`
+// Activations as operands, columns behind the last one as 0: eight consecutive values of a row, from column + offset + within on (`row` points `within`
 // values into the row), are kPieces x 4 registers.
 // 16-bit rows on 16-byte boundaries, whole blocks.
 template <typename T> struct RowsWhole {
@@ -118,6 +118,33 @@ template <typename T> struct RowsWhole {
         b[0][0] = r.w.x; b[0][1] = r.w.y; b[0][2] = r.w.z; b[0][3] = r.w.w;
     }
 };
+// 16-bit rows on 16-byte boundaries, of whole eights.
+template <typename T> struct RowsEights {
+    using Elem = T;
+    using Mma = T;
+    static constexpr int kPieces = 1;
+    struct Raw { uint4 w; };
+    int cols;
+    __device__ __forceinline__ void load(Raw& r, const T* row, int column, int offset, int within) const {
+        r.w = make_uint4(0u, 0u, 0u, 0u);
+        if (column + offset + within < cols) r.w = *reinterpret_cast<const uint4*>(row + column + offset);
+    }
+    __device__ __forceinline__ void operand(const Raw& r, uint32_t (&b)[1][4]) const {
+        b[0][0] = r.w.x; b[0][1] = r.w.y; b[0][2] = r.w.z; b[0][3] = r.w.w;
+    }
+};
+// Eight binary32 values in three parts.
+__device__ __forceinline__ void parts3(const float (&v)[8], uint32_t (&b)[3][4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a0, b0, c0, a1, b1, c1;
+        split3(v[2 * i], a0, b0, c0);
+        split3(v[2 * i + 1], a1, b1, c1);
+        b[0][i] = pack16(a0, a1, __nv_bfloat16());
+        b[1][i] = top16(b0, b1);
+        b[2][i] = pack16(c0, c1, __nv_bfloat16());
+    }
+}
 // Rows that lie anywhere, of any length and type.
 template <typename T> struct RowsAny {
     using Elem = T;
@@ -146,15 +173,7 @@ template <> struct RowsAny<float> {
     __device__ __forceinline__ void operand(const Raw& r, uint32_t (&b)[3][4]) const {
         float v[8];
         r.get(v);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float a0, b0, c0, a1, b1, c1;
-            split3(v[2 * i], a0, b0, c0);
-            split3(v[2 * i + 1], a1, b1, c1);
-            b[0][i] = pack16(a0, a1, __nv_bfloat16());
-            b[1][i] = top16(b0, b1);
-            b[2][i] = pack16(c0, c1, __nv_bfloat16());
-        }
+        parts3(v, b);
     }
 };
 // Rows of P bf16 parts, one after another, whose sum a value is; whole blocks.

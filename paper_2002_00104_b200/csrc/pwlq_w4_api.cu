@@ -70,8 +70,15 @@ int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ld
     return from_cuda(pwlq::launch_w4_decode(*w, y, dtype, ldy, ldm, as_stream(stream)));
 }
 
+size_t pwlq_w4_linear_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols, int dtype, int x_aligned) {
+    if (tokens < 1 || check_size(1, rows, cols, 0) || !is_dtype(dtype) ||
+        !pwlq::w4_copies(rows, cols, dtype, x_aligned != 0) || tokens > kMaxTokens)
+        return 0;
+    return pwlq::w4_copy_bytes(tokens, cols, dtype);
+}
+
 int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, int64_t ldx, void* y,
-                   int64_t ldy, void* stream) {
+                   int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
     if (int rc = check_w4(w)) return rc;
     if (w->matrices != 1 || !is_dtype(dtype) || tokens < 0) return PWLQ_ERR_INVALID_ARG;
     if (tokens > kMaxTokens) return PWLQ_ERR_UNSUPPORTED;
@@ -80,7 +87,11 @@ int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, i
     if (bad_rows(x, dtype, ldx, w->cols) || bad_rows(y, dtype, ldy, outputs) ||
         overlap(x, ldx, w->cols, y, ldy, outputs, tokens, pwlq::type_size(dtype)))
         return PWLQ_ERR_INVALID_ARG;
-    return from_cuda(pwlq::launch_w4_linear(*w, x, dtype, tokens, ldx, y, ldy, as_stream(stream)));
+    const size_t need = pwlq_w4_linear_workspace_bytes(tokens, w->rows, w->cols, dtype,
+                                                       pwlq::rows_aligned(x, ldx, pwlq::type_size(dtype)));
+    if (need && (!workspace || workspace_bytes < need)) return PWLQ_ERR_WORKSPACE;
+    if (need && misaligned(workspace, 256)) return PWLQ_ERR_INVALID_ARG;
+    return from_cuda(pwlq::launch_w4_linear(*w, x, dtype, tokens, ldx, y, ldy, workspace, as_stream(stream)));
 }
 
 size_t pwlq_w4_moe_workspace_bytes(int64_t tokens, int64_t top, int64_t features, int64_t hidden) {

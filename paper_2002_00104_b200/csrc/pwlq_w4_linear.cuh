@@ -9,10 +9,12 @@ namespace {
 
 constexpr int kWarps = 8;
 
-template <typename T> struct LinearArgs {
+// T: the type of y; S: how the activations lie.
+template <typename T, class S> struct LinearArgs {
     W4View w;
-    const T* x;
+    const typename S::Elem* x;
     int64_t ldx, tokens;
+    int part;                              // columns of a row, or of one of its parts
     T* y;
     int64_t ldy;
     int team_shift;                        // log2 of the warps that share tiles
@@ -20,8 +22,8 @@ template <typename T> struct LinearArgs {
 
 // A warp's part of MT tiles: one segment.
 struct NoTag {};
-template <int MT, typename T> struct LinearSteps {
-    const LinearArgs<T>* a;
+template <int MT, typename T, class S> struct LinearSteps {
+    const LinearArgs<T, S>* a;
     int64_t tile;
     int first, count;                                     // blocks
     int64_t token;                                        // of this lane's first column
@@ -36,13 +38,13 @@ template <int MT, typename T> struct LinearSteps {
     __device__ __forceinline__ NoTag tag() const { return {}; }
     __device__ __forceinline__ int column() const { return first * kBlockCols; }
     // columns past the last token repeat it; nobody reads their sums
-    __device__ __forceinline__ const T* row(int n) const { return a->x + min(token + 8 * n, a->tokens - 1) * a->ldx; }
+    __device__ __forceinline__ const typename S::Elem* row(int n) const { return a->x + min(token + 8 * n, a->tokens - 1) * a->ldx; }
 };
 
 // A team of warps shares MT tiles along the columns.  The warps' sums meet in shared memory, where a warp's take its
 // ring's place, and are added in a fixed order.
 template <int MT, int NT, int ENDS, typename T, class S>
-__global__ void __launch_bounds__(kWarps * 32, 2) w4_linear_kernel(const LinearArgs<T> a) {
+__global__ void __launch_bounds__(kWarps * 32, 2) w4_linear_kernel(const LinearArgs<T, S> a) {
     constexpr int kCols = 8 * NT, kRing = kRingBytes<MT, ENDS>, kPitch = kCols + 1;
     static_assert(kRing >= 16 * MT * kPitch * 4 && kRing % 16 == 0, "sums are larger than a ring");
     extern __shared__ __align__(16) uint8_t shared[];
@@ -57,8 +59,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_linear_kernel(const LinearA
     bool none = true;
     if (mine * MT < a.w.tiles) {
         S source;
-        source.cols = a.w.cols;
-        const LinearSteps<MT, T> steps = {&a, mine * MT, begin, end - begin, token + (lane >> 2), w4_block_bytes(ENDS)};
+        source.cols = a.part;
+        const LinearSteps<MT, T, S> steps = {&a, mine * MT, begin, end - begin, token + (lane >> 2), w4_block_bytes(ENDS)};
         w4_stream<MT, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
                                 [&](NoTag, const float (&acc)[MT][NT][4]) {
             none = false;
@@ -100,7 +102,7 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_linear_kernel(const LinearA
 }
 
 template <int MT, int NT, int ENDS, typename T, class S>
-cudaError_t launch(LinearArgs<T> a, cudaStream_t stream) {
+cudaError_t launch(LinearArgs<T, S> a, cudaStream_t stream) {
     a.team_shift = 0;
     while (a.team_shift < 3 && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
     const int teams = kWarps >> a.team_shift;
@@ -111,17 +113,19 @@ cudaError_t launch(LinearArgs<T> a, cudaStream_t stream) {
 }
 
 template <int ENDS, typename T, class S>
-cudaError_t linear(const LinearArgs<T>& a, cudaStream_t stream) {
+cudaError_t linear(const LinearArgs<T, S>& a, cudaStream_t stream) {
     // Two tiles at a time save a third of what is not a product, and leave half as many CTAs: 8192 x 8192 12.4
     // against 13.4 us, 22528 x 8192 27.3 against 30.1, but 14336 x 4096 13.2 against 12.2, 1024 x 4096 4.6 against 3.7.
     if (a.tokens <= 8)
         return a.w.blocks >= 64 && a.w.tiles >= 256 ? launch<2, 1, ENDS, T, S>(a, stream)
                                                     : launch<1, 1, ENDS, T, S>(a, stream);
+    // sixteen at a time: the weights are taken apart again for every sixteen, which for some hundreds of tokens costs what
+    // a kernel of larger tiles with the activations in shared memory did, and less for fewer (64 x 8192 x 8192 45 us)
     return launch<2, 2, ENDS, T, S>(a, stream);
 }
 
 template <typename T, class S>
-cudaError_t linear(const LinearArgs<T>& a, cudaStream_t stream) {
+cudaError_t linear(const LinearArgs<T, S>& a, cudaStream_t stream) {
     if (a.w.ends == 4) return linear<4, T, S>(a, stream);
     return a.w.ends == 2 ? linear<2, T, S>(a, stream) : linear<1, T, S>(a, stream);
 }
@@ -129,15 +133,22 @@ cudaError_t linear(const LinearArgs<T>& a, cudaStream_t stream) {
 }  // namespace
 
 template <typename T>
-cudaError_t w4_linear_of(const pwlq_w4& w, const void* x, int64_t tokens, int64_t ldx, void* y, int64_t ldy,
+cudaError_t w4_linear_of(const pwlq_w4& w, const void* x, bool copied, int64_t tokens, int64_t ldx, void* y, int64_t ldy,
                          cudaStream_t stream) {
-    if (tokens > 16) return w4_wide_of<T>(w, x, tokens, ldx, y, ldy, stream);
-    const LinearArgs<T> a = {w4_view(w, !std::is_same<T, __half>::value), static_cast<const T*>(x), ldx, tokens,
-                             static_cast<T*>(y), ldy};
+    const W4View v = w4_view(w, !std::is_same<T, __half>::value);
+    T* const out = static_cast<T*>(y);
     if constexpr (sizeof(T) == 2) {
-        if (w.cols % kBlockCols == 0 && rows_aligned(x, ldx, sizeof(T))) return linear<T, RowsWhole<T>>(a, stream);
+        const T* const values = static_cast<const T*>(x);
+        const bool aligned = copied || rows_aligned(x, ldx, sizeof(T));
+        if (aligned && (copied || w.cols % kBlockCols == 0))
+            return linear<T, RowsWhole<T>>({v, values, ldx, tokens, v.cols, out, ldy, 0}, stream);
+        if (aligned && w.cols % 8 == 0) return linear<T, RowsEights<T>>({v, values, ldx, tokens, v.cols, out, ldy, 0}, stream);
+    } else {
+        if (copied)
+            return linear<T, RowsParts<3>>({v, static_cast<const __nv_bfloat16*>(x), ldx, tokens, (int)w4_padded(w.cols), out,
+                                            ldy, 0}, stream);
     }
-    return linear<T, RowsAny<T>>(a, stream);
+    return linear<T, RowsAny<T>>({v, static_cast<const T*>(x), ldx, tokens, v.cols, out, ldy, 0}, stream);
 }
 
 }  // namespace pwlq

@@ -1,5 +1,5 @@
 #include "pwlq_w4_linear.cuh"
 
 namespace pwlq {
-template cudaError_t w4_linear_of<__nv_bfloat16>(const pwlq_w4&, const void*, int64_t, int64_t, void*, int64_t, cudaStream_t);
+template cudaError_t w4_linear_of<__nv_bfloat16>(const pwlq_w4&, const void*, bool, int64_t, int64_t, void*, int64_t, cudaStream_t);
 }

@@ -17,8 +17,6 @@ struct Routing {
     int tokens, experts, top;
 };
 
-inline int64_t w4_padded(int64_t cols) { return w4_blocks(cols) * kBlockCols; }
-
 // Binary32 values as the products take them, in three bf16 parts, and rows that do not lie in whole 16-byte blocks: the
 // first launch leaves tokens like that in the workspace, each part in whole blocks of columns.
 inline bool moe_copies(const pwlq_w4_moe_args& a) {

@@ -107,7 +107,8 @@ _SIGNATURES = {
     "pwlq_w4_bytes": (_SZ, [_I64, _I64, _I64, _I64, _I64]),
     "pwlq_w4_encode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
     "pwlq_w4_decode": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P]),
-    "pwlq_w4_linear": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P, _I64, _P]),
+    "pwlq_w4_linear_workspace_bytes": (_SZ, [_I64, _I64, _I64, _INT, _INT]),
+    "pwlq_w4_linear": (_INT, [_STRUCT, _P, _INT, _I64, _I64, _P, _I64, _P, _SZ, _P]),
     "pwlq_w4_moe_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I64]),
     "pwlq_w4_moe": (_INT, [_STRUCT, _P]),
     "pwlq_device_status": (_INT, []),
@@ -836,7 +837,7 @@ def _calls():
                    "pwlq_block_norm_backward_workspace_bytes", "pwlq_block_norm_backward",
                    "pwlq_act8_weight_grad_workspace_bytes", "pwlq_act8_weight_grad",
                    "pwlq_w4_bytes", "pwlq_w4_encode", "pwlq_w4_decode",
-                   "pwlq_w4_linear", "pwlq_w4_moe_workspace_bytes", "pwlq_w4_moe")
+                   "pwlq_w4_linear_workspace_bytes", "pwlq_w4_linear", "pwlq_w4_moe_workspace_bytes", "pwlq_w4_moe")
         module.init(tuple(ctypes.cast(getattr(lib, name), _P).value for name in entries), PwlqError)
         _calls_module = module
     return _calls_module
@@ -1151,13 +1152,18 @@ def w4_decode(packed: W4, dtype=torch.float32, out=None, stream=None):
     return _calls().w4_decode(packed._fields, packed._memory, _dtype_code(dtype), len(packed._shape) == 3, out)
 
 
-def w4_linear(x, packed: W4, out=None, stream=None):
+def w4_linear_workspace_bytes(tokens: int, rows: int, cols: int, dtype, x_aligned=True) -> int:
+    return int(load_library().pwlq_w4_linear_workspace_bytes(tokens, rows, cols, _dtype_code(dtype),
+                                                             int(x_aligned)))
+
+
+def w4_linear(x, packed: W4, out=None, workspace=None, stream=None):
     """``pwlq_w4_linear``: x @ w.T for a few tokens x [tokens, cols], or for a paired matrix
     silu(x @ gate.T) * (x @ up.T), [tokens, rows / 2].  No backward pass."""
     if stream is not None:
         with _on(stream):
-            return w4_linear(x, packed, out)
-    return _calls().w4_linear(x, packed._fields, packed._memory, out)
+            return w4_linear(x, packed, out, workspace)
+    return _calls().w4_linear(x, packed._fields, packed._memory, out, workspace)
 
 
 def w4_moe_workspace_bytes(tokens: int, top: int, features: int, hidden: int) -> int:

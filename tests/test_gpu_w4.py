@@ -103,7 +103,8 @@ def test_memory_that_is_written_again():
 SHAPES = [(1, 1, 1, 32), (1, 16, 128, 128), (1, 17, 127, 64), (2, 4096, 64, 32), (3, 100, 1000, 256), (5, 333, 1285, 32),
           (7, 16, 8192, 128), (8, 500, 520, 64), (9, 48, 640, 128), (13, 33, 4096, 64), (16, 130, 1025, 128),
           (17, 64, 256, 32), (31, 70, 900, 64), (33, 96, 384, 128), (64, 200, 2048, 64), (100, 40, 515, 256), (1, 4112, 8200, 128),
-          (4, 4097, 8192, 64)]
+          (4, 4097, 8192, 64), (5, 8000, 1030, 32), (12, 6001, 1601, 64), (32, 5000, 1700, 64), (33, 8193, 200, 128),
+          (64, 8200, 520, 32), (65, 100, 300, 64), (130, 256, 4096, 128)]
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
@@ -128,7 +129,7 @@ def test_products_of_whole_numbers_are_exact(dtype, tokens, rows, cols, group):
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("paired", [False, True])
 @pytest.mark.parametrize("tokens,rows,cols,group", [(1, 2, 1, 64), (1, 1000, 2048, 64), (6, 36, 777, 32), (8, 8, 9000, 128),
-                                                    (12, 130, 384, 256), (40, 34, 1029, 64), (64, 256, 512, 128)])
+                                                    (12, 130, 384, 256), (40, 34, 1029, 64), (64, 256, 512, 128), (70, 66, 777, 64)])
 def test_products(dtype, paired, tokens, rows, cols, group):
     from paper_2002_00104_b200 import pwlq
     dt = TYPES[dtype]
@@ -193,6 +194,29 @@ def test_largest_and_smallest_activations():
     x[3, 0] = 2.0 ** -100
     y = pwlq.w4_linear(x.cuda(), packed).cpu()
     assert torch.equal(y.double(), (x.double() @ U.held(w, 128, 1.0).t()).float().double())
+
+
+@pytest.mark.parametrize("dtype,cols", [("fp32", 256), ("bf16", 129), ("bf16", 300), ("fp16", 300)])
+def test_workspaces(dtype, cols):
+    from paper_2002_00104_b200 import pwlq
+    dt = TYPES[dtype]
+    rows = 16 * 2100
+    w, x = _w(1, rows, cols), _w(2, 5, cols, dtype=dt, scale=1.0)
+    x[2, 7], x[4, cols - 1] = float("inf"), float("nan")
+    packed, x = pwlq.w4_encode(w.cuda()), x.cuda()
+    need = pwlq.w4_linear_workspace_bytes(5, rows, cols, dt)
+    assert need > 0
+    few = pwlq.w4_linear(x, pwlq.w4_encode(w[:4096].cuda()))         # without a copy
+    assert pwlq.w4_linear_workspace_bytes(5, 4096, cols, dt) == 0
+    assert torch.equal(torch.nan_to_num(pwlq.w4_linear(x, packed)[:, :4096], 7.0), torch.nan_to_num(few, 7.0))
+    x = x.nan_to_num(1.0, 1.0)
+    workspace = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(pwlq.w4_linear(x, packed, workspace=workspace), pwlq.w4_linear(x, packed))
+    with pytest.raises(pwlq.PwlqError) as e:
+        pwlq.w4_linear(x, packed, workspace=workspace[:-1])
+    assert e.value.status == pwlq.ERR_WORKSPACE
+    with pytest.raises(ValueError):
+        pwlq.w4_linear(x, packed, workspace=workspace.cpu())
 
 
 def test_no_tokens():

@@ -71,7 +71,16 @@ def test_encode_and_decode(pwlq, call):
 
 def test_linear(pwlq):
     lib = pwlq.load_library()
-    good = [_w4(), B, pwlq.BF16, 4, 100, C, 32, None]
+    size, large = lib.pwlq_w4_linear_workspace_bytes, 16 * 4096
+    need = size(4, large, 100, pwlq.BF16, 1)
+    assert need == size(4, large, 104, pwlq.BF16, 0) == 4 * 128 * 2
+    assert size(3, large, 128, pwlq.F32, 1) == 2304
+    assert size(4, large, 104, pwlq.BF16, 1) == size((1 << 19) + 1, large, 100, pwlq.F32, 0) == size(4, large - 16, 100, pwlq.F32, 0) == 0
+    for bad in ((0, large, 100, 0, 0), (4, large, 0, 0, 0), (4, large, 100, 3, 0), (-1, large, 100, 0, 0), (4, 0, 100, 0, 0),
+                (4, large, 2 ** 32 + 100, 0, 0), (4, -large, 100, 0, 0)):
+        assert size(*bad) == 0, bad
+    good = [_w4(), B, pwlq.BF16, 4, 100, C, 32, 0x50000, need, None]
+    big = [_w4(rows=large), B, pwlq.BF16, 4, 100, 0x10000000, large, 0x50000, need, None]
 
     def rc(*changes):
         args = list(good)
@@ -83,6 +92,10 @@ def test_linear(pwlq):
                  (6, 31), (5, B), (5, B + 2 * 99), (5, B - 2)):
         assert rc((i, v)) == pwlq.ERR_INVALID_ARG, (i, v)
     assert rc((3, (1 << 19) + 1)) == pwlq.ERR_UNSUPPORTED
+    for i, v, status in ((7, None, pwlq.ERR_WORKSPACE), (8, need - 1, pwlq.ERR_WORKSPACE), (7, 0x50000 + 128, pwlq.ERR_INVALID_ARG)):
+        args = list(big)
+        args[i] = v
+        assert lib.pwlq_w4_linear(*args) == status
     assert rc((3, 0), (1, None), (5, None)) == pwlq.OK
     # columns of the same rows: beside each other they are no overlap, but the call would launch; off by one they are
     assert rc((4, 200), (6, 200), (5, B + 2 * 99)) == pwlq.ERR_INVALID_ARG
