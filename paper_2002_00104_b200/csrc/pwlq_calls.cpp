@@ -424,7 +424,8 @@ struct Packed {
             if (*to[i] == -1 && PyErr_Occurred()) throw python_error();
         }
         bytes = (int64_t)lib.w4_bytes(w.matrices, w.rows, w.cols, w.group, w.paired);
-        if (!bytes) throw Failed{PWLQ_ERR_INVALID_ARG, "packed matrix"};
+        const bool none = w.matrices < 1 || w.rows < 1 || w.cols < 1;
+        if (!bytes) throw Failed{none ? PWLQ_ERR_INVALID_ARG : PWLQ_ERR_UNSUPPORTED, "packed matrix"};
     }
     void place(const at::Tensor& m, int device) {
         TORCH_CHECK_VALUE(m.scalar_type() == at::kByte && m.is_contiguous() && m.is_cuda() && m.get_device() == device &&

@@ -227,7 +227,7 @@ __global__ void __launch_bounds__(256) w4_decode_kernel(const W4View v, W4Write 
 template <typename T>
 __global__ void __launch_bounds__(128) w4_copy_kernel(const T* __restrict__ x, int64_t ldx, int64_t cols, void* __restrict__ copy,
                                                       int64_t padded) {
-    const int64_t col = ((int64_t)blockIdx.x * 128 + threadIdx.x) * 8, token = blockIdx.y;
+    const int64_t col = ((int64_t)blockIdx.y * 128 + threadIdx.x) * 8, token = blockIdx.x;
     allow_dependents();                                   // few CTAs: the next launch may take its places
     await_previous();
     if (col >= padded) return;
@@ -291,7 +291,7 @@ cudaError_t launch_w4_decode(const pwlq_w4& w, void* y, int dtype, int64_t ldy, 
 
 cudaError_t launch_w4_copy(const void* x, int dtype, int64_t tokens, int64_t cols, int64_t ldx, void* copy, cudaStream_t stream) {
     const int64_t padded = w4_padded(cols);
-    const dim3 grid((unsigned)((padded / 8 + 127) / 128), (unsigned)tokens), threads(128);
+    const dim3 grid((unsigned)tokens, (unsigned)((padded / 8 + 127) / 128)), threads(128);
     if (dtype == kF32)
         return launch_dependent(w4_copy_kernel<float>, grid, threads, 0, stream, static_cast<const float*>(x), ldx, cols, copy, padded);
     if (dtype == kBf16)

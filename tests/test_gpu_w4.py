@@ -88,6 +88,18 @@ def test_slices_and_outputs_off_their_alignment(dtype, offset, pad):
     assert torch.equal(pwlq.w4_encode(w.contiguous(), group=64, ratio=0.375).memory, packed.memory)
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols,paired", [(994, 1000, True), (1001, 777, False), (1000, 768, True)])
+def test_many_matrices_at_once(dtype, rows, cols, paired):
+    """Enough of them that a CTA goes through several tiles, and not whole numbers of these."""
+    from paper_2002_00104_b200 import pwlq
+    w = (torch.randn(40, rows, cols, generator=torch.Generator("cuda").manual_seed(rows), device="cuda") * 0.05).to(TYPES[dtype])
+    packed = pwlq.w4_encode(w, group=256, ratio=0.375, paired=paired)
+    each = [pwlq.w4_encode(v, group=256, ratio=0.375, paired=paired).memory for v in w]
+    assert torch.equal(packed.memory, torch.cat(each))
+    _same(pwlq.w4_decode(packed)[39], U.held(w[39], 256, 0.375))
+
+
 def test_memory_that_is_written_again():
     from paper_2002_00104_b200 import pwlq
     a, b = _w(1, 40, 300).cuda(), _w(2, 40, 300).cuda()
@@ -265,6 +277,17 @@ def test_rows_far_apart():
     far[:, :512] = x
     y = pwlq.w4_linear(far[:, :512], packed, out=far[:, 1024:1064])
     assert torch.equal(y, pwlq.w4_linear(x, packed))
+
+
+@pytest.mark.parametrize("cols", [1023, 1024])
+def test_very_many_tokens(cols):
+    """More than a grid's second axis holds, of rows that are copied first and of others."""
+    from paper_2002_00104_b200 import pwlq
+    packed = pwlq.w4_encode(_w(8, 8192, cols, dtype=torch.bfloat16).cuda(), group=64)
+    x = torch.randn(66001, cols, generator=torch.Generator("cuda").manual_seed(1), device="cuda").bfloat16()
+    y = pwlq.w4_linear(x, packed)
+    for at in (0, 65520, 65536, 65990):
+        assert torch.equal(y[at:at + 11], pwlq.w4_linear(x[at:at + 11], packed))
 
 
 def test_best_ratio_of_a_weight_matrix():

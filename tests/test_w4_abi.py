@@ -170,6 +170,17 @@ def test_shapes_and_memory(pwlq):
             setattr(packed, name, 1)
 
 
+def test_sizes_beyond_the_limits(pwlq):
+    for shape in ((65536, 16, 128), (1, (1 << 24) + 1, 128), (16, (1 << 20) + 1), (65535, 1 << 20, 1 << 20)):
+        with pytest.raises(pwlq.PwlqError) as e:
+            pwlq.w4_bytes(shape)
+        assert e.value.status == pwlq.ERR_UNSUPPORTED
+    wide = torch.zeros(1, dtype=torch.bfloat16).expand(16, (1 << 20) + 1)
+    with pytest.raises(pwlq.PwlqError) as e:
+        pwlq.w4_encode(wide)
+    assert e.value.status == pwlq.ERR_UNSUPPORTED
+
+
 def test_tensors_that_are_not_on_the_device(pwlq):
     x = torch.zeros(16, 128)
     packed = pwlq.W4(torch.zeros(1056, dtype=torch.uint8), (16, 128))
