@@ -226,7 +226,8 @@ __device__ __forceinline__ W4Table in_registers(const W4Table& t) {
 // cycles (address arithmetic, moves by multiplication and 16-bit arithmetic included): 13 to a word of eight weights, 28
 // cycles with the matrix instruction.  At 1.9 GHz that is 5.2 TB/s of codes; so all else is kept small.  Two tiles
 // share an activation operand; blocks come to shared memory by asynchronous copies, kStages - 1 steps ahead and across
-// the ends of segments, and activations are requested a block ahead.
+// the ends of segments, and activations are requested a block ahead.  36 cycles a word in all: 1 token 22528 x 8192
+// 27.4 us, 3.5 TB/s.
 constexpr int kStages = 4;
 template <int MT, int ENDS> constexpr int kRingBytes = kStages * MT * w4_block_bytes(ENDS);       // of a warp
 

@@ -262,7 +262,9 @@ template <int MT, int NT, typename T> struct DownSteps {
 };
 
 // A CTA per MT tiles of 16 features: the blocks of all chosen experts' rows are one list that the warps share; a warp
-// adds what an expert gives to its own sums, [16 MT][tokens], and these are added in a fixed order at the end.
+// adds what an expert gives to its own sums, [16 MT][tokens], and these are added in a fixed order at the end.  So no
+// partial sum leaves the CTA; what is left is that 128 or 256 CTAs do not divide by 148.  4 tokens, 8 experts of 4096 x
+// 8192: 40 us, 53 with single tiles.
 template <int MT, int NT, int ENDS, typename T>
 __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const DownArgs<T> a) {
     using H = Hidden<T>;
