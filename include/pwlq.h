@@ -603,8 +603,8 @@ int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, i
  *           precision: which experts are chosen does not depend on the order of a sum
  *   chosen, weights   [tokens, top] each, int32 and binary32, largest score first; or NULL
  *   workspace         pwlq_w4_moe_workspace_bytes(...) bytes, 256-byte aligned; 0 for invalid arguments
- * Sums are binary32 in a fixed order (bit-reproducible).  silu(gate) * up * weight lies in the workspace with 16
- * bits of precision (24 for binary32 tokens) and binary32's range.  A token's values reach no other token's. */
+ * Sums are binary32 in a fixed order (bit-reproducible).  silu(gate) * up * weight lies in the workspace with all of
+ * binary32's 24 bits and its range, whatever dtype is.  A token's values reach no other token's. */
 #define PWLQ_W4_MOE_MAX_TOKENS 64
 #define PWLQ_W4_MOE_MAX_EXPERTS 1024
 #define PWLQ_W4_MOE_MAX_TOP 32

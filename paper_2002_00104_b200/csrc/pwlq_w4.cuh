@@ -269,7 +269,9 @@ __device__ __forceinline__ void w4_stream(Steps steps, const S& source, const W4
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) fill(i * kCodes);
     // the products
-    constexpr int kAhead = NT == 1 && S::kPieces < 3 ? 4 : 2;            // quarters of a block, of activations
+    // quarters of a block, of activations: as many as registers hold (three parts and one tile: 64 tokens, 8 of 128
+    // experts of 3 x 768 x 2048 binary32 246 us with two quarters, 182 with four)
+    constexpr int kAhead = NT == 1 && (S::kPieces < 3 || MT == 1) ? 4 : 2;
     typename S::Raw raw[kAhead][NT];
     const typename S::Elem* row[NT];
     int column = 0;

@@ -82,25 +82,19 @@ __device__ __forceinline__ int build_lists(const Lists& l, const Routing& r) {
     return *l.active;
 }
 
-// What lies between the two products, a row for each pair: bf16 parts, two of a 16-bit type (16 bits of each value:
-// with them the result is rounded once, as if there were nothing between; one 16-bit value would add as much error
-// again) or three of binary32.  Rows are padded with zeros to whole blocks.
-template <typename T> struct Hidden {
-    static constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
+// What lies between the two products, a row for each pair: three bf16 parts whose sum a value is (24 bits, and
+// binary32's range), so that nothing is rounded there, whatever the tokens' type.  Two parts, 16 bits, would do for an
+// error against the real numbers that a 16-bit result hides, but would move a few in a thousand results to the next
+// 16-bit number, and lose what is left of large values that cancel.  Rows are padded with zeros to whole blocks.
+struct Hidden {
+    static constexpr int kParts = 3;
     using Source = RowsParts<kParts>;
     using Elem = __nv_bfloat16;
     static __device__ __forceinline__ void put(Elem* row, int64_t padded, int64_t i, float v) {
-        if (kParts == 3) {
-            float p[3];
-            split3(v, p[0], p[1], p[2]);
+        float p[kParts];
+        split3(v, p[0], p[1], p[2]);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) row[k * padded + i] = __float2bfloat16_rn(p[k]);
-        } else {
-            const __nv_bfloat16 high = __float2bfloat16_rn(v);
-            const float rest = v - __bfloat162float(high);
-            row[i] = high;
-            row[padded + i] = __float2bfloat16_rn(abs_bits(__bfloat162float(high)) < kInfBits ? rest : 0.0f);
-        }
+        for (int k = 0; k < kParts; ++k) row[k * padded + i] = __float2bfloat16_rn(p[k]);
     }
 };
 // The tokens: as they are given, or the copy that the first launch has made.
@@ -113,7 +107,7 @@ template <typename T> struct UpArgs {
     const typename Tokens<T>::Source::Elem* x;
     int64_t ldx;
     int part;                                             // columns of a part of x
-    typename Hidden<T>::Elem* h;
+    Hidden::Elem* h;
     int64_t padded;                                       // hidden in whole blocks
     int team_shift;                                       // log2 of the warps of a team
 };
@@ -206,11 +200,11 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
             }
             const int tile = at.tile * MT + m, f = tile * 8 + r;
             if (tile >= a.w.tiles) continue;
-            typename Hidden<T>::Elem* const to = a.h + pair * Hidden<T>::kParts * a.padded;
-            Hidden<T>::put(to, a.padded, f,
+            Hidden::Elem* const to = a.h + pair * Hidden::kParts * a.padded;
+            Hidden::put(to, a.padded, f,
                            f < hidden ? silu_of(gate * 256.0f) * (up * 256.0f) * a.r.weights[pair] : 0.0f);
             if (tile == a.w.tiles - 1)
-                for (int z = f + 8; z < a.padded; z += 8) Hidden<T>::put(to, a.padded, z, 0.0f);
+                for (int z = f + 8; z < a.padded; z += 8) Hidden::put(to, a.padded, z, 0.0f);
         }
         meet();
     });
@@ -219,7 +213,7 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
 template <typename T> struct DownArgs {
     W4View w;                                             // [experts, features, hidden]
     Routing r;
-    const typename Hidden<T>::Elem* h;
+    const Hidden::Elem* h;
     int64_t padded;
     T* y;
     int64_t ldy;
@@ -228,7 +222,6 @@ template <typename T> struct DownArgs {
 // A warp's way through its part of a tile's blocks, which are those of all chosen experts one after another.
 struct DownTag { int first, count; };
 template <int MT, int NT, typename T> struct DownSteps {
-    using H = Hidden<T>;
     const Lists* l;
     const DownArgs<T>* a;
     int64_t tile;                                         // the first of MT
@@ -255,9 +248,9 @@ template <int MT, int NT, typename T> struct DownSteps {
     }
     __device__ __forceinline__ DownTag tag() const { return {first, count}; }
     __device__ __forceinline__ int column() const { return from * kBlockCols; }
-    __device__ __forceinline__ const typename H::Elem* row(int n) const {
+    __device__ __forceinline__ const Hidden::Elem* row(int n) const {
         const int c = min(8 * n + ((int)(threadIdx.x & 31) >> 2), count - 1);
-        return a->h + l->pair[first + c] * H::kParts * a->padded;
+        return a->h + l->pair[first + c] * Hidden::kParts * a->padded;
     }
 };
 
@@ -267,7 +260,6 @@ template <int MT, int NT, typename T> struct DownSteps {
 // 8192: 40 us, 53 with single tiles.
 template <int MT, int NT, int ENDS, typename T>
 __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const DownArgs<T> a) {
-    using H = Hidden<T>;
     constexpr int kRing = kRingBytes<MT, ENDS>, kRows = 16 * MT;
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
     const int warp = warp_index(), lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
@@ -278,7 +270,7 @@ __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const Down
     for (int i = lane; i < kRows * pitch; i += 32) mine[i] = 0.0f;
     await_previous();
     const int total = build_lists(l, a.r) * a.w.blocks;
-    typename H::Source source;
+    Hidden::Source source;
     source.cols = (int)a.padded;
     const DownSteps<MT, NT, T> steps = {&l, &a, (int64_t)blockIdx.x * MT, (int)((int64_t)total * warp / kDownWarps),
                                         (int)((int64_t)total * (warp + 1) / kDownWarps), w4_block_bytes(ENDS)};
@@ -352,7 +344,7 @@ inline double filled(int64_t ctas) { return (double)ctas / (double)(148 * ((ctas
 template <int NT, typename T>
 cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* copy, void* hidden, cudaStream_t stream) {
     const int64_t padded = w4_padded(a.down->cols), part = w4_padded(a.up->cols);
-    auto* const h = static_cast<typename Hidden<T>::Elem*>(hidden);
+    auto* const h = static_cast<Hidden::Elem*>(hidden);
     const bool copied = moe_copies(a);
     const UpArgs<T> up = {w4_view(*a.up, !std::is_same<T, __half>::value), r,
                           static_cast<const typename Tokens<T>::Source::Elem*>(copied ? copy : a.x),
