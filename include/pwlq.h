@@ -585,7 +585,10 @@ int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ld
 /* y[t, n] = sum over k of x[t, k] w[n, k], for a paired matrix y[t, n] = silu(gate) * up of the sums with gate row
  * n and up row n, [tokens, rows / 2].  matrices = 1.  x [tokens, cols] and y of type dtype; made for few tokens (any
  * number is taken; from some hundreds on decoding once and a dense product are faster).  Products are exact, the
- * sums binary32 in a fixed order (bit-reproducible), y is rounded once.  tokens may be 0.  y must not overlap x.
+ * sums binary32 in a fixed order (bit-reproducible), y is rounded once.  x may have any finite value: no sum on the way
+ * leaves binary32's range where the result does not come near its end.  Sums are kept to 2^-134 or better, so that
+ * results below 2^-110 have fewer than 24 bits; so have binary32 values of x below 2^-109.  tokens may be 0.  y must
+ * not overlap x.
  *   workspace   pwlq_w4_linear_workspace_bytes(...) bytes, 256-byte aligned: for a large matrix, a copy of tokens
  *               that are binary32 (in three bf16 parts whose sum they are), or whose rows do not start on 16-byte
  *               boundaries (x_aligned) or are not whole eights; 0 bytes (workspace may be NULL) otherwise */
@@ -600,7 +603,8 @@ int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, i
  *   up      paired [experts][2 hidden, features], G then U;   down   [experts][features, hidden]
  *   x, y    [tokens, features] of type dtype; y may be x (same pitch)
  *   router  [experts, features] of type router_dtype (PWLQ_F32 or dtype).  Scores are summed in twice binary32's
- *           precision: which experts are chosen does not depend on the order of a sum
+ *           precision (and its range: every product has to lie in it): which experts are chosen does not depend on
+ *           the order of a sum
  *   chosen, weights   [tokens, top] each, int32 and binary32, largest score first; or NULL
  *   workspace         pwlq_w4_moe_workspace_bytes(...) bytes, 256-byte aligned; 0 for invalid arguments
  * Sums are binary32 in a fixed order (bit-reproducible).  silu(gate) * up * weight lies in the workspace with all of

@@ -16,11 +16,11 @@ W4View w4_view(const pwlq_w4& w, bool bf16) {
     for (int i = 0; i < 8; ++i) {
         const int n = i < 4 ? i * b : 3 * b + (i - 4) * (64 - b);
         uint32_t bits = 0;
-        if (n > 0) {                                      // n / 256 = 1.m * 2^(e - 8)
+        if (n > 0) {                                      // n / kUnit = 1.m * 2^(e - kUnitBits)
             int e = 0;
             while (n >> (e + 1)) ++e;
-            bits = bf16 ? (uint32_t)(e - 8 + 127) << 7 | ((uint32_t)(n << 7) >> e & 127)
-                        : (uint32_t)(e - 8 + 15) << 10 | ((uint32_t)(n << 10) >> e & 1023);
+            bits = bf16 ? (uint32_t)(e - kUnitBits<__nv_bfloat16> + 127) << 7 | ((uint32_t)(n << 7) >> e & 127)
+                        : (uint32_t)(e - kUnitBits<__half> + 15) << 10 | ((uint32_t)(n << 10) >> e & 1023);
         }
         v.table.high[i >> 2] |= (bits >> 8) << 8 * (i & 3);
         v.table.low[i >> 2] |= (bits & 255) << 8 * (i & 3);
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(256) w4_decode_kernel(const W4View v, W4Write 
             const int64_t row = w.row_of(tile, g + 8 * i);
             const float scale = __uint_as_float(i ? s & 0xffff0000u : s << 16);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) out[i][k] = (out[i][k] * 256.0f) * scale;
+            for (int k = 0; k < 8; ++k) out[i][k] = (out[i][k] * kUnit<__nv_bfloat16>) * scale;
             if constexpr (VEC) {
                 const int valid = row < 0 ? 0 : (int)max((int64_t)0, min(w.cols - col, (int64_t)8));
                 T* const to = y + matrix * ldm + (row < 0 ? 0 : row) * ldy + col;

@@ -3,17 +3,23 @@
 #pragma once
 
 #include <cooperative_groups.h>
+#include <type_traits>
 
 #include "pwlq_act8.cuh"
 #include "pwlq_w4.h"
 
 namespace pwlq {
 
-// The eight magnitudes that region and level can stand for, n / 256 in a 16-bit type (exact: n <= 192 has
+// The eight magnitudes that region and level can stand for, n / kUnit in a 16-bit type (exact: n <= 192 has
 // eight bits), as bytes: a byte permutation with four codes for selectors looks four values up at once.
 struct W4Table {
     uint32_t high[2], low[2];
 };
+// The products of a group, 128 at a time, are summed before they meet their scale: 128 * 192 / 2^15 < 1, so that no sum
+// of bf16 values (parts of binary32 ones among them) leaves the range that the values themselves are in, however small
+// the scale makes the result.  fp16 values are below 2^16 and their table is above 2^-14: any unit between will do.
+template <typename T> constexpr int kUnitBits = std::is_same<T, __half>::value ? 8 : 15;
+template <typename T> constexpr float kUnit = (float)(1 << kUnitBits<T>);
 
 // A packed matrix (format: include/pwlq.h) as kernels see it.  A block of 16 rows x 128 columns is 32 lanes x
 // 8 words; word j of lane 4 g + q holds rows g and g + 8, columns 32 (j / 2) + 8 q + 4 (j & 1) .. + 3, so that
@@ -219,7 +225,7 @@ __device__ __forceinline__ W4Table in_registers(const W4Table& t) {
 // A warp's way through its blocks.  `Steps` is a list of segments, blocks of MT tiles with the same activation rows:
 // next() goes on to one, of blocks() blocks, whose codes begin at code(tile), whose first column and rows (of column
 // 8 n + g for this lane) are column() and row(n); tag() is what done(tag, acc) gets with the segment's sums,
-// of n / 256 * s * x.  The products of a group (of 128 columns, if it is longer) are summed by the matrix instructions
+// of n / kUnit * s * x.  The products of a group (of 128 columns, if it is longer) are summed by the matrix instructions
 // in binary32 and enter acc times the scales of their rows.
 //
 // What bounds this for a few tokens is, next to the weights' bytes, the integer pipe, which takes an instruction in two

@@ -88,8 +88,8 @@ __global__ void __launch_bounds__(kWarps * 32, 2) w4_linear_kernel(const LinearA
             lo += v[0];
             hi += v[8 * kPitch];
         }
-        lo *= 256.0f;
-        hi *= 256.0f;
+        lo *= kUnit<typename S::Mma>;
+        hi *= kUnit<typename S::Mma>;
         const int64_t tile = (first + k) * MT + m;
         T* const y = a.y + (token + c) * a.ldy;
         if (a.w.paired) {

@@ -161,6 +161,7 @@ template <int MT, int NT, typename T> struct UpSteps {
 template <int MT, int NT, int ENDS, typename T>
 __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T> a) {
     constexpr int kPitch = 8 * NT + 1, kRing = kRingBytes<MT, ENDS>;
+    constexpr float kScale = kUnit<typename Tokens<T>::Source::Mma>;
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
     float* const sums = reinterpret_cast<float*>(shared + kUpWarps * kRing);
     const Lists l(reinterpret_cast<uint8_t*>(sums + kUpWarps * MT * 16 * kPitch), a.r);
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(kUpWarps * 32, 2) moe_up_kernel(const UpArgs<T
             if (tile >= a.w.tiles) continue;
             Hidden::Elem* const to = a.h + pair * Hidden::kParts * a.padded;
             Hidden::put(to, a.padded, f,
-                           f < hidden ? silu_of(gate * 256.0f) * (up * 256.0f) * a.r.weights[pair] : 0.0f);
+                        f < hidden ? silu_of(gate * kScale) * (up * kScale) * a.r.weights[pair] : 0.0f);
             if (tile == a.w.tiles - 1)
                 for (int z = f + 8; z < a.padded; z += 8) Hidden::put(to, a.padded, z, 0.0f);
         }
@@ -298,7 +299,7 @@ __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const Down
 #pragma unroll
         for (int j = 0; j < kDownWarps; ++j) sum += sums[(j * kRows + r) * pitch + t];
         const int64_t d = (int64_t)blockIdx.x * kRows + r;
-        if (d < a.w.rows) a.y[t * a.ldy + d] = from_f32<T>(sum * 256.0f);
+        if (d < a.w.rows) a.y[t * a.ldy + d] = from_f32<T>(sum * kUnit<Hidden::Source::Mma>);
     }
 }
 

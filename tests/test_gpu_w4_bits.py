@@ -39,3 +39,52 @@ def test_all_bits_between_the_products(dtype, tokens, features):
     down[:, 0], down[:, 1] = c, -c
     y = _one_expert(up, down, x, TYPES[dtype])
     assert torch.equal(y.float(), (c * 96 * 2.0 ** -20).expand(tokens, -1))
+
+
+def _thirds(seed, rows, cols, top):
+    """Values 0, +-m / 3, +-2 m / 3, +-m, with m = 3 * top in every group of 32."""
+    g = torch.Generator().manual_seed(seed)
+    w = torch.randint(-3, 4, (rows, cols), generator=g).float()
+    w[:, ::32] = 3.0
+    return w * top
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tokens,rows,cols,group", [(1, 40, 256, 32), (3, 40, 301, 64), (8, 4096, 8192, 128), (9, 48, 384, 256),
+                                                    (5, 33600, 300, 128), (70, 20, 128, 64)])
+def test_the_largest_activations(dtype, tokens, rows, cols, group):
+    """Values up to the largest bf16 ones, whose sum before the scales lies behind binary32's range, and the result
+    far within it."""
+    from paper_2002_00104_b200 import pwlq
+    w = _thirds(rows, rows, cols, 2.0 ** -16)
+    x = torch.tensor([1.0, -1.0, 1.9921875, -1.9921875, 0.0])[torch.randint(0, 5, (tokens, cols), generator=torch.Generator().manual_seed(cols))]
+    x = (x.double() * 2.0 ** 127).float()
+    assert torch.isfinite(x).all() and torch.equal(x.bfloat16().float(), x)
+    y = pwlq.w4_linear(x.to(TYPES[dtype]).cuda(), _pack(w, group)).cpu()
+    assert torch.equal(y, (x.double() @ w.double().t()).to(y.dtype))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tokens,rows,cols,group", [(1, 40, 256, 32), (3, 40, 301, 64), (9, 48, 384, 256), (5, 33600, 300, 128)])
+def test_the_smallest_activations(dtype, tokens, rows, cols, group):
+    """Values at the lower end of the normal numbers, products of which with the levels alone are below it."""
+    from paper_2002_00104_b200 import pwlq
+    w = _thirds(rows, rows, cols, 2.0 ** 30)
+    x = torch.randint(-3, 4, (tokens, cols), generator=torch.Generator().manual_seed(cols)).float() * 2.0 ** -126
+    y = pwlq.w4_linear(x.to(TYPES[dtype]).cuda(), _pack(w, group)).cpu()
+    assert torch.equal(y, (x.double() @ w.double().t()).to(y.dtype))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("tokens,features", [(1, 64), (2, 4096), (20, 70)])
+def test_the_largest_values_in_a_layer(dtype, tokens, features):
+    """The same in both products: of values of 2^127, and of 27 * 2^120 between them."""
+    hidden = 40
+    up, down = torch.zeros(2 * hidden, features), _thirds(features, features, hidden, 2.0 ** -40)
+    x = torch.zeros(tokens, features)
+    x[:, :3] = 2.0 ** 127
+    up[:hidden, :3] = 3 * 2.0 ** -98                     # gate 9 * 2^29: its sigmoid is 1
+    up[hidden:, 0] = 3 * 2.0 ** -36                      # up 3 * 2^91
+    want = (torch.full((hidden,), 27.0 * 2.0 ** 120).double() @ down.double().t()).expand(tokens, -1)
+    y = _one_expert(up, down, x, TYPES[dtype])
+    assert torch.equal(y, want.to(y.dtype))
