@@ -383,10 +383,15 @@ __device__ __forceinline__ float silu_of(float v) { return __fdiv_rn(v, 1.0f + e
 // Launches a kernel as a dependent of the launch before it.  Its own dependents start when it ends: begun earlier,
 // their CTAs take places on the multiprocessors from those of this one that still wait for theirs (4096 x 4096, one
 // token, back to back: 5.0 us, 6.1 with the trigger at the beginning).
-template <typename A>
+// kMost: the most shared memory that any call of this kernel asks for.  Calls from several threads share what a kernel is
+// allowed, so that it is never a call's own size: a smaller one set between another's setting and launch made that fail.
+constexpr size_t kMostShared = 227 * 1024;                // of a CTA
+template <size_t kMost, typename A>
 cudaError_t launch_w4(void (*kernel)(A), const A& args, dim3 grid, int threads, size_t smem, cudaStream_t stream) {
+    static_assert(kMost <= kMostShared, "more shared memory than there is");
+    if (smem > kMost) return cudaErrorInvalidValue;
     if (smem > 48 * 1024) {
-        const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost);
         if (err != cudaSuccess) return err;
     }
     return launch_dependent(kernel, grid, dim3((unsigned)threads), smem, stream, args);

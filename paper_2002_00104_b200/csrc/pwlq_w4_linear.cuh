@@ -107,9 +107,10 @@ cudaError_t launch(LinearArgs<T, S> a, cudaStream_t stream) {
     while (a.team_shift < 3 && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
     const int teams = kWarps >> a.team_shift;
     const int64_t units = (a.w.tiles + MT - 1) / MT;
-    return launch_w4(w4_linear_kernel<MT, NT, ENDS, T, S>, a,
-                     dim3((unsigned)((units + teams - 1) / teams), (unsigned)((a.tokens + 8 * NT - 1) / (8 * NT))),
-                     kWarps * 32, kWarps * kRingBytes<MT, ENDS>, stream);
+    constexpr size_t smem = kWarps * kRingBytes<MT, ENDS>;
+    return launch_w4<smem>(w4_linear_kernel<MT, NT, ENDS, T, S>, a,
+                           dim3((unsigned)((units + teams - 1) / teams), (unsigned)((a.tokens + 8 * NT - 1) / (8 * NT))),
+                           kWarps * 32, smem, stream);
 }
 
 template <int ENDS, typename T, class S>

@@ -21,10 +21,12 @@ struct Lists {
         : mask(reinterpret_cast<u64*>(at)), index(reinterpret_cast<uint16_t*>(mask + r.experts)), expert(index + r.experts),
           first(expert + r.experts), pair(first + r.experts + 1),
           active(reinterpret_cast<int*>(at + (bytes(r) - 16))) {}
-    static __host__ __device__ int bytes(const Routing& r) {
-        return (r.experts * 14 + 2 + r.tokens * r.top * 2 + 15) / 16 * 16 + 16;
+    static constexpr __host__ __device__ int bytes(int experts, int pairs) {
+        return (experts * 14 + 2 + pairs * 2 + 15) / 16 * 16 + 16;
     }
+    static __host__ __device__ int bytes(const Routing& r) { return bytes(r.experts, r.tokens * r.top); }
 };
+constexpr int kMostLists = Lists::bytes(kMaxExperts, kMaxTokens * kMaxTop);
 
 // Returns how many experts are active.
 __device__ __forceinline__ int build_lists(const Lists& l, const Routing& r) {
@@ -323,19 +325,23 @@ cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
     const int64_t ctas = ((most << a.team_shift) + kUpWarps - 1) / kUpWarps;
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
-        const size_t smem = kUpWarps * (kRingBytes<MT, kEnds> + MT * 16 * (8 * NT + 1) * 4) + Lists::bytes(a.r);
-        return launch_w4(moe_up_kernel<MT, NT, kEnds, T>, a, dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
-                         smem, stream);
+        constexpr size_t kRings = kUpWarps * (kRingBytes<MT, kEnds> + MT * 16 * (8 * NT + 1) * 4);
+        return launch_w4<kRings + kMostLists>(moe_up_kernel<MT, NT, kEnds, T>, a,
+                                              dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
+                                              kRings + Lists::bytes(a.r), stream);
     });
 }
+
+constexpr int kPairedTokens = 8;         // of two tiles at a time: the warps' sums of many tokens leave no room for them
 
 template <int MT, int NT, typename T>
 cudaError_t down_launch(const DownArgs<T>& a, cudaStream_t stream) {
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
-        const size_t smem = kDownWarps * (kRingBytes<MT, kEnds> + MT * 16 * (a.r.tokens | 1) * 4) + Lists::bytes(a.r);
-        return launch_w4(moe_down_kernel<MT, NT, kEnds, T>, a, dim3((unsigned)((a.w.tiles + MT - 1) / MT)), kDownWarps * 32, smem,
-                         stream);
+        const auto smem = [](int tokens) { return (size_t)kDownWarps * (kRingBytes<MT, kEnds> + MT * 16 * (tokens | 1) * 4); };
+        return launch_w4<smem(MT == 2 ? kPairedTokens : kMaxTokens) + kMostLists>(
+            moe_down_kernel<MT, NT, kEnds, T>, a, dim3((unsigned)((a.w.tiles + MT - 1) / MT)), kDownWarps * 32,
+            smem(a.r.tokens) + Lists::bytes(a.r), stream);
     });
 }
 
@@ -360,8 +366,7 @@ cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* co
     if (err != cudaSuccess) return err;
     const DownArgs<T> down = {w4_view(*a.down, true), r, h, padded, static_cast<T*>(a.y), a.ldy};
     if constexpr (NT == 1) {
-        // the warps' sums of many tokens leave no room for it
-        if (a.tokens <= 8 && filled((down.w.tiles + 1) / 2) >= filled(down.w.tiles)) return down_launch<2, NT, T>(down, stream);
+        if (a.tokens <= kPairedTokens && filled((down.w.tiles + 1) / 2) >= filled(down.w.tiles)) return down_launch<2, NT, T>(down, stream);
     }
     return down_launch<1, NT, T>(down, stream);
 }

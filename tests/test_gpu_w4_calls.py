@@ -1,0 +1,65 @@
+"""Calls on 4-bit weights as a host program makes them: from several threads at once through the C ABI."""
+import ctypes
+import struct
+import threading
+
+import pytest
+import torch
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a CUDA device")]
+
+W4 = struct.Struct("6q Q")                       # pwlq_w4 and pwlq_w4_moe_args of include/pwlq.h
+MOE = struct.Struct("5q Qq Qq QQ Qq QQ Qq")
+
+
+def _weights(seed, *shape):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return (torch.randn(*shape, generator=g, device="cuda") * shape[-1] ** -0.5).bfloat16()
+
+
+class _Layer:
+    """A call of pwlq_w4_moe with memory of its own."""
+
+    def __init__(self, seed, tokens, experts, features, hidden, top):
+        from paper_2002_00104_b200 import pwlq
+        self.lib, self.stream = pwlq.load_library(), torch.cuda.Stream()
+        up = pwlq.w4_encode(_weights(seed, experts, 2 * hidden, features), group=64, paired=True)
+        down = pwlq.w4_encode(_weights(seed + 1, experts, features, hidden), group=64)
+        router, x = _weights(seed + 2, experts, features), _weights(seed + 3, tokens, features)
+        self.want = pwlq.w4_moe(x, router, up, down, top)
+        self.y = torch.zeros_like(x)
+        need = pwlq.w4_moe_workspace_bytes(tokens, top, features, hidden)
+        workspace = torch.zeros(need, dtype=torch.uint8, device="cuda")
+        blocks = [ctypes.create_string_buffer(W4.pack(*p._fields, p.memory.data_ptr())) for p in (up, down)]
+        self.keep = up, down, router, x, workspace, blocks
+        self.args = MOE.pack(tokens, top, pwlq.BF16, pwlq.BF16, 1, x.data_ptr(), features, router.data_ptr(), features,
+                             *(ctypes.addressof(b) for b in blocks), self.y.data_ptr(), features, 0, 0,
+                             workspace.data_ptr(), need)
+
+    def call(self):
+        return self.lib.pwlq_w4_moe(self.args, self.stream.cuda_stream)
+
+
+def test_layers_of_different_sizes_from_several_threads():
+    """The same kernels with different amounts of shared memory: no thread's launch depends on what another's asks for."""
+    layers = [_Layer(1, 1, 64, 48, 64, 4), _Layer(11, 64, 64, 48, 64, 4), _Layer(21, 9, 1024, 48, 64, 4)]
+    torch.cuda.synchronize()
+    failed = [0] * len(layers)
+
+    def work(i):
+        torch.cuda.set_device(0)
+        for n in range(1500):
+            failed[i] += layers[i].call() != 0
+            if n % 100 == 99:
+                layers[i].stream.synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(layers))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert failed == [0] * len(layers)
+    for v in layers:
+        assert torch.equal(v.y, v.want)
