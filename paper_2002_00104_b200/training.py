@@ -23,14 +23,18 @@ class Checkpoints:
 
 
 def best_ratio(x: torch.Tensor, group: int = 128, candidates: int = 32, bits: int = 7) -> float:
-    """The breakpoint ratio with the smallest total squared error on x [rows, cols] (every group a
-    row of the search with this many bits: 7 for checkpoints, 3 for 4-bit weights; the last values of a row that do not fill one left out; rows shorter than
-    a group are one each); candidates are k / candidates, the last one (no tail) left out."""
+    """The breakpoint ratio with the smallest total squared error on x [rows, cols], or on several
+    matrices [matrices, rows, cols] together.  Every group is a row of the search with this many bits: 7
+    for checkpoints, 3 for 4-bit weights.  The last values of a row that do not fill a group are left out;
+    rows shorter than a group are one each.  Candidates are k / candidates, the last one (no tail) left
+    out."""
+    if x.dim() not in (2, 3):
+        raise ValueError(f"x must be [rows, cols] or [matrices, rows, cols], it is {list(x.shape)}")
     if x.numel() == 0 or candidates < 2:
         raise ValueError(f"no candidates, or no values: x is {list(x.shape)}")
-    group = min(group, x.shape[1])
-    cols = x.shape[1] // group * group
-    rows = x[:, :cols].float().reshape(-1, group).contiguous()
+    group = min(group, x.shape[-1])
+    cols = x.shape[-1] // group * group
+    rows = x[..., :cols].float().reshape(-1, group).contiguous()
     ratios = torch.arange(1, candidates, device=x.device, dtype=torch.float32) / candidates
     sse = pwlq.search(rows, bits, ratios, want_sse=True)["sse"]
     return float(ratios[sse.double().sum(dim=0).argmin()])
