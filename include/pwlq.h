@@ -578,7 +578,8 @@ typedef struct {
 size_t pwlq_w4_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t group, int64_t paired);
 
 /* x, y [matrices, rows, cols] of type dtype; ldx / ldy the pitch of a row, ldm that of a matrix (ignored for one).
- * Every byte of data is written. */
+ * Every byte of data is written.  x's matrices may overlap (ldm may be 0); y's must
+ * not, one after another or with their rows between one another's. */
 int pwlq_w4_encode(const pwlq_w4* w, const void* x, int dtype, int64_t ldx, int64_t ldm, void* stream);
 int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ldm, void* stream);
 

@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/pwlq.h"
+#include "pwlq_overlap.h"
 
 namespace {
 
@@ -487,7 +488,7 @@ PyObject* w4_decode(Args a) {
         out = three ? at::empty({p.w.matrices, p.w.rows, p.w.cols}, options) : at::empty({p.w.rows, p.w.cols}, options);
     }
     const Values v = values(out, "out", p.w, device);
-    TORCH_CHECK_VALUE(p.w.matrices < 2 || v.ldm >= (p.w.rows - 1) * v.ld + p.w.cols, "out: matrices overlap");
+    TORCH_CHECK_VALUE(!pwlq::matrices_meet(p.w.matrices, p.w.rows, p.w.cols, v.ld, v.ldm), "out: matrices overlap");
     check(lib.w4_decode(&p.w, v.p, dtype_code(out.scalar_type()), v.ld, v.ldm, stream_of(device)), "pwlq_w4_decode");
     return wrap(out);
 }

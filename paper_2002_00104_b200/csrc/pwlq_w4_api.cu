@@ -1,5 +1,6 @@
 // C ABI of the operators on 4-bit weights: argument checks and kernel launches, nothing else.
 #include "../../include/pwlq.h"
+#include "pwlq_overlap.h"
 #include "pwlq_w4.h"
 
 namespace {
@@ -66,7 +67,9 @@ int pwlq_w4_encode(const pwlq_w4* w, const void* x, int dtype, int64_t ldx, int6
 
 int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ldm, void* stream) {
     if (int rc = check_w4(w)) return rc;
-    if (bad_matrices(*w, y, dtype, ldy, ldm)) return PWLQ_ERR_INVALID_ARG;
+    if (bad_matrices(*w, y, dtype, ldy, ldm) ||
+        pwlq::matrices_meet(w->matrices, w->rows, w->cols, ldy, ldm))
+        return PWLQ_ERR_INVALID_ARG;
     return from_cuda(pwlq::launch_w4_decode(*w, y, dtype, ldy, ldm, as_stream(stream)));
 }
 

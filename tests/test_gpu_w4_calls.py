@@ -63,3 +63,18 @@ def test_layers_of_different_sizes_from_several_threads():
     assert failed == [0] * len(layers)
     for v in layers:
         assert torch.equal(v.y, v.want)
+
+
+def test_decoding_to_matrices_whose_rows_lie_between_one_another_s():
+    from paper_2002_00104_b200 import pwlq
+    packed = pwlq.w4_encode(_weights(31, 3, 40, 200), group=64)
+    want = pwlq.w4_decode(packed)
+    for gap in (0, 5):
+        out = torch.full((40, 3, 200 + gap), 7.0, device="cuda")
+        view = out.transpose(0, 1)[..., :200]
+        pwlq.w4_decode(packed, out=view)
+        assert torch.equal(view, want) and (out[..., 200:] == 7).all()
+    flat = torch.zeros(40 * 600, device="cuda")
+    for strides in ((199, 600, 1), (100, 200, 1), (200, 500, 1), (0, 200, 1)):
+        with pytest.raises(ValueError):
+            pwlq.w4_decode(packed, out=flat.as_strided((3, 40, 200), strides))
