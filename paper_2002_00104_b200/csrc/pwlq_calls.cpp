@@ -555,7 +555,8 @@ PyObject* w4_moe(Args a) {
     t = matrix(y, "out", m.tokens, up.w.cols, type, device);
     m.y = t.p;
     m.ldy = t.ld;
-    // sizes that memory is made from, before the library sees them
+    // sizes that memory is made from, before the library sees them; with the library's statuses, in its order
+    if (m.top < 1 || m.top > up.w.matrices) throw Failed{PWLQ_ERR_INVALID_ARG, "pwlq_w4_moe"};
     const int64_t need = (int64_t)lib.moe_bytes(m.tokens, m.top, down.w.rows, down.w.cols);
     if (!need) throw Failed{m.tokens > PWLQ_W4_MOE_MAX_TOKENS || m.top > PWLQ_W4_MOE_MAX_TOP ? PWLQ_ERR_UNSUPPORTED
                                                                                        : PWLQ_ERR_INVALID_ARG, "pwlq_w4_moe"};

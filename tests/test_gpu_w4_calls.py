@@ -78,3 +78,30 @@ def test_decoding_to_matrices_whose_rows_lie_between_one_another_s():
     for strides in ((199, 600, 1), (100, 200, 1), (200, 500, 1), (0, 200, 1)):
         with pytest.raises(ValueError):
             pwlq.w4_decode(packed, out=flat.as_strided((3, 40, 200), strides))
+
+
+def test_what_a_layer_refuses_and_as_what():
+    """The C entry's status for each, whoever finds it."""
+    from paper_2002_00104_b200 import pwlq
+    experts, features, hidden = 40, 128, 64
+    up = pwlq.w4_encode(_weights(41, experts, 2 * hidden, features), group=64, paired=True)
+    down = pwlq.w4_encode(_weights(42, experts, features, hidden), group=64)
+    router, x = _weights(43, experts, features), _weights(44, 4, features)
+    few = [pwlq.w4_encode(pwlq.w4_decode(v)[:8], group=64, paired=v.paired) for v in (up, down)]
+    workspace = torch.zeros(pwlq.w4_moe_workspace_bytes(4, 2, features, hidden), dtype=torch.uint8, device="cuda")
+    unpaired = pwlq.w4_encode(_weights(45, experts, 2 * hidden, features), group=64)
+    many = pwlq.w4_encode(_weights(46, 1, 32, 32).expand(1025, 32, 32), group=32, paired=True)
+    for status, args, kw in (
+            (pwlq.ERR_INVALID_ARG, (x, router, up, down, 0), {}), (pwlq.ERR_INVALID_ARG, (x, router, up, down, -1), {}),
+            (pwlq.ERR_INVALID_ARG, (x, router[:8], *few, 9), {}), (pwlq.ERR_INVALID_ARG, (x, router[:8], *few, 33), {}),
+            (pwlq.ERR_INVALID_ARG, (x, router, up, down, 41), {}), (pwlq.ERR_INVALID_ARG, (x, router, up, down, 2 ** 32 + 2), {}),
+            (pwlq.ERR_UNSUPPORTED, (x, router, up, down, 33), {}), (pwlq.ERR_UNSUPPORTED, (x[:1].repeat(65, 1), router, up, down, 2), {}),
+            (pwlq.ERR_INVALID_ARG, (x, router, up, up, 2), {}), (pwlq.ERR_INVALID_ARG, (x, router, unpaired, down, 2), {}),
+            (pwlq.ERR_INVALID_ARG, (x, router, up, few[1], 2), {}),
+            (pwlq.ERR_UNSUPPORTED, (x[:, :32], _weights(47, 1025, 32), many, pwlq.w4_encode(_weights(48, 1, 32, 16).expand(1025, 32, 16), group=32), 2), {}),
+            (pwlq.ERR_WORKSPACE, (x, router, up, down, 2), dict(workspace=workspace[:-1])),
+            (pwlq.ERR_WORKSPACE, (x, router, up, down, 2), dict(workspace=workspace[:0])),
+            (pwlq.ERR_INVALID_ARG, (x, router, up, down, 2), dict(workspace=torch.zeros(workspace.numel() + 8, dtype=torch.uint8, device="cuda")[8:]))):
+        with pytest.raises(pwlq.PwlqError) as e:
+            pwlq.w4_moe(*args, **kw)
+        assert e.value.status == status, (args[4], kw, e.value)
