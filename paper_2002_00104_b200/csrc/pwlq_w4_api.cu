@@ -36,14 +36,6 @@ int check_w4(const pwlq_w4* w) {
 bool bad_rows(const void* p, int64_t dtype, int64_t ld, int64_t cols) {
     return !p || misaligned(p, pwlq::type_size((int)dtype)) || ld < cols || ld > kMaxPitch;
 }
-// Whether rows of `a` values at x and of `b` values at y have a value in common.
-bool overlap(const void* x, int64_t ldx, int64_t a, const void* y, int64_t ldy, int64_t b, int64_t rows, int64_t size) {
-    const int64_t from = (int64_t)reinterpret_cast<uintptr_t>(x), to = (int64_t)reinterpret_cast<uintptr_t>(y);
-    if (from + ((rows - 1) * ldx + a) * size <= to || to + ((rows - 1) * ldy + b) * size <= from) return false;
-    if (ldx != ldy || rows == 1) return true;
-    const int64_t pitch = ldx * size, off = ((to - from) % pitch + pitch) % pitch;
-    return off < a * size || off + b * size > pitch;      // y's values lie behind x's in rows that both share
-}
 // Values [matrices, rows, cols].
 bool bad_matrices(const pwlq_w4& w, const void* p, int dtype, int64_t ld, int64_t ldm) {
     return !is_dtype(dtype) || bad_rows(p, dtype, ld, w.cols) || (w.matrices > 1 && (ldm < 0 || ldm > kMaxPitch));
@@ -88,7 +80,7 @@ int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, i
     if (tokens == 0) return PWLQ_OK;
     const int64_t outputs = w->paired ? w->rows / 2 : w->rows;
     if (bad_rows(x, dtype, ldx, w->cols) || bad_rows(y, dtype, ldy, outputs) ||
-        overlap(x, ldx, w->cols, y, ldy, outputs, tokens, pwlq::type_size(dtype)))
+        pwlq::rows_meet(x, ldx, w->cols, y, ldy, outputs, tokens, (int64_t)pwlq::type_size(dtype)))
         return PWLQ_ERR_INVALID_ARG;
     const size_t need = pwlq_w4_linear_workspace_bytes(tokens, w->rows, w->cols, dtype,
                                                        pwlq::rows_aligned(x, ldx, pwlq::type_size(dtype)));

@@ -105,3 +105,24 @@ def test_what_a_layer_refuses_and_as_what():
         with pytest.raises(pwlq.PwlqError) as e:
             pwlq.w4_moe(*args, **kw)
         assert e.value.status == status, (args[4], kw, e.value)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_products_into_the_gaps_of_their_tokens_rows(dtype):
+    """x and out in one piece of memory with different pitches: what does not meet is taken, what does is refused."""
+    from paper_2002_00104_b200 import pwlq
+    packed = pwlq.w4_encode(_weights(51, 16, 40), group=32)
+    values = torch.randn(4, 40, generator=torch.Generator("cuda").manual_seed(5), device="cuda").to(dtype)
+    want = pwlq.w4_linear(values, packed)
+    memory = torch.full((2048,), 7.0, dtype=dtype, device="cuda")
+    x = memory.as_strided((4, 40), (100, 1), 0)          # 0-39, 100-139, 200-239, 300-339
+    x.copy_(values)
+    for at, pitch in ((40, 120), (60, 110), (60, 108), (340, 16), (40, 100)):
+        y = memory.as_strided((4, 16), (pitch, 1), at)
+        pwlq.w4_linear(x, packed, out=y)
+        assert torch.equal(y, want) and torch.equal(x, values), (at, pitch)
+        y.fill_(7.0)
+    for at, pitch in ((39, 120), (40, 90), (60, 90), (25, 300), (60, 65), (124, 16)):
+        with pytest.raises(pwlq.PwlqError) as e:
+            pwlq.w4_linear(x, packed, out=memory.as_strided((4, 16), (pitch, 1), at))
+        assert e.value.status == pwlq.ERR_INVALID_ARG and torch.equal(x, values)
