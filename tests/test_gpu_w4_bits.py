@@ -88,3 +88,19 @@ def test_the_largest_values_in_a_layer(dtype, tokens, features):
     want = (torch.full((hidden,), 27.0 * 2.0 ** 120).double() @ down.double().t()).expand(tokens, -1)
     y = _one_expert(up, down, x, TYPES[dtype])
     assert torch.equal(y, want.to(y.dtype))
+
+
+@pytest.mark.parametrize("tokens,features", [(1, 64), (2, 4096), (7, 70), (20, 64), (33, 130)])
+def test_all_bits_of_binary32_tokens_in_a_layer(tokens, features):
+    """Tokens that differ in their 24th bit: gate and up sums of two that cancel are all that is left of them."""
+    hidden = 40
+    up, down = torch.zeros(2 * hidden, features), torch.zeros(features, hidden)
+    x = torch.zeros(tokens, features)
+    x[:, 0] = 1.0 + 2.0 ** -12 + 2.0 ** -23
+    x[:, 1] = 1.0 + 2.0 ** -12
+    up[0, 0], up[0, 1] = 3 * 2.0 ** 30, -3 * 2.0 ** 30   # gate 3 * 2^7: its sigmoid is 1
+    up[hidden, 0], up[hidden, 1] = 3 * 2.0 ** 10, -3 * 2.0 ** 10     # up 3 * 2^-13
+    c = 3.0 * 2.0 ** torch.randint(-3, 4, (features,), generator=torch.Generator().manual_seed(features)).float()
+    down[:, 0] = c
+    y = _one_expert(up, down, x, torch.float32)
+    assert torch.equal(y, (c * 384 * 3 * 2.0 ** -13).expand(tokens, -1))
