@@ -11,6 +11,15 @@ namespace pwlq {
 // into tiles whose partial sums are combined in a fixed order by a second kernel.
 constexpr int kSearchTile = 8192;
 
+// Allows a search kernel the dynamic shared memory of a call, where it could be more than a launch may have anyway (48
+// KB, with the kernel's own, less than 1 KB).  What it is set to is `most`, the most that any call asks for: calls from
+// several threads share it, and a smaller one set between another's setting and launch made that launch fail.
+template <typename K>
+cudaError_t allow_search_smem(K* kernel, size_t smem, size_t most) {
+    if (smem <= 47 * 1024) return cudaSuccess;
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
+
 // shift (here and below): for a slice of a longer list of ragged rows -- row_offsets points at the
 // slice's first offset, the data pointers were advanced by `shift` values, `total` counts the
 // slice's values; every offset read is reduced by `shift`.  0 for whole tensors.

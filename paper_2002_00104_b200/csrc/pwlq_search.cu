@@ -34,6 +34,7 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "../../include/pwlq.h"
 #include "pwlq_common.cuh"
 #include "pwlq_kernels.h"
 
@@ -921,12 +922,10 @@ cudaError_t launch_search(const float* x, const int64_t* row_offsets, int64_t C,
             classes[1] = classes[2] = RowClass{INT64_MAX, INT64_MAX, 64};   // never launched
         }
         size_t off[7];
-        const size_t smem_max = sorted_smem_layout(a.cap, K, kSWarps, off);
-        if (smem_max > 48 * 1024) {  // above the default limit: opt in (idempotent, per device)
-            e = cudaFuncSetAttribute(search_sorted_kernel,
-                                     cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_max);
-            if (e != cudaSuccess) return e;
-        }
+        // the layout grows with both: several slices of few candidates are fewer sums than one of 1024
+        e = allow_search_smem(search_sorted_kernel, sorted_smem_layout(a.cap, K, kSWarps, off),
+                              sorted_smem_layout(kSearchTile, kSortMaxK, kSWarps, off));
+        if (e != cudaSuccess) return e;
         if (plan.tile == kSearchTile && total / C < 512) {
             // Mostly short rows (the library sees the mean length only): the small-CTA classes
             // hold the bulk of the work and go first, so that the stream does not end with their
@@ -974,11 +973,9 @@ cudaError_t launch_search(const float* x, const int64_t* row_offsets, int64_t C,
         a.grid_tiles = plan.tiles;
         const size_t smem = (((size_t)a.cap * 4 + 15) & ~(size_t)15) +
                             sizeof(double) * (size_t)E * (size_t)K;
-        if (smem > 48 * 1024) {
-            e = cudaFuncSetAttribute(search_generic_kernel,
-                                     cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-            if (e != cudaSuccess) return e;
-        }
+        // so many candidates are one slice
+        e = allow_search_smem(search_generic_kernel, smem, sizeof(float) * kSearchTile + sizeof(double) * PWLQ_MAX_K);
+        if (e != cudaSuccess) return e;
         search_generic_kernel<<<(unsigned)(C * plan.tiles), kSThreads, smem, stream>>>(a);
     }
     e = cudaGetLastError();

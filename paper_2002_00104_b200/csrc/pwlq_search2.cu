@@ -591,11 +591,8 @@ cudaError_t launch_search2(const float* x, const int64_t* row_offsets, int64_t C
     a.status = static_cast<int*>(workspace);
     size_t off[9];
     const size_t smem = search2_smem(a.cap, K, off);
-    if (smem > 48 * 1024) {
-        e = cudaFuncSetAttribute(search2_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)smem);
-        if (e != cudaSuccess) return e;
-    }
+    e = allow_search_smem(search2_kernel, smem, search2_smem(kSearchTile, kSearch2MaxK, off));
+    if (e != cudaSuccess) return e;
     search2_kernel<<<(unsigned)(C * a.tiles), kS2Threads, smem, stream>>>(a);
     e = cudaGetLastError();
     if (e != cudaSuccess || a.tiles == 1) return e;
