@@ -224,15 +224,15 @@ template <typename T> struct DownArgs {
 
 // A warp's way through its part of a tile's blocks, which are those of all chosen experts one after another.
 struct DownTag { int first, count; };
-template <int MT, int NT, typename T> struct DownSteps {
+template <int MT, typename T> struct DownSteps {
     const Lists* l;
     const DownArgs<T>* a;
     int64_t tile;                                         // the first of MT
     int now, end, bytes;                                  // the block after this segment, the last one
     int expert = 0, first = 0, count = 0, from = 0, n_blocks = 0;
     __device__ __forceinline__ bool next() {
-        first += 8 * NT;
-        count -= 8 * NT;
+        first += 8;
+        count -= 8;
         if (count > 0) return true;
         if (now >= end) return false;
         const int at = now / a->w.blocks;
@@ -251,17 +251,19 @@ template <int MT, int NT, typename T> struct DownSteps {
     }
     __device__ __forceinline__ DownTag tag() const { return {first, count}; }
     __device__ __forceinline__ int column() const { return from * kBlockCols; }
-    __device__ __forceinline__ const Hidden::Elem* row(int n) const {
-        const int c = min(8 * n + ((int)(threadIdx.x & 31) >> 2), count - 1);
+    __device__ __forceinline__ const Hidden::Elem* row(int) const {
+        const int c = min((int)(threadIdx.x & 31) >> 2, count - 1);
         return a->h + l->pair[first + c] * Hidden::kParts * a->padded;
     }
 };
 
 // A CTA per MT tiles of 16 features: the blocks of all chosen experts' rows are one list that the warps share; a warp
 // adds what an expert gives to its own sums, [16 MT][tokens], and these are added in a fixed order at the end.  So no
-// partial sum leaves the CTA; what is left is that 128 or 256 CTAs do not divide by 148.  4 tokens, 8 experts of 4096 x
-// 8192: 40 us, 53 with single tiles.
-template <int MT, int NT, int ENDS, typename T>
+// partial sum leaves the CTA; what is left is that 128 or 256 CTAs do not divide by 148.  An expert's tokens are taken eight
+// at a time: sixteen leave too few registers for activations of three parts ahead (64 tokens, 8 of 32 experts of 3 x 768 x
+// 2048 bf16, the whole layer: 109 us, 95 with eight; 2 of 8 of 3 x 2048 x 4096 131, 120).  4 tokens, 2 of 8 experts of 4096 x
+// 8192: 50 us; with single tiles 55.
+template <int MT, int ENDS, typename T>
 __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const DownArgs<T> a) {
     constexpr int kRing = kRingBytes<MT, ENDS>, kRows = 16 * MT;
     extern __shared__ __align__(16) uint8_t shared[];     // rings, sums, lists
@@ -275,23 +277,21 @@ __global__ void __launch_bounds__(kDownWarps * 32, 1) moe_down_kernel(const Down
     const int total = build_lists(l, a.r) * a.w.blocks;
     Hidden::Source source;
     source.cols = (int)a.padded;
-    const DownSteps<MT, NT, T> steps = {&l, &a, (int64_t)blockIdx.x * MT, (int)((int64_t)total * warp / kDownWarps),
+    const DownSteps<MT, T> steps = {&l, &a, (int64_t)blockIdx.x * MT, (int)((int64_t)total * warp / kDownWarps),
                                         (int)((int64_t)total * (warp + 1) / kDownWarps), w4_block_bytes(ENDS)};
-    w4_stream<MT, NT, ENDS>(steps, source, a.w.table, shared + warp * kRing,
-                            [&](const DownTag& at, const float (&acc)[MT][NT][4]) {
+    w4_stream<MT, 1, ENDS>(steps, source, a.w.table, shared + warp * kRing,
+                           [&](const DownTag& at, const float (&acc)[MT][1][4]) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < 2; ++i) {
+            const int c = 2 * q + i;
+            if (c >= at.count) continue;
+            float* const to = mine + g * pitch + l.pair[at.first + c] / a.r.top;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int c = 8 * n + 2 * q + i;
-                if (c >= at.count) continue;
-                float* const to = mine + g * pitch + l.pair[at.first + c] / a.r.top;
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    to[16 * m * pitch] += acc[m][n][i];
-                    to[(16 * m + 8) * pitch] += acc[m][n][i + 2];
-                }
+            for (int m = 0; m < MT; ++m) {
+                to[16 * m * pitch] += acc[m][0][i];
+                to[(16 * m + 8) * pitch] += acc[m][0][i + 2];
             }
+        }
         __syncwarp();
     });
     __syncthreads();
@@ -334,13 +334,13 @@ cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
 
 constexpr int kPairedTokens = 8;         // of two tiles at a time: the warps' sums of many tokens leave no room for them
 
-template <int MT, int NT, typename T>
+template <int MT, typename T>
 cudaError_t down_launch(const DownArgs<T>& a, cudaStream_t stream) {
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
         const auto smem = [](int tokens) { return (size_t)kDownWarps * (kRingBytes<MT, kEnds> + MT * 16 * (tokens | 1) * 4); };
         return launch_w4<smem(MT == 2 ? kPairedTokens : kMaxTokens) + kMostLists>(
-            moe_down_kernel<MT, NT, kEnds, T>, a, dim3((unsigned)((a.w.tiles + MT - 1) / MT)), kDownWarps * 32,
+            moe_down_kernel<MT, kEnds, T>, a, dim3((unsigned)((a.w.tiles + MT - 1) / MT)), kDownWarps * 32,
             smem(a.r.tokens) + Lists::bytes(a.r), stream);
     });
 }
@@ -365,10 +365,8 @@ cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* co
     }
     if (err != cudaSuccess) return err;
     const DownArgs<T> down = {w4_view(*a.down, true), r, h, padded, static_cast<T*>(a.y), a.ldy};
-    if constexpr (NT == 1) {
-        if (a.tokens <= kPairedTokens && filled((down.w.tiles + 1) / 2) >= filled(down.w.tiles)) return down_launch<2, NT, T>(down, stream);
-    }
-    return down_launch<1, NT, T>(down, stream);
+    return a.tokens <= kPairedTokens && filled((down.w.tiles + 1) / 2) >= filled(down.w.tiles) ? down_launch<2, T>(down, stream)
+                                                                                              : down_launch<1, T>(down, stream);
 }
 
 }  // namespace
@@ -376,7 +374,7 @@ cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* co
 template <typename T>
 cudaError_t launch_moe_products(const pwlq_w4_moe_args& a, const Routing& r, const void* copy, void* hidden,
                                 cudaStream_t stream) {
-    // tokens are taken eight or sixteen at a time: an expert's are, on average, few
+    // the up projections take an expert's tokens eight or sixteen at a time: they are, on average, few
     return a.tokens <= 8 || a.tokens * a.top <= 6 * r.experts ? products<1, T>(a, r, copy, hidden, stream)
                                                               : products<2, T>(a, r, copy, hidden, stream);
 }
