@@ -560,9 +560,10 @@ int pwlq_act8_weight_grad(const void* dy, int dtype, int64_t rows, int64_t outpu
  * and with the breakpoint b, a whole number in 1..64 for the whole tensor (p = m * b / 64), the values are
  * whole multiples of s:
  *     tail = a > 3 b s;   n = tail ? 3 b + q (64 - b) : q b,   q in 0..3 the nearest level, ties to even
- * (a = |w|); a nibble is sign << 3 | tail << 2 | q, of a value held as 0 it is 0.  Every bound between two levels is exact in binary32, and so is every value n * s: encoding and
- * decoding round nothing but s.  n <= 192 has eight bits, so that n / 256 is exact in bf16 and fp16 as well and
- * the products below take weights without rounding them.  |w| up to 2^126.
+ * (a = |w|); a nibble is sign << 3 | tail << 2 | q, of a value held as 0 it is 0.  Every bound between two
+ * levels is exact in binary32, and so is every value n * s: encoding and decoding round nothing but s.  n <= 192
+ * has eight bits, so that n times a power of two is exact in bf16 and fp16 as well and the products below take
+ * weights without rounding them.  |w| up to 2^126.
  *   paired   1: the matrix is two of rows / 2 rows each, gate rows then up rows (rows even), which the
  *            products take together: silu(gate) * up
  *   data     pwlq_w4_bytes() bytes, 16-byte aligned, in the order in which the products read them:
@@ -578,18 +579,23 @@ typedef struct {
 size_t pwlq_w4_bytes(int64_t matrices, int64_t rows, int64_t cols, int64_t group, int64_t paired);
 
 /* x, y [matrices, rows, cols] of type dtype; ldx / ldy the pitch of a row, ldm that of a matrix (ignored for one).
- * Every byte of data is written.  x's matrices may overlap (ldm may be 0); y's must
- * not, one after another or with their rows between one another's. */
+ * Every byte of data is written.  x's matrices may overlap (ldm may be 0); y's must not, but may lie one after
+ * another or with their rows between one another's. */
 int pwlq_w4_encode(const pwlq_w4* w, const void* x, int dtype, int64_t ldx, int64_t ldm, void* stream);
 int pwlq_w4_decode(const pwlq_w4* w, void* y, int dtype, int64_t ldy, int64_t ldm, void* stream);
 
 /* y[t, n] = sum over k of x[t, k] w[n, k], for a paired matrix y[t, n] = silu(gate) * up of the sums with gate row
- * n and up row n, [tokens, rows / 2].  matrices = 1.  x [tokens, cols] and y of type dtype; made for few tokens (any
- * number is taken; from some hundreds on decoding once and a dense product are faster).  Products are exact, the
- * sums binary32 in a fixed order (bit-reproducible), y is rounded once.  x may have any finite value: no sum on the way
- * leaves binary32's range where the result does not come near its end.  Sums are kept to 2^-134 or better, so that
- * results below 2^-110 have fewer than 24 bits; so have binary32 values of x below 2^-109.  tokens may be 0.  y must
- * not overlap x.
+ * n and up row n, [tokens, rows / 2].  matrices = 1.  x [tokens, cols] and y of type dtype.  Made for few tokens; any
+ * number is taken, but weights are taken apart again for every sixteen: with 16-bit tokens a pwlq_w4_decode and a dense
+ * product are faster from about 64 (4096 x 4096) to 85 (4096 x 14336) on, a dense product alone, of weights that are kept
+ * decoded, from about 30; with binary32 tokens neither is up to 512.
+ *   Products are exact.  Sums are those of matrix instructions with binary32 sums, in a fixed order (bit-reproducible):
+ * each adds 16 products to the sum so far and keeps 24 bits or more below the largest of the 17, cut off, not rounded:
+ * within 17 * 2^-23 of the magnitudes' sum.  A group, or 128 columns of a longer one, are 8 of them or fewer (24 with
+ * binary32 tokens) and meet their scale and the other groups in one binary32 rounding.  Measured, the whole error is 2e-7
+ * to 5e-7 of the result's size, where binary32 additions have 1e-7 to 2e-7.  y is rounded once.  x may have any finite value: no sum on the way leaves binary32's range where the result
+ * does not come near its end.  Sums are kept to 2^-134 or better, so that results below 2^-110 have fewer than 24 bits;
+ * so have binary32 values of x below 2^-109.  tokens may be 0.  y must not overlap x.
  *   workspace   pwlq_w4_linear_workspace_bytes(...) bytes, 256-byte aligned: for a large matrix, a copy of tokens
  *               that are binary32 (in three bf16 parts whose sum they are), or whose rows do not start on 16-byte
  *               boundaries (x_aligned) or are not whole eights; 0 bytes (workspace may be NULL) otherwise */
@@ -608,7 +614,7 @@ int pwlq_w4_linear(const pwlq_w4* w, const void* x, int dtype, int64_t tokens, i
  *           the order of a sum
  *   chosen, weights   [tokens, top] each, int32 and binary32, largest score first; or NULL
  *   workspace         pwlq_w4_moe_workspace_bytes(...) bytes, 256-byte aligned; 0 for invalid arguments
- * Sums are binary32 in a fixed order (bit-reproducible).  silu(gate) * up * weight lies in the workspace with all of
+ * Sums are those of pwlq_w4_linear, in a fixed order (bit-reproducible).  silu(gate) * up * weight lies in the workspace with all of
  * binary32's 24 bits and its range, whatever dtype is.  A token's values reach no other token's. */
 #define PWLQ_W4_MOE_MAX_TOKENS 64
 #define PWLQ_W4_MOE_MAX_EXPERTS 1024

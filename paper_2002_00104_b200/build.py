@@ -18,7 +18,8 @@ SOURCES = ["pwlq_api.cu", "pwlq_absmax.cu", "pwlq_search.cu", "pwlq_quantize.cu"
            "pwlq_noalloc.cu", "pwlq_select.cu", "pwlq_search2.cu", "pwlq_bias.cu", "pwlq_rowmap.cu",
            "pwlq_act8.cu", "pwlq_block_norm.cu", "pwlq_weight_grad.cu", "pwlq_train_api.cu",
            "pwlq_w4.cu", "pwlq_w4_linear_f32.cu", "pwlq_w4_linear_bf16.cu", "pwlq_w4_linear_f16.cu",
-           "pwlq_w4_moe.cu", "pwlq_w4_moe_route.cu", "pwlq_w4_moe_f32.cu", "pwlq_w4_moe_bf16.cu", "pwlq_w4_moe_f16.cu", "pwlq_w4_api.cu"]
+           "pwlq_w4_moe.cu", "pwlq_w4_moe_route.cu", "pwlq_w4_moe_f32.cu", "pwlq_w4_moe_bf16.cu",
+           "pwlq_w4_moe_f16.cu", "pwlq_w4_api.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
     "-fmad=false",            # no implicit FMA contraction: every fused op is an explicit fmaf

@@ -258,7 +258,7 @@ cudaError_t encode(const pwlq_w4& w, const T* x, int64_t ldx, int64_t ldm, cudaS
     const W4Write to = writer(w);
     // several tiles to a CTA where that leaves enough of them: 8192 x 8192 bf16 82 -> 70 us with four
     const int64_t columns = (w.cols + 255) / 256;
-    const int each = to.tiles * columns * w.matrices >= 4 * 8 * 148 ? 4 : 1;
+    const int each = to.tiles * columns * w.matrices >= 4 * 8 * kMultiprocessors ? 4 : 1;
     const dim3 grid((unsigned)((to.tiles + each - 1) / each), (unsigned)columns, (unsigned)w.matrices);
     const bool aligned = rows_aligned(x, ldx, sizeof(T)) && (w.matrices == 1 || rows_aligned(x, ldm, sizeof(T)));
     return aligned ? launch_dependent(w4_encode_kernel<true, T>, grid, dim3(256), 0, stream, x, ldx, ldm, to, each)

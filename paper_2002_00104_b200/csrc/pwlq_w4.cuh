@@ -34,9 +34,6 @@ struct W4View {
     int ends;                              // groups of a block
     int paired;
     W4Table table;
-    __device__ __forceinline__ const uint8_t* tile(int64_t matrix, int64_t t) const {
-        return data + (matrix * tiles + t) * blocks * w4_block_bytes(ends);
-    }
 };
 
 W4View w4_view(const pwlq_w4& w, bool bf16);
@@ -108,8 +105,8 @@ __device__ __forceinline__ uint32_t top16(float lo, float hi) {
     return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);
 }
 
-// Activations as operands, columns behind the last one as 0: eight consecutive values of a row, from column + offset + within on (`row` points `within`
-// values into the row), are kPieces x 4 registers.
+// Activations as operands, columns behind the last one as 0: eight consecutive values of a row, from column + offset +
+// within on (`row` points `within` values into the row), are kPieces x 4 registers.
 // 16-bit rows on 16-byte boundaries, whole blocks.
 template <typename T> struct RowsWhole {
     using Elem = T;
@@ -230,10 +227,11 @@ __device__ __forceinline__ W4Table in_registers(const W4Table& t) {
 //
 // What bounds this for a few tokens is, next to the weights' bytes, the integer pipe, which takes an instruction in two
 // cycles (address arithmetic, moves by multiplication and 16-bit arithmetic included): 13 to a word of eight weights, 28
-// cycles with the matrix instruction.  At 1.9 GHz that is 5.2 TB/s of codes; so all else is kept small.  Two tiles
+// cycles with the matrix instruction.  At 1.9 GHz that is 5.1 TB/s of codes; so all else is kept small.  Two tiles
 // share an activation operand; blocks come to shared memory by asynchronous copies, kStages - 1 steps ahead and across
-// the ends of segments, and activations are requested a block ahead.  36 cycles a word in all: 1 token 22528 x 8192
-// 27.4 us, 3.5 TB/s.
+// the ends of segments, and activations are requested a block ahead.  1 token 22528 x 8192: 27.4 us, 3.4 TB/s of codes,
+// 43 cycles of 1.9 GHz a word; 38 of them while a multiprocessor has work, the integer pipe busy in 69 % of these, and the
+// rest the beginning and 704 CTAs on 296 places.
 constexpr int kStages = 4;
 template <int MT, int ENDS> constexpr int kRingBytes = kStages * MT * w4_block_bytes(ENDS);       // of a warp
 

@@ -5,6 +5,7 @@
 
 namespace pwlq {
 
+constexpr int kMultiprocessors = 148;    // of a B200
 constexpr int kTileRows = 16;            // rows of a tile
 constexpr int kBlockCols = 128;          // columns of a block: 16 x 128 values, and the scales of its groups
 constexpr int kCodeBytes = kTileRows * kBlockCols / 2;
@@ -18,8 +19,14 @@ __host__ __device__ constexpr int w4_block_bytes(int ends) { return kCodeBytes +
 cudaError_t launch_w4_encode(const pwlq_w4& w, const void* x, int dtype, int64_t ldx, int64_t ldm, cudaStream_t stream);
 cudaError_t launch_w4_decode(const pwlq_w4& w, void* y, int dtype, int64_t ldy, int64_t ldm, cudaStream_t stream);
 // The product takes rows as they are, or in parts, a copy that a launch of its own makes (see include/pwlq.h), where they
-// would otherwise be turned and taken apart for every tile of a large matrix: 1 token 8192 x 8192 binary32 24.8 -> 17.4 us,
-// 8 tokens 8191 x 8191 bf16 21.4 -> 14.0, but 1 x 1000 x 2048 binary32, called one by one, 5.0 -> 7.4.
+// would otherwise be turned and taken apart for every tile of a large matrix, one of 4096 blocks and more.  us without and
+// with the copy, of calls back to back in a graph; a call on its own pays 2.4 for the second launch (1 x 1000 x 2048
+// binary32 5.0, 7.4):
+//     blocks               binary32: 1, 8, 16 tokens             bf16, a column fewer
+//      1024  1024 x 2048   4.6  4.0, 4.8  4.7,  9.5  7.6         2.7  3.4,  5.2  4.0,  8.5  4.8
+//      4096  4096 x 2048   6.5  5.5, 6.8  6.7, 10.1 11.5         3.9  4.4,  6.3  5.0,  9.3  6.8
+//      8192  4096 x 4096   10.8 7.3, 11.1 8.8, 16.9 18.0         5.6  5.9, 10.1  7.3, 16.6  9.7
+//     32768  8192 x 8192   24.7 17.4, 25.6 18.1, 43.2 31.9       14.0 13.4, 21.5 14.0, 33.7 16.8
 inline int64_t w4_padded(int64_t cols) { return w4_blocks(cols) * kBlockCols; }
 inline bool w4_copies(int64_t rows, int64_t cols, int dtype, bool aligned) {
     return (dtype == kF32 || cols % 8 != 0 || !aligned) && (rows / 16) * w4_blocks(cols) >= 4096;

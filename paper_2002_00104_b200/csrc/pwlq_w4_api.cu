@@ -9,7 +9,7 @@ constexpr int64_t kMaxRows = (int64_t)1 << 24;
 constexpr int64_t kMaxCols = (int64_t)1 << 20;
 constexpr int64_t kMaxMatrices = 65535;
 constexpr int64_t kMaxBlocks = (int64_t)1 << 30;           // of 1 KB
-constexpr int64_t kMaxTokens = (int64_t)1 << 19;           // blocks of eight along a grid's second axis
+constexpr int64_t kMaxTokens = (int64_t)1 << 19;           // blocks of sixteen along a grid's second axis (65535)
 constexpr int64_t kMaxPitch = (int64_t)1 << 40;
 
 inline bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }

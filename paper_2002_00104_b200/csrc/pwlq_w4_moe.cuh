@@ -321,13 +321,13 @@ cudaError_t up_launch(UpArgs<T> a, cudaStream_t stream) {
     const double spared = std::pow(1.0 - (double)a.r.top / a.r.experts, a.r.tokens);
     const double items = a.r.experts * (1.0 - spared) * (double)units;
     a.team_shift = a.w.blocks >= 2;
-    while (a.team_shift < 3 && items * (1 << a.team_shift) < 12 * 148 && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
+    while (a.team_shift < 3 && items * (1 << a.team_shift) < 12 * kMultiprocessors && a.w.blocks >> a.team_shift > 1) ++a.team_shift;
     const int64_t ctas = ((most << a.team_shift) + kUpWarps - 1) / kUpWarps;
     return with_ends(a.w.ends, [&](auto ends) {
         constexpr int kEnds = decltype(ends)::value;
         constexpr size_t kRings = kUpWarps * (kRingBytes<MT, kEnds> + MT * 16 * (8 * NT + 1) * 4);
         return launch_w4<kRings + kMostLists>(moe_up_kernel<MT, NT, kEnds, T>, a,
-                                              dim3((unsigned)std::min<int64_t>(ctas, 2 * 148)), kUpWarps * 32,
+                                              dim3((unsigned)std::min<int64_t>(ctas, 2 * kMultiprocessors)), kUpWarps * 32,
                                               kRings + Lists::bytes(a.r), stream);
     });
 }
@@ -346,7 +346,9 @@ cudaError_t down_launch(const DownArgs<T>& a, cudaStream_t stream) {
 }
 
 // How much of a last round of single CTAs to a multiprocessor is used.
-inline double filled(int64_t ctas) { return (double)ctas / (double)(148 * ((ctas + 147) / 148)); }
+inline double filled(int64_t ctas) {
+    return (double)ctas / (double)((ctas + kMultiprocessors - 1) / kMultiprocessors * kMultiprocessors);
+}
 
 template <int NT, typename T>
 cudaError_t products(const pwlq_w4_moe_args& a, const Routing& r, const void* copy, void* hidden, cudaStream_t stream) {
